@@ -297,6 +297,117 @@ int griffin_prompt_phase(const griffin_layer *L, const void *W2p, int64_t ldw, c
                          void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * ---------------------------------------------------------------- around the block
+ * What a layer has beside its FF block when it generates: the norms and the residual sum on both sides of a
+ * block, the paged cache of keys and values, and the attention that reads it.  The rows of a batch that shares
+ * one set (griffin_ff_decode, Eq. 7) usually continue one prompt; its keys and values are then held once and
+ * read once for all of them.
+ */
+typedef enum { GRIFFIN_NORM_RMS = 0, GRIFFIN_NORM_LAYER = 1 } griffin_norm_kind;
+
+/*
+ * Norms around a block.  With N(v; w, b) = v / sqrt(mean(v^2) + eps) * (w + w_offset) + b for GRIFFIN_NORM_RMS and
+ * (v - mean(v)) / sqrt(var(v) + eps) * (w + w_offset) + b for GRIFFIN_NORM_LAYER (var the mean of the squared deviations),
+ * griffin_norm_residual computes, row by row,
+ *   u  = N(y; w_post, b_post)                    the norm behind the block, or u = y without w_post
+ *   h' = h_scale * h + y_scale * gate * u        the residual stream behind it
+ *   x  = N(h'; w_pre, b_pre)                     the input of the next block
+ */
+typedef struct {
+    int32_t d;          /* row width: a multiple of 8, at most 32768 */
+    int32_t dtype;      /* of y, x, gate, weights and biases */
+    int32_t kind;       /* griffin_norm_kind */
+    float eps;          /* > 0 and finite */
+    float w_offset;     /* 0, or 1 where the weights are stored as w - 1 */
+    float h_scale, y_scale;
+    const void *w_pre, *b_pre;     /* [d]; w_pre is needed when x is written, b_pre may be NULL */
+    const void *w_post, *b_post;   /* [d]; w_post NULL: no norm behind the block (then b_post is NULL) */
+} griffin_norm;
+
+/*
+ *   h      [rows][d], row stride ldh elements, h_dtype: the residual stream, which may be fp32 beside bf16 blocks
+ *          (h_dtype GRIFFIN_BF16 needs N->dtype GRIFFIN_BF16)
+ *   y      [rows][d] stride ldy, the block's output; NULL: h' = h as it is (the first norm of a stack)
+ *   gate   [d] with ldg == 0, or one row for every row of y with stride ldg >= d; NULL: 1
+ *   h_out  [rows][d] stride ldo, h_dtype, NULL: not written.  May be h itself (same stride).
+ *   x      [rows][d] stride ldx, N->dtype, NULL: not written.  May be y itself (same stride).
+ * All strides are multiples of 8 and all pointers 16-byte aligned.  x is formed from h' in fp32, before h' is rounded
+ * to its type; sums are fp32.  rows <= 2^30; rows == 0 does nothing.
+ */
+int griffin_norm_residual(const griffin_norm *N, int64_t rows, const void *h, int64_t ldh, int32_t h_dtype, const void *y, int64_t ldy,
+                          const void *gate, int64_t ldg, void *h_out, int64_t ldo, void *x, int64_t ldx, void *stream);
+
+/*
+ * Paged pools of keys and values.  Token s of kv head g in page p is the row of `dim` elements at
+ * p * page_stride + g * head_stride + s * token_stride of K and of V: pages that hold [head][token][dim] or
+ * [token][head][dim], with or without gaps.
+ */
+typedef struct {
+    void *K, *V;             /* device, 16-byte aligned */
+    int32_t dtype;           /* griffin_dtype of keys, values, queries and outputs */
+    int32_t kv_heads;
+    int32_t dim;             /* features of a head: a multiple of 8, at most 256 */
+    int32_t page_size;       /* tokens in a page: a power of two from 16 to 65536 */
+    int64_t n_pages;         /* pages in the pools, at most 2^31 - 1 */
+    int64_t page_stride, head_stride, token_stride;   /* elements, multiples of 8; token_stride, head_stride >= dim */
+} griffin_kv_cache;
+
+/*
+ * One step of a batch: sequence b brings the new tokens cu[b] .. cu[b+1]-1 (rows of q, k, v and out) behind the
+ * n_prefix tokens that all sequences share and the lens[b] tokens of its own that are in the cache before the step.  A new
+ * token sees the whole prefix, its sequence's own tokens and the new tokens of its sequence up to itself.
+ * The caller advances lens (by cu[b+1] - cu[b]) after the last layer of a step; all layers of a step use the same.
+ * A prompt that is to be shared goes in as one sequence whose pages are later named as prefix_pages.
+ */
+typedef struct {
+    const int32_t *cu_seqlens;     /* HOST int32 [n_seqs+1]: cu[0] = 0, non-decreasing.  Read before a call returns. */
+    int32_t n_seqs;                /* 1 .. GRIFFIN_MAX_SEQS */
+    int32_t max_len;               /* own tokens of any sequence after the step are at most so many, at least 1; what lies beyond is
+                                      neither written nor read */
+    const int32_t *lens;           /* device [n_seqs], below 0 counts as 0 */
+    const int32_t *pages;          /* device [n_seqs][ld_pages]: the pages of a sequence's own tokens */
+    int64_t ld_pages;              /* >= ceil(max_len / page_size) */
+    int32_t n_prefix;              /* tokens shared by all sequences, 0 or more */
+    const int32_t *prefix_pages;   /* device [ceil(n_prefix / page_size)], NULL without a prefix */
+} griffin_kv_batch;                /* page numbers outside [0, n_pages) are clamped instead of faulting */
+
+typedef enum { GRIFFIN_ROT_HALF = 0, GRIFFIN_ROT_PAIRS = 1 } griffin_rot_style;
+
+/*
+ * Writes the keys and values of a step's new tokens into their pages, the keys rotated by their positions on the way,
+ * and rotates the queries.  Token i of sequence b has the position m = n_prefix + lens[b] + i and goes into slot
+ * lens[b] + i of its sequence's pages.  With (a, b) = features (j, j + rot/2) (GRIFFIN_ROT_HALF) or (2j, 2j + 1)
+ * (GRIFFIN_ROT_PAIRS), j < rot/2, the rotation gives (a cos - b sin, b cos + a sin), cos and sin from entry j of row m;
+ * features from rot on are copied.  Computed in fp32, rounded once.
+ *   k, v       [tokens][kv_heads][dim], token and head strides in elements (ldk, hsk; ldv, hsv), C->dtype
+ *   q, q_out   [tokens][n_heads][dim] likewise, or both NULL.  q_out may be q itself (same strides).
+ *   cos, sin   fp32 [n_pos][rot/2] contiguous, 16-byte aligned, NULL with rot == 0.  Positions from n_pos on take the last row.
+ *   rot        rotated features: even, 0 .. dim
+ * Strides are multiples of 8, pointers 16-byte aligned.  Two new tokens never share a slot as long as no page is in use
+ * by two sequences.
+ */
+int griffin_kv_append(const griffin_kv_cache *C, const griffin_kv_batch *B, const void *k, int64_t ldk, int64_t hsk, const void *v,
+                      int64_t ldv, int64_t hsv, const void *q, int64_t ldq, int64_t hsq, void *q_out, int64_t ldo, int64_t hso,
+                      int32_t n_heads, const float *cos, const float *sin, int64_t n_pos, int32_t rot, int32_t style, void *stream);
+
+/*
+ * Attention of a step's new tokens, which griffin_kv_append has put into the cache:
+ *   out[t][h] = sum_k softmax_k(scale * q[t][h] . K_k) V_k      over the keys that token t sees, kv head h / (n_heads / kv_heads)
+ * (zeros where all scores are -inf).  The prefix's keys and values are read
+ * once for up to 64 rows (tokens times heads of a group) or more, whichever sequences they belong to.  Scores, the softmax's maximum and sum and the
+ * weighted sum are fp32; bf16 caches take the weights rounded to bf16 into the second product (2^-8 each).  Keys that a token does not
+ * see do not reach its output, whatever they hold.
+ *   q, out     [tokens][n_heads][dim], token and head strides (ldq, hsq; ldo, hso), multiples of 8, 16-byte aligned; out is not q
+ *   n_heads    a multiple of C->kv_heads, at most 1024
+ *   scale      > 0 and finite
+ *   workspace  griffin_attention_workspace_bytes(C, B, n_heads) bytes or more (may be 0), 256-byte aligned.  The query depends on sizes
+ *              alone: kv_heads, dim, dtype, page_size, cu_seqlens, max_len, n_prefix
+ */
+size_t griffin_attention_workspace_bytes(const griffin_kv_cache *C, const griffin_kv_batch *B, int32_t n_heads);
+int griffin_attention(const griffin_kv_cache *C, const griffin_kv_batch *B, const void *q, int64_t ldq, int64_t hsq, void *out, int64_t ldo,
+                      int64_t hso, int32_t n_heads, float scale, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * MEASUREMENT ONLY -- not part of the method's interface and the one entry point that keeps state
  * between calls (a one-shot, per-thread note of three event handles; every other entry point is
  * stateless, apart from addresses and kernel attributes looked up once per device).  It exists so that a benchmark can time the kernels of a decode call on the stream

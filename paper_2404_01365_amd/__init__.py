@@ -18,6 +18,8 @@ OK, EINVAL, ESHAPE, EWORKSPACE, EUNSUPPORTED, EHIP = range(6)
 ACT_SILU, ACT_GELU_TANH, ACT_RELU = 0, 1, 2
 F32, BF16 = 0, 1
 MAX_SEQS, MAX_BATCH = 256, 64
+NORM_RMS, NORM_LAYER = 0, 1
+ROT_HALF, ROT_PAIRS = 0, 1
 
 
 class GriffinError(RuntimeError):
@@ -39,6 +41,30 @@ class griffin_layer(ctypes.Structure):
     ]
 
 
+class griffin_norm(ctypes.Structure):
+    _fields_ = [
+        ("d", ctypes.c_int32), ("dtype", ctypes.c_int32), ("kind", ctypes.c_int32), ("eps", ctypes.c_float),
+        ("w_offset", ctypes.c_float), ("h_scale", ctypes.c_float), ("y_scale", ctypes.c_float),
+        ("w_pre", ctypes.c_void_p), ("b_pre", ctypes.c_void_p), ("w_post", ctypes.c_void_p), ("b_post", ctypes.c_void_p),
+    ]
+
+
+class griffin_kv_cache(ctypes.Structure):
+    _fields_ = [
+        ("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("dtype", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+        ("dim", ctypes.c_int32), ("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int64),
+        ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64),
+    ]
+
+
+class griffin_kv_batch(ctypes.Structure):
+    _fields_ = [
+        ("cu_seqlens", ctypes.POINTER(ctypes.c_int32)), ("n_seqs", ctypes.c_int32), ("max_len", ctypes.c_int32),
+        ("lens", ctypes.c_void_p), ("pages", ctypes.c_void_p), ("ld_pages", ctypes.c_int64),
+        ("n_prefix", ctypes.c_int32), ("prefix_pages", ctypes.c_void_p),
+    ]
+
+
 def _load() -> ctypes.CDLL:
     # libgriffin.so needs libamdhip64.so.7.  PyTorch ships its own copy of that runtime; a
     # process must not end up with two HIP runtimes (the second one sees no device), so
@@ -56,6 +82,8 @@ lib = _load()
 _vp, _i32, _i64, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
 _LP = ctypes.POINTER(griffin_layer)
 _IP = ctypes.POINTER(ctypes.c_int32)
+_NP, _CP, _BP = (ctypes.POINTER(t) for t in (griffin_norm, griffin_kv_cache, griffin_kv_batch))
+_f32 = ctypes.c_float
 
 _SIGS = {
     "griffin_status_string": (ctypes.c_char_p, [ctypes.c_int]),
@@ -85,6 +113,10 @@ _SIGS = {
     "griffin_index_sets_bytes": (_sz, [_i32, _i32]),
     "griffin_index_sets_build": (ctypes.c_int, [_vp, _i32, _i32, _i32, _vp, _sz, _vp]),
     "griffin_ff_decode_indexed_sets": (ctypes.c_int, [_LP, _vp, _i32, _vp, _i32, _vp, _vp, _vp, _sz, _vp]),
+    "griffin_norm_residual": (ctypes.c_int, [_NP, _i64, _vp, _i64, _i32, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp]),
+    "griffin_kv_append": (ctypes.c_int, [_CP, _BP] + 4 * [_vp, _i64, _i64] + [_i32, _vp, _vp, _i64, _i32, _i32, _vp]),
+    "griffin_attention_workspace_bytes": (_sz, [_CP, _BP, _i32]),
+    "griffin_attention": (ctypes.c_int, [_CP, _BP, _vp, _i64, _i64, _vp, _i64, _i64, _i32, _f32, _vp, _sz, _vp]),
 }
 for _name, (_res, _args) in _SIGS.items():
     _fn = getattr(lib, _name)
@@ -298,3 +330,151 @@ def griffin_ff_prompt_out(Z, W2p, Y, *, b2=None, dtype: Optional[int] = None, wo
     _check(lib.griffin_ff_prompt_out(_ptr(Z), Z.stride(0), Z.shape[0], Z.shape[1], W2p.shape[0], dtype,
                                      _ptr(W2p), W2p.stride(0), _ptr(b2), _ptr(Y), Y.stride(0),
                                      _ptr(workspace), _nbytes(workspace), _stream(stream)), "griffin_ff_prompt_out")
+
+
+# ------------------------------------------------------------------ around the block
+def _dtype_of(t) -> int:
+    import torch
+    if t.dtype == torch.bfloat16:
+        return BF16
+    if t.dtype == torch.float32:
+        return F32
+    raise TypeError("%s is neither float32 nor bfloat16" % t.dtype)
+
+
+def _shape(what: str, t, *sizes) -> None:
+    """Sizes (None: any) of a tensor whose last axis is dense; the library sees pointers and strides only."""
+    if t.dim() != len(sizes) or any(n is not None and m != n for m, n in zip(t.shape, sizes)) or (t.shape[-1] > 1 and t.stride(-1) != 1):
+        raise ValueError("%s: shape %s, strides %s" % (what, tuple(t.shape), t.stride()))
+
+
+def _strides(t, width: int):
+    """A tensor's strides but the last; an axis of one element has whatever stride it was made with, so a dense one is taken."""
+    if t is None:
+        return (0, 0)
+    return tuple(st if n > 1 else -(-width // 8) * 8 for n, st in zip(t.shape[:-1], t.stride()))
+
+
+def _same_type(what: str, dtype: int, *tensors) -> None:
+    for t in tensors:
+        if t is not None and _dtype_of(t) != dtype:
+            raise TypeError("%s: %s beside %s" % (what, t.dtype, "bfloat16" if dtype == BF16 else "float32"))
+
+
+def norm(w_pre=None, *, b_pre=None, w_post=None, b_post=None, eps: float, w_offset: float = 0.0, kind: int = NORM_RMS,
+         h_scale: float = 1.0, y_scale: float = 1.0, d: Optional[int] = None, dtype: Optional[int] = None) -> griffin_norm:
+    """Describe the norms around a block ([d] weights and biases; w_pre in front of the next block, w_post behind this one)."""
+    some = w_pre if w_pre is not None else w_post
+    N = griffin_norm()
+    N.d = some.shape[0] if d is None else d
+    N.dtype = _dtype_of(some) if dtype is None else dtype
+    for name, t in (("w_pre", w_pre), ("b_pre", b_pre), ("w_post", w_post), ("b_post", b_post)):
+        if t is not None:
+            _shape("norm: " + name, t, N.d)
+            _same_type("norm: " + name, N.dtype, t)
+    N.kind, N.eps, N.w_offset, N.h_scale, N.y_scale = kind, eps, w_offset, h_scale, y_scale
+    N.w_pre, N.b_pre, N.w_post, N.b_post = _ptr(w_pre), _ptr(b_pre), _ptr(w_post), _ptr(b_post)
+    N._keep = (w_pre, b_pre, w_post, b_post)
+    return N
+
+
+def griffin_norm_residual(N: griffin_norm, h, y=None, h_out=None, x=None, *, gate=None, stream=None) -> None:
+    """h_out = h_scale h + y_scale gate N_post(y), x = N_pre(h_out); [rows][d] tensors, gate [d] or [rows][d]."""
+    rows = h.shape[0]
+    for name, t in (("h", h), ("y", y), ("h_out", h_out), ("x", x)):
+        if t is not None:
+            _shape("griffin_norm_residual: " + name, t, rows, N.d)
+    h_dtype = _dtype_of(h)
+    _same_type("griffin_norm_residual", N.dtype, y, gate, x)
+    _same_type("griffin_norm_residual", h_dtype, h_out)
+    ld = lambda t: _strides(t, N.d)[0]  # noqa: E731
+    ldg = 0
+    if gate is not None:
+        _shape("griffin_norm_residual: gate", gate, *((rows, N.d) if gate.dim() == 2 else (N.d,)))
+        ldg = ld(gate) if gate.dim() == 2 else 0
+    _check(lib.griffin_norm_residual(ctypes.byref(N), rows, _ptr(h), ld(h), h_dtype, _ptr(y), ld(y), _ptr(gate), ldg, _ptr(h_out),
+                                     ld(h_out), _ptr(x), ld(x), _stream(stream)), "griffin_norm_residual")
+
+
+def kv_cache(K, V) -> griffin_kv_cache:
+    """Describe pools of pages, K and V indexed [page][kv head][token][feature] with the same strides (a pool that holds
+    [page][token][kv head][feature] is given as pool.transpose(1, 2))."""
+    _shape("kv_cache: K", K, None, None, None, None)
+    _shape("kv_cache: V", V, *K.shape)
+    if K.stride() != V.stride():
+        raise ValueError("kv_cache: K and V have strides %s and %s" % (K.stride(), V.stride()))
+    C = griffin_kv_cache()
+    C.K, C.V, C.dtype = _ptr(K), _ptr(V), _dtype_of(K)
+    _same_type("kv_cache", C.dtype, V)
+    C.n_pages, C.kv_heads, C.page_size, C.dim = K.shape
+    C.page_stride, C.head_stride, C.token_stride = _strides(K, C.dim)
+    C._keep = (K, V)
+    return C
+
+
+def kv_batch(cu_seqlens: Sequence[int], lens, pages, max_len: int, *, prefix_pages=None, n_prefix: int = 0) -> griffin_kv_batch:
+    """Describe one step of a batch: its new tokens (host cu_seqlens), and on the device (int32) the sequences' own tokens in the cache,
+    their pages [n_seqs][..] and those of the prefix that they share."""
+    import torch
+    B = griffin_kv_batch()
+    B.n_seqs = len(cu_seqlens) - 1
+    for name, t in (("lens", lens), ("pages", pages), ("prefix_pages", prefix_pages)):
+        if t is not None and t.dtype != torch.int32:
+            raise TypeError("kv_batch: %s is %s, not int32" % (name, t.dtype))
+    _shape("kv_batch: lens", lens, B.n_seqs)
+    _shape("kv_batch: pages", pages, B.n_seqs, None)
+    arr = _cu_array(cu_seqlens)
+    B.cu_seqlens = ctypes.cast(arr, _IP)
+    B.max_len, B.lens, B.pages = max_len, _ptr(lens), _ptr(pages)
+    B.ld_pages = pages.shape[1] if B.n_seqs == 1 else pages.stride(0)
+    if pages.shape[1] > B.ld_pages:
+        raise ValueError("kv_batch: rows of pages overlap")
+    B.n_prefix, B.prefix_pages = n_prefix, _ptr(prefix_pages) if n_prefix > 0 else None
+    B._total, B._prefix_room = int(cu_seqlens[-1]), 0 if prefix_pages is None else prefix_pages.numel()
+    B._row_pages = pages.shape[1]
+    B._keep = (arr, lens, pages, prefix_pages)
+    return B
+
+
+def _check_room(where: str, C: griffin_kv_cache, B: griffin_kv_batch) -> None:
+    if B._row_pages * C.page_size < B.max_len or B._prefix_room * C.page_size < B.n_prefix:
+        raise ValueError("%s: fewer pages than max_len or n_prefix need" % where)
+
+
+def griffin_kv_append(C: griffin_kv_cache, B: griffin_kv_batch, k, v, *, q=None, q_out=None, cos=None, sin=None,
+                      style: int = ROT_HALF, stream=None) -> None:
+    """New keys (rotated) and values [tokens][kv_heads][dim] into their pages; queries [tokens][n_heads][dim] rotated into q_out.
+    cos, sin: fp32 [positions][rot / 2], None: nothing is rotated."""
+    where = "griffin_kv_append"
+    heads = 0 if q is None else q.shape[1]
+    for name, t, n in (("k", k, C.kv_heads), ("v", v, C.kv_heads), ("q", q, heads), ("q_out", q_out, heads)):
+        if t is not None:
+            _shape(where + ": " + name, t, B._total, n, C.dim)
+    _same_type(where, C.dtype, k, v, q, q_out)
+    _check_room(where, C, B)
+    rot = n_pos = 0
+    if cos is not None:
+        import torch
+        n_pos, rot = cos.shape[0], 2 * cos.shape[1]
+        if cos.dtype != torch.float32 or sin.dtype != torch.float32 or sin.shape != cos.shape or not cos.is_contiguous() or not sin.is_contiguous():
+            raise ValueError(where + ": cos and sin are not two dense float32 tables of one shape")
+    st = lambda t: _strides(t, C.dim)  # noqa: E731
+    _check(lib.griffin_kv_append(ctypes.byref(C), ctypes.byref(B), _ptr(k), *st(k), _ptr(v), *st(v), _ptr(q), *st(q), _ptr(q_out), *st(q_out),
+                                 heads, _ptr(cos), _ptr(sin), n_pos, rot, style, _stream(stream)), where)
+
+
+def griffin_attention_workspace_bytes(C: griffin_kv_cache, B: griffin_kv_batch, n_heads: int) -> int:
+    return int(lib.griffin_attention_workspace_bytes(ctypes.byref(C), ctypes.byref(B), n_heads))
+
+
+def griffin_attention(C: griffin_kv_cache, B: griffin_kv_batch, q, out, *, scale: Optional[float] = None, workspace=None, stream=None) -> None:
+    """out = softmax(scale q K^T) V over the shared prefix and the sequences' own tokens; q, out [tokens][n_heads][dim]."""
+    where = "griffin_attention"
+    heads = q.shape[1]
+    _shape(where + ": q", q, B._total, heads, C.dim)
+    _shape(where + ": out", out, B._total, heads, C.dim)
+    _same_type(where, C.dtype, q, out)
+    _check_room(where, C, B)
+    (ldq, hsq), (ldo, hso) = _strides(q, C.dim), _strides(out, C.dim)
+    _check(lib.griffin_attention(ctypes.byref(C), ctypes.byref(B), _ptr(q), ldq, hsq, _ptr(out), ldo, hso, heads,
+                                 C.dim ** -0.5 if scale is None else scale, _ptr(workspace), _nbytes(workspace), _stream(stream)), where)

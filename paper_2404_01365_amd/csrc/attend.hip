@@ -1,0 +1,712 @@
+// Attention of a step's new tokens over the prefix that all sequences share and over each sequence's own pages
+// (griffin_attention): o = sum_k softmax_k(scale q.k) v_k.
+//
+// One pass over the keys with the running maximum m and sum l of the softmax: a step forms the scores of a few keys, takes
+// m' = max(m, scores), scales o and l by 2^(m - m') and adds the step's weights and weighted values (exponents to base 2, the factor
+// log2(e) goes into the scale).  A row is a token and a head; the rows of all heads that share a kv head go together, and in the prefix those of all
+// sequences, so that keys and values are read once for 16 to 64 rows.
+//
+// A wavefront streams keys on its own, global memory -> registers -> matrix cores, no LDS.  Scores are formed transposed, S^T = K Q^T, with
+// keys as the rows of the A operand: the result's column, lane & 15, is the query row, so m, l and the factors are a lane's own.  The result's
+// rows are keys 4 (lane >> 4) .. + 3 of a tile of 16, and exactly these, as they stand, are the k positions that lane has to hold in the B operand of
+// O^T = V^T P^T, if V's A operand takes its keys in the same order.  That operand wants consecutive keys of one feature where memory has
+// consecutive features of one key: a lane loads the 8 x 8 block (keys x features) whose transpose is its share of eight A operands (row r of operand e:
+// feature 8 r + e) and turns it with 32 byte permutes.
+//
+// Long key ranges are cut into chunks for as many workgroups as fill the chip; each leaves its rows' o, m and l, and a second kernel joins them.
+#include "layer.h"
+
+namespace griffin {
+
+typedef __attribute__((ext_vector_type(4))) float att_f32x4;
+typedef __attribute__((ext_vector_type(8))) __bf16 att_bf16x8;
+typedef __attribute__((ext_vector_type(4))) uint32_t att_u32x4;
+
+constexpr int ATT_WAVES = 4;
+
+struct AttendParams {
+    const void *q, *K, *V;
+    void *out;
+    float *part;             // [tokens][n_heads][chunks][dim] unscaled sums, or NULL: one chunk, written to `out`
+    float2 *part_ml;         // [tokens][n_heads][chunks] maximum (base 2) and sum
+    const int32_t *lens, *pages, *prefix_pages;
+    int64_t ldq, hsq, ldo, hso, page_stride, head_stride, token_stride, ld_pages;
+    float scale2;            // scale log2(e)
+    int32_t n_heads, kv_heads, group, dim, page_shift, last_page, max_len, n_prefix;
+    int32_t chunk, chunks_prefix, chunks_own, tiles_prefix;   // keys a chunk (a multiple of a workgroup's step); row tiles of the prefix
+    SeqTable seqs;
+    int32_t tiles_own[GRIFFIN_MAX_SEQS + 1];                  // row tiles of the sequences before
+};
+
+// maximum over the lanes l, l ^ 16, l ^ 32, l ^ 48
+__device__ __forceinline__ float lane_groups_max(float v)
+{
+    typedef __attribute__((ext_vector_type(2))) uint32_t pair_t;
+    pair_t r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(r.x), __uint_as_float(r.y));
+    r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r.x), __uint_as_float(r.y));
+}
+
+// Shapes of a wavefront's step for one type and padded head width DB
+template <bool BF16, int DB>
+struct AttShape {
+    static constexpr int KT = BF16 ? 2 : 1;                // tiles of 16 keys a step
+    static constexpr int KS = 16 * KT;                     // keys a step
+    static constexpr int E = BF16 ? 8 : 4;                 // features in 16 bytes
+    static constexpr int NQ = DB / (4 * E);                // 16-byte pieces of a key that a lane holds (four lanes share a key)
+    static constexpr int VD = DB / 16 < E ? DB / 16 : E;   // consecutive features of a value that a lane holds
+    static constexpr int NC = DB / (16 * VD);              // ... and how many such runs, 16 VD apart
+    static constexpr int NO = NC * VD;                     // tiles of 16 features of the output
+    static constexpr int VK = BF16 ? 8 : 4;                // keys of a step whose values a lane holds
+    static constexpr int VW = BF16 ? VD / 2 : VD;          // words of such a run
+};
+
+// rows of one wavefront: their queries and where they end, and what it has summed
+template <bool BF16, int DB, int NT>
+struct AttRows {
+    using S = AttShape<BF16, DB>;
+    att_u32x4 q[NT][S::NQ];
+    int32_t end[NT];             // keys from here on are not seen by the lane's row
+    float m[NT], l[NT];
+    att_f32x4 o[NT][S::NO];
+};
+
+// a step's keys and values in registers
+template <bool BF16, int DB>
+struct AttKeys {
+    using S = AttShape<BF16, DB>;
+    att_u32x4 k[S::KT][S::NQ];
+};
+template <bool BF16, int DB>
+struct AttVals {
+    using S = AttShape<BF16, DB>;
+    uint32_t v[S::VK][S::NC][S::VW];
+};
+
+template <bool BF16, int DB, int NT>
+using AttScores = att_f32x4[NT][AttShape<BF16, DB>::KT];
+
+// where the tiles of a step lie: tile t's page and its first slot there, kept in range of the keys that there are
+struct AttTile {
+    int64_t base;                // elements from the head's begin
+    int32_t rows;                // its valid slots less one
+};
+
+__device__ __forceinline__ AttTile att_tile(const AttendParams &p, const int32_t *pages, int32_t key0, int32_t end)
+{
+    const int32_t last = (end - 1) & ~15;
+    key0 = key0 < last ? key0 : last;
+    key0 = __builtin_amdgcn_readfirstlane(key0);
+    AttTile t;
+    t.base = page_of(pages, key0 >> p.page_shift, p.last_page) * p.page_stride + (int64_t)(key0 & ((1 << p.page_shift) - 1)) * p.token_stride;
+    t.rows = end - 1 - key0 < 15 ? end - 1 - key0 : 15;
+    return t;
+}
+
+template <bool BF16, int DB, bool FULL>
+__device__ __forceinline__ void att_load_keys(AttKeys<BF16, DB> &f, const AttendParams &p, const char *Kh, const AttTile *t, int lane)
+{
+    using S = AttShape<BF16, DB>;
+#pragma unroll
+    for (int i = 0; i < S::KT; ++i) {
+        const int row = (lane & 15) < t[i].rows ? (lane & 15) : t[i].rows;
+        const char *at = Kh + (t[i].base + row * p.token_stride) * (BF16 ? 2 : 4) + (lane >> 4) * 16;
+#pragma unroll
+        for (int s = 0; s < S::NQ; ++s) {
+            // features from dim on are zero here and in the queries: they add nothing, whatever the row's gap holds
+            if (FULL || (s * 4 + (lane >> 4)) * S::E < p.dim)
+                f.k[i][s] = *(const att_u32x4 *)(at + s * 64);
+            else
+                f.k[i][s] = att_u32x4{0, 0, 0, 0};
+        }
+    }
+}
+
+template <bool BF16, int DB, bool FULL>
+__device__ __forceinline__ void att_load_vals(AttVals<BF16, DB> &f, const AttendParams &p, const char *Vh, const AttTile *t, int lane)
+{
+    using S = AttShape<BF16, DB>;
+#pragma unroll
+    for (int j = 0; j < S::VK; ++j) {
+        const int i = j >> 2, want = (lane >> 4) * 4 + (j & 3), row = want < t[i].rows ? want : t[i].rows;
+        const char *at = Vh + (t[i].base + row * p.token_stride) * (BF16 ? 2 : 4);
+#pragma unroll
+        for (int c = 0; c < S::NC; ++c) {
+            // features from dim on end in outputs that are not stored: any of the row's own will do
+            const int d0 = c * 16 * S::VD + (lane & 15) * S::VD, d = FULL || d0 < p.dim ? d0 : 0;
+            if (S::VW == 4)
+                *(att_u32x4 *)f.v[j][c] = *(const att_u32x4 *)(at + d * (BF16 ? 2 : 4));
+            else
+                *(uint2 *)f.v[j][c] = *(const uint2 *)(at + d * (BF16 ? 2 : 4));
+        }
+    }
+}
+
+template <bool BF16, int DB, int NT>
+__device__ __forceinline__ void att_scores(AttScores<BF16, DB, NT> &s, const AttKeys<BF16, DB> &f, const AttRows<BF16, DB, NT> &r)
+{
+    using S = AttShape<BF16, DB>;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < S::KT; ++i)
+            s[n][i] = att_f32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int c = 0; c < S::NQ; ++c)
+#pragma unroll
+        for (int i = 0; i < S::KT; ++i)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                if constexpr (BF16)
+                    s[n][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(att_bf16x8, f.k[i][c]), __builtin_bit_cast(att_bf16x8, r.q[n][c]),
+                                                                      s[n][i], 0, 0, 0);
+                else
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        s[n][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(f.k[i][c][e]), __uint_as_float(r.q[n][c][e]), s[n][i], 0, 0, 0);
+            }
+}
+
+// Scores to weights: the rows' maximum and sum carried on, o scaled to the new maximum.  MASKED: keys from r.end on get weight 0.
+template <bool BF16, int DB, int NT, bool MASKED>
+__device__ __forceinline__ void att_softmax(AttScores<BF16, DB, NT> &s, AttRows<BF16, DB, NT> &r, float scale2, int32_t key0, int lane)
+{
+    using S = AttShape<BF16, DB>;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < S::KT; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (MASKED && key0 + 16 * i + (lane >> 4) * 4 + e >= r.end[n])
+                    s[n][i][e] = -INFINITY;
+                top = fmaxf(top, s[n][i][e]);
+            }
+        const float m = fmaxf(r.m[n], lane_groups_max(top) * scale2);
+        const float base = m == -INFINITY ? 0.0f : m;          // nothing seen yet: weights 2^-inf = 0
+        const float f = exp2f(r.m[n] - base);
+        r.m[n] = m;
+        float l = 0;
+#pragma unroll
+        for (int i = 0; i < S::KT; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                s[n][i][e] = __builtin_amdgcn_exp2f(s[n][i][e] * scale2 - base);
+                l += s[n][i][e];
+            }
+        r.l[n] = r.l[n] * f + l;
+#pragma unroll
+        for (int c = 0; c < S::NO; ++c)
+            r.o[n][c] *= f;
+    }
+}
+
+// O^T += V^T P^T
+template <bool BF16, int DB, int NT>
+__device__ __forceinline__ void att_weigh(const AttScores<BF16, DB, NT> &s, const AttVals<BF16, DB> &f, AttRows<BF16, DB, NT> &r)
+{
+    using S = AttShape<BF16, DB>;
+    if constexpr (BF16) {
+        att_u32x4 w[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                w[n][2 * i] = f32x2_to_bf16x2(s[n][i][0], s[n][i][1]);
+                w[n][2 * i + 1] = f32x2_to_bf16x2(s[n][i][2], s[n][i][3]);
+            }
+#pragma unroll
+        for (int c = 0; c < S::NC; ++c)
+#pragma unroll
+            for (int e = 0; e < S::VD; ++e) {
+                att_u32x4 a;
+#pragma unroll
+                for (int h = 0; h < 4; ++h)        // feature e of keys 2h and 2h + 1
+                    a[h] = __builtin_amdgcn_perm(f.v[2 * h + 1][c][e / 2], f.v[2 * h][c][e / 2], e & 1 ? 0x07060302 : 0x05040100);
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+                    r.o[n][c * S::VD + e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(att_bf16x8, a), __builtin_bit_cast(att_bf16x8, w[n]),
+                                                                                   r.o[n][c * S::VD + e], 0, 0, 0);
+            }
+    } else {
+#pragma unroll
+        for (int c = 0; c < S::NC; ++c)
+#pragma unroll
+            for (int e = 0; e < S::VD; ++e)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+                        r.o[n][c * S::VD + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(f.v[i][c][e]), s[n][0][i], r.o[n][c * S::VD + e], 0, 0, 0);
+    }
+}
+
+template <bool BF16>
+__device__ __forceinline__ int att_key_of(int j, int lane) { return 16 * (j >> 2) + (lane >> 4) * 4 + (j & 3); }
+
+// Is any of the lane's values infinite or NaN (all exponent bits set)?
+template <bool BF16, int DB>
+__device__ __forceinline__ bool att_not_finite(const AttVals<BF16, DB> &f)
+{
+    using S = AttShape<BF16, DB>;
+    uint32_t any = 0;
+#pragma unroll
+    for (int j = 0; j < S::VK; ++j)
+#pragma unroll
+        for (int c = 0; c < S::NC; ++c)
+#pragma unroll
+            for (int w = 0; w < S::VW; ++w)
+                any |= BF16 ? (f.v[j][c][w] & 0x7F807F80u) + 0x00800080u : ((f.v[j][c][w] & 0x7F800000u) + 0x00800000u);
+    return (any & (BF16 ? 0x80008000u : 0x80000000u)) != 0;
+}
+
+// 1 (in the value's type) where a value is NaN or infinite with sign `minus`, else 0
+template <bool BF16>
+__device__ __forceinline__ uint32_t att_infinite(uint32_t w, bool minus)
+{
+    const auto one = [minus](uint32_t bits, uint32_t inf, uint32_t sign) {
+        const uint32_t size = bits & ~sign;
+        return size > inf || bits == (minus ? inf | sign : inf);
+    };
+    if (!BF16)
+        return one(w, 0x7F800000u, 0x80000000u) ? 0x3F800000u : 0;
+    return (one(w & 0xFFFF, 0x7F80, 0x8000) ? 0x3F80u : 0) | (one(w >> 16, 0x7F80, 0x8000) ? 0x3F800000u : 0);
+}
+
+template <bool BF16>
+__device__ __forceinline__ uint32_t att_finite_or_0(uint32_t w)
+{
+    if (!BF16)
+        return (w & 0x7F800000u) == 0x7F800000u ? 0 : w;
+    return ((w & 0x7F80u) == 0x7F80u ? 0 : w & 0xFFFFu) | ((w & 0x7F800000u) == 0x7F800000u ? 0 : w & 0xFFFF0000u);
+}
+
+// Where some rows see a key that others do not, an infinite or NaN value of it must not reach the others, as 0 x Inf in the second
+// product would.  Such values are counted, per row that sees them and by sign, in a product of ones; sums they are in become infinite or NaN
+// here, and the values zero for the product that follows.
+template <bool BF16, int DB, int NT>
+__device__ __forceinline__ void att_take_infinite(AttVals<BF16, DB> &f, AttRows<BF16, DB, NT> &r, int32_t key0, int lane)
+{
+    using S = AttShape<BF16, DB>;
+    for (int minus = 0; minus < 2; ++minus) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            att_u32x4 seen;
+            if (BF16)
+#pragma unroll
+                for (int h = 0; h < 4; ++h)
+                    seen[h] = (key0 + att_key_of<BF16>(2 * h, lane) < r.end[n] ? 0x3F80u : 0) |
+                              (key0 + att_key_of<BF16>(2 * h + 1, lane) < r.end[n] ? 0x3F800000u : 0);
+            else
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    seen[i] = key0 + att_key_of<BF16>(i, lane) < r.end[n] ? 0x3F800000u : 0;
+#pragma unroll
+            for (int c = 0; c < S::NC; ++c)
+#pragma unroll
+                for (int e = 0; e < S::VD; ++e) {
+                    att_f32x4 count = {0, 0, 0, 0};
+                    if constexpr (BF16) {
+                        att_u32x4 a;
+#pragma unroll
+                        for (int h = 0; h < 4; ++h)
+                            a[h] = att_infinite<true>(
+                                __builtin_amdgcn_perm(f.v[2 * h + 1][c][e / 2], f.v[2 * h][c][e / 2], e & 1 ? 0x07060302 : 0x05040100), minus);
+                        count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(att_bf16x8, a), __builtin_bit_cast(att_bf16x8, seen), count,
+                                                                        0, 0, 0);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            count = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(att_infinite<false>(f.v[i][c][e], minus)),
+                                                                         __uint_as_float(seen[i]), count, 0, 0, 0);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        r.o[n][c * S::VD + e][i] += count[i] > 0 ? (minus ? -INFINITY : INFINITY) : 0.0f;
+                }
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < S::VK; ++j)
+#pragma unroll
+        for (int c = 0; c < S::NC; ++c)
+#pragma unroll
+            for (int w = 0; w < S::VW; ++w)
+                f.v[j][c][w] = att_finite_or_0<BF16>(f.v[j][c][w]);
+}
+
+// Before a masked step's second product: values behind the last key become zero (0 x NaN is NaN), those that only some rows see are looked at
+template <bool BF16, int DB, int NT>
+__device__ __forceinline__ void att_mask_vals(AttVals<BF16, DB> &f, AttRows<BF16, DB, NT> &r, int32_t key0, int32_t end, int32_t least, int lane)
+{
+    using S = AttShape<BF16, DB>;
+    if (key0 + S::KS > end)
+#pragma unroll
+        for (int j = 0; j < S::VK; ++j) {
+            const bool in = key0 + att_key_of<BF16>(j, lane) < end;
+#pragma unroll
+            for (int c = 0; c < S::NC; ++c)
+#pragma unroll
+                for (int w = 0; w < S::VW; ++w)
+                    f.v[j][c][w] = in ? f.v[j][c][w] : 0;
+        }
+    if (__any(least < end && least < key0 + S::KS) && __any(att_not_finite<BF16, DB>(f)))
+        att_take_infinite<BF16, DB, NT>(f, r, key0, lane);
+}
+
+// Rows first .. first + 16 NT - 1 of the `rows` rows whose tokens begin at token0 (row = token * group + member of the group), against keys
+// [begin, end) of a list of pages, for kv head hk.  own: the position of token0 among its sequence's own tokens; -1: every row sees every key.
+template <bool BF16, int DB, bool FULL, int NT>
+__device__ __forceinline__ void attend_rows(const AttendParams &p, float *lds, const int32_t *pages, int32_t begin, int32_t end, int32_t own, int hk,
+                                            int32_t token0, int32_t rows, int32_t first, int32_t split)
+{
+    using S = AttShape<BF16, DB>;
+    constexpr int ES = BF16 ? 2 : 4;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    AttRows<BF16, DB, NT> r;
+    int32_t token[NT], head[NT];
+    int32_t least = end;                                   // keys that all of the lane's rows see
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        int32_t row = first + 16 * n + (lane & 15);
+        row = row < rows ? row : rows - 1;                 // rows behind the last repeat it and are not stored
+        token[n] = token0 + row / p.group;
+        head[n] = hk * p.group + row % p.group;
+        r.end[n] = end;
+        if (own >= 0) {
+            const int32_t sees = own + row / p.group + 1;
+            r.end[n] = sees < end ? sees : end;
+        }
+        least = r.end[n] < least ? r.end[n] : least;
+        const char *at = (const char *)p.q + ((int64_t)token[n] * p.ldq + (int64_t)head[n] * p.hsq) * ES + (lane >> 4) * 16;
+#pragma unroll
+        for (int s = 0; s < S::NQ; ++s) {
+            if (FULL || (s * 4 + (lane >> 4)) * S::E < p.dim)
+                r.q[n][s] = *(const att_u32x4 *)(at + s * 64);
+            else
+                r.q[n][s] = att_u32x4{0, 0, 0, 0};
+        }
+        r.m[n] = -INFINITY;
+        r.l[n] = 0;
+#pragma unroll
+        for (int c = 0; c < S::NO; ++c)
+            r.o[n][c] = att_f32x4{0, 0, 0, 0};
+    }
+    const char *Kh = (const char *)p.K + hk * p.head_stride * ES, *Vh = (const char *)p.V + hk * p.head_stride * ES;
+    int32_t key0 = begin + wave * S::KS;
+    if (key0 < end) {
+        AttKeys<BF16, DB> fk;
+        AttVals<BF16, DB> fv;
+        AttTile t[S::KT], next[S::KT];
+#pragma unroll
+        for (int i = 0; i < S::KT; ++i)
+            t[i] = att_tile(p, pages, key0 + 16 * i, end);
+        att_load_keys<BF16, DB, FULL>(fk, p, Kh, t, lane);
+        att_load_vals<BF16, DB, FULL>(fv, p, Vh, t, lane);
+        for (; key0 < end; key0 += ATT_WAVES * S::KS) {
+            // the next step's keys leave as soon as this step's scores have taken the registers' old content, its values after the second product;
+            // behind the last step they are the last tile's again
+#pragma unroll
+            for (int i = 0; i < S::KT; ++i)
+                next[i] = att_tile(p, pages, key0 + ATT_WAVES * S::KS + 16 * i, end);
+            att_f32x4 s[NT][S::KT];
+            att_scores<BF16, DB, NT>(s, fk, r);
+            __builtin_amdgcn_sched_barrier(0);
+            att_load_keys<BF16, DB, FULL>(fk, p, Kh, next, lane);
+            __builtin_amdgcn_sched_barrier(0);
+            if (__all(key0 + S::KS <= least))
+                att_softmax<BF16, DB, NT, false>(s, r, p.scale2, key0, lane);
+            else {
+                att_softmax<BF16, DB, NT, true>(s, r, p.scale2, key0, lane);
+                att_mask_vals<BF16, DB, NT>(fv, r, key0, end, least, lane);
+            }
+            att_weigh<BF16, DB, NT>(s, fv, r);
+            __builtin_amdgcn_sched_barrier(0);
+            att_load_vals<BF16, DB, FULL>(fv, p, Vh, next, lane);
+        }
+    }
+    // the four wavefronts' sums come together in two steps (2 and 3 to 0 and 1, then 1 to 0), lane by lane
+    float *mine = lds + (wave & 1) * (S::NO * 4 + 2) * 64;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        r.l[n] = lane_groups_sum(r.l[n]);
+#pragma unroll
+        for (int step = ATT_WAVES / 2; step >= 1; step >>= 1) {
+            __syncthreads();
+            if (wave >= step && wave < 2 * step) {
+#pragma unroll
+                for (int c = 0; c < S::NO; ++c)
+                    *(att_f32x4 *)(mine + c * 256 + lane * 4) = r.o[n][c];
+                mine[S::NO * 256 + lane] = r.m[n];
+                mine[S::NO * 256 + 64 + lane] = r.l[n];
+            }
+            __syncthreads();
+            if (wave < step) {
+                const float *from = lds + ((wave + step) & 1) * (S::NO * 4 + 2) * 64;
+                const float m2 = from[S::NO * 256 + lane], m = fmaxf(r.m[n], m2), base = m == -INFINITY ? 0.0f : m;
+                const float f1 = exp2f(r.m[n] - base), f2 = exp2f(m2 - base);
+                r.m[n] = m;
+                r.l[n] = r.l[n] * f1 + from[S::NO * 256 + 64 + lane] * f2;
+#pragma unroll
+                for (int c = 0; c < S::NO; ++c)
+                    r.o[n][c] = r.o[n][c] * f1 + *(const att_f32x4 *)(from + c * 256 + lane * 4) * f2;
+            }
+        }
+    }
+    if (wave != 0)
+        return;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        if (first + 16 * n + (lane & 15) >= rows)
+            continue;
+        const int64_t slot = ((int64_t)token[n] * p.n_heads + head[n]) * (p.chunks_prefix + p.chunks_own) + split;
+        const float f = p.part ? 1.0f : (r.l[n] == 0.0f ? 0.0f : 1.0f / r.l[n]);        // a row without keys: zeros
+        if (p.part && lane < 16)
+            p.part_ml[slot] = make_float2(r.m[n], r.l[n]);
+#pragma unroll
+        for (int c = 0; c < S::NC; ++c)
+#pragma unroll
+            for (int h = 0; h < S::VD / 2; ++h) {          // eight consecutive features of the lane's run of 4 VD
+                const int d = (c * 16 + (lane >> 4) * 4) * S::VD + h * 8;
+                if (!FULL && d >= p.dim)
+                    continue;
+                float x[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    x[j] = r.o[n][c * S::VD + (h * 8 + j) % S::VD][(h * 8 + j) / S::VD] * f;
+                if (p.part) {
+                    *(float4 *)(p.part + slot * p.dim + d) = make_float4(x[0], x[1], x[2], x[3]);
+                    *(float4 *)(p.part + slot * p.dim + d + 4) = make_float4(x[4], x[5], x[6], x[7]);
+                } else {
+                    char *at = (char *)p.out + ((int64_t)token[n] * p.ldo + (int64_t)head[n] * p.hso + d) * ES;
+                    if (BF16)
+                        *(uint4 *)at = make_uint4(f32x2_to_bf16x2(x[0], x[1]), f32x2_to_bf16x2(x[2], x[3]), f32x2_to_bf16x2(x[4], x[5]),
+                                                  f32x2_to_bf16x2(x[6], x[7]));
+                    else {
+                        *(float4 *)at = make_float4(x[0], x[1], x[2], x[3]);
+                        *(float4 *)(at + 16) = make_float4(x[4], x[5], x[6], x[7]);
+                    }
+                }
+            }
+    }
+}
+
+// Workgroups: first the prefix, [row tile][chunk][kv head], then the sequences' own parts, [row tile][chunk][kv head]
+template <bool BF16, int DB, bool FULL, int NTP, int NTO>
+__global__ __launch_bounds__(ATT_WAVES * 64) void attend_rows_kernel(AttendParams p)
+{
+    __shared__ float lds[2 * (AttShape<BF16, DB>::NO * 4 + 2) * 64];
+    const int32_t n_prefix_wgs = p.tiles_prefix * p.chunks_prefix * p.kv_heads;
+    int32_t id = blockIdx.x;
+    if (id < n_prefix_wgs) {
+        const int hk = id % p.kv_heads, chunk = id / p.kv_heads % p.chunks_prefix, tile = id / p.kv_heads / p.chunks_prefix;
+        const int32_t begin = chunk * p.chunk, end = begin + p.chunk < p.n_prefix ? begin + p.chunk : p.n_prefix;
+        attend_rows<BF16, DB, FULL, NTP>(p, lds, p.prefix_pages, begin, end, -1, hk, 0, p.seqs.cu[p.seqs.n] * p.group, tile * 16 * NTP, chunk);
+        return;
+    }
+    id -= n_prefix_wgs;
+    const int hk = id % p.kv_heads, chunk = id / p.kv_heads % p.chunks_own, tile = id / p.kv_heads / p.chunks_own;
+    int b = 0, hi = p.seqs.n - 1;                          // the last sequence whose tiles begin at or before this one
+    while (b < hi) {
+        const int mid = (b + hi + 1) / 2;
+        if (p.tiles_own[mid] <= tile) b = mid;
+        else hi = mid - 1;
+    }
+    const int32_t rows = (p.seqs.cu[b + 1] - p.seqs.cu[b]) * p.group, first = (tile - p.tiles_own[b]) * 16 * NTO;
+    const int32_t held = p.lens[b] < 0 ? 0 : (p.lens[b] < p.max_len ? p.lens[b] : p.max_len);
+    const int32_t last = first + 16 * NTO < rows ? first + 16 * NTO - 1 : rows - 1;       // the tile's last row sees the most keys
+    int32_t end = held + last / p.group + 1 < p.max_len ? held + last / p.group + 1 : p.max_len;
+    const int32_t begin = chunk * p.chunk;
+    end = begin + p.chunk < end ? begin + p.chunk : end;
+    if (begin >= end)                                      // no row reads this chunk's partial sums
+        return;
+    attend_rows<BF16, DB, FULL, NTO>(p, lds, p.pages + (int64_t)b * p.ld_pages, begin, end, held, hk, p.seqs.cu[b], rows, first,
+                                     p.chunks_prefix + chunk);
+}
+
+// Joins a row's chunks: with M = max m_c, o = sum o_c 2^(m_c - M) / sum l_c 2^(m_c - M).  A row per WPR wavefronts; a wavefront takes
+// 64 / (DB / 4) chunks at a time, four features a lane.
+template <bool BF16, int DB, int WPR>
+__global__ __launch_bounds__(256) void attend_join_kernel(AttendParams p)
+{
+    constexpr int LANES = DB / 4, PAR = 64 / LANES;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = lane / LANES, d = lane % LANES * 4;
+    const int64_t row = (int64_t)blockIdx.x * (4 / WPR) + (WPR == 1 ? wave : 0);
+    if (WPR == 1 && row >= (int64_t)p.seqs.cu[p.seqs.n] * p.n_heads)
+        return;
+    const int32_t token = __builtin_amdgcn_readfirstlane((int32_t)(row / p.n_heads)), head = __builtin_amdgcn_readfirstlane((int32_t)(row % p.n_heads));
+    int b = 0, hi = p.seqs.n - 1;                          // the last sequence that begins at or before the token
+    while (b < hi) {
+        const int mid = (b + hi + 1) / 2;
+        if (p.seqs.cu[mid] <= token) b = mid;
+        else hi = mid - 1;
+    }
+    const int32_t held = p.lens[b] < 0 ? 0 : (p.lens[b] < p.max_len ? p.lens[b] : p.max_len);
+    const int32_t seen = held + token - p.seqs.cu[b] + 1 < p.max_len ? held + token - p.seqs.cu[b] + 1 : p.max_len;
+    const int chunks = p.chunks_prefix + (seen + p.chunk - 1) / p.chunk;
+    const int64_t slot0 = row * (p.chunks_prefix + p.chunks_own);
+    float m = -INFINITY;
+    for (int c = lane; c < chunks; c += 64)
+        m = fmaxf(m, p.part_ml[slot0 + c].x);
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1)
+        m = fmaxf(m, __shfl_xor(m, off));
+    const float base = m == -INFINITY ? 0.0f : m;
+    float l = 0;
+    att_f32x4 o = {0, 0, 0, 0};
+    const bool in = d < p.dim;
+#pragma unroll 8
+    for (int c = (WPR == 1 ? 0 : wave * PAR) + sub; c < chunks; c += WPR * PAR) {
+        const float2 ml = p.part_ml[slot0 + c];
+        const float f = exp2f(ml.x - base);
+        l += ml.y * f;
+        if (in)
+            o += *(const att_f32x4 *)(p.part + (slot0 + c) * p.dim + d) * f;
+    }
+#pragma unroll
+    for (int off = LANES; off < 64; off <<= 1) {
+        l += __shfl_xor(l, off);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            o[e] += __shfl_xor(o[e], off);
+    }
+    if (WPR > 1) {
+        __shared__ float lds[WPR][LANES * 4 + 1];
+        if (sub == 0) {
+            *(float *)&lds[wave][0] = l;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                lds[wave][1 + d + e] = o[e];
+        }
+        __syncthreads();
+        if (wave != 0)
+            return;
+        l = 0;
+        o = att_f32x4{0, 0, 0, 0};
+        for (int w = 0; w < WPR; ++w) {
+            l += lds[w][0];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                o[e] += lds[w][1 + d + e];
+        }
+    }
+    if (sub != 0 || !in)
+        return;
+    const float f = l == 0.0f ? 0.0f : 1.0f / l;
+    const int64_t at = (int64_t)token * p.ldo + (int64_t)head * p.hso + d;
+    if (BF16)
+        *(uint2 *)((uint16_t *)p.out + at) = make_uint2(f32x2_to_bf16x2(o[0] * f, o[1] * f), f32x2_to_bf16x2(o[2] * f, o[3] * f));
+    else
+        *(att_f32x4 *)((float *)p.out + at) = o * f;
+}
+
+// ------------------------------------------------------------------ host side
+struct AttPlan {
+    int ntp, nto;                       // tiles of 16 rows a wavefront takes, of the prefix and of own parts
+    int32_t chunk, chunks_prefix, chunks_own, tiles_prefix, tiles_own;
+};
+
+static AttPlan attend_plan(const griffin_kv_cache &C, const griffin_kv_batch &B, const SeqTable &seqs, int32_t n_heads)
+{
+    AttPlan pl;
+    const bool bf16 = C.dtype == GRIFFIN_BF16;
+    const int widest = C.dim > 128 ? 1 : 2;
+    const int32_t group = n_heads / C.kv_heads;
+    const int64_t rows = (int64_t)seqs.cu[seqs.n] * group;
+    int64_t longest = 0;
+    for (int b = 0; b < seqs.n; ++b)
+        longest = std::max(longest, (int64_t)(seqs.cu[b + 1] - seqs.cu[b]) * group);
+    pl.nto = longest <= 32 ? 1 : widest;
+    pl.ntp = pl.nto > 1 ? pl.nto : (rows <= 16 ? 1 : (rows <= 32 ? 2 : widest));
+    int64_t tiles = 0;
+    for (int b = 0; b < seqs.n; ++b)
+        tiles += ((int64_t)(seqs.cu[b + 1] - seqs.cu[b]) * group + 16 * pl.nto - 1) / (16 * pl.nto);
+    pl.tiles_own = (int32_t)tiles;
+    pl.tiles_prefix = B.n_prefix > 0 ? (int32_t)((rows + 16 * pl.ntp - 1) / (16 * pl.ntp)) : 0;
+    // as many keys a chunk as leave about two workgroups a CU
+    const int64_t quantum = ATT_WAVES * (bf16 ? 32 : 16);
+    const int64_t work = C.kv_heads * (pl.tiles_prefix * (int64_t)B.n_prefix + tiles * B.max_len);
+    pl.chunk = (int32_t)((std::max(work / 512, (int64_t)1) + quantum - 1) / quantum * quantum);
+    pl.chunks_prefix = (B.n_prefix + pl.chunk - 1) / pl.chunk;
+    pl.chunks_own = (B.max_len + pl.chunk - 1) / pl.chunk;
+    return pl;
+}
+
+size_t attend_floats(const griffin_kv_cache &C, const griffin_kv_batch &B, const SeqTable &seqs, int32_t n_heads)
+{
+    const AttPlan pl = attend_plan(C, B, seqs, n_heads);
+    const size_t slots = (size_t)seqs.cu[seqs.n] * n_heads * (pl.chunks_prefix + pl.chunks_own);
+    return pl.chunks_prefix + pl.chunks_own < 2 ? 0 : slots * (C.dim + 2);
+}
+
+template <bool BF16, int DB, bool FULL, int NTP, int NTO>
+static int go_rows(const AttendParams &p, int32_t wgs, hipStream_t st)
+{
+    hipLaunchKernelGGL((attend_rows_kernel<BF16, DB, FULL, NTP, NTO>), dim3(wgs), dim3(ATT_WAVES * 64), 0, st, p);
+    return check_launch("attend_rows_kernel");
+}
+
+template <bool BF16, int DB>
+static int attend_typed(const AttendParams &p, const AttPlan &pl, int32_t wgs, hipStream_t st)
+{
+    int rc;
+#define ATT_GO(NTP, NTO) \
+    rc = p.dim == DB ? go_rows<BF16, DB, true, NTP, NTO>(p, wgs, st) : go_rows<BF16, DB, false, NTP, NTO>(p, wgs, st)
+    if constexpr (DB <= 128) {
+        if (pl.nto == 2) ATT_GO(2, 2);
+        else if (pl.ntp == 2) ATT_GO(2, 1);
+        else ATT_GO(1, 1);
+    } else
+        ATT_GO(1, 1);
+#undef ATT_GO
+    if (rc != GRIFFIN_OK || !p.part)
+        return rc;
+    const int64_t rows = (int64_t)p.seqs.cu[p.seqs.n] * p.n_heads;
+    // few rows of many chunks: four wavefronts a row
+    if (rows <= 2048 && pl.chunks_prefix + pl.chunks_own > 8)
+        hipLaunchKernelGGL((attend_join_kernel<BF16, DB, 4>), dim3((uint32_t)rows), dim3(256), 0, st, p);
+    else
+        hipLaunchKernelGGL((attend_join_kernel<BF16, DB, 1>), dim3((uint32_t)((rows + 3) / 4)), dim3(256), 0, st, p);
+    return check_launch("attend_join_kernel");
+}
+
+template <bool BF16>
+static int attend_width(const AttendParams &p, const AttPlan &pl, int32_t wgs, hipStream_t st)
+{
+    if (p.dim <= 64)
+        return attend_typed<BF16, 64>(p, pl, wgs, st);
+    return p.dim <= 128 ? attend_typed<BF16, 128>(p, pl, wgs, st) : attend_typed<BF16, 256>(p, pl, wgs, st);
+}
+
+int launch_attend(const AttendJob &job, const SeqTable &seqs, hipStream_t st)
+{
+    const griffin_kv_cache &C = job.C;
+    const griffin_kv_batch &B = job.B;
+    const AttPlan pl = attend_plan(C, B, seqs, job.n_heads);
+    const int64_t wgs = (int64_t)C.kv_heads * ((int64_t)pl.tiles_prefix * pl.chunks_prefix + (int64_t)pl.tiles_own * pl.chunks_own);
+    if (wgs >= 1 << 24 || (int64_t)seqs.cu[seqs.n] * job.n_heads >= 1 << 24)      // a launch holds fewer than 2^32 threads
+        return GRIFFIN_EUNSUPPORTED;
+    AttendParams p = {};
+    p.q = job.q; p.K = C.K; p.V = C.V; p.out = job.out;
+    if (pl.chunks_prefix + pl.chunks_own > 1) {
+        p.part = job.ws;
+        p.part_ml = (float2 *)(job.ws + (size_t)seqs.cu[seqs.n] * job.n_heads * (pl.chunks_prefix + pl.chunks_own) * C.dim);
+    }
+    p.lens = B.lens; p.pages = B.pages; p.prefix_pages = B.prefix_pages;
+    p.ldq = job.ldq; p.hsq = job.hsq; p.ldo = job.ldo; p.hso = job.hso;
+    p.page_stride = C.page_stride; p.head_stride = C.head_stride; p.token_stride = C.token_stride; p.ld_pages = B.ld_pages;
+    p.scale2 = job.scale * 1.4426950408889634f;
+    p.n_heads = job.n_heads; p.kv_heads = C.kv_heads; p.group = job.n_heads / C.kv_heads; p.dim = C.dim;
+    p.page_shift = __builtin_ctz(C.page_size);
+    p.last_page = (int32_t)(C.n_pages - 1);
+    p.max_len = B.max_len; p.n_prefix = B.n_prefix;
+    p.chunk = pl.chunk; p.chunks_prefix = pl.chunks_prefix; p.chunks_own = pl.chunks_own; p.tiles_prefix = pl.tiles_prefix;
+    p.seqs = seqs;
+    for (int b = 0; b < GRIFFIN_MAX_SEQS; ++b)
+        p.tiles_own[b + 1] = p.tiles_own[b] + (int32_t)(((int64_t)(seqs.cu[b + 1] - seqs.cu[b]) * p.group + 16 * pl.nto - 1) / (16 * pl.nto));
+    return C.dtype == GRIFFIN_BF16 ? attend_width<true>(p, pl, (int32_t)wgs, st) : attend_width<false>(p, pl, (int32_t)wgs, st);
+}
+
+}  // namespace griffin
