@@ -333,32 +333,67 @@ def griffin_ff_prompt_out(Z, W2p, Y, *, b2=None, dtype: Optional[int] = None, wo
 
 
 # ------------------------------------------------------------------ around the block
+# These calls are a few microseconds of work for one token, so their arguments are looked at once: every tensor's shape, type and
+# strides in one helper.
+_TORCH_TYPE = {}
+
+
+def _torch_type(dtype: int):
+    if not _TORCH_TYPE:
+        import torch
+        _TORCH_TYPE.update({F32: torch.float32, BF16: torch.bfloat16})
+    return _TORCH_TYPE[dtype]
+
+
 def _dtype_of(t) -> int:
-    import torch
-    if t.dtype == torch.bfloat16:
-        return BF16
-    if t.dtype == torch.float32:
-        return F32
+    for dtype in (BF16, F32):
+        if t.dtype is _torch_type(dtype):
+            return dtype
     raise TypeError("%s is neither float32 nor bfloat16" % t.dtype)
 
 
-def _shape(what: str, t, *sizes) -> None:
-    """Sizes (None: any) of a tensor whose last axis is dense; the library sees pointers and strides only."""
-    if t.dim() != len(sizes) or any(n is not None and m != n for m, n in zip(t.shape, sizes)) or (t.shape[-1] > 1 and t.stride(-1) != 1):
-        raise ValueError("%s: shape %s, strides %s" % (what, tuple(t.shape), t.stride()))
+def _refuse(what: str, t, shape, dtype) -> None:
+    if dtype is not None and t.dtype is not dtype:
+        raise TypeError("%s is %s, not %s" % (what, t.dtype, dtype))
+    raise ValueError("%s has shape %s and strides %s; shape %s with a dense last axis is needed"
+                     % (what, tuple(t.shape), t.stride(), tuple(shape)))
 
 
-def _strides(t, width: int):
-    """A tensor's strides but the last; an axis of one element has whatever stride it was made with, so a dense one is taken."""
+def _dense(width: int) -> int:
+    return -(-width // 8) * 8
+
+
+def _row(what: str, t, width: int, dtype):
+    """Address of a vector, or None."""
     if t is None:
-        return (0, 0)
-    return tuple(st if n > 1 else -(-width // 8) * 8 for n, st in zip(t.shape[:-1], t.stride()))
+        return None
+    if t.shape != (width,) or t.dtype is not dtype or (t.stride(0) != 1 and width > 1):
+        _refuse(what, t, (width,), dtype)
+    return t.data_ptr()
 
 
-def _same_type(what: str, dtype: int, *tensors) -> None:
-    for t in tensors:
-        if t is not None and _dtype_of(t) != dtype:
-            raise TypeError("%s: %s beside %s" % (what, t.dtype, "bfloat16" if dtype == BF16 else "float32"))
+def _mat(what: str, t, shape, dtype):
+    """Address and row stride of a matrix, or of None.  A single row has whatever stride it was made with: a dense one is taken."""
+    if t is None:
+        return None, 0
+    if t.shape != shape or t.dtype is not dtype:
+        _refuse(what, t, shape, dtype)
+    ld, one = t.stride()
+    if one != 1 and shape[1] > 1:
+        _refuse(what, t, shape, dtype)
+    return t.data_ptr(), ld if shape[0] > 1 else _dense(shape[1])
+
+
+def _heads(what: str, t, shape, dtype):
+    """Address, token stride and head stride of [tokens][heads][features], or of None."""
+    if t is None:
+        return None, 0, 0
+    if t.shape != shape or t.dtype is not dtype:
+        _refuse(what, t, shape, dtype)
+    ld, hs, one = t.stride()
+    if one != 1 and shape[2] > 1:
+        _refuse(what, t, shape, dtype)
+    return t.data_ptr(), ld if shape[0] > 1 else _dense(shape[2]), hs if shape[1] > 1 else _dense(shape[2])
 
 
 def norm(w_pre=None, *, b_pre=None, w_post=None, b_post=None, eps: float, w_offset: float = 0.0, kind: int = NORM_RMS,
@@ -368,46 +403,45 @@ def norm(w_pre=None, *, b_pre=None, w_post=None, b_post=None, eps: float, w_offs
     N = griffin_norm()
     N.d = some.shape[0] if d is None else d
     N.dtype = _dtype_of(some) if dtype is None else dtype
-    for name, t in (("w_pre", w_pre), ("b_pre", b_pre), ("w_post", w_post), ("b_post", b_post)):
-        if t is not None:
-            _shape("norm: " + name, t, N.d)
-            _same_type("norm: " + name, N.dtype, t)
+    N._type = _torch_type(N.dtype)
     N.kind, N.eps, N.w_offset, N.h_scale, N.y_scale = kind, eps, w_offset, h_scale, y_scale
-    N.w_pre, N.b_pre, N.w_post, N.b_post = _ptr(w_pre), _ptr(b_pre), _ptr(w_post), _ptr(b_post)
+    for name, t in (("w_pre", w_pre), ("b_pre", b_pre), ("w_post", w_post), ("b_post", b_post)):
+        setattr(N, name, _row("norm: " + name, t, N.d, N._type))
     N._keep = (w_pre, b_pre, w_post, b_post)
     return N
 
 
 def griffin_norm_residual(N: griffin_norm, h, y=None, h_out=None, x=None, *, gate=None, stream=None) -> None:
     """h_out = h_scale h + y_scale gate N_post(y), x = N_pre(h_out); [rows][d] tensors, gate [d] or [rows][d]."""
-    rows = h.shape[0]
-    for name, t in (("h", h), ("y", y), ("h_out", h_out), ("x", x)):
-        if t is not None:
-            _shape("griffin_norm_residual: " + name, t, rows, N.d)
-    h_dtype = _dtype_of(h)
-    _same_type("griffin_norm_residual", N.dtype, y, gate, x)
-    _same_type("griffin_norm_residual", h_dtype, h_out)
-    ld = lambda t: _strides(t, N.d)[0]  # noqa: E731
-    ldg = 0
-    if gate is not None:
-        _shape("griffin_norm_residual: gate", gate, *((rows, N.d) if gate.dim() == 2 else (N.d,)))
-        ldg = ld(gate) if gate.dim() == 2 else 0
-    _check(lib.griffin_norm_residual(ctypes.byref(N), rows, _ptr(h), ld(h), h_dtype, _ptr(y), ld(y), _ptr(gate), ldg, _ptr(h_out),
-                                     ld(h_out), _ptr(x), ld(x), _stream(stream)), "griffin_norm_residual")
+    shape, htype, dtype = (h.shape[0], N.d), h.dtype, N._type
+    if gate is None:
+        at_g, ldg = None, 0
+    elif gate.dim() == 2:
+        at_g, ldg = _mat("griffin_norm_residual: gate", gate, shape, dtype)
+    else:
+        at_g, ldg = _row("griffin_norm_residual: gate", gate, N.d, dtype), 0
+    at_h, ldh = _mat("griffin_norm_residual: h", h, shape, htype)
+    at_y, ldy = _mat("griffin_norm_residual: y", y, shape, dtype)
+    at_o, ldo = _mat("griffin_norm_residual: h_out", h_out, shape, htype)
+    at_x, ldx = _mat("griffin_norm_residual: x", x, shape, dtype)
+    _check(lib.griffin_norm_residual(N, shape[0], at_h, ldh, _dtype_of(h), at_y, ldy, at_g, ldg, at_o, ldo, at_x, ldx, _stream(stream)),
+           "griffin_norm_residual")
 
 
 def kv_cache(K, V) -> griffin_kv_cache:
     """Describe pools of pages, K and V indexed [page][kv head][token][feature] with the same strides (a pool that holds
     [page][token][kv head][feature] is given as pool.transpose(1, 2))."""
-    _shape("kv_cache: K", K, None, None, None, None)
-    _shape("kv_cache: V", V, *K.shape)
-    if K.stride() != V.stride():
-        raise ValueError("kv_cache: K and V have strides %s and %s" % (K.stride(), V.stride()))
     C = griffin_kv_cache()
-    C.K, C.V, C.dtype = _ptr(K), _ptr(V), _dtype_of(K)
-    _same_type("kv_cache", C.dtype, V)
+    C.dtype = _dtype_of(K)
+    C._type = _torch_type(C.dtype)
+    if K.dim() != 4 or (K.stride(3) != 1 and K.shape[3] > 1):
+        _refuse("kv_cache: K", K, (0, 0, 0, 0), None)
+    if V.shape != K.shape or V.dtype is not C._type or V.stride() != K.stride():
+        _refuse("kv_cache: V", V, K.shape, C._type)
+    C.K, C.V = _ptr(K), _ptr(V)
     C.n_pages, C.kv_heads, C.page_size, C.dim = K.shape
-    C.page_stride, C.head_stride, C.token_stride = _strides(K, C.dim)
+    C.page_stride, C.head_stride, C.token_stride = (st if n > 1 else _dense(C.dim) for n, st in zip(K.shape, K.stride()[:3]))
+    C._heads, C._dim = C.kv_heads, C.dim
     C._keep = (K, V)
     return C
 
@@ -417,27 +451,28 @@ def kv_batch(cu_seqlens: Sequence[int], lens, pages, max_len: int, *, prefix_pag
     their pages [n_seqs][..] and those of the prefix that they share."""
     import torch
     B = griffin_kv_batch()
-    B.n_seqs = len(cu_seqlens) - 1
-    for name, t in (("lens", lens), ("pages", pages), ("prefix_pages", prefix_pages)):
-        if t is not None and t.dtype != torch.int32:
-            raise TypeError("kv_batch: %s is %s, not int32" % (name, t.dtype))
-    _shape("kv_batch: lens", lens, B.n_seqs)
-    _shape("kv_batch: pages", pages, B.n_seqs, None)
+    B.n_seqs = n = len(cu_seqlens) - 1
     arr = _cu_array(cu_seqlens)
     B.cu_seqlens = ctypes.cast(arr, _IP)
-    B.max_len, B.lens, B.pages = max_len, _ptr(lens), _ptr(pages)
-    B.ld_pages = pages.shape[1] if B.n_seqs == 1 else pages.stride(0)
+    B.lens = _row("kv_batch: lens", lens, n, torch.int32)
+    B.pages, B.ld_pages = _mat("kv_batch: pages", pages, (n, pages.shape[-1]), torch.int32)
+    if n == 1:
+        B.ld_pages = pages.shape[1]
     if pages.shape[1] > B.ld_pages:
         raise ValueError("kv_batch: rows of pages overlap")
-    B.n_prefix, B.prefix_pages = n_prefix, _ptr(prefix_pages) if n_prefix > 0 else None
-    B._total, B._prefix_room = int(cu_seqlens[-1]), 0 if prefix_pages is None else prefix_pages.numel()
-    B._row_pages = pages.shape[1]
+    B.max_len, B.n_prefix = max_len, n_prefix
+    if n_prefix > 0 and prefix_pages is not None:
+        B.prefix_pages = _row("kv_batch: prefix_pages", prefix_pages, prefix_pages.numel(), torch.int32)
+    # what a call compares with a cache's page size
+    B._total, B._pages, B._max_len = int(cu_seqlens[-1]), pages.shape[1], max_len
+    B._prefix_pages, B._n_prefix = 0 if prefix_pages is None else prefix_pages.numel(), n_prefix
     B._keep = (arr, lens, pages, prefix_pages)
     return B
 
 
 def _check_room(where: str, C: griffin_kv_cache, B: griffin_kv_batch) -> None:
-    if B._row_pages * C.page_size < B.max_len or B._prefix_room * C.page_size < B.n_prefix:
+    size = C.page_size
+    if B._pages * size < B._max_len or B._prefix_pages * size < B._n_prefix:
         raise ValueError("%s: fewer pages than max_len or n_prefix need" % where)
 
 
@@ -445,22 +480,23 @@ def griffin_kv_append(C: griffin_kv_cache, B: griffin_kv_batch, k, v, *, q=None,
                       style: int = ROT_HALF, stream=None) -> None:
     """New keys (rotated) and values [tokens][kv_heads][dim] into their pages; queries [tokens][n_heads][dim] rotated into q_out.
     cos, sin: fp32 [positions][rot / 2], None: nothing is rotated."""
-    where = "griffin_kv_append"
-    heads = 0 if q is None else q.shape[1]
-    for name, t, n in (("k", k, C.kv_heads), ("v", v, C.kv_heads), ("q", q, heads), ("q_out", q_out, heads)):
-        if t is not None:
-            _shape(where + ": " + name, t, B._total, n, C.dim)
-    _same_type(where, C.dtype, k, v, q, q_out)
-    _check_room(where, C, B)
-    rot = n_pos = 0
+    dtype, tokens, dim = C._type, B._total, C._dim
+    kv, heads = (tokens, C._heads, dim), 0 if q is None else q.shape[1]
+    at_k, ldk, hsk = _heads("griffin_kv_append: k", k, kv, dtype)
+    at_v, ldv, hsv = _heads("griffin_kv_append: v", v, kv, dtype)
+    at_q, ldq, hsq = _heads("griffin_kv_append: q", q, (tokens, heads, dim), dtype)
+    at_o, ldo, hso = _heads("griffin_kv_append: q_out", q_out, (tokens, heads, dim), dtype)
+    _check_room("griffin_kv_append", C, B)
+    n_pos = half = 0
+    at_c = at_s = None
     if cos is not None:
-        import torch
-        n_pos, rot = cos.shape[0], 2 * cos.shape[1]
-        if cos.dtype != torch.float32 or sin.dtype != torch.float32 or sin.shape != cos.shape or not cos.is_contiguous() or not sin.is_contiguous():
-            raise ValueError(where + ": cos and sin are not two dense float32 tables of one shape")
-    st = lambda t: _strides(t, C.dim)  # noqa: E731
-    _check(lib.griffin_kv_append(ctypes.byref(C), ctypes.byref(B), _ptr(k), *st(k), _ptr(v), *st(v), _ptr(q), *st(q), _ptr(q_out), *st(q_out),
-                                 heads, _ptr(cos), _ptr(sin), n_pos, rot, style, _stream(stream)), where)
+        n_pos, half = shape = cos.shape
+        at_c, ldc = _mat("griffin_kv_append: cos", cos, shape, _torch_type(F32))
+        at_s, lds = _mat("griffin_kv_append: sin", sin, shape, _torch_type(F32))
+        if n_pos > 1 and (ldc != half or lds != half):
+            raise ValueError("griffin_kv_append: rows of cos and sin are not dense")
+    _check(lib.griffin_kv_append(C, B, at_k, ldk, hsk, at_v, ldv, hsv, at_q, ldq, hsq, at_o, ldo, hso, heads, at_c, at_s, n_pos, 2 * half,
+                                 style, _stream(stream)), "griffin_kv_append")
 
 
 def griffin_attention_workspace_bytes(C: griffin_kv_cache, B: griffin_kv_batch, n_heads: int) -> int:
@@ -469,12 +505,9 @@ def griffin_attention_workspace_bytes(C: griffin_kv_cache, B: griffin_kv_batch, 
 
 def griffin_attention(C: griffin_kv_cache, B: griffin_kv_batch, q, out, *, scale: Optional[float] = None, workspace=None, stream=None) -> None:
     """out = softmax(scale q K^T) V over the shared prefix and the sequences' own tokens; q, out [tokens][n_heads][dim]."""
-    where = "griffin_attention"
-    heads = q.shape[1]
-    _shape(where + ": q", q, B._total, heads, C.dim)
-    _shape(where + ": out", out, B._total, heads, C.dim)
-    _same_type(where, C.dtype, q, out)
-    _check_room(where, C, B)
-    (ldq, hsq), (ldo, hso) = _strides(q, C.dim), _strides(out, C.dim)
-    _check(lib.griffin_attention(ctypes.byref(C), ctypes.byref(B), _ptr(q), ldq, hsq, _ptr(out), ldo, hso, heads,
-                                 C.dim ** -0.5 if scale is None else scale, _ptr(workspace), _nbytes(workspace), _stream(stream)), where)
+    shape, dtype = (B._total, q.shape[1], C._dim), C._type
+    at_q, ldq, hsq = _heads("griffin_attention: q", q, shape, dtype)
+    at_o, ldo, hso = _heads("griffin_attention: out", out, shape, dtype)
+    _check_room("griffin_attention", C, B)
+    _check(lib.griffin_attention(C, B, at_q, ldq, hsq, at_o, ldo, hso, shape[1], shape[2] ** -0.5 if scale is None else scale, _ptr(workspace),
+                                 _nbytes(workspace), _stream(stream)), "griffin_attention")

@@ -14,39 +14,9 @@
 // feature 8 r + e) and turns it with 32 byte permutes.
 //
 // Long key ranges are cut into chunks for as many workgroups as fill the chip; each leaves its rows' o, m and l, and a second kernel joins them.
-#include "layer.h"
+#include "attend.h"
 
 namespace griffin {
-
-typedef __attribute__((ext_vector_type(4))) float att_f32x4;
-typedef __attribute__((ext_vector_type(8))) __bf16 att_bf16x8;
-typedef __attribute__((ext_vector_type(4))) uint32_t att_u32x4;
-
-constexpr int ATT_WAVES = 4;
-
-struct AttendParams {
-    const void *q, *K, *V;
-    void *out;
-    float *part;             // [tokens][n_heads][chunks][dim] unscaled sums, or NULL: one chunk, written to `out`
-    float2 *part_ml;         // [tokens][n_heads][chunks] maximum (base 2) and sum
-    const int32_t *lens, *pages, *prefix_pages;
-    int64_t ldq, hsq, ldo, hso, page_stride, head_stride, token_stride, ld_pages;
-    float scale2;            // scale log2(e)
-    int32_t n_heads, kv_heads, group, dim, page_shift, last_page, max_len, n_prefix;
-    int32_t chunk, chunks_prefix, chunks_own, tiles_prefix;   // keys a chunk (a multiple of a workgroup's step); row tiles of the prefix
-    SeqTable seqs;
-    int32_t tiles_own[GRIFFIN_MAX_SEQS + 1];                  // row tiles of the sequences before
-};
-
-// maximum over the lanes l, l ^ 16, l ^ 32, l ^ 48
-__device__ __forceinline__ float lane_groups_max(float v)
-{
-    typedef __attribute__((ext_vector_type(2))) uint32_t pair_t;
-    pair_t r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    v = fmaxf(__uint_as_float(r.x), __uint_as_float(r.y));
-    r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return fmaxf(__uint_as_float(r.x), __uint_as_float(r.y));
-}
 
 // Shapes of a wavefront's step for one type and padded head width DB
 template <bool BF16, int DB>
@@ -86,23 +56,6 @@ struct AttVals {
 
 template <bool BF16, int DB, int NT>
 using AttScores = att_f32x4[NT][AttShape<BF16, DB>::KT];
-
-// where the tiles of a step lie: tile t's page and its first slot there, kept in range of the keys that there are
-struct AttTile {
-    int64_t base;                // elements from the head's begin
-    int32_t rows;                // its valid slots less one
-};
-
-__device__ __forceinline__ AttTile att_tile(const AttendParams &p, const int32_t *pages, int32_t key0, int32_t end)
-{
-    const int32_t last = (end - 1) & ~15;
-    key0 = key0 < last ? key0 : last;
-    key0 = __builtin_amdgcn_readfirstlane(key0);
-    AttTile t;
-    t.base = page_of(pages, key0 >> p.page_shift, p.last_page) * p.page_stride + (int64_t)(key0 & ((1 << p.page_shift) - 1)) * p.token_stride;
-    t.rows = end - 1 - key0 < 15 ? end - 1 - key0 : 15;
-    return t;
-}
 
 template <bool BF16, int DB, bool FULL>
 __device__ __forceinline__ void att_load_keys(AttKeys<BF16, DB> &f, const AttendParams &p, const char *Kh, const AttTile *t, int lane)
@@ -262,27 +215,6 @@ __device__ __forceinline__ bool att_not_finite(const AttVals<BF16, DB> &f)
     return (any & (BF16 ? 0x80008000u : 0x80000000u)) != 0;
 }
 
-// 1 (in the value's type) where a value is NaN or infinite with sign `minus`, else 0
-template <bool BF16>
-__device__ __forceinline__ uint32_t att_infinite(uint32_t w, bool minus)
-{
-    const auto one = [minus](uint32_t bits, uint32_t inf, uint32_t sign) {
-        const uint32_t size = bits & ~sign;
-        return size > inf || bits == (minus ? inf | sign : inf);
-    };
-    if (!BF16)
-        return one(w, 0x7F800000u, 0x80000000u) ? 0x3F800000u : 0;
-    return (one(w & 0xFFFF, 0x7F80, 0x8000) ? 0x3F80u : 0) | (one(w >> 16, 0x7F80, 0x8000) ? 0x3F800000u : 0);
-}
-
-template <bool BF16>
-__device__ __forceinline__ uint32_t att_finite_or_0(uint32_t w)
-{
-    if (!BF16)
-        return (w & 0x7F800000u) == 0x7F800000u ? 0 : w;
-    return ((w & 0x7F80u) == 0x7F80u ? 0 : w & 0xFFFFu) | ((w & 0x7F800000u) == 0x7F800000u ? 0 : w & 0xFFFF0000u);
-}
-
 // Where some rows see a key that others do not, an infinite or NaN value of it must not reach the others, as 0 x Inf in the second
 // product would.  Such values are counted, per row that sees them and by sign, in a product of ones; sums they are in become infinite or NaN
 // here, and the values zero for the product that follows.
@@ -307,6 +239,7 @@ __device__ __forceinline__ void att_take_infinite(AttVals<BF16, DB> &f, AttRows<
             for (int c = 0; c < S::NC; ++c)
 #pragma unroll
                 for (int e = 0; e < S::VD; ++e) {
+                    __builtin_amdgcn_sched_barrier(0);         // one at a time: this is not where registers are to go
                     att_f32x4 count = {0, 0, 0, 0};
                     if constexpr (BF16) {
                         att_u32x4 a;
@@ -356,14 +289,14 @@ __device__ __forceinline__ void att_mask_vals(AttVals<BF16, DB> &f, AttRows<BF16
         att_take_infinite<BF16, DB, NT>(f, r, key0, lane);
 }
 
-// Rows first .. first + 16 NT - 1 of the `rows` rows whose tokens begin at token0 (row = token * group + member of the group), against keys
-// [begin, end) of a list of pages, for kv head hk.  own: the position of token0 among its sequence's own tokens; -1: every row sees every key.
+// The item's rows first .. first + 16 NT - 1
 template <bool BF16, int DB, bool FULL, int NT>
-__device__ __forceinline__ void attend_rows(const AttendParams &p, float *lds, const int32_t *pages, int32_t begin, int32_t end, int32_t own, int hk,
-                                            int32_t token0, int32_t rows, int32_t first, int32_t split)
+__device__ __forceinline__ void attend_rows(const AttendParams &p, float *lds, const AttendItem &it)
 {
     using S = AttShape<BF16, DB>;
     constexpr int ES = BF16 ? 2 : 4;
+    const int32_t begin = it.begin, end = it.end, own = it.own, rows = it.rows, first = it.first, hk = it.hk;
+    const int32_t *pages = it.pages;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     AttRows<BF16, DB, NT> r;
     int32_t token[NT], head[NT];
@@ -372,7 +305,7 @@ __device__ __forceinline__ void attend_rows(const AttendParams &p, float *lds, c
     for (int n = 0; n < NT; ++n) {
         int32_t row = first + 16 * n + (lane & 15);
         row = row < rows ? row : rows - 1;                 // rows behind the last repeat it and are not stored
-        token[n] = token0 + row / p.group;
+        token[n] = it.token0 + row / p.group;
         head[n] = hk * p.group + row % p.group;
         r.end[n] = end;
         if (own >= 0) {
@@ -461,7 +394,7 @@ __device__ __forceinline__ void attend_rows(const AttendParams &p, float *lds, c
     for (int n = 0; n < NT; ++n) {
         if (first + 16 * n + (lane & 15) >= rows)
             continue;
-        const int64_t slot = ((int64_t)token[n] * p.n_heads + head[n]) * (p.chunks_prefix + p.chunks_own) + split;
+        const int64_t slot = ((int64_t)token[n] * p.n_heads + head[n]) * (p.chunks_prefix + p.chunks_own) + it.split;
         const float f = p.part ? 1.0f : (r.l[n] == 0.0f ? 0.0f : 1.0f / r.l[n]);        // a row without keys: zeros
         if (p.part && lane < 16)
             p.part_ml[slot] = make_float2(r.m[n], r.l[n]);
@@ -493,37 +426,17 @@ __device__ __forceinline__ void attend_rows(const AttendParams &p, float *lds, c
     }
 }
 
-// Workgroups: first the prefix, [row tile][chunk][kv head], then the sequences' own parts, [row tile][chunk][kv head]
 template <bool BF16, int DB, bool FULL, int NTP, int NTO>
 __global__ __launch_bounds__(ATT_WAVES * 64) void attend_rows_kernel(AttendParams p)
 {
     __shared__ float lds[2 * (AttShape<BF16, DB>::NO * 4 + 2) * 64];
-    const int32_t n_prefix_wgs = p.tiles_prefix * p.chunks_prefix * p.kv_heads;
-    int32_t id = blockIdx.x;
-    if (id < n_prefix_wgs) {
-        const int hk = id % p.kv_heads, chunk = id / p.kv_heads % p.chunks_prefix, tile = id / p.kv_heads / p.chunks_prefix;
-        const int32_t begin = chunk * p.chunk, end = begin + p.chunk < p.n_prefix ? begin + p.chunk : p.n_prefix;
-        attend_rows<BF16, DB, FULL, NTP>(p, lds, p.prefix_pages, begin, end, -1, hk, 0, p.seqs.cu[p.seqs.n] * p.group, tile * 16 * NTP, chunk);
+    AttendItem it;
+    if (!att_item<16 * NTP, 16 * NTO, false>(p, blockIdx.x, it))
         return;
-    }
-    id -= n_prefix_wgs;
-    const int hk = id % p.kv_heads, chunk = id / p.kv_heads % p.chunks_own, tile = id / p.kv_heads / p.chunks_own;
-    int b = 0, hi = p.seqs.n - 1;                          // the last sequence whose tiles begin at or before this one
-    while (b < hi) {
-        const int mid = (b + hi + 1) / 2;
-        if (p.tiles_own[mid] <= tile) b = mid;
-        else hi = mid - 1;
-    }
-    const int32_t rows = (p.seqs.cu[b + 1] - p.seqs.cu[b]) * p.group, first = (tile - p.tiles_own[b]) * 16 * NTO;
-    const int32_t held = p.lens[b] < 0 ? 0 : (p.lens[b] < p.max_len ? p.lens[b] : p.max_len);
-    const int32_t last = first + 16 * NTO < rows ? first + 16 * NTO - 1 : rows - 1;       // the tile's last row sees the most keys
-    int32_t end = held + last / p.group + 1 < p.max_len ? held + last / p.group + 1 : p.max_len;
-    const int32_t begin = chunk * p.chunk;
-    end = begin + p.chunk < end ? begin + p.chunk : end;
-    if (begin >= end)                                      // no row reads this chunk's partial sums
-        return;
-    attend_rows<BF16, DB, FULL, NTO>(p, lds, p.pages + (int64_t)b * p.ld_pages, begin, end, held, hk, p.seqs.cu[b], rows, first,
-                                     p.chunks_prefix + chunk);
+    if (NTP != NTO && it.own < 0)
+        attend_rows<BF16, DB, FULL, NTP>(p, lds, it);
+    else
+        attend_rows<BF16, DB, FULL, NTO>(p, lds, it);
 }
 
 // Joins a row's chunks: with M = max m_c, o = sum o_c 2^(m_c - M) / sum l_c 2^(m_c - M).  A row per WPR wavefronts; a wavefront takes
@@ -545,7 +458,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendParams p)
     }
     const int32_t held = p.lens[b] < 0 ? 0 : (p.lens[b] < p.max_len ? p.lens[b] : p.max_len);
     const int32_t seen = held + token - p.seqs.cu[b] + 1 < p.max_len ? held + token - p.seqs.cu[b] + 1 : p.max_len;
-    const int chunks = p.chunks_prefix + (seen + p.chunk - 1) / p.chunk;
+    const int chunks = p.chunks_prefix + (seen + p.chunk_own - 1) / p.chunk_own;
     const int64_t slot0 = row * (p.chunks_prefix + p.chunks_own);
     float m = -INFINITY;
     for (int c = lane; c < chunks; c += 64)
@@ -604,33 +517,48 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendParams p)
 
 // ------------------------------------------------------------------ host side
 struct AttPlan {
-    int ntp, nto;                       // tiles of 16 rows a wavefront takes, of the prefix and of own parts
-    int32_t chunk, chunks_prefix, chunks_own, tiles_prefix, tiles_own;
+    bool tile_prefix, tile_own;         // many rows: attend_tile.hip
+    int ntp, nto;                       // else tiles of 16 rows that a wavefront takes
+    int32_t rows_prefix, rows_own;      // rows of a workgroup
+    int32_t chunk_prefix, chunk_own, chunks_prefix, chunks_own, tiles_prefix, tiles_own;
 };
 
 static AttPlan attend_plan(const griffin_kv_cache &C, const griffin_kv_batch &B, const SeqTable &seqs, int32_t n_heads)
 {
     AttPlan pl;
     const bool bf16 = C.dtype == GRIFFIN_BF16;
-    const int widest = C.dim > 128 ? 1 : 2;
+    const int widest = C.dim > 128 ? 1 : 2;                // what the registers hold beside a step's keys and values
     const int32_t group = n_heads / C.kv_heads;
     const int64_t rows = (int64_t)seqs.cu[seqs.n] * group;
     int64_t longest = 0;
     for (int b = 0; b < seqs.n; ++b)
         longest = std::max(longest, (int64_t)(seqs.cu[b + 1] - seqs.cu[b]) * group);
+    pl.tile_own = bf16 && longest > 64;
+    pl.tile_prefix = bf16 && rows > 64;
     pl.nto = longest <= 32 ? 1 : widest;
-    pl.ntp = pl.nto > 1 ? pl.nto : (rows <= 16 ? 1 : (rows <= 32 ? 2 : widest));
+    pl.ntp = rows <= 16 ? 1 : widest;
+    if (!pl.tile_own && !pl.tile_prefix && B.n_prefix > 0)
+        pl.ntp = std::max(pl.nto, pl.ntp);
+    pl.rows_own = pl.tile_own ? att_tile_rows(C.dim) : 16 * pl.nto;
+    pl.rows_prefix = pl.tile_prefix ? att_tile_rows(C.dim) : 16 * pl.ntp;
     int64_t tiles = 0;
     for (int b = 0; b < seqs.n; ++b)
-        tiles += ((int64_t)(seqs.cu[b + 1] - seqs.cu[b]) * group + 16 * pl.nto - 1) / (16 * pl.nto);
+        tiles += ((int64_t)(seqs.cu[b + 1] - seqs.cu[b]) * group + pl.rows_own - 1) / pl.rows_own;
     pl.tiles_own = (int32_t)tiles;
-    pl.tiles_prefix = B.n_prefix > 0 ? (int32_t)((rows + 16 * pl.ntp - 1) / (16 * pl.ntp)) : 0;
-    // as many keys a chunk as leave about two workgroups a CU
-    const int64_t quantum = ATT_WAVES * (bf16 ? 32 : 16);
-    const int64_t work = C.kv_heads * (pl.tiles_prefix * (int64_t)B.n_prefix + tiles * B.max_len);
-    pl.chunk = (int32_t)((std::max(work / 512, (int64_t)1) + quantum - 1) / quantum * quantum);
-    pl.chunks_prefix = (B.n_prefix + pl.chunk - 1) / pl.chunk;
-    pl.chunks_own = (B.max_len + pl.chunk - 1) / pl.chunk;
+    pl.tiles_prefix = B.n_prefix > 0 ? (int32_t)((rows + pl.rows_prefix - 1) / pl.rows_prefix) : 0;
+    // as many keys a chunk as leave a workgroup a CU, or two of the smaller ones; own parts of many rows are one chunk if they fill the chip
+    const int64_t step = ATT_WAVES * (bf16 ? 32 : 16);
+    const int64_t work_prefix = C.kv_heads * (int64_t)pl.tiles_prefix * B.n_prefix, work_own = C.kv_heads * tiles * B.max_len;
+    const auto chunk = [&](bool tile, int64_t work) {
+        const int64_t quantum = tile ? ATT_TILE_KEYS : step;
+        return (int32_t)((std::max(work / (tile ? 256 : 512), (int64_t)1) + quantum - 1) / quantum * quantum);
+    };
+    pl.chunk_prefix = chunk(pl.tile_prefix, pl.tile_prefix == pl.tile_own ? work_prefix + work_own : work_prefix);
+    pl.chunk_own = chunk(pl.tile_own, pl.tile_prefix == pl.tile_own ? work_prefix + work_own : work_own);
+    if (pl.tile_own && C.kv_heads * tiles >= 256)
+        pl.chunk_own = (B.max_len + ATT_TILE_KEYS - 1) / ATT_TILE_KEYS * ATT_TILE_KEYS;
+    pl.chunks_prefix = (B.n_prefix + pl.chunk_prefix - 1) / pl.chunk_prefix;
+    pl.chunks_own = (B.max_len + pl.chunk_own - 1) / pl.chunk_own;
     return pl;
 }
 
@@ -641,26 +569,43 @@ size_t attend_floats(const griffin_kv_cache &C, const griffin_kv_batch &B, const
     return pl.chunks_prefix + pl.chunks_own < 2 ? 0 : slots * (C.dim + 2);
 }
 
-template <bool BF16, int DB, bool FULL, int NTP, int NTO>
+template <bool BF16, int DB, int NTP, int NTO>
 static int go_rows(const AttendParams &p, int32_t wgs, hipStream_t st)
 {
-    hipLaunchKernelGGL((attend_rows_kernel<BF16, DB, FULL, NTP, NTO>), dim3(wgs), dim3(ATT_WAVES * 64), 0, st, p);
+    if (p.dim == DB)
+        hipLaunchKernelGGL((attend_rows_kernel<BF16, DB, true, NTP, NTO>), dim3(wgs), dim3(ATT_WAVES * 64), 0, st, p);
+    else
+        hipLaunchKernelGGL((attend_rows_kernel<BF16, DB, false, NTP, NTO>), dim3(wgs), dim3(ATT_WAVES * 64), 0, st, p);
     return check_launch("attend_rows_kernel");
 }
 
 template <bool BF16, int DB>
-static int attend_typed(const AttendParams &p, const AttPlan &pl, int32_t wgs, hipStream_t st)
+static int launch_rows(const AttendParams &p, int ntp, int nto, int32_t wgs, hipStream_t st)
 {
-    int rc;
-#define ATT_GO(NTP, NTO) \
-    rc = p.dim == DB ? go_rows<BF16, DB, true, NTP, NTO>(p, wgs, st) : go_rows<BF16, DB, false, NTP, NTO>(p, wgs, st)
     if constexpr (DB <= 128) {
-        if (pl.nto == 2) ATT_GO(2, 2);
-        else if (pl.ntp == 2) ATT_GO(2, 1);
-        else ATT_GO(1, 1);
-    } else
-        ATT_GO(1, 1);
-#undef ATT_GO
+        if (nto == 2)
+            return go_rows<BF16, DB, 2, 2>(p, wgs, st);
+        if (ntp == 2)
+            return go_rows<BF16, DB, 2, 1>(p, wgs, st);
+    }
+    return go_rows<BF16, DB, 1, 1>(p, wgs, st);
+}
+
+template <bool BF16, int DB>
+static int attend_typed(AttendParams &p, const AttPlan &pl, hipStream_t st)
+{
+    int rc = GRIFFIN_OK;
+    const int32_t wgs_prefix = p.kv_heads * pl.tiles_prefix * pl.chunks_prefix, wgs_own = p.kv_heads * pl.tiles_own * pl.chunks_own;
+    const int32_t tiled = (pl.tile_prefix ? wgs_prefix : 0) + (pl.tile_own ? wgs_own : 0), others = wgs_prefix + wgs_own - tiled;
+    if constexpr (BF16)
+        if (tiled > 0) {
+            p.wgs_prefix = pl.tile_prefix ? wgs_prefix : 0;
+            rc = launch_attend_tiles(p, tiled, st);
+        }
+    if (rc == GRIFFIN_OK && others > 0) {
+        p.wgs_prefix = pl.tile_prefix ? 0 : wgs_prefix;
+        rc = launch_rows<BF16, DB>(p, pl.tile_prefix || wgs_prefix == 0 ? pl.nto : pl.ntp, pl.tile_own ? 1 : pl.nto, others, st);
+    }
     if (rc != GRIFFIN_OK || !p.part)
         return rc;
     const int64_t rows = (int64_t)p.seqs.cu[p.seqs.n] * p.n_heads;
@@ -673,11 +618,11 @@ static int attend_typed(const AttendParams &p, const AttPlan &pl, int32_t wgs, h
 }
 
 template <bool BF16>
-static int attend_width(const AttendParams &p, const AttPlan &pl, int32_t wgs, hipStream_t st)
+static int attend_width(AttendParams &p, const AttPlan &pl, hipStream_t st)
 {
     if (p.dim <= 64)
-        return attend_typed<BF16, 64>(p, pl, wgs, st);
-    return p.dim <= 128 ? attend_typed<BF16, 128>(p, pl, wgs, st) : attend_typed<BF16, 256>(p, pl, wgs, st);
+        return attend_typed<BF16, 64>(p, pl, st);
+    return p.dim <= 128 ? attend_typed<BF16, 128>(p, pl, st) : attend_typed<BF16, 256>(p, pl, st);
 }
 
 int launch_attend(const AttendJob &job, const SeqTable &seqs, hipStream_t st)
@@ -686,7 +631,7 @@ int launch_attend(const AttendJob &job, const SeqTable &seqs, hipStream_t st)
     const griffin_kv_batch &B = job.B;
     const AttPlan pl = attend_plan(C, B, seqs, job.n_heads);
     const int64_t wgs = (int64_t)C.kv_heads * ((int64_t)pl.tiles_prefix * pl.chunks_prefix + (int64_t)pl.tiles_own * pl.chunks_own);
-    if (wgs >= 1 << 24 || (int64_t)seqs.cu[seqs.n] * job.n_heads >= 1 << 24)      // a launch holds fewer than 2^32 threads
+    if (wgs >= 1 << 23 || (int64_t)seqs.cu[seqs.n] * job.n_heads >= 1 << 24)      // a launch holds fewer than 2^32 threads
         return GRIFFIN_EUNSUPPORTED;
     AttendParams p = {};
     p.q = job.q; p.K = C.K; p.V = C.V; p.out = job.out;
@@ -702,11 +647,12 @@ int launch_attend(const AttendJob &job, const SeqTable &seqs, hipStream_t st)
     p.page_shift = __builtin_ctz(C.page_size);
     p.last_page = (int32_t)(C.n_pages - 1);
     p.max_len = B.max_len; p.n_prefix = B.n_prefix;
-    p.chunk = pl.chunk; p.chunks_prefix = pl.chunks_prefix; p.chunks_own = pl.chunks_own; p.tiles_prefix = pl.tiles_prefix;
+    p.chunk_prefix = pl.chunk_prefix; p.chunk_own = pl.chunk_own;
+    p.chunks_prefix = pl.chunks_prefix; p.chunks_own = pl.chunks_own; p.tiles_prefix = pl.tiles_prefix;
     p.seqs = seqs;
     for (int b = 0; b < GRIFFIN_MAX_SEQS; ++b)
-        p.tiles_own[b + 1] = p.tiles_own[b] + (int32_t)(((int64_t)(seqs.cu[b + 1] - seqs.cu[b]) * p.group + 16 * pl.nto - 1) / (16 * pl.nto));
-    return C.dtype == GRIFFIN_BF16 ? attend_width<true>(p, pl, (int32_t)wgs, st) : attend_width<false>(p, pl, (int32_t)wgs, st);
+        p.tiles_own[b + 1] = p.tiles_own[b] + (int32_t)(((int64_t)(seqs.cu[b + 1] - seqs.cu[b]) * p.group + pl.rows_own - 1) / pl.rows_own);
+    return C.dtype == GRIFFIN_BF16 ? attend_width<true>(p, pl, st) : attend_width<false>(p, pl, st);
 }
 
 }  // namespace griffin
