@@ -11,8 +11,14 @@ typedef __attribute__((ext_vector_type(8))) __bf16 att_bf16x8;
 typedef __attribute__((ext_vector_type(4))) uint32_t att_u32x4;
 
 constexpr int ATT_WAVES = 4;            // of a workgroup of attend.hip
-constexpr int ATT_TILE_WAVES = 8;       // ... of attend_tile.hip
-constexpr int ATT_TILE_KEYS = 64;       // its step
+#ifndef TW
+#define TW 8
+#define TK 64
+#define TN 1
+#endif
+constexpr int ATT_TILE_WAVES = TW;       // ... of attend_tile.hip
+constexpr int ATT_TILE_KEYS = TK;       // its step
+constexpr int ATT_TILE_NT = TN;
 
 struct AttendParams {
     const void *q, *K, *V;
@@ -64,25 +70,10 @@ __device__ __forceinline__ AttTile att_tile(const AttendParams &p, const int32_t
     return t;
 }
 
-// 1 (in the value's type) where a value is NaN or infinite with sign `minus`, else 0
-template <bool BF16>
-__device__ __forceinline__ uint32_t att_infinite(uint32_t w, bool minus)
+// All bits of the two bf16 in a word that are neither infinite nor NaN (an exponent of all ones)
+__device__ __forceinline__ uint32_t att_finite_mask(uint32_t w)
 {
-    const auto one = [minus](uint32_t bits, uint32_t inf, uint32_t sign) {
-        const uint32_t size = bits & ~sign;
-        return size > inf || bits == (minus ? inf | sign : inf);
-    };
-    if (!BF16)
-        return one(w, 0x7F800000u, 0x80000000u) ? 0x3F800000u : 0;
-    return (one(w & 0xFFFF, 0x7F80, 0x8000) ? 0x3F80u : 0) | (one(w >> 16, 0x7F80, 0x8000) ? 0x3F800000u : 0);
-}
-
-template <bool BF16>
-__device__ __forceinline__ uint32_t att_finite_or_0(uint32_t w)
-{
-    if (!BF16)
-        return (w & 0x7F800000u) == 0x7F800000u ? 0 : w;
-    return ((w & 0x7F80u) == 0x7F80u ? 0 : w & 0xFFFFu) | ((w & 0x7F800000u) == 0x7F800000u ? 0 : w & 0xFFFF0000u);
+    return ((w & 0x7F80u) == 0x7F80u ? 0 : 0xFFFFu) | ((w & 0x7F800000u) == 0x7F800000u ? 0 : 0xFFFF0000u);
 }
 
 // The item of workgroup `id`; false: no row needs it.  Workgroups go [tile of ROWS rows][chunk][kv head], the prefix's first; TOP: own tiles from
@@ -130,6 +121,6 @@ __device__ __forceinline__ bool att_item(const AttendParams &p, int32_t id, Atte
 
 // launches the `wgs` workgroups of p on tiles of att_tile_rows(dim) rows; bf16 only
 int launch_attend_tiles(const AttendParams &p, int32_t wgs, hipStream_t st);
-constexpr int att_tile_rows(int32_t dim) { return 16 * ATT_TILE_WAVES * (dim > 128 ? 1 : 2); }
+constexpr int att_tile_rows(int32_t dim) { return 16 * ATT_TILE_WAVES * ATT_TILE_NT * (dim > 128 ? 1 : 2); }
 
 }  // namespace griffin

@@ -196,9 +196,6 @@ __device__ __forceinline__ void att_weigh(const AttScores<BF16, DB, NT> &s, cons
     }
 }
 
-template <bool BF16>
-__device__ __forceinline__ int att_key_of(int j, int lane) { return 16 * (j >> 2) + (lane >> 4) * 4 + (j & 3); }
-
 // Is any of the lane's values infinite or NaN (all exponent bits set)?
 template <bool BF16, int DB>
 __device__ __forceinline__ bool att_not_finite(const AttVals<BF16, DB> &f)
@@ -215,78 +212,49 @@ __device__ __forceinline__ bool att_not_finite(const AttVals<BF16, DB> &f)
     return (any & (BF16 ? 0x80008000u : 0x80000000u)) != 0;
 }
 
-// Where some rows see a key that others do not, an infinite or NaN value of it must not reach the others, as 0 x Inf in the second
-// product would.  Such values are counted, per row that sees them and by sign, in a product of ones; sums they are in become infinite or NaN
-// here, and the values zero for the product that follows.
-template <bool BF16, int DB, int NT>
-__device__ __forceinline__ void att_take_infinite(AttVals<BF16, DB> &f, AttRows<BF16, DB, NT> &r, int32_t key0, int lane)
+// Before a masked step's second product.  Infinite and NaN values of keys that a row does not see must not reach it, as 0 x Inf would: if there are any
+// (`true`), they are made zero here and added to the rows that do see them at the end (att_add_infinite).
+template <bool BF16, int DB>
+__device__ __forceinline__ bool att_clear_infinite(AttVals<BF16, DB> &f)
 {
     using S = AttShape<BF16, DB>;
-    for (int minus = 0; minus < 2; ++minus) {
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            att_u32x4 seen;
-            if (BF16)
-#pragma unroll
-                for (int h = 0; h < 4; ++h)
-                    seen[h] = (key0 + att_key_of<BF16>(2 * h, lane) < r.end[n] ? 0x3F80u : 0) |
-                              (key0 + att_key_of<BF16>(2 * h + 1, lane) < r.end[n] ? 0x3F800000u : 0);
-            else
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    seen[i] = key0 + att_key_of<BF16>(i, lane) < r.end[n] ? 0x3F800000u : 0;
-#pragma unroll
-            for (int c = 0; c < S::NC; ++c)
-#pragma unroll
-                for (int e = 0; e < S::VD; ++e) {
-                    __builtin_amdgcn_sched_barrier(0);         // one at a time: this is not where registers are to go
-                    att_f32x4 count = {0, 0, 0, 0};
-                    if constexpr (BF16) {
-                        att_u32x4 a;
-#pragma unroll
-                        for (int h = 0; h < 4; ++h)
-                            a[h] = att_infinite<true>(
-                                __builtin_amdgcn_perm(f.v[2 * h + 1][c][e / 2], f.v[2 * h][c][e / 2], e & 1 ? 0x07060302 : 0x05040100), minus);
-                        count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(att_bf16x8, a), __builtin_bit_cast(att_bf16x8, seen), count,
-                                                                        0, 0, 0);
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            count = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(att_infinite<false>(f.v[i][c][e], minus)),
-                                                                         __uint_as_float(seen[i]), count, 0, 0, 0);
-                    }
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        r.o[n][c * S::VD + e][i] += count[i] > 0 ? (minus ? -INFINITY : INFINITY) : 0.0f;
-                }
-        }
-    }
+    if (!__any(att_not_finite<BF16, DB>(f)))
+        return false;
 #pragma unroll
     for (int j = 0; j < S::VK; ++j)
 #pragma unroll
         for (int c = 0; c < S::NC; ++c)
 #pragma unroll
             for (int w = 0; w < S::VW; ++w)
-                f.v[j][c][w] = att_finite_or_0<BF16>(f.v[j][c][w]);
+                f.v[j][c][w] &= BF16 ? att_finite_mask(f.v[j][c][w]) : ((f.v[j][c][w] & 0x7F800000u) == 0x7F800000u ? 0 : ~0u);
+    return true;
 }
 
-// Before a masked step's second product: values behind the last key become zero (0 x NaN is NaN), those that only some rows see are looked at
-template <bool BF16, int DB, int NT>
-__device__ __forceinline__ void att_mask_vals(AttVals<BF16, DB> &f, AttRows<BF16, DB, NT> &r, int32_t key0, int32_t end, int32_t least, int lane)
+// ... of the keys from `key` on of one step
+template <bool BF16, int DB, bool FULL, int NT>
+__device__ __forceinline__ void att_add_infinite(const AttendParams &p, const AttendItem &it, AttRows<BF16, DB, NT> &r, int32_t key)
 {
     using S = AttShape<BF16, DB>;
-    if (key0 + S::KS > end)
+    const int32_t stop = key + S::KS < it.end ? key + S::KS : it.end;
+    for (; key < stop; ++key) {
+        const AttTile tile = att_tile(p, it.pages, key & ~15, it.end);
+        const char *at = (const char *)p.V + (it.hk * p.head_stride + tile.base + (key & 15) * p.token_stride) * (BF16 ? 2 : 4);
 #pragma unroll
-        for (int j = 0; j < S::VK; ++j) {
-            const bool in = key0 + att_key_of<BF16>(j, lane) < end;
+        for (int c = 0; c < S::NC; ++c)
 #pragma unroll
-            for (int c = 0; c < S::NC; ++c)
+            for (int i = 0; i < 4; ++i) {                  // elements i of the lane's sums: features (c 16 + (lane >> 4) 4 + i) VD + e
+                __builtin_amdgcn_sched_barrier(0);
+                const int d = (c * 16 + (threadIdx.x >> 4 & 3) * 4 + i) * S::VD;
 #pragma unroll
-                for (int w = 0; w < S::VW; ++w)
-                    f.v[j][c][w] = in ? f.v[j][c][w] : 0;
-        }
-    if (__any(least < end && least < key0 + S::KS) && __any(att_not_finite<BF16, DB>(f)))
-        att_take_infinite<BF16, DB, NT>(f, r, key0, lane);
+                for (int e = 0; e < S::VD; ++e) {
+                    const float x = FULL || d + e < p.dim ? load_scalar<BF16>(at, d + e) : 0.0f;
+                    const bool odd = (__float_as_uint(x) & 0x7F800000u) == 0x7F800000u;
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+                        r.o[n][c * S::VD + e][i] += odd && key < r.end[n] ? x : 0.0f;
+                }
+            }
+    }
 }
 
 // The item's rows first .. first + 16 NT - 1
@@ -329,6 +297,7 @@ __device__ __forceinline__ void attend_rows(const AttendParams &p, float *lds, c
     }
     const char *Kh = (const char *)p.K + hk * p.head_stride * ES, *Vh = (const char *)p.V + hk * p.head_stride * ES;
     int32_t key0 = begin + wave * S::KS;
+    bool odd = false;
     if (key0 < end) {
         AttKeys<BF16, DB> fk;
         AttVals<BF16, DB> fv;
@@ -353,13 +322,17 @@ __device__ __forceinline__ void attend_rows(const AttendParams &p, float *lds, c
                 att_softmax<BF16, DB, NT, false>(s, r, p.scale2, key0, lane);
             else {
                 att_softmax<BF16, DB, NT, true>(s, r, p.scale2, key0, lane);
-                att_mask_vals<BF16, DB, NT>(fv, r, key0, end, least, lane);
+                odd |= att_clear_infinite<BF16, DB>(fv);
             }
             att_weigh<BF16, DB, NT>(s, fv, r);
             __builtin_amdgcn_sched_barrier(0);
             att_load_vals<BF16, DB, FULL>(fv, p, Vh, next, lane);
         }
     }
+    if (odd)
+        for (key0 = begin + wave * S::KS; key0 < end; key0 += ATT_WAVES * S::KS)
+            if (!__all(key0 + S::KS <= least))
+                att_add_infinite<BF16, DB, FULL, NT>(p, it, r, key0);
     // the four wavefronts' sums come together in two steps (2 and 3 to 0 and 1, then 1 to 0), lane by lane
     float *mine = lds + (wave & 1) * (S::NO * 4 + 2) * 64;
 #pragma unroll

@@ -13,14 +13,15 @@
 namespace griffin {
 
 typedef __attribute__((ext_vector_type(4))) short att_s16x4;
-typedef __attribute__((address_space(3))) att_s16x4 lds_s16x4;
+typedef __attribute__((address_space(3))) att_s16x4 lds_s16x4;       // LDS is addressed by 32-bit offsets
+typedef __attribute__((address_space(3))) att_u32x4 lds_u32x4;
 
 template <int DB>
 struct TileShape {
     static constexpr int NQ = DB / 32;                        // 32-feature pieces of a key
     static constexpr int NO = DB / 16;                        // tiles of 16 features of the output
     static constexpr int KT = ATT_TILE_KEYS / 16;             // tiles of 16 keys of a step
-    static constexpr int NT = DB > 128 ? 1 : 2;               // tiles of 16 rows of a wavefront
+    static constexpr int NT = ATT_TILE_NT * (DB > 128 ? 1 : 2);               // tiles of 16 rows of a wavefront
     static constexpr int ROW = DB * 2;                        // bytes of a value's row
     static constexpr int BYTES = ATT_TILE_KEYS * ROW;         // of a step's keys, and of its values
     static constexpr int PIECES = BYTES / (16 * 64 * ATT_TILE_WAVES);      // 16-byte pieces of either that a thread brings in
@@ -39,55 +40,93 @@ struct TileRows {
 template <int DB>
 __device__ __forceinline__ int tile_turn(int row) { return DB >= 128 ? row & 7 : (row >> 1) & 3; }
 
-template <int DB, bool FULL>
-__device__ __forceinline__ void tile_load(att_u32x4 (&k)[TileShape<DB>::PIECES], att_u32x4 (&v)[TileShape<DB>::PIECES], const AttendParams &p,
-                                          const AttendItem &it, int32_t key0)
-{
+// A step's keys (VALS: values) on their way: looked up (a page's number comes from memory, so a step ahead of the loads), loaded into registers, stored in LDS
+template <int DB, bool FULL, bool VALS>
+struct TilePart {
     using S = TileShape<DB>;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const char *Kh = (const char *)p.K + it.hk * p.head_stride * 2, *Vh = (const char *)p.V + it.hk * p.head_stride * 2;
-#pragma unroll
-    for (int i = 0; i < S::PIECES; ++i) {
-        const int f = wave + ATT_TILE_WAVES * i, t = f / S::NQ, s = f % S::NQ;
-        const AttTile tile = att_tile(p, it.pages, key0 + 16 * t, it.end);
-        const int row = (lane & 15) < tile.rows ? (lane & 15) : tile.rows, d = s * 32 + (lane >> 4) * 8;
-        if (FULL || d < p.dim)
-            k[i] = *(const att_u32x4 *)(Kh + (tile.base + row * p.token_stride + d) * 2);
-        else
-            k[i] = att_u32x4{0, 0, 0, 0};
-    }
-#pragma unroll
-    for (int i = 0; i < S::PIECES; ++i) {
-        const int first = (wave * 64 + 64 * ATT_TILE_WAVES * i) / (DB / 8), row = first + lane / (DB / 8), d = lane % (DB / 8) * 8;
-        const AttTile tile = att_tile(p, it.pages, key0 + (first & ~15), it.end);
-        const int at = (row & 15) < tile.rows ? (row & 15) : tile.rows;
-        v[i] = *(const att_u32x4 *)(Vh + (tile.base + at * p.token_stride + (FULL || d < p.dim ? d : 0)) * 2);
-    }
-}
+    AttTile at[S::PIECES];
+    att_u32x4 x[S::PIECES];
 
-template <int DB>
-__device__ __forceinline__ void tile_store(char *lds, const att_u32x4 (&k)[TileShape<DB>::PIECES], const att_u32x4 (&v)[TileShape<DB>::PIECES])
-{
-    using S = TileShape<DB>;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int i = 0; i < S::PIECES; ++i) {
-        *(att_u32x4 *)(lds + (wave + ATT_TILE_WAVES * i) * 1024 + lane * 16) = k[i];
-        const int row = (wave * 64 + 64 * ATT_TILE_WAVES * i) / (DB / 8) + lane / (DB / 8), piece = lane % (DB / 8);
-        *(att_u32x4 *)(lds + S::BYTES + row * S::ROW + (piece ^ tile_turn<DB>(row) << 1) * 16) = v[i];
+    // the tile of 16 keys, and within it the key and the feature, that the lane's piece i begins at
+    static __device__ __forceinline__ int tile_of(int wave, int i)
+    {
+        return VALS ? (wave * 64 + 64 * ATT_TILE_WAVES * i) / (DB / 8) / 16 : (wave + ATT_TILE_WAVES * i) / S::NQ;
     }
-}
+    static __device__ __forceinline__ int key_of(int wave, int lane, int i)
+    {
+        return VALS ? ((wave * 64 + 64 * ATT_TILE_WAVES * i) / (DB / 8) + lane / (DB / 8)) & 15 : lane & 15;
+    }
+    static __device__ __forceinline__ int feature_of(int wave, int lane, int i)
+    {
+        return VALS ? lane % (DB / 8) * 8 : (wave + ATT_TILE_WAVES * i) % S::NQ * 32 + (lane >> 4) * 8;
+    }
 
-// A operand of V^T: features 16 e .. + 15 of the keys of tiles 2h and 2h + 1, in the order in which the lanes hold their scores
+    __device__ __forceinline__ void look_up(const AttendParams &p, const AttendItem &it, int32_t key0, int wave)
+    {
+#pragma unroll
+        for (int i = 0; i < S::PIECES; ++i)
+            at[i] = att_tile(p, it.pages, key0 + 16 * tile_of(wave, i), it.end);
+    }
+
+    __device__ __forceinline__ void load(const AttendParams &p, const AttendItem &it, int wave, int lane)
+    {
+        const char *pool = (const char *)(VALS ? p.V : p.K) + it.hk * p.head_stride * 2;
+        const int32_t stride = (int32_t)p.token_stride;
+#pragma unroll
+        for (int i = 0; i < S::PIECES; ++i) {
+            const int want = key_of(wave, lane, i), key = want < at[i].rows ? want : at[i].rows, d = feature_of(wave, lane, i);
+            // keys' features from dim on are zero, as the queries' are; values' end in outputs that are not stored, so that any will do
+            if (FULL || VALS || d < p.dim)
+                x[i] = *(const att_u32x4 *)(pool + at[i].base * 2 + (uint32_t)(key * stride + (FULL || d < p.dim ? d : 0)) * 2);
+            else
+                x[i] = att_u32x4{0, 0, 0, 0};
+        }
+    }
+
+    // infinite and NaN as zeros, true if there were any
+    __device__ __forceinline__ bool clear()
+    {
+        uint32_t kept = ~0u;
+#pragma unroll
+        for (int i = 0; i < S::PIECES; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t m = att_finite_mask(x[i][j]);
+                x[i][j] &= m;
+                kept &= m;
+            }
+        return kept != ~0u;
+    }
+
+    __device__ __forceinline__ void store(uint32_t lds, int wave, int lane) const
+    {
+#pragma unroll
+        for (int i = 0; i < S::PIECES; ++i) {
+            const int row = tile_of(wave, i) * 16 + key_of(wave, lane, i), piece = lane % (DB / 8);
+            const uint32_t to = VALS ? row * S::ROW + (piece ^ tile_turn<DB>(row) << 1) * 16 : (wave + ATT_TILE_WAVES * i) * 1024 + lane * 16;
+            *(lds_u32x4 *)(uintptr_t)(lds + to) = x[i];
+        }
+    }
+};
+
+// A operand of V^T: features 16 e .. + 15 of the keys of tiles 2h and 2h + 1, in the order in which the lanes hold their scores.  `at` is the
+// lane's place for e = 0 (tile_vals_at); the others' differ from it in the bits of the turned pieces.
 template <int DB>
-__device__ __forceinline__ att_u32x4 tile_vals(const char *vals, int e, int h)
+__device__ __forceinline__ uint32_t tile_vals_at(uint32_t lds)
 {
     using S = TileShape<DB>;
     const int lane = threadIdx.x & 63, row = (lane >> 4) * 4 + ((lane >> 2) & 3);
-    const char *at = vals + row * S::ROW + (e ^ tile_turn<DB>(row)) * 32 + (lane & 3) * 8;
+    return lds + row * S::ROW + tile_turn<DB>(row) * 32 + (lane & 3) * 8;
+}
+
+template <int DB>
+__device__ __forceinline__ att_u32x4 tile_vals(uint32_t at, int e, int h)
+{
+    using S = TileShape<DB>;
     typedef __attribute__((ext_vector_type(2))) uint32_t pair_t;
-    const pair_t lo = __builtin_bit_cast(pair_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + 2 * h * 16 * S::ROW)));
-    const pair_t hi = __builtin_bit_cast(pair_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + (2 * h + 1) * 16 * S::ROW)));
+    const uint32_t x = at ^ e * 32;
+    const pair_t lo = __builtin_bit_cast(pair_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)(x + 2 * h * 16 * S::ROW)));
+    const pair_t hi = __builtin_bit_cast(pair_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)(x + (2 * h + 1) * 16 * S::ROW)));
     return att_u32x4{lo.x, lo.y, hi.x, hi.y};
 }
 
@@ -96,86 +135,108 @@ __device__ __forceinline__ att_f32x4 att_mfma(att_u32x4 a, att_u32x4 b, att_f32x
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(att_bf16x8, a), __builtin_bit_cast(att_bf16x8, b), c, 0, 0, 0);
 }
 
-// A step in which rows differ in the keys that they see, or in which keys end: infinite and NaN values of keys that a row does not see must not
-// reach it, as 0 x Inf would.  A product of all values with zeros is NaN if there are any.  If so, they are counted per row that sees them and by sign
-// in a product of ones, the sums they are in become infinite or NaN, and `true` says that the product to come has to take them as zeros.
-template <int DB>
-__device__ __forceinline__ bool tile_take_infinite(const char *vals, TileRows<DB> &r, int32_t key0)
+// In steps in which rows differ in the keys that they see, or in which keys end, infinite and NaN values of keys that a row does not see must not reach
+// it, as 0 x Inf would: there they are stored as zeros, and what was made zero is added at the end to the rows that do see it.
+template <int DB, bool FULL>
+__device__ __forceinline__ void tile_add_infinite(const AttendParams &p, const AttendItem &it, TileRows<DB> &r, int32_t key, int32_t most)
 {
     using S = TileShape<DB>;
-    const att_u32x4 zero = {0, 0, 0, 0};
-    att_f32x4 sum = {0, 0, 0, 0};
+    const int d = (threadIdx.x >> 4 & 3) * 4;
+    for (; key < most; ++key) {
+        const AttTile tile = att_tile(p, it.pages, key & ~15, it.end);
+        const uint16_t *at = (const uint16_t *)p.V + it.hk * p.head_stride + tile.base + (key & 15) * p.token_stride + d;
 #pragma unroll
-    for (int e = 0; e < S::NO; ++e)
-#pragma unroll
-        for (int h = 0; h < S::KT / 2; ++h)
-            sum = att_mfma(tile_vals<DB>(vals, e, h), zero, sum);
-    if (!__any(sum[0] != sum[0] || sum[1] != sum[1] || sum[2] != sum[2] || sum[3] != sum[3]))
-        return false;
-    const int lane = threadIdx.x & 63;
-    for (int minus = 0; minus < 2; ++minus)
-#pragma unroll
-        for (int e = 0; e < S::NO; ++e)
-#pragma unroll
-            for (int n = 0; n < S::NT; ++n) {
-                __builtin_amdgcn_sched_barrier(0);            // one at a time: this is not where registers are to go
-                att_f32x4 count = {0, 0, 0, 0};
-                for (int h = 0; h < S::KT / 2; ++h) {
-                    att_u32x4 a = tile_vals<DB>(vals, e, h), seen;
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) {
-                        a[w] = att_infinite<true>(a[w], minus);
-                        const int32_t key = key0 + h * 32 + (w >> 1) * 16 + (lane >> 4) * 4 + (w & 1) * 2;
-                        seen[w] = (key < r.end[n] ? 0x3F80u : 0) | (key + 1 < r.end[n] ? 0x3F800000u : 0);
-                    }
-                    count = att_mfma(a, seen, count);
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    r.o[n][e][i] += count[i] > 0 ? (minus ? -INFINITY : INFINITY) : 0.0f;
-            }
-    return true;
-}
-
-template <int DB, bool CLEAN>
-__device__ __forceinline__ void tile_weigh(const char *vals, const att_u32x4 (&w)[TileShape<DB>::NT][TileShape<DB>::KT / 2], TileRows<DB> &r)
-{
-    using S = TileShape<DB>;
-#pragma unroll
-    for (int e = 0; e < S::NO; ++e)
-#pragma unroll
-        for (int h = 0; h < S::KT / 2; ++h) {
-            att_u32x4 a = tile_vals<DB>(vals, e, h);
-            if (CLEAN)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    a[i] = att_finite_or_0<true>(a[i]);
+        for (int e = 0; e < S::NO; ++e) {
+            __builtin_amdgcn_sched_barrier(0);
+            const uint2 x = FULL || e * 16 + d < p.dim ? *(const uint2 *)(at + e * 16) : make_uint2(0, 0);
+            const uint32_t odd[2] = {x.x & ~att_finite_mask(x.x), x.y & ~att_finite_mask(x.y)};
 #pragma unroll
             for (int n = 0; n < S::NT; ++n)
-                r.o[n][e] = att_mfma(a, w[n][h], r.o[n][e]);
-        }
-}
-
-// Keys key0 .. key0 + 63, in LDS, for the wavefront's rows.  MASKED: some rows do not see some of them.
-template <int DB, bool MASKED>
-__device__ __forceinline__ void tile_step(const char *lds, TileRows<DB> &r, float scale2, int32_t key0)
-{
-    using S = TileShape<DB>;
-    const int lane = threadIdx.x & 63;
-    att_f32x4 s[S::NT][S::KT];
 #pragma unroll
-    for (int t = 0; t < S::KT; ++t) {
-#pragma unroll
-        for (int n = 0; n < S::NT; ++n)
-            s[n][t] = att_f32x4{0, 0, 0, 0};
-#pragma unroll
-        for (int c = 0; c < S::NQ; ++c) {
-            const att_u32x4 a = *(const att_u32x4 *)(lds + (t * S::NQ + c) * 1024 + lane * 16);
-#pragma unroll
-            for (int n = 0; n < S::NT; ++n)
-                s[n][t] = att_mfma(a, r.q[n][c], s[n][t]);
+                for (int i = 0; i < 4; ++i)
+                    r.o[n][e][i] += key < r.end[n] ? (i & 1 ? bf16_hi(odd[i / 2]) : bf16_lo(odd[i / 2])) : 0.0f;
         }
     }
+}
+
+// O^T += V^T P^T
+template <int DB>
+__device__ __forceinline__ void tile_weigh(uint32_t vals, const att_u32x4 (&w)[TileShape<DB>::NT][TileShape<DB>::KT / 2], TileRows<DB> &r)
+{
+    using S = TileShape<DB>;
+    constexpr int H = S::KT / 2, G = 4 / H;                   // operands of G tiles of features are read while those before are multiplied
+    att_u32x4 a[2][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        a[0][i] = tile_vals<DB>(vals, i / H, i % H);
+#pragma unroll
+    for (int e = 0; e < S::NO; e += G) {
+        const int now = e / G & 1;
+        __builtin_amdgcn_sched_barrier(0);
+        if (e + G < S::NO)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                a[now ^ 1][i] = tile_vals<DB>(vals, e + G + i / H, i % H);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+#pragma unroll
+            for (int n = 0; n < S::NT; ++n)
+                r.o[n][e + i / H] = att_mfma(a[now][i], w[n][i % H], r.o[n][e + i / H]);
+        }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+template <int DB>
+using TileScores = att_f32x4[TileShape<DB>::NT][TileShape<DB>::KT];
+
+// S^T = K Q^T
+template <int DB>
+__device__ __forceinline__ void tile_scores(uint32_t keys, TileScores<DB> &s, const TileRows<DB> &r)
+{
+    using S = TileShape<DB>;
+    constexpr int G = S::NQ < 4 ? S::NQ : 4, STEPS = S::KT * S::NQ / G;       // G pieces of keys are read while those before are multiplied
+    const uint32_t at = keys + (threadIdx.x & 63) * 16;
+    att_u32x4 a[2][G];
+#pragma unroll
+    for (int i = 0; i < G; ++i)
+        a[0][i] = *(const lds_u32x4 *)(uintptr_t)(at + i * 1024);
+#pragma unroll
+    for (int f = 0; f < STEPS; ++f) {
+        __builtin_amdgcn_sched_barrier(0);
+        if (f + 1 < STEPS)
+#pragma unroll
+            for (int i = 0; i < G; ++i)
+                a[f + 1 & 1][i] = *(const lds_u32x4 *)(uintptr_t)(at + ((f + 1) * G + i) * 1024);
+        __builtin_amdgcn_sched_barrier(0);
+        const int t = f * G / S::NQ;
+#pragma unroll
+        for (int i = 0; i < G; ++i)
+#pragma unroll
+            for (int n = 0; n < S::NT; ++n) {
+                const int c = f * G % S::NQ + i;
+                s[n][t] = att_mfma(a[f & 1][i], r.q[n][c], c == 0 ? att_f32x4{0, 0, 0, 0} : s[n][t]);
+            }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// Scores to weights in bf16; the rows' reference and sum carried on, o scaled when the reference moves
+template <int DB>
+__device__ __forceinline__ void tile_softmax(bool masked, TileScores<DB> &s, att_u32x4 (&w)[TileShape<DB>::NT][TileShape<DB>::KT / 2], TileRows<DB> &r,
+                                             float scale2, int32_t key0)
+{
+    using S = TileShape<DB>;
+    const int lane = threadIdx.x & 63;
+    if (masked)
+#pragma unroll
+        for (int n = 0; n < S::NT; ++n)
+#pragma unroll
+            for (int t = 0; t < S::KT; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    s[n][t][e] = key0 + 16 * t + (lane >> 4) * 4 + e >= r.end[n] ? -INFINITY : s[n][t][e];
     float top[S::NT];
     bool grown = false;
 #pragma unroll
@@ -184,11 +245,8 @@ __device__ __forceinline__ void tile_step(const char *lds, TileRows<DB> &r, floa
 #pragma unroll
         for (int t = 0; t < S::KT; ++t)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if (MASKED && key0 + 16 * t + (lane >> 4) * 4 + e >= r.end[n])
-                    s[n][t][e] = -INFINITY;
+            for (int e = 0; e < 4; ++e)
                 top[n] = fmaxf(top[n], s[n][t][e]);
-            }
         top[n] *= scale2;
         grown |= top[n] > r.m[n] + 8.0f;
     }
@@ -203,52 +261,56 @@ __device__ __forceinline__ void tile_step(const char *lds, TileRows<DB> &r, floa
             for (int e = 0; e < S::NO; ++e)
                 r.o[n][e] *= f;
         }
-    att_u32x4 w[S::NT][S::KT / 2];
 #pragma unroll
     for (int n = 0; n < S::NT; ++n) {
         const float base = r.m[n] == -INFINITY ? 0.0f : r.m[n];
-        float l[S::KT];
 #pragma unroll
         for (int t = 0; t < S::KT; ++t) {
             float x[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 x[e] = __builtin_amdgcn_exp2f(s[n][t][e] * scale2 - base);
-            l[t] = (x[0] + x[1]) + (x[2] + x[3]);
+            r.l[n] += (x[0] + x[1]) + (x[2] + x[3]);
             w[n][t / 2][t % 2 * 2] = f32x2_to_bf16x2(x[0], x[1]);
             w[n][t / 2][t % 2 * 2 + 1] = f32x2_to_bf16x2(x[2], x[3]);
         }
-        r.l[n] += (l[0] + l[1]) + (l[2] + l[3]);
     }
-    if (MASKED && tile_take_infinite<DB>(lds + S::BYTES, r, key0))
-        tile_weigh<DB, true>(lds + S::BYTES, w, r);
-    else
-        tile_weigh<DB, false>(lds + S::BYTES, w, r);
+}
+
+// All that a wavefront has asked of LDS is done, then the workgroup meets.  (Loads from memory may be on their way.)
+__device__ __forceinline__ void tile_meet()
+{
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
 }
 
 template <int DB, bool FULL>
 __global__ __launch_bounds__(64 * ATT_TILE_WAVES) void attend_tile_kernel(AttendParams p)
 {
     using S = TileShape<DB>;
-    extern __shared__ __align__(16) char tile_lds[];          // two steps of keys and values
+    extern __shared__ __align__(1024) char tile_lds[];        // two steps of keys and values
+    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)tile_lds;
     AttendItem it;
     if (!att_item<att_tile_rows(DB), att_tile_rows(DB), true>(p, blockIdx.x, it))
         return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    TileRows<DB> r;
-    int32_t token[S::NT], head[S::NT], least = it.end, most = it.begin;       // keys that all rows of the wavefront see, and that any sees
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int32_t first = it.first + wave * 16 * S::NT;
+    const auto sees = [&](int32_t row) {                      // where the keys that a row sees end
+        const int32_t to = it.own + row / p.group + 1;
+        return it.own < 0 || to > it.end ? it.end : to;
+    };
+    // rows behind the last repeat it and are not stored
+    const auto of = [&](int n) { return first + 16 * n + (lane & 15) < it.rows ? first + 16 * n + (lane & 15) : it.rows - 1; };
+    TileRows<DB> r;
 #pragma unroll
     for (int n = 0; n < S::NT; ++n) {
-        int32_t row = first + 16 * n + (lane & 15);
-        const bool in = row < it.rows;                        // rows behind the last repeat it and are not stored
-        row = in ? row : it.rows - 1;
-        token[n] = it.token0 + row / p.group;
-        head[n] = it.hk * p.group + row % p.group;
-        r.end[n] = it.own < 0 || it.own + row / p.group + 1 > it.end ? it.end : it.own + row / p.group + 1;
-        least = r.end[n] < least ? r.end[n] : least;
-        most = in && r.end[n] > most ? r.end[n] : most;
-        const char *at = (const char *)p.q + ((int64_t)token[n] * p.ldq + (int64_t)head[n] * p.hsq) * 2 + (lane >> 4) * 16;
+        const int32_t row = of(n);
+        r.end[n] = sees(row);
+        const char *at = (const char *)p.q + ((int64_t)(it.token0 + row / p.group) * p.ldq + (int64_t)(it.hk * p.group + row % p.group) * p.hsq) * 2 +
+                         (lane >> 4) * 16;
 #pragma unroll
         for (int s = 0; s < S::NQ; ++s) {
             if (FULL || s * 32 + (lane >> 4) * 8 < p.dim)
@@ -262,44 +324,75 @@ __global__ __launch_bounds__(64 * ATT_TILE_WAVES) void attend_tile_kernel(Attend
         for (int e = 0; e < S::NO; ++e)
             r.o[n][e] = att_f32x4{0, 0, 0, 0};
     }
-    att_u32x4 k[S::PIECES], v[S::PIECES];
-    tile_load<DB, FULL>(k, v, p, it, it.begin);
-    tile_store<DB>(tile_lds, k, v);
+    // keys that all rows of the wavefront see, and that any sees (none: it has no rows)
+    const int32_t least = first < it.rows ? sees(first) : it.begin;
+    const int32_t most = first < it.rows ? sees(first + 16 * S::NT < it.rows ? first + 16 * S::NT - 1 : it.rows - 1) : it.begin;
+    // steps from the one that begins at `clear` on have keys that some row of the workgroup does not see
+    const int32_t clear = it.begin + (sees(it.first) - it.begin) / ATT_TILE_KEYS * ATT_TILE_KEYS;
+    TilePart<DB, FULL, false> k;
+    TilePart<DB, FULL, true> v;
+    bool odd = false;
+    k.look_up(p, it, it.begin, wave);
+    v.look_up(p, it, it.begin, wave);
+    k.load(p, it, wave, lane);
+    v.load(p, it, wave, lane);
+    k.look_up(p, it, it.begin + ATT_TILE_KEYS, wave);
+    v.look_up(p, it, it.begin + ATT_TILE_KEYS, wave);
+    if (it.begin >= clear)
+        odd |= v.clear();
+    k.store(lds, wave, lane);
+    v.store(lds + 2 * S::BYTES, wave, lane);
     __syncthreads();
-    int room = 0;
+    uint32_t room = 0;
     for (int32_t key0 = it.begin; key0 < it.end; key0 += ATT_TILE_KEYS) {
         const bool more = key0 + ATT_TILE_KEYS < it.end;
-        if (more)
-            tile_load<DB, FULL>(k, v, p, it, key0 + ATT_TILE_KEYS);
-        if (__any(key0 < most) && __all(key0 + ATT_TILE_KEYS <= least))
-            tile_step<DB, false>(tile_lds + room * 2 * S::BYTES, r, p.scale2, key0);
-        else if (__any(key0 < most))
-            tile_step<DB, true>(tile_lds + room * 2 * S::BYTES, r, p.scale2, key0);
-        room ^= 1;
-        if (more)
-            tile_store<DB>(tile_lds + room * 2 * S::BYTES, k, v);
+        if (more) {
+            k.load(p, it, wave, lane);
+            v.load(p, it, wave, lane);
+            k.look_up(p, it, key0 + 2 * ATT_TILE_KEYS, wave);
+            v.look_up(p, it, key0 + 2 * ATT_TILE_KEYS, wave);
+        }
+        if (key0 < most) {
+            TileScores<DB> s;
+            att_u32x4 w[S::NT][S::KT / 2];
+            tile_scores<DB>(lds + room, s, r);
+            tile_softmax<DB>(key0 + ATT_TILE_KEYS > least, s, w, r, p.scale2, key0);
+            tile_weigh<DB>(tile_vals_at<DB>(lds + 2 * S::BYTES + room), w, r);
+        }
+        room ^= S::BYTES;
+        if (more) {
+            if (key0 + ATT_TILE_KEYS >= clear)
+                odd |= v.clear();
+            k.store(lds + room, wave, lane);
+            v.store(lds + 2 * S::BYTES + room, wave, lane);
+        }
         __syncthreads();
     }
+    if (__syncthreads_or(odd))
+        tile_add_infinite<DB, FULL>(p, it, r, clear, most);
 #pragma unroll
     for (int n = 0; n < S::NT; ++n) {
         const float l = lane_groups_sum(r.l[n]);
         if (first + 16 * n + (lane & 15) >= it.rows)
             continue;
-        const int64_t slot = ((int64_t)token[n] * p.n_heads + head[n]) * (p.chunks_prefix + p.chunks_own) + it.split;
-        const float f = p.part ? 1.0f : (l == 0.0f ? 0.0f : 1.0f / l);        // a row without keys: zeros
-        if (p.part && lane < 16)
-            p.part_ml[slot] = make_float2(r.m[n], l);
+        const int32_t row = of(n), token = it.token0 + row / p.group, head = it.hk * p.group + row % p.group;
+        if (p.part) {
+            const int64_t slot = ((int64_t)token * p.n_heads + head) * (p.chunks_prefix + p.chunks_own) + it.split;
+            if (lane < 16)
+                p.part_ml[slot] = make_float2(r.m[n], l);
+            float *at = p.part + slot * p.dim + (lane >> 4) * 4;
 #pragma unroll
-        for (int e = 0; e < S::NO; ++e) {
-            const int d = e * 16 + (lane >> 4) * 4;
-            if (!FULL && d >= p.dim)
-                continue;
-            const att_f32x4 x = r.o[n][e] * f;
-            if (p.part)
-                *(att_f32x4 *)(p.part + slot * p.dim + d) = x;
-            else
-                *(uint2 *)((uint16_t *)p.out + (int64_t)token[n] * p.ldo + (int64_t)head[n] * p.hso + d) =
-                    make_uint2(f32x2_to_bf16x2(x[0], x[1]), f32x2_to_bf16x2(x[2], x[3]));
+            for (int e = 0; e < S::NO; ++e)
+                if (FULL || e * 16 + (lane >> 4) * 4 < p.dim)
+                    *(att_f32x4 *)(at + e * 16) = r.o[n][e];
+        } else {
+            const float f = l == 0.0f ? 0.0f : 1.0f / l;      // a row without keys: zeros
+            uint16_t *at = (uint16_t *)p.out + (int64_t)token * p.ldo + (int64_t)head * p.hso + (lane >> 4) * 4;
+#pragma unroll
+            for (int e = 0; e < S::NO; ++e)
+                if (FULL || e * 16 + (lane >> 4) * 4 < p.dim)
+                    *(uint2 *)(at + e * 16) = make_uint2(f32x2_to_bf16x2(r.o[n][e][0] * f, r.o[n][e][1] * f),
+                                                         f32x2_to_bf16x2(r.o[n][e][2] * f, r.o[n][e][3] * f));
         }
     }
 }
