@@ -11,14 +11,8 @@ typedef __attribute__((ext_vector_type(8))) __bf16 att_bf16x8;
 typedef __attribute__((ext_vector_type(4))) uint32_t att_u32x4;
 
 constexpr int ATT_WAVES = 4;            // of a workgroup of attend.hip
-#ifndef TW
-#define TW 8
-#define TK 64
-#define TN 1
-#endif
-constexpr int ATT_TILE_WAVES = TW;       // ... of attend_tile.hip
-constexpr int ATT_TILE_KEYS = TK;       // its step
-constexpr int ATT_TILE_NT = TN;
+constexpr int ATT_TILE_WAVES = 8;       // ... of attend_tile.hip
+constexpr int ATT_TILE_KEYS = 64;       // its step
 
 struct AttendParams {
     const void *q, *K, *V;
@@ -27,6 +21,7 @@ struct AttendParams {
     float2 *part_ml;         // [tokens][n_heads][chunks] maximum (base 2) and sum
     const int32_t *lens, *pages, *prefix_pages;
     int64_t ldq, hsq, ldo, hso, page_stride, head_stride, token_stride, ld_pages;
+    uint32_t page_stride16;  // page_stride in 16 bytes (of bf16)
     float scale2;            // scale log2(e)
     int32_t n_heads, kv_heads, group, dim, page_shift, last_page, max_len, n_prefix;
     // keys a chunk (a multiple of a workgroup's step), chunks, and tiles of rows of the prefix
@@ -52,6 +47,9 @@ __device__ __forceinline__ float lane_groups_max(float v)
     r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return fmaxf(__uint_as_float(r.x), __uint_as_float(r.y));
 }
+
+// a page's number, kept in the pools
+__device__ __forceinline__ int64_t att_page(int32_t page, int32_t last_page) { return page < 0 ? 0 : (page > last_page ? last_page : page); }
 
 // where the tiles of a step lie: tile t's page and its first slot there, kept in range of the keys that there are
 struct AttTile {
@@ -121,6 +119,6 @@ __device__ __forceinline__ bool att_item(const AttendParams &p, int32_t id, Atte
 
 // launches the `wgs` workgroups of p on tiles of att_tile_rows(dim) rows; bf16 only
 int launch_attend_tiles(const AttendParams &p, int32_t wgs, hipStream_t st);
-constexpr int att_tile_rows(int32_t dim) { return 16 * ATT_TILE_WAVES * ATT_TILE_NT * (dim > 128 ? 1 : 2); }
+constexpr int att_tile_rows(int32_t dim) { return 16 * ATT_TILE_WAVES * (dim > 128 ? 1 : 2); }
 
 }  // namespace griffin

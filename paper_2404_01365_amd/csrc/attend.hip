@@ -615,6 +615,7 @@ int launch_attend(const AttendJob &job, const SeqTable &seqs, hipStream_t st)
     p.lens = B.lens; p.pages = B.pages; p.prefix_pages = B.prefix_pages;
     p.ldq = job.ldq; p.hsq = job.hsq; p.ldo = job.ldo; p.hso = job.hso;
     p.page_stride = C.page_stride; p.head_stride = C.head_stride; p.token_stride = C.token_stride; p.ld_pages = B.ld_pages;
+    p.page_stride16 = (uint32_t)(C.page_stride / 8);
     p.scale2 = job.scale * 1.4426950408889634f;
     p.n_heads = job.n_heads; p.kv_heads = C.kv_heads; p.group = job.n_heads / C.kv_heads; p.dim = C.dim;
     p.page_shift = __builtin_ctz(C.page_size);

@@ -21,7 +21,7 @@ struct TileShape {
     static constexpr int NQ = DB / 32;                        // 32-feature pieces of a key
     static constexpr int NO = DB / 16;                        // tiles of 16 features of the output
     static constexpr int KT = ATT_TILE_KEYS / 16;             // tiles of 16 keys of a step
-    static constexpr int NT = ATT_TILE_NT * (DB > 128 ? 1 : 2);               // tiles of 16 rows of a wavefront
+    static constexpr int NT = DB > 128 ? 1 : 2;               // tiles of 16 rows of a wavefront
     static constexpr int ROW = DB * 2;                        // bytes of a value's row
     static constexpr int BYTES = ATT_TILE_KEYS * ROW;         // of a step's keys, and of its values
     static constexpr int PIECES = BYTES / (16 * 64 * ATT_TILE_WAVES);      // 16-byte pieces of either that a thread brings in
@@ -40,50 +40,86 @@ struct TileRows {
 template <int DB>
 __device__ __forceinline__ int tile_turn(int row) { return DB >= 128 ? row & 7 : (row >> 1) & 3; }
 
-// A step's keys (VALS: values) on their way: looked up (a page's number comes from memory, so a step ahead of the loads), loaded into registers, stored in LDS
-template <int DB, bool FULL, bool VALS>
-struct TilePart {
+// A step's keys and values on their way: page numbers looked up (they come from memory, so two steps ahead), made places, loaded into registers, stored in
+// LDS.  A wavefront brings in pieces of the same tiles of 16 keys of both: of keys a piece of 32 features in the order of the A operands, of values whole rows.
+template <int DB, bool FULL>
+struct TileStage {
     using S = TileShape<DB>;
-    AttTile at[S::PIECES];
-    att_u32x4 x[S::PIECES];
+    const char *K, *V;                       // of the kv head
+    uint32_t stride, at_k, at_v;             // bytes from key to key; the lane's place in a tile
+    int32_t last;                            // where the last tile begins
+    int32_t page[S::PIECES];
+    int32_t over[S::PIECES];                 // keys that the tile is short of
+    uint64_t base[S::PIECES];
+    att_u32x4 k[S::PIECES], v[S::PIECES];
 
-    // the tile of 16 keys, and within it the key and the feature, that the lane's piece i begins at
-    static __device__ __forceinline__ int tile_of(int wave, int i)
+    static __device__ __forceinline__ int tile_of(int wave, int i) { return (wave + ATT_TILE_WAVES * i) / S::NQ; }
+    static __device__ __forceinline__ int row_of(int wave, int lane) { return (wave * 64 / (DB / 8) + lane / (DB / 8)) & 15; }
+    static_assert(64 / (DB / 8) * S::NQ == 16 && 64 * ATT_TILE_WAVES / (DB / 8) % 16 == 0, "tile_of holds for keys and values, row_of for all pieces");
+
+    __device__ __forceinline__ TileStage(const AttendParams &p, const AttendItem &it, int wave, int lane)
     {
-        return VALS ? (wave * 64 + 64 * ATT_TILE_WAVES * i) / (DB / 8) / 16 : (wave + ATT_TILE_WAVES * i) / S::NQ;
+        K = (const char *)p.K + it.hk * p.head_stride * 2;
+        V = (const char *)p.V + it.hk * p.head_stride * 2;
+        stride = (uint32_t)p.token_stride * 2;
+        at_k = (lane & 15) * stride + (wave % S::NQ * 32 + (lane >> 4) * 8) * 2;
+        at_v = row_of(wave, lane) * stride + lane % (DB / 8) * 16;
+        last = (it.end - 1) & ~15;
     }
-    static __device__ __forceinline__ int key_of(int wave, int lane, int i)
+
+    __device__ __forceinline__ int32_t key_of(int32_t key0, int wave, int i) const
     {
-        return VALS ? ((wave * 64 + 64 * ATT_TILE_WAVES * i) / (DB / 8) + lane / (DB / 8)) & 15 : lane & 15;
-    }
-    static __device__ __forceinline__ int feature_of(int wave, int lane, int i)
-    {
-        return VALS ? lane % (DB / 8) * 8 : (wave + ATT_TILE_WAVES * i) % S::NQ * 32 + (lane >> 4) * 8;
+        const int32_t key = key0 + 16 * tile_of(wave, i);
+        return key < last ? key : last;      // behind the last tile: it again
     }
 
     __device__ __forceinline__ void look_up(const AttendParams &p, const AttendItem &it, int32_t key0, int wave)
     {
 #pragma unroll
-        for (int i = 0; i < S::PIECES; ++i)
-            at[i] = att_tile(p, it.pages, key0 + 16 * tile_of(wave, i), it.end);
-    }
-
-    __device__ __forceinline__ void load(const AttendParams &p, const AttendItem &it, int wave, int lane)
-    {
-        const char *pool = (const char *)(VALS ? p.V : p.K) + it.hk * p.head_stride * 2;
-        const int32_t stride = (int32_t)p.token_stride;
-#pragma unroll
         for (int i = 0; i < S::PIECES; ++i) {
-            const int want = key_of(wave, lane, i), key = want < at[i].rows ? want : at[i].rows, d = feature_of(wave, lane, i);
-            // keys' features from dim on are zero, as the queries' are; values' end in outputs that are not stored, so that any will do
-            if (FULL || VALS || d < p.dim)
-                x[i] = *(const att_u32x4 *)(pool + at[i].base * 2 + (uint32_t)(key * stride + (FULL || d < p.dim ? d : 0)) * 2);
-            else
-                x[i] = att_u32x4{0, 0, 0, 0};
+            // by the vector memory path: a wait for a scalar load is one for all that is asked of LDS behind it, too
+            int32_t at = key_of(key0, wave, i) >> p.page_shift;
+            asm volatile("" : "+v"(at));
+            page[i] = it.pages[at];
         }
     }
 
-    // infinite and NaN as zeros, true if there were any
+    __device__ __forceinline__ void place(const AttendParams &p, const AttendItem &it, int32_t key0, int wave)
+    {
+#pragma unroll
+        for (int i = 0; i < S::PIECES; ++i) {
+            const int32_t key = key_of(key0, wave, i);
+            base[i] = (uint64_t)(uint32_t)att_page(__builtin_amdgcn_readfirstlane(page[i]), p.last_page) * p.page_stride16 * 16 +
+                      (uint64_t)(uint32_t)(key & ((1 << p.page_shift) - 1)) * stride;
+            over[i] = 16 - (it.end - key);
+        }
+    }
+
+    __device__ __forceinline__ void load(const AttendParams &p, int wave, int lane)
+    {
+#pragma unroll
+        for (int i = 0; i < S::PIECES; ++i) {
+            uint32_t ak = at_k, av = at_v;
+            if (over[i] > 0) {                // keys behind the last: it again
+                const int32_t k_over = over[i] - (15 - (lane & 15)), v_over = over[i] - (15 - row_of(wave, lane));
+                ak -= (uint32_t)(k_over > 0 ? k_over : 0) * stride;
+                av -= (uint32_t)(v_over > 0 ? v_over : 0) * stride;
+            }
+            // the piece's features are the same in every round of ATT_TILE_WAVES pieces.  Keys' features from dim on are zero, as the queries' are;
+            // values' end in outputs that are not stored
+            if (FULL || wave % S::NQ * 32 + (lane >> 4) * 8 < p.dim)
+                k[i] = *(const att_u32x4 *)(K + base[i] + ak);
+            else
+                k[i] = att_u32x4{0, 0, 0, 0};
+            if (FULL || lane % (DB / 8) * 8 < p.dim)
+                v[i] = *(const att_u32x4 *)(V + base[i] + av);
+            else
+                v[i] = att_u32x4{0, 0, 0, 0};
+        }
+    }
+    static_assert(ATT_TILE_WAVES % S::NQ == 0, "a wavefront's pieces of keys have the same features");
+
+    // infinite and NaN values as zeros, true if there were any
     __device__ __forceinline__ bool clear()
     {
         uint32_t kept = ~0u;
@@ -91,20 +127,20 @@ struct TilePart {
         for (int i = 0; i < S::PIECES; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const uint32_t m = att_finite_mask(x[i][j]);
-                x[i][j] &= m;
+                const uint32_t m = att_finite_mask(v[i][j]);
+                v[i][j] &= m;
                 kept &= m;
             }
         return kept != ~0u;
     }
 
-    __device__ __forceinline__ void store(uint32_t lds, int wave, int lane) const
+    __device__ __forceinline__ void store(uint32_t keys, uint32_t vals, int wave, int lane) const
     {
 #pragma unroll
         for (int i = 0; i < S::PIECES; ++i) {
-            const int row = tile_of(wave, i) * 16 + key_of(wave, lane, i), piece = lane % (DB / 8);
-            const uint32_t to = VALS ? row * S::ROW + (piece ^ tile_turn<DB>(row) << 1) * 16 : (wave + ATT_TILE_WAVES * i) * 1024 + lane * 16;
-            *(lds_u32x4 *)(uintptr_t)(lds + to) = x[i];
+            const int row = tile_of(wave, i) * 16 + row_of(wave, lane);
+            *(lds_u32x4 *)(uintptr_t)(keys + (wave + ATT_TILE_WAVES * i) * 1024 + lane * 16) = k[i];
+            *(lds_u32x4 *)(uintptr_t)(vals + row * S::ROW + (lane % (DB / 8) ^ tile_turn<DB>(row) << 1) * 16) = v[i];
         }
     }
 };
@@ -168,7 +204,7 @@ __device__ __forceinline__ void tile_weigh(uint32_t vals, const att_u32x4 (&w)[T
     att_u32x4 a[2][4];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-        a[0][i] = tile_vals<DB>(vals, i / H, i % H);
+        a[0][i] = tile_vals<DB>(vals, i % G, i / G);
 #pragma unroll
     for (int e = 0; e < S::NO; e += G) {
         const int now = e / G & 1;
@@ -176,13 +212,13 @@ __device__ __forceinline__ void tile_weigh(uint32_t vals, const att_u32x4 (&w)[T
         if (e + G < S::NO)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                a[now ^ 1][i] = tile_vals<DB>(vals, e + G + i / H, i % H);
+                a[now ^ 1][i] = tile_vals<DB>(vals, e + G + i % G, i / G);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
 #pragma unroll
             for (int n = 0; n < S::NT; ++n)
-                r.o[n][e + i / H] = att_mfma(a[now][i], w[n][i % H], r.o[n][e + i / H]);
+                r.o[n][e + i % G] = att_mfma(a[now][i], w[n][i / G], r.o[n][e + i % G]);
         }
     }
     __builtin_amdgcn_sched_barrier(0);
@@ -196,26 +232,30 @@ template <int DB>
 __device__ __forceinline__ void tile_scores(uint32_t keys, TileScores<DB> &s, const TileRows<DB> &r)
 {
     using S = TileShape<DB>;
-    constexpr int G = S::NQ < 4 ? S::NQ : 4, STEPS = S::KT * S::NQ / G;       // G pieces of keys are read while those before are multiplied
+    // two pieces of two tiles of keys are read while those before are multiplied: sums that follow each other are different ones
+    constexpr int STEPS = S::KT / 2 * S::NQ / 2;
     const uint32_t at = keys + (threadIdx.x & 63) * 16;
-    att_u32x4 a[2][G];
+    const auto read = [&](int f, int i) {
+        const int t = f / (S::NQ / 2) * 2 + (i & 1), c = f % (S::NQ / 2) * 2 + (i >> 1);
+        return *(const lds_u32x4 *)(uintptr_t)(at + (t * S::NQ + c) * 1024);
+    };
+    att_u32x4 a[2][4];
 #pragma unroll
-    for (int i = 0; i < G; ++i)
-        a[0][i] = *(const lds_u32x4 *)(uintptr_t)(at + i * 1024);
+    for (int i = 0; i < 4; ++i)
+        a[0][i] = read(0, i);
 #pragma unroll
     for (int f = 0; f < STEPS; ++f) {
         __builtin_amdgcn_sched_barrier(0);
         if (f + 1 < STEPS)
 #pragma unroll
-            for (int i = 0; i < G; ++i)
-                a[f + 1 & 1][i] = *(const lds_u32x4 *)(uintptr_t)(at + ((f + 1) * G + i) * 1024);
+            for (int i = 0; i < 4; ++i)
+                a[f + 1 & 1][i] = read(f + 1, i);
         __builtin_amdgcn_sched_barrier(0);
-        const int t = f * G / S::NQ;
 #pragma unroll
-        for (int i = 0; i < G; ++i)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int n = 0; n < S::NT; ++n) {
-                const int c = f * G % S::NQ + i;
+                const int t = f / (S::NQ / 2) * 2 + (i & 1), c = f % (S::NQ / 2) * 2 + (i >> 1);
                 s[n][t] = att_mfma(a[f & 1][i], r.q[n][c], c == 0 ? att_f32x4{0, 0, 0, 0} : s[n][t]);
             }
     }
@@ -277,16 +317,6 @@ __device__ __forceinline__ void tile_softmax(bool masked, TileScores<DB> &s, att
     }
 }
 
-// All that a wavefront has asked of LDS is done, then the workgroup meets.  (Loads from memory may be on their way.)
-__device__ __forceinline__ void tile_meet()
-{
-    __builtin_amdgcn_sched_barrier(0);
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_sched_barrier(0);
-}
-
 template <int DB, bool FULL>
 __global__ __launch_bounds__(64 * ATT_TILE_WAVES) void attend_tile_kernel(AttendParams p)
 {
@@ -329,29 +359,22 @@ __global__ __launch_bounds__(64 * ATT_TILE_WAVES) void attend_tile_kernel(Attend
     const int32_t most = first < it.rows ? sees(first + 16 * S::NT < it.rows ? first + 16 * S::NT - 1 : it.rows - 1) : it.begin;
     // steps from the one that begins at `clear` on have keys that some row of the workgroup does not see
     const int32_t clear = it.begin + (sees(it.first) - it.begin) / ATT_TILE_KEYS * ATT_TILE_KEYS;
-    TilePart<DB, FULL, false> k;
-    TilePart<DB, FULL, true> v;
+    TileStage<DB, FULL> in(p, it, wave, lane);
     bool odd = false;
-    k.look_up(p, it, it.begin, wave);
-    v.look_up(p, it, it.begin, wave);
-    k.load(p, it, wave, lane);
-    v.load(p, it, wave, lane);
-    k.look_up(p, it, it.begin + ATT_TILE_KEYS, wave);
-    v.look_up(p, it, it.begin + ATT_TILE_KEYS, wave);
+    in.look_up(p, it, it.begin, wave);
+    in.place(p, it, it.begin, wave);
+    in.load(p, wave, lane);
+    in.look_up(p, it, it.begin + ATT_TILE_KEYS, wave);
     if (it.begin >= clear)
-        odd |= v.clear();
-    k.store(lds, wave, lane);
-    v.store(lds + 2 * S::BYTES, wave, lane);
+        odd |= in.clear();
+    in.store(lds, lds + 2 * S::BYTES, wave, lane);
+    in.place(p, it, it.begin + ATT_TILE_KEYS, wave);
     __syncthreads();
     uint32_t room = 0;
     for (int32_t key0 = it.begin; key0 < it.end; key0 += ATT_TILE_KEYS) {
-        const bool more = key0 + ATT_TILE_KEYS < it.end;
-        if (more) {
-            k.load(p, it, wave, lane);
-            v.load(p, it, wave, lane);
-            k.look_up(p, it, key0 + 2 * ATT_TILE_KEYS, wave);
-            v.look_up(p, it, key0 + 2 * ATT_TILE_KEYS, wave);
-        }
+        // the next step's loads; behind the last step the last tile's again
+        in.load(p, wave, lane);
+        in.look_up(p, it, key0 + 2 * ATT_TILE_KEYS, wave);
         if (key0 < most) {
             TileScores<DB> s;
             att_u32x4 w[S::NT][S::KT / 2];
@@ -360,12 +383,10 @@ __global__ __launch_bounds__(64 * ATT_TILE_WAVES) void attend_tile_kernel(Attend
             tile_weigh<DB>(tile_vals_at<DB>(lds + 2 * S::BYTES + room), w, r);
         }
         room ^= S::BYTES;
-        if (more) {
-            if (key0 + ATT_TILE_KEYS >= clear)
-                odd |= v.clear();
-            k.store(lds + room, wave, lane);
-            v.store(lds + 2 * S::BYTES + room, wave, lane);
-        }
+        if (key0 + ATT_TILE_KEYS >= clear)
+            odd |= in.clear() && key0 + ATT_TILE_KEYS < it.end;
+        in.store(lds + room, lds + 2 * S::BYTES + room, wave, lane);
+        in.place(p, it, key0 + 2 * ATT_TILE_KEYS, wave);
         __syncthreads();
     }
     if (__syncthreads_or(odd))
