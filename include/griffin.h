@@ -350,7 +350,7 @@ typedef struct {
     int32_t page_size;       /* tokens in a page: a power of two from 16 to 65536 */
     int64_t n_pages;         /* pages in the pools, at most 2^31 - 1 */
     int64_t page_stride, head_stride, token_stride;   /* elements, multiples of 8; token_stride, head_stride >= dim,
-                                                         token_stride <= 2^26, page_stride <= 2^34 */
+                                                         token_stride <= 2^26, page_stride <= 2^33 */
 } griffin_kv_cache;
 
 /*

@@ -21,12 +21,14 @@ struct AttendParams {
     float2 *part_ml;         // [tokens][n_heads][chunks] maximum (base 2) and sum
     const int32_t *lens, *pages, *prefix_pages;
     int64_t ldq, hsq, ldo, hso, page_stride, head_stride, token_stride, ld_pages;
-    uint32_t page_stride16;  // page_stride in 16 bytes (of bf16)
+    uint32_t page_stride16;  // page_stride in 16 bytes
     float scale2;            // scale log2(e)
     int32_t n_heads, kv_heads, group, dim, page_shift, last_page, max_len, n_prefix;
     // keys a chunk (a multiple of a workgroup's step), chunks, and tiles of rows of the prefix
     int32_t chunk_prefix, chunk_own, chunks_prefix, chunks_own, tiles_prefix;
     int32_t wgs_prefix;      // workgroups of this launch that take the prefix, ahead of those that take own parts
+    int32_t items_own;       // own items of this launch
+    int32_t each, tiles_each;                                 // new tokens, and tiles of rows, of every sequence where they are equally many, else 0
     SeqTable seqs;
     int32_t tiles_own[GRIFFIN_MAX_SEQS + 1];                  // tiles of rows of the sequences before
 };
@@ -35,6 +37,7 @@ struct AttendParams {
 // [begin, end) of a list of pages, for kv head hk.  own: the position of token0 among its sequence's own tokens; -1: every row sees every key.
 struct AttendItem {
     const int32_t *pages;
+    int32_t last_entry;      // of the list that may be read
     int32_t begin, end, own, hk, token0, rows, first, split;
 };
 
@@ -49,72 +52,89 @@ __device__ __forceinline__ float lane_groups_max(float v)
 }
 
 // a page's number, kept in the pools
-__device__ __forceinline__ int64_t att_page(int32_t page, int32_t last_page) { return page < 0 ? 0 : (page > last_page ? last_page : page); }
+__device__ __forceinline__ uint32_t att_page(int32_t page, int32_t last_page) { return page < 0 ? 0 : (page > last_page ? last_page : page); }
 
-// where the tiles of a step lie: tile t's page and its first slot there, kept in range of the keys that there are
-struct AttTile {
-    int64_t base;                // elements from the head's begin
-    int32_t rows;                // its valid slots less one
-};
-
-__device__ __forceinline__ AttTile att_tile(const AttendParams &p, const int32_t *pages, int32_t key0, int32_t end)
+// The number of the page that holds a tile of 16 keys.  Keys behind the last one are read like others (the table's entry, clamped into the pools: some memory of
+// theirs), get no weight, and their values are made zero before they are multiplied by it.  By the vector memory path: a wait for a scalar load is one for all
+// that is asked of LDS behind it, too.
+__device__ __forceinline__ int32_t att_look_up(const AttendParams &p, const AttendItem &it, int32_t key)
 {
-    const int32_t last = (end - 1) & ~15;
-    key0 = key0 < last ? key0 : last;
-    key0 = __builtin_amdgcn_readfirstlane(key0);
-    AttTile t;
-    t.base = page_of(pages, key0 >> p.page_shift, p.last_page) * p.page_stride + (int64_t)(key0 & ((1 << p.page_shift) - 1)) * p.token_stride;
-    t.rows = end - 1 - key0 < 15 ? end - 1 - key0 : 15;
-    return t;
+    int32_t at = key >> p.page_shift;
+    at = at < it.last_entry ? at : it.last_entry;
+    asm volatile("" : "+v"(at));
+    return it.pages[at];
+}
+
+// where that tile begins, in bytes from the kv head's begin
+template <int ES>
+__device__ __forceinline__ uint64_t att_place(const AttendParams &p, int32_t page, int32_t key)
+{
+    return (uint64_t)att_page(__builtin_amdgcn_readfirstlane(page), p.last_page) * p.page_stride16 * 16 +
+           (uint64_t)(uint32_t)(key & ((1 << p.page_shift) - 1)) * ((uint32_t)p.token_stride * ES);
 }
 
 // All bits of the two bf16 in a word that are neither infinite nor NaN (an exponent of all ones)
 __device__ __forceinline__ uint32_t att_finite_mask(uint32_t w)
 {
-    return ((w & 0x7F80u) == 0x7F80u ? 0 : 0xFFFFu) | ((w & 0x7F800000u) == 0x7F800000u ? 0 : 0xFFFF0000u);
+    typedef __attribute__((ext_vector_type(2))) uint16_t pair_t;
+    const pair_t missing = __builtin_bit_cast(pair_t, ~w & 0x7F807F80u);      // 0: all ones
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(missing, pair_t{1, 1}) * pair_t{0xFFFF, 0xFFFF});
 }
 
-// The item of workgroup `id`; false: no row needs it.  Workgroups go [tile of ROWS rows][chunk][kv head], the prefix's first; TOP: own tiles from
-// the last to the first, those that see the most keys ahead
-template <int ROWS_PREFIX, int ROWS_OWN, bool TOP>
-__device__ __forceinline__ bool att_item(const AttendParams &p, int32_t id, AttendItem &it)
+// The sequence that `at` falls to, of `per` (tokens or tiles of rows) each or, with per == 0, by the sums in `first`
+__device__ __forceinline__ int att_sequence(int32_t at, int32_t per, const int32_t *first, int n)
 {
-    if (id < p.wgs_prefix) {
-        const int chunk = id / p.kv_heads % p.chunks_prefix, tile = id / p.kv_heads / p.chunks_prefix;
-        it.hk = id % p.kv_heads;
-        it.pages = p.prefix_pages;
-        it.begin = chunk * p.chunk_prefix;
-        it.end = it.begin + p.chunk_prefix < p.n_prefix ? it.begin + p.chunk_prefix : p.n_prefix;
-        it.own = -1;
-        it.token0 = 0;
-        it.rows = p.seqs.cu[p.seqs.n] * p.group;
-        it.first = tile * ROWS_PREFIX;
-        it.split = chunk;
-        return true;
+    if (per > 0)
+        return at / per;
+    int b = 0, hi = n - 1;                                    // the last sequence that begins at or before `at`
+    while (b < hi) {
+        const int mid = (b + hi + 1) / 2;
+        if (first[mid] <= at) b = mid;
+        else hi = mid - 1;
     }
-    id -= p.wgs_prefix;
+    return b;
+}
+
+// Prefix item `id` of [tile of ROWS rows][chunk][kv head]
+template <int ROWS>
+__device__ __forceinline__ void att_prefix_item(const AttendParams &p, int32_t id, AttendItem &it)
+{
+    const int chunk = id / p.kv_heads % p.chunks_prefix, tile = id / p.kv_heads / p.chunks_prefix;
+    it.hk = id % p.kv_heads;
+    it.pages = p.prefix_pages;
+    it.last_entry = (p.n_prefix - 1) >> p.page_shift;
+    it.begin = chunk * p.chunk_prefix;
+    it.end = it.begin + p.chunk_prefix < p.n_prefix ? it.begin + p.chunk_prefix : p.n_prefix;
+    it.own = -1;
+    it.token0 = 0;
+    it.rows = p.seqs.cu[p.seqs.n] * p.group;
+    it.first = tile * ROWS;
+    it.split = chunk;
+}
+
+// Own item `id` of [tile of ROWS rows][chunk][kv head]; TOP: from the last tile to the first, those that see the most keys ahead.  false: no row needs it.
+template <int ROWS, bool TOP>
+__device__ __forceinline__ bool att_own_item(const AttendParams &p, int32_t id, AttendItem &it)
+{
     const int chunk = id / p.kv_heads % p.chunks_own;
     int tile = id / p.kv_heads / p.chunks_own;
     if (TOP)
         tile = p.tiles_own[p.seqs.n] - 1 - tile;
     it.hk = id % p.kv_heads;
-    int b = 0, hi = p.seqs.n - 1;                          // the last sequence whose tiles begin at or before this one
-    while (b < hi) {
-        const int mid = (b + hi + 1) / 2;
-        if (p.tiles_own[mid] <= tile) b = mid;
-        else hi = mid - 1;
-    }
+    const int b = att_sequence(tile, p.tiles_each, p.tiles_own, p.seqs.n);
+    const int32_t len = p.lens[b];
+    it.pages = p.pages + (int64_t)b * p.ld_pages;
+    it.last_entry = (p.max_len - 1) >> p.page_shift;
     it.token0 = p.seqs.cu[b];
     it.rows = (p.seqs.cu[b + 1] - p.seqs.cu[b]) * p.group;
-    it.first = (tile - p.tiles_own[b]) * ROWS_OWN;
-    it.own = p.lens[b] < 0 ? 0 : (p.lens[b] < p.max_len ? p.lens[b] : p.max_len);
-    const int32_t last = it.first + ROWS_OWN < it.rows ? it.first + ROWS_OWN - 1 : it.rows - 1;       // the tile's last row sees the most keys
+    it.first = (tile - p.tiles_own[b]) * ROWS;
+    it.own = len < 0 ? 0 : (len < p.max_len ? len : p.max_len);
+    const int32_t last = it.first + ROWS < it.rows ? it.first + ROWS - 1 : it.rows - 1;               // the tile's last row sees the most keys
     const int32_t end = it.own + last / p.group + 1 < p.max_len ? it.own + last / p.group + 1 : p.max_len;
-    it.pages = p.pages + (int64_t)b * p.ld_pages;
     it.begin = chunk * p.chunk_own;
     it.end = it.begin + p.chunk_own < end ? it.begin + p.chunk_own : end;
     it.split = p.chunks_prefix + chunk;
-    return it.begin < it.end;                              // else no row reads this chunk's partial sums
+    return it.begin < it.end;                                 // else no row reads this chunk's partial sums
 }
 
 // launches the `wgs` workgroups of p on tiles of att_tile_rows(dim) rows; bf16 only

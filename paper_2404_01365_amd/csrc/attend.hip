@@ -57,44 +57,73 @@ struct AttVals {
 template <bool BF16, int DB, int NT>
 using AttScores = att_f32x4[NT][AttShape<BF16, DB>::KT];
 
+// A step's tiles of 16 keys: their pages' numbers (looked up a step ahead of their use) and places, and the lane's place in a tile
 template <bool BF16, int DB, bool FULL>
-__device__ __forceinline__ void att_load_keys(AttKeys<BF16, DB> &f, const AttendParams &p, const char *Kh, const AttTile *t, int lane)
-{
+struct AttStage {
     using S = AttShape<BF16, DB>;
-#pragma unroll
-    for (int i = 0; i < S::KT; ++i) {
-        const int row = (lane & 15) < t[i].rows ? (lane & 15) : t[i].rows;
-        const char *at = Kh + (t[i].base + row * p.token_stride) * (BF16 ? 2 : 4) + (lane >> 4) * 16;
-#pragma unroll
-        for (int s = 0; s < S::NQ; ++s) {
-            // features from dim on are zero here and in the queries: they add nothing, whatever the row's gap holds
-            if (FULL || (s * 4 + (lane >> 4)) * S::E < p.dim)
-                f.k[i][s] = *(const att_u32x4 *)(at + s * 64);
-            else
-                f.k[i][s] = att_u32x4{0, 0, 0, 0};
-        }
-    }
-}
+    static constexpr int ES = BF16 ? 2 : 4;
+    const char *K, *V;                       // of the kv head
+    uint32_t at_k, at_v[4];                  // of values: keys 4 (lane >> 4) + j
+    int32_t page[S::KT];
+    uint64_t base[S::KT];
 
-template <bool BF16, int DB, bool FULL>
-__device__ __forceinline__ void att_load_vals(AttVals<BF16, DB> &f, const AttendParams &p, const char *Vh, const AttTile *t, int lane)
-{
-    using S = AttShape<BF16, DB>;
+    __device__ __forceinline__ AttStage(const AttendParams &p, int hk, int lane)
+    {
+        const uint32_t stride = (uint32_t)p.token_stride * ES;
+        K = (const char *)p.K + hk * p.head_stride * ES;
+        V = (const char *)p.V + hk * p.head_stride * ES;
+        at_k = (lane & 15) * stride + (lane >> 4) * 16;
+        // features from dim on end in outputs that are not stored: any of the row's own will do
+        const int d = FULL || (lane & 15) * S::VD < p.dim ? (lane & 15) * S::VD : 0;
 #pragma unroll
-    for (int j = 0; j < S::VK; ++j) {
-        const int i = j >> 2, want = (lane >> 4) * 4 + (j & 3), row = want < t[i].rows ? want : t[i].rows;
-        const char *at = Vh + (t[i].base + row * p.token_stride) * (BF16 ? 2 : 4);
-#pragma unroll
-        for (int c = 0; c < S::NC; ++c) {
-            // features from dim on end in outputs that are not stored: any of the row's own will do
-            const int d0 = c * 16 * S::VD + (lane & 15) * S::VD, d = FULL || d0 < p.dim ? d0 : 0;
-            if (S::VW == 4)
-                *(att_u32x4 *)f.v[j][c] = *(const att_u32x4 *)(at + d * (BF16 ? 2 : 4));
-            else
-                *(uint2 *)f.v[j][c] = *(const uint2 *)(at + d * (BF16 ? 2 : 4));
-        }
+        for (int j = 0; j < 4; ++j)
+            at_v[j] = ((lane >> 4) * 4 + j) * stride + d * ES;
     }
-}
+
+    __device__ __forceinline__ void look_up(const AttendParams &p, const AttendItem &it, int32_t key0)
+    {
+#pragma unroll
+        for (int i = 0; i < S::KT; ++i)
+            page[i] = att_look_up(p, it, key0 + 16 * i);
+    }
+
+    __device__ __forceinline__ void place(const AttendParams &p, int32_t key0)
+    {
+#pragma unroll
+        for (int i = 0; i < S::KT; ++i)
+            base[i] = att_place<ES>(p, page[i], key0 + 16 * i);
+    }
+
+    __device__ __forceinline__ void load_keys(AttKeys<BF16, DB> &f, const AttendParams &p, int lane) const
+    {
+#pragma unroll
+        for (int i = 0; i < S::KT; ++i)
+#pragma unroll
+            for (int s = 0; s < S::NQ; ++s) {
+                // features from dim on are zero here and in the queries: they add nothing, whatever the row's gap holds
+                if (FULL || (s * 4 + (lane >> 4)) * S::E < p.dim)
+                    f.k[i][s] = *(const att_u32x4 *)(K + base[i] + at_k + s * 64);
+                else
+                    f.k[i][s] = att_u32x4{0, 0, 0, 0};
+            }
+    }
+
+    __device__ __forceinline__ void load_vals(AttVals<BF16, DB> &f, const AttendParams &p, int lane) const
+    {
+#pragma unroll
+        for (int j = 0; j < S::VK; ++j)
+#pragma unroll
+            for (int c = 0; c < S::NC; ++c) {
+                const char *at = V + base[j >> 2] + at_v[j & 3];
+                if (FULL || c == 0 || c * 16 * S::VD + (lane & 15) * S::VD < p.dim)
+                    at += c * 16 * S::VD * ES;
+                if (S::VW == 4)
+                    *(att_u32x4 *)f.v[j][c] = *(const att_u32x4 *)at;
+                else
+                    *(uint2 *)f.v[j][c] = *(const uint2 *)at;
+            }
+    }
+};
 
 template <bool BF16, int DB, int NT>
 __device__ __forceinline__ void att_scores(AttScores<BF16, DB, NT> &s, const AttKeys<BF16, DB> &f, const AttRows<BF16, DB, NT> &r)
@@ -121,9 +150,9 @@ __device__ __forceinline__ void att_scores(AttScores<BF16, DB, NT> &s, const Att
             }
 }
 
-// Scores to weights: the rows' maximum and sum carried on, o scaled to the new maximum.  MASKED: keys from r.end on get weight 0.
-template <bool BF16, int DB, int NT, bool MASKED>
-__device__ __forceinline__ void att_softmax(AttScores<BF16, DB, NT> &s, AttRows<BF16, DB, NT> &r, float scale2, int32_t key0, int lane)
+// Scores to weights: the rows' maximum and sum carried on, o scaled to the new maximum
+template <bool BF16, int DB, int NT>
+__device__ __forceinline__ void att_softmax(AttScores<BF16, DB, NT> &s, AttRows<BF16, DB, NT> &r, float scale2)
 {
     using S = AttShape<BF16, DB>;
 #pragma unroll
@@ -132,14 +161,11 @@ __device__ __forceinline__ void att_softmax(AttScores<BF16, DB, NT> &s, AttRows<
 #pragma unroll
         for (int i = 0; i < S::KT; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if (MASKED && key0 + 16 * i + (lane >> 4) * 4 + e >= r.end[n])
-                    s[n][i][e] = -INFINITY;
+            for (int e = 0; e < 4; ++e)
                 top = fmaxf(top, s[n][i][e]);
-            }
         const float m = fmaxf(r.m[n], lane_groups_max(top) * scale2);
         const float base = m == -INFINITY ? 0.0f : m;          // nothing seen yet: weights 2^-inf = 0
-        const float f = exp2f(r.m[n] - base);
+        const float f = __builtin_amdgcn_exp2f(r.m[n] - base);
         r.m[n] = m;
         float l = 0;
 #pragma unroll
@@ -154,6 +180,19 @@ __device__ __forceinline__ void att_softmax(AttScores<BF16, DB, NT> &s, AttRows<
         for (int c = 0; c < S::NO; ++c)
             r.o[n][c] *= f;
     }
+}
+
+// Keys from r.end on out of the scores
+template <bool BF16, int DB, int NT>
+__device__ __forceinline__ void att_mask(AttScores<BF16, DB, NT> &s, const AttRows<BF16, DB, NT> &r, int32_t key0, int lane)
+{
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < AttShape<BF16, DB>::KT; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                s[n][i][e] = key0 + 16 * i + (lane >> 4) * 4 + e < r.end[n] ? s[n][i][e] : -INFINITY;
 }
 
 // O^T += V^T P^T
@@ -196,38 +235,27 @@ __device__ __forceinline__ void att_weigh(const AttScores<BF16, DB, NT> &s, cons
     }
 }
 
-// Is any of the lane's values infinite or NaN (all exponent bits set)?
+// Before a masked step's second product.  Infinite and NaN values of keys that a row does not see must not reach it, as 0 x Inf would.  Values behind the last
+// key are made zero, and so are infinite and NaN ones; if there were any of these (`true`), they are added to the rows that do see them at the end
+// (att_add_infinite).
 template <bool BF16, int DB>
-__device__ __forceinline__ bool att_not_finite(const AttVals<BF16, DB> &f)
+__device__ __forceinline__ bool att_clear_infinite(AttVals<BF16, DB> &f, int32_t key0, int32_t end, int lane)
 {
     using S = AttShape<BF16, DB>;
-    uint32_t any = 0;
+    uint32_t odd = 0;
 #pragma unroll
-    for (int j = 0; j < S::VK; ++j)
+    for (int j = 0; j < S::VK; ++j) {
+        const uint32_t in = key0 + 16 * (j >> 2) + (lane >> 4) * 4 + (j & 3) < end ? ~0u : 0;
 #pragma unroll
         for (int c = 0; c < S::NC; ++c)
 #pragma unroll
-            for (int w = 0; w < S::VW; ++w)
-                any |= BF16 ? (f.v[j][c][w] & 0x7F807F80u) + 0x00800080u : ((f.v[j][c][w] & 0x7F800000u) + 0x00800000u);
-    return (any & (BF16 ? 0x80008000u : 0x80000000u)) != 0;
-}
-
-// Before a masked step's second product.  Infinite and NaN values of keys that a row does not see must not reach it, as 0 x Inf would: if there are any
-// (`true`), they are made zero here and added to the rows that do see them at the end (att_add_infinite).
-template <bool BF16, int DB>
-__device__ __forceinline__ bool att_clear_infinite(AttVals<BF16, DB> &f)
-{
-    using S = AttShape<BF16, DB>;
-    if (!__any(att_not_finite<BF16, DB>(f)))
-        return false;
-#pragma unroll
-    for (int j = 0; j < S::VK; ++j)
-#pragma unroll
-        for (int c = 0; c < S::NC; ++c)
-#pragma unroll
-            for (int w = 0; w < S::VW; ++w)
-                f.v[j][c][w] &= BF16 ? att_finite_mask(f.v[j][c][w]) : ((f.v[j][c][w] & 0x7F800000u) == 0x7F800000u ? 0 : ~0u);
-    return true;
+            for (int w = 0; w < S::VW; ++w) {
+                const uint32_t m = BF16 ? att_finite_mask(f.v[j][c][w]) : ((f.v[j][c][w] & 0x7F800000u) == 0x7F800000u ? 0 : ~0u);
+                f.v[j][c][w] &= m & in;
+                odd |= ~m & in;
+            }
+    }
+    return __any(odd != 0);
 }
 
 // ... of the keys from `key` on of one step
@@ -237,8 +265,7 @@ __device__ __forceinline__ void att_add_infinite(const AttendParams &p, const At
     using S = AttShape<BF16, DB>;
     const int32_t stop = key + S::KS < it.end ? key + S::KS : it.end;
     for (; key < stop; ++key) {
-        const AttTile tile = att_tile(p, it.pages, key & ~15, it.end);
-        const char *at = (const char *)p.V + (it.hk * p.head_stride + tile.base + (key & 15) * p.token_stride) * (BF16 ? 2 : 4);
+        const char *at = (const char *)p.V + it.hk * p.head_stride * (BF16 ? 2 : 4) + att_place<BF16 ? 2 : 4>(p, att_look_up(p, it, key), key);
 #pragma unroll
         for (int c = 0; c < S::NC; ++c)
 #pragma unroll
@@ -257,18 +284,22 @@ __device__ __forceinline__ void att_add_infinite(const AttendParams &p, const At
     }
 }
 
-// The item's rows first .. first + 16 NT - 1
-template <bool BF16, int DB, bool FULL, int NT>
+// The item's rows first .. first + 16 NT - 1, by the WAVES wavefronts of a workgroup (in turn, a step each) or by one alone
+template <bool BF16, int DB, bool FULL, int NT, int WAVES>
 __device__ __forceinline__ void attend_rows(const AttendParams &p, float *lds, const AttendItem &it)
 {
     using S = AttShape<BF16, DB>;
     constexpr int ES = BF16 ? 2 : 4;
     const int32_t begin = it.begin, end = it.end, own = it.own, rows = it.rows, first = it.first, hk = it.hk;
-    const int32_t *pages = it.pages;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = WAVES == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int32_t key0 = begin + wave * S::KS;
+    AttStage<BF16, DB, FULL> in(p, hk, lane);
+    in.look_up(p, it, key0);
     AttRows<BF16, DB, NT> r;
     int32_t token[NT], head[NT];
-    int32_t least = end;                                   // keys that all of the lane's rows see
+    int32_t least = end;                                   // keys that all rows see
+    if (own >= 0 && own + first / p.group + 1 < end)
+        least = own + first / p.group + 1;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         int32_t row = first + 16 * n + (lane & 15);
@@ -280,7 +311,6 @@ __device__ __forceinline__ void attend_rows(const AttendParams &p, float *lds, c
             const int32_t sees = own + row / p.group + 1;
             r.end[n] = sees < end ? sees : end;
         }
-        least = r.end[n] < least ? r.end[n] : least;
         const char *at = (const char *)p.q + ((int64_t)token[n] * p.ldq + (int64_t)head[n] * p.hsq) * ES + (lane >> 4) * 16;
 #pragma unroll
         for (int s = 0; s < S::NQ; ++s) {
@@ -295,43 +325,37 @@ __device__ __forceinline__ void attend_rows(const AttendParams &p, float *lds, c
         for (int c = 0; c < S::NO; ++c)
             r.o[n][c] = att_f32x4{0, 0, 0, 0};
     }
-    const char *Kh = (const char *)p.K + hk * p.head_stride * ES, *Vh = (const char *)p.V + hk * p.head_stride * ES;
-    int32_t key0 = begin + wave * S::KS;
     bool odd = false;
     if (key0 < end) {
         AttKeys<BF16, DB> fk;
         AttVals<BF16, DB> fv;
-        AttTile t[S::KT], next[S::KT];
-#pragma unroll
-        for (int i = 0; i < S::KT; ++i)
-            t[i] = att_tile(p, pages, key0 + 16 * i, end);
-        att_load_keys<BF16, DB, FULL>(fk, p, Kh, t, lane);
-        att_load_vals<BF16, DB, FULL>(fv, p, Vh, t, lane);
-        for (; key0 < end; key0 += ATT_WAVES * S::KS) {
+        in.place(p, key0);
+        in.load_keys(fk, p, lane);
+        in.look_up(p, it, key0 + WAVES * S::KS);
+        in.load_vals(fv, p, lane);
+        for (; key0 < end; key0 += WAVES * S::KS) {
             // the next step's keys leave as soon as this step's scores have taken the registers' old content, its values after the second product;
-            // behind the last step they are the last tile's again
-#pragma unroll
-            for (int i = 0; i < S::KT; ++i)
-                next[i] = att_tile(p, pages, key0 + ATT_WAVES * S::KS + 16 * i, end);
+            // behind the last step they are some that nobody looks at
             att_f32x4 s[NT][S::KT];
             att_scores<BF16, DB, NT>(s, fk, r);
             __builtin_amdgcn_sched_barrier(0);
-            att_load_keys<BF16, DB, FULL>(fk, p, Kh, next, lane);
+            in.place(p, key0 + WAVES * S::KS);
+            in.load_keys(fk, p, lane);
+            in.look_up(p, it, key0 + 2 * WAVES * S::KS);
             __builtin_amdgcn_sched_barrier(0);
-            if (__all(key0 + S::KS <= least))
-                att_softmax<BF16, DB, NT, false>(s, r, p.scale2, key0, lane);
-            else {
-                att_softmax<BF16, DB, NT, true>(s, r, p.scale2, key0, lane);
-                odd |= att_clear_infinite<BF16, DB>(fv);
+            if (key0 + S::KS > least) {
+                att_mask<BF16, DB, NT>(s, r, key0, lane);
+                odd |= att_clear_infinite<BF16, DB>(fv, key0, end, lane);
             }
+            att_softmax<BF16, DB, NT>(s, r, p.scale2);
             att_weigh<BF16, DB, NT>(s, fv, r);
             __builtin_amdgcn_sched_barrier(0);
-            att_load_vals<BF16, DB, FULL>(fv, p, Vh, next, lane);
+            in.load_vals(fv, p, lane);
         }
     }
     if (odd)
-        for (key0 = begin + wave * S::KS; key0 < end; key0 += ATT_WAVES * S::KS)
-            if (!__all(key0 + S::KS <= least))
+        for (key0 = begin + wave * S::KS; key0 < end; key0 += WAVES * S::KS)
+            if (key0 + S::KS > least)
                 att_add_infinite<BF16, DB, FULL, NT>(p, it, r, key0);
     // the four wavefronts' sums come together in two steps (2 and 3 to 0 and 1, then 1 to 0), lane by lane
     float *mine = lds + (wave & 1) * (S::NO * 4 + 2) * 64;
@@ -339,7 +363,7 @@ __device__ __forceinline__ void attend_rows(const AttendParams &p, float *lds, c
     for (int n = 0; n < NT; ++n) {
         r.l[n] = lane_groups_sum(r.l[n]);
 #pragma unroll
-        for (int step = ATT_WAVES / 2; step >= 1; step >>= 1) {
+        for (int step = WAVES / 2; step >= 1; step >>= 1) {
             __syncthreads();
             if (wave >= step && wave < 2 * step) {
 #pragma unroll
@@ -399,17 +423,25 @@ __device__ __forceinline__ void attend_rows(const AttendParams &p, float *lds, c
     }
 }
 
-template <bool BF16, int DB, bool FULL, int NTP, int NTO>
-__global__ __launch_bounds__(ATT_WAVES * 64) void attend_rows_kernel(AttendParams p)
+// LONE: own items go a wavefront each
+template <bool BF16, int DB, bool FULL, int NTP, int NTO, bool LONE>
+__global__ __launch_bounds__(ATT_WAVES * 64, DB > 128 || (!BF16 && DB > 64 && NTP > 1) ? 1 : 2) void attend_rows_kernel(AttendParams p)
 {
     __shared__ float lds[2 * (AttShape<BF16, DB>::NO * 4 + 2) * 64];
     AttendItem it;
-    if (!att_item<16 * NTP, 16 * NTO, false>(p, blockIdx.x, it))
+    if ((int32_t)blockIdx.x < p.wgs_prefix) {
+        att_prefix_item<16 * NTP>(p, blockIdx.x, it);
+        attend_rows<BF16, DB, FULL, NTP, ATT_WAVES>(p, lds, it);
         return;
-    if (NTP != NTO && it.own < 0)
-        attend_rows<BF16, DB, FULL, NTP>(p, lds, it);
-    else
-        attend_rows<BF16, DB, FULL, NTO>(p, lds, it);
+    }
+    int32_t id = blockIdx.x - p.wgs_prefix;
+    if (LONE) {
+        id = id * ATT_WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        if (id >= p.items_own)
+            return;
+    }
+    if (att_own_item<16 * NTO, false>(p, id, it))
+        attend_rows<BF16, DB, FULL, NTO, LONE ? 1 : ATT_WAVES>(p, lds, it);
 }
 
 // Joins a row's chunks: with M = max m_c, o = sum o_c 2^(m_c - M) / sum l_c 2^(m_c - M).  A row per WPR wavefronts; a wavefront takes
@@ -423,12 +455,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendParams p)
     if (WPR == 1 && row >= (int64_t)p.seqs.cu[p.seqs.n] * p.n_heads)
         return;
     const int32_t token = __builtin_amdgcn_readfirstlane((int32_t)(row / p.n_heads)), head = __builtin_amdgcn_readfirstlane((int32_t)(row % p.n_heads));
-    int b = 0, hi = p.seqs.n - 1;                          // the last sequence that begins at or before the token
-    while (b < hi) {
-        const int mid = (b + hi + 1) / 2;
-        if (p.seqs.cu[mid] <= token) b = mid;
-        else hi = mid - 1;
-    }
+    const int b = att_sequence(token, p.each, p.seqs.cu, p.seqs.n);
     const int32_t held = p.lens[b] < 0 ? 0 : (p.lens[b] < p.max_len ? p.lens[b] : p.max_len);
     const int32_t seen = held + token - p.seqs.cu[b] + 1 < p.max_len ? held + token - p.seqs.cu[b] + 1 : p.max_len;
     const int chunks = p.chunks_prefix + (seen + p.chunk_own - 1) / p.chunk_own;
@@ -491,6 +518,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendParams p)
 // ------------------------------------------------------------------ host side
 struct AttPlan {
     bool tile_prefix, tile_own;         // many rows: attend_tile.hip
+    bool lone;                          // own items of a few rows go a wavefront each
     int ntp, nto;                       // else tiles of 16 rows that a wavefront takes
     int32_t rows_prefix, rows_own;      // rows of a workgroup
     int32_t chunk_prefix, chunk_own, chunks_prefix, chunks_own, tiles_prefix, tiles_own;
@@ -510,8 +538,8 @@ static AttPlan attend_plan(const griffin_kv_cache &C, const griffin_kv_batch &B,
     pl.tile_prefix = bf16 && rows > 64;
     pl.nto = longest <= 32 ? 1 : widest;
     pl.ntp = rows <= 16 ? 1 : widest;
-    if (!pl.tile_own && !pl.tile_prefix && B.n_prefix > 0)
-        pl.ntp = std::max(pl.nto, pl.ntp);
+    if (!pl.tile_own && !pl.tile_prefix && pl.nto == widest)        // compiled pairs: (1, 1), (2, 1), (2, 2)
+        pl.ntp = widest;
     pl.rows_own = pl.tile_own ? att_tile_rows(C.dim) : 16 * pl.nto;
     pl.rows_prefix = pl.tile_prefix ? att_tile_rows(C.dim) : 16 * pl.ntp;
     int64_t tiles = 0;
@@ -519,6 +547,8 @@ static AttPlan attend_plan(const griffin_kv_cache &C, const griffin_kv_batch &B,
         tiles += ((int64_t)(seqs.cu[b + 1] - seqs.cu[b]) * group + pl.rows_own - 1) / pl.rows_own;
     pl.tiles_own = (int32_t)tiles;
     pl.tiles_prefix = B.n_prefix > 0 ? (int32_t)((rows + pl.rows_prefix - 1) / pl.rows_prefix) : 0;
+    // own parts that fill the chip as they are, a wavefront each, are not cut
+    pl.lone = !pl.tile_own && C.kv_heads * tiles >= 1024;
     // as many keys a chunk as leave a workgroup a CU, or two of the smaller ones; own parts of many rows are one chunk if they fill the chip
     const int64_t step = ATT_WAVES * (bf16 ? 32 : 16);
     const int64_t work_prefix = C.kv_heads * (int64_t)pl.tiles_prefix * B.n_prefix, work_own = C.kv_heads * tiles * B.max_len;
@@ -526,10 +556,11 @@ static AttPlan attend_plan(const griffin_kv_cache &C, const griffin_kv_batch &B,
         const int64_t quantum = tile ? ATT_TILE_KEYS : step;
         return (int32_t)((std::max(work / (tile ? 256 : 512), (int64_t)1) + quantum - 1) / quantum * quantum);
     };
-    pl.chunk_prefix = chunk(pl.tile_prefix, pl.tile_prefix == pl.tile_own ? work_prefix + work_own : work_prefix);
-    pl.chunk_own = chunk(pl.tile_own, pl.tile_prefix == pl.tile_own ? work_prefix + work_own : work_own);
-    if (pl.tile_own && C.kv_heads * tiles >= 256)
-        pl.chunk_own = (B.max_len + ATT_TILE_KEYS - 1) / ATT_TILE_KEYS * ATT_TILE_KEYS;
+    const bool together = pl.tile_prefix == pl.tile_own && !pl.lone;
+    pl.chunk_prefix = chunk(pl.tile_prefix, together ? work_prefix + work_own : work_prefix);
+    pl.chunk_own = chunk(pl.tile_own, together ? work_prefix + work_own : work_own);
+    if (pl.lone || (pl.tile_own && C.kv_heads * tiles >= 256))
+        pl.chunk_own = (int32_t)((B.max_len + step - 1) / step * step);
     pl.chunks_prefix = (B.n_prefix + pl.chunk_prefix - 1) / pl.chunk_prefix;
     pl.chunks_own = (B.max_len + pl.chunk_own - 1) / pl.chunk_own;
     return pl;
@@ -542,26 +573,27 @@ size_t attend_floats(const griffin_kv_cache &C, const griffin_kv_batch &B, const
     return pl.chunks_prefix + pl.chunks_own < 2 ? 0 : slots * (C.dim + 2);
 }
 
-template <bool BF16, int DB, int NTP, int NTO>
-static int go_rows(const AttendParams &p, int32_t wgs, hipStream_t st)
+template <bool BF16, int DB, int NTP, int NTO, bool LONE>
+static int go_rows(const AttendParams &p, hipStream_t st)
 {
+    const int32_t wgs = p.wgs_prefix + (LONE ? (p.items_own + ATT_WAVES - 1) / ATT_WAVES : p.items_own);
     if (p.dim == DB)
-        hipLaunchKernelGGL((attend_rows_kernel<BF16, DB, true, NTP, NTO>), dim3(wgs), dim3(ATT_WAVES * 64), 0, st, p);
+        hipLaunchKernelGGL((attend_rows_kernel<BF16, DB, true, NTP, NTO, LONE>), dim3(wgs), dim3(ATT_WAVES * 64), 0, st, p);
     else
-        hipLaunchKernelGGL((attend_rows_kernel<BF16, DB, false, NTP, NTO>), dim3(wgs), dim3(ATT_WAVES * 64), 0, st, p);
+        hipLaunchKernelGGL((attend_rows_kernel<BF16, DB, false, NTP, NTO, LONE>), dim3(wgs), dim3(ATT_WAVES * 64), 0, st, p);
     return check_launch("attend_rows_kernel");
 }
 
-template <bool BF16, int DB>
-static int launch_rows(const AttendParams &p, int ntp, int nto, int32_t wgs, hipStream_t st)
+template <bool BF16, int DB, bool LONE>
+static int launch_rows(const AttendParams &p, int ntp, int nto, hipStream_t st)
 {
     if constexpr (DB <= 128) {
         if (nto == 2)
-            return go_rows<BF16, DB, 2, 2>(p, wgs, st);
+            return go_rows<BF16, DB, 2, 2, LONE>(p, st);
         if (ntp == 2)
-            return go_rows<BF16, DB, 2, 1>(p, wgs, st);
+            return go_rows<BF16, DB, 2, 1, LONE>(p, st);
     }
-    return go_rows<BF16, DB, 1, 1>(p, wgs, st);
+    return go_rows<BF16, DB, 1, 1, LONE>(p, st);
 }
 
 template <bool BF16, int DB>
@@ -577,7 +609,9 @@ static int attend_typed(AttendParams &p, const AttPlan &pl, hipStream_t st)
         }
     if (rc == GRIFFIN_OK && others > 0) {
         p.wgs_prefix = pl.tile_prefix ? 0 : wgs_prefix;
-        rc = launch_rows<BF16, DB>(p, pl.tile_prefix || wgs_prefix == 0 ? pl.nto : pl.ntp, pl.tile_own ? 1 : pl.nto, others, st);
+        p.items_own = pl.tile_own ? 0 : wgs_own;
+        const int ntp = p.wgs_prefix > 0 ? pl.ntp : 1, nto = p.items_own > 0 ? pl.nto : 1;
+        rc = pl.lone ? launch_rows<BF16, DB, true>(p, ntp, nto, st) : launch_rows<BF16, DB, false>(p, ntp, nto, st);
     }
     if (rc != GRIFFIN_OK || !p.part)
         return rc;
@@ -615,7 +649,7 @@ int launch_attend(const AttendJob &job, const SeqTable &seqs, hipStream_t st)
     p.lens = B.lens; p.pages = B.pages; p.prefix_pages = B.prefix_pages;
     p.ldq = job.ldq; p.hsq = job.hsq; p.ldo = job.ldo; p.hso = job.hso;
     p.page_stride = C.page_stride; p.head_stride = C.head_stride; p.token_stride = C.token_stride; p.ld_pages = B.ld_pages;
-    p.page_stride16 = (uint32_t)(C.page_stride / 8);
+    p.page_stride16 = (uint32_t)(C.page_stride / (C.dtype == GRIFFIN_BF16 ? 8 : 4));
     p.scale2 = job.scale * 1.4426950408889634f;
     p.n_heads = job.n_heads; p.kv_heads = C.kv_heads; p.group = job.n_heads / C.kv_heads; p.dim = C.dim;
     p.page_shift = __builtin_ctz(C.page_size);
@@ -626,6 +660,12 @@ int launch_attend(const AttendJob &job, const SeqTable &seqs, hipStream_t st)
     p.seqs = seqs;
     for (int b = 0; b < GRIFFIN_MAX_SEQS; ++b)
         p.tiles_own[b + 1] = p.tiles_own[b] + (int32_t)(((int64_t)(seqs.cu[b + 1] - seqs.cu[b]) * p.group + pl.rows_own - 1) / pl.rows_own);
+    p.each = seqs.cu[1];
+    p.tiles_each = p.tiles_own[1];
+    for (int b = 1; b < seqs.n; ++b) {
+        p.each = seqs.cu[b + 1] - seqs.cu[b] == seqs.cu[1] ? p.each : 0;
+        p.tiles_each = p.tiles_own[b + 1] - p.tiles_own[b] == p.tiles_own[1] ? p.tiles_each : 0;
+    }
     return C.dtype == GRIFFIN_BF16 ? attend_width<true>(p, pl, st) : attend_width<false>(p, pl, st);
 }
 

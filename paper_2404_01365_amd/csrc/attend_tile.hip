@@ -47,9 +47,7 @@ struct TileStage {
     using S = TileShape<DB>;
     const char *K, *V;                       // of the kv head
     uint32_t stride, at_k, at_v;             // bytes from key to key; the lane's place in a tile
-    int32_t last;                            // where the last tile begins
     int32_t page[S::PIECES];
-    int32_t over[S::PIECES];                 // keys that the tile is short of
     uint64_t base[S::PIECES];
     att_u32x4 k[S::PIECES], v[S::PIECES];
 
@@ -64,73 +62,54 @@ struct TileStage {
         stride = (uint32_t)p.token_stride * 2;
         at_k = (lane & 15) * stride + (wave % S::NQ * 32 + (lane >> 4) * 8) * 2;
         at_v = row_of(wave, lane) * stride + lane % (DB / 8) * 16;
-        last = (it.end - 1) & ~15;
-    }
-
-    __device__ __forceinline__ int32_t key_of(int32_t key0, int wave, int i) const
-    {
-        const int32_t key = key0 + 16 * tile_of(wave, i);
-        return key < last ? key : last;      // behind the last tile: it again
     }
 
     __device__ __forceinline__ void look_up(const AttendParams &p, const AttendItem &it, int32_t key0, int wave)
     {
 #pragma unroll
-        for (int i = 0; i < S::PIECES; ++i) {
-            // by the vector memory path: a wait for a scalar load is one for all that is asked of LDS behind it, too
-            int32_t at = key_of(key0, wave, i) >> p.page_shift;
-            asm volatile("" : "+v"(at));
-            page[i] = it.pages[at];
-        }
+        for (int i = 0; i < S::PIECES; ++i)
+            page[i] = att_look_up(p, it, key0 + 16 * tile_of(wave, i));
     }
 
-    __device__ __forceinline__ void place(const AttendParams &p, const AttendItem &it, int32_t key0, int wave)
+    __device__ __forceinline__ void place(const AttendParams &p, int32_t key0, int wave)
     {
 #pragma unroll
-        for (int i = 0; i < S::PIECES; ++i) {
-            const int32_t key = key_of(key0, wave, i);
-            base[i] = (uint64_t)(uint32_t)att_page(__builtin_amdgcn_readfirstlane(page[i]), p.last_page) * p.page_stride16 * 16 +
-                      (uint64_t)(uint32_t)(key & ((1 << p.page_shift) - 1)) * stride;
-            over[i] = 16 - (it.end - key);
-        }
+        for (int i = 0; i < S::PIECES; ++i)
+            base[i] = att_place<2>(p, page[i], key0 + 16 * tile_of(wave, i));
     }
 
     __device__ __forceinline__ void load(const AttendParams &p, int wave, int lane)
     {
 #pragma unroll
         for (int i = 0; i < S::PIECES; ++i) {
-            uint32_t ak = at_k, av = at_v;
-            if (over[i] > 0) {                // keys behind the last: it again
-                const int32_t k_over = over[i] - (15 - (lane & 15)), v_over = over[i] - (15 - row_of(wave, lane));
-                ak -= (uint32_t)(k_over > 0 ? k_over : 0) * stride;
-                av -= (uint32_t)(v_over > 0 ? v_over : 0) * stride;
-            }
             // the piece's features are the same in every round of ATT_TILE_WAVES pieces.  Keys' features from dim on are zero, as the queries' are;
             // values' end in outputs that are not stored
             if (FULL || wave % S::NQ * 32 + (lane >> 4) * 8 < p.dim)
-                k[i] = *(const att_u32x4 *)(K + base[i] + ak);
+                k[i] = *(const att_u32x4 *)(K + base[i] + at_k);
             else
                 k[i] = att_u32x4{0, 0, 0, 0};
             if (FULL || lane % (DB / 8) * 8 < p.dim)
-                v[i] = *(const att_u32x4 *)(V + base[i] + av);
+                v[i] = *(const att_u32x4 *)(V + base[i] + at_v);
             else
                 v[i] = att_u32x4{0, 0, 0, 0};
         }
     }
     static_assert(ATT_TILE_WAVES % S::NQ == 0, "a wavefront's pieces of keys have the same features");
 
-    // infinite and NaN values as zeros, true if there were any
-    __device__ __forceinline__ bool clear()
+    // values behind the last key, and infinite and NaN ones, as zeros; true if there were any of these
+    __device__ __forceinline__ bool clear(int32_t key0, int32_t end, int wave, int lane)
     {
         uint32_t kept = ~0u;
 #pragma unroll
-        for (int i = 0; i < S::PIECES; ++i)
+        for (int i = 0; i < S::PIECES; ++i) {
+            const bool in = key0 + 16 * tile_of(wave, i) + row_of(wave, lane) < end;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const uint32_t m = att_finite_mask(v[i][j]);
-                v[i][j] &= m;
-                kept &= m;
+                v[i][j] = in ? v[i][j] & m : 0;
+                kept &= in ? m : ~0u;
             }
+        }
         return kept != ~0u;
     }
 
@@ -179,8 +158,8 @@ __device__ __forceinline__ void tile_add_infinite(const AttendParams &p, const A
     using S = TileShape<DB>;
     const int d = (threadIdx.x >> 4 & 3) * 4;
     for (; key < most; ++key) {
-        const AttTile tile = att_tile(p, it.pages, key & ~15, it.end);
-        const uint16_t *at = (const uint16_t *)p.V + it.hk * p.head_stride + tile.base + (key & 15) * p.token_stride + d;
+        const uint16_t *at = (const uint16_t *)((const char *)((const uint16_t *)p.V + it.hk * p.head_stride) +
+                                                att_place<2>(p, att_look_up(p, it, key), key)) + d;
 #pragma unroll
         for (int e = 0; e < S::NO; ++e) {
             __builtin_amdgcn_sched_barrier(0);
@@ -324,7 +303,9 @@ __global__ __launch_bounds__(64 * ATT_TILE_WAVES) void attend_tile_kernel(Attend
     extern __shared__ __align__(1024) char tile_lds[];        // two steps of keys and values
     const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)tile_lds;
     AttendItem it;
-    if (!att_item<att_tile_rows(DB), att_tile_rows(DB), true>(p, blockIdx.x, it))
+    if ((int32_t)blockIdx.x < p.wgs_prefix)
+        att_prefix_item<att_tile_rows(DB)>(p, blockIdx.x, it);
+    else if (!att_own_item<att_tile_rows(DB), true>(p, blockIdx.x - p.wgs_prefix, it))
         return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int32_t first = it.first + wave * 16 * S::NT;
@@ -362,17 +343,17 @@ __global__ __launch_bounds__(64 * ATT_TILE_WAVES) void attend_tile_kernel(Attend
     TileStage<DB, FULL> in(p, it, wave, lane);
     bool odd = false;
     in.look_up(p, it, it.begin, wave);
-    in.place(p, it, it.begin, wave);
+    in.place(p, it.begin, wave);
     in.load(p, wave, lane);
     in.look_up(p, it, it.begin + ATT_TILE_KEYS, wave);
     if (it.begin >= clear)
-        odd |= in.clear();
+        odd |= in.clear(it.begin, it.end, wave, lane);
     in.store(lds, lds + 2 * S::BYTES, wave, lane);
-    in.place(p, it, it.begin + ATT_TILE_KEYS, wave);
+    in.place(p, it.begin + ATT_TILE_KEYS, wave);
     __syncthreads();
     uint32_t room = 0;
     for (int32_t key0 = it.begin; key0 < it.end; key0 += ATT_TILE_KEYS) {
-        // the next step's loads; behind the last step the last tile's again
+        // the next step's loads; behind the last step some keys that nobody reads
         in.load(p, wave, lane);
         in.look_up(p, it, key0 + 2 * ATT_TILE_KEYS, wave);
         if (key0 < most) {
@@ -384,9 +365,9 @@ __global__ __launch_bounds__(64 * ATT_TILE_WAVES) void attend_tile_kernel(Attend
         }
         room ^= S::BYTES;
         if (key0 + ATT_TILE_KEYS >= clear)
-            odd |= in.clear() && key0 + ATT_TILE_KEYS < it.end;
+            odd |= in.clear(key0 + ATT_TILE_KEYS, it.end, wave, lane);
         in.store(lds + room, lds + 2 * S::BYTES + room, wave, lane);
-        in.place(p, it, key0 + 2 * ATT_TILE_KEYS, wave);
+        in.place(p, key0 + 2 * ATT_TILE_KEYS, wave);
         __syncthreads();
     }
     if (__syncthreads_or(odd))

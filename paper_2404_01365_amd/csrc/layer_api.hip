@@ -17,7 +17,7 @@ static int check_cache(const griffin_kv_cache *C)
     if (C->dim % 8 != 0 || !aligned16(C->K) || !aligned16(C->V) || !row_stride(C->token_stride, C->dim) ||
         !row_stride(C->head_stride, C->dim) || C->page_stride < 0 || C->page_stride % 8 != 0 || C->n_pages > INT32_MAX)
         return GRIFFIN_ESHAPE;
-    if (C->dim > 256 || C->token_stride > (1 << 26) || C->page_stride > (1ll << 34) || C->page_size < 16 || C->page_size > 65536 || (C->page_size & (C->page_size - 1)) || C->kv_heads > 1024)
+    if (C->dim > 256 || C->token_stride > (1 << 26) || C->page_stride > (1ll << 33) || C->page_size < 16 || C->page_size > 65536 || (C->page_size & (C->page_size - 1)) || C->kv_heads > 1024)
         return GRIFFIN_EUNSUPPORTED;
     return GRIFFIN_OK;
 }
