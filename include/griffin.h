@@ -399,7 +399,7 @@ int griffin_kv_append(const griffin_kv_cache *C, const griffin_kv_batch *B, cons
  * weighted sum are fp32; bf16 caches take the weights rounded to bf16 into the second product (2^-8 each).  Keys that a token does not
  * see do not reach its output, whatever they hold.
  *   q, out     [tokens][n_heads][dim], token and head strides (ldq, hsq; ldo, hso), multiples of 8, 16-byte aligned; out is not q
- *   n_heads    a multiple of C->kv_heads, at most 1024
+ *   n_heads    a multiple of C->kv_heads, at most 1024; tokens * n_heads^2 < 2^32
  *   scale      > 0 and finite
  *   workspace  griffin_attention_workspace_bytes(C, B, n_heads) bytes or more (may be 0), 256-byte aligned.  The query depends on sizes
  *              alone: kv_heads, dim, dtype, page_size, cu_seqlens, max_len, n_prefix

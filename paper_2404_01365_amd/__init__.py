@@ -136,10 +136,27 @@ def _ptr(t) -> Optional[int]:
     return t.data_ptr()
 
 
+_raw_stream = _device = None
+
+
+def _current_stream() -> int:
+    """Handle of PyTorch's current stream.  torch.cuda.current_stream() makes an object for it, which takes as long as a small launch
+    (2.7 us); once the runtime is up the handle alone is asked for, where this PyTorch has a call for it."""
+    global _raw_stream, _device
+    if _raw_stream is None:
+        import torch
+        if not torch.cuda.is_initialized():
+            return torch.cuda.current_stream().cuda_stream
+        _device = getattr(torch._C, "_cuda_getDevice", None)
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if _device is None or _raw_stream is None:
+            _device, _raw_stream = (lambda: None), (lambda device: torch.cuda.current_stream().cuda_stream)
+    return _raw_stream(_device())
+
+
 def _stream(stream) -> Optional[int]:
     if stream is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream or None
+        return _current_stream() or None
     if isinstance(stream, int):
         return stream or None
     return stream.cuda_stream or None

@@ -14,6 +14,13 @@ constexpr int ATT_WAVES = 4;            // of a workgroup of attend.hip
 constexpr int ATT_TILE_WAVES = 8;       // ... of attend_tile.hip
 constexpr int ATT_TILE_KEYS = 64;       // its step
 
+// Division by a number that the host knows, exact while the dividend times it is below 2^32
+struct AttDiv {
+    uint32_t by, mul;
+
+    __device__ __forceinline__ int32_t operator()(int32_t x) const { return by == 1 ? x : (int32_t)__umulhi((uint32_t)x, mul); }
+};
+
 struct AttendParams {
     const void *q, *K, *V;
     void *out;
@@ -23,12 +30,13 @@ struct AttendParams {
     int64_t ldq, hsq, ldo, hso, page_stride, head_stride, token_stride, ld_pages;
     uint32_t page_stride16;  // page_stride in 16 bytes
     float scale2;            // scale log2(e)
-    int32_t n_heads, kv_heads, group, dim, page_shift, last_page, max_len, n_prefix;
+    int32_t tokens, n_heads, kv_heads, group, dim, page_shift, last_page, max_len, n_prefix;
+    AttDiv by_heads, by_kv_heads, by_group, by_chunks_prefix, by_chunks_own;
     // keys a chunk (a multiple of a workgroup's step), chunks, and tiles of rows of the prefix
     int32_t chunk_prefix, chunk_own, chunks_prefix, chunks_own, tiles_prefix;
     int32_t wgs_prefix;      // workgroups of this launch that take the prefix, ahead of those that take own parts
     int32_t items_own;       // own items of this launch
-    int32_t each, tiles_each;                                 // new tokens, and tiles of rows, of every sequence where they are equally many, else 0
+    AttDiv each, tiles_each;                                  // new tokens, and tiles of rows, of every sequence where they are equally many, else by 0
     SeqTable seqs;
     int32_t tiles_own[GRIFFIN_MAX_SEQS + 1];                  // tiles of rows of the sequences before
 };
@@ -81,11 +89,11 @@ __device__ __forceinline__ uint32_t att_finite_mask(uint32_t w)
     return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(missing, pair_t{1, 1}) * pair_t{0xFFFF, 0xFFFF});
 }
 
-// The sequence that `at` falls to, of `per` (tokens or tiles of rows) each or, with per == 0, by the sums in `first`
-__device__ __forceinline__ int att_sequence(int32_t at, int32_t per, const int32_t *first, int n)
+// The sequence that `at` falls to, of `per` (tokens or tiles of rows) each or, with per 0, by the sums in `first`
+__device__ __forceinline__ int att_sequence(int32_t at, const AttDiv &per, const int32_t *first, int n)
 {
-    if (per > 0)
-        return at / per;
+    if (per.by > 0)
+        return per(at);
     int b = 0, hi = n - 1;                                    // the last sequence that begins at or before `at`
     while (b < hi) {
         const int mid = (b + hi + 1) / 2;
@@ -99,15 +107,15 @@ __device__ __forceinline__ int att_sequence(int32_t at, int32_t per, const int32
 template <int ROWS>
 __device__ __forceinline__ void att_prefix_item(const AttendParams &p, int32_t id, AttendItem &it)
 {
-    const int chunk = id / p.kv_heads % p.chunks_prefix, tile = id / p.kv_heads / p.chunks_prefix;
-    it.hk = id % p.kv_heads;
+    const int32_t of_heads = p.by_kv_heads(id), tile = p.by_chunks_prefix(of_heads), chunk = of_heads - tile * p.chunks_prefix;
+    it.hk = id - of_heads * p.kv_heads;
     it.pages = p.prefix_pages;
     it.last_entry = (p.n_prefix - 1) >> p.page_shift;
     it.begin = chunk * p.chunk_prefix;
     it.end = it.begin + p.chunk_prefix < p.n_prefix ? it.begin + p.chunk_prefix : p.n_prefix;
     it.own = -1;
     it.token0 = 0;
-    it.rows = p.seqs.cu[p.seqs.n] * p.group;
+    it.rows = p.tokens * p.group;
     it.first = tile * ROWS;
     it.split = chunk;
 }
@@ -116,11 +124,9 @@ __device__ __forceinline__ void att_prefix_item(const AttendParams &p, int32_t i
 template <int ROWS, bool TOP>
 __device__ __forceinline__ bool att_own_item(const AttendParams &p, int32_t id, AttendItem &it)
 {
-    const int chunk = id / p.kv_heads % p.chunks_own;
-    int tile = id / p.kv_heads / p.chunks_own;
-    if (TOP)
-        tile = p.tiles_own[p.seqs.n] - 1 - tile;
-    it.hk = id % p.kv_heads;
+    const int32_t of_heads = p.by_kv_heads(id), of_chunks = p.by_chunks_own(of_heads), chunk = of_heads - of_chunks * p.chunks_own;
+    const int32_t tile = TOP ? p.tiles_own[p.seqs.n] - 1 - of_chunks : of_chunks;
+    it.hk = id - of_heads * p.kv_heads;
     const int b = att_sequence(tile, p.tiles_each, p.tiles_own, p.seqs.n);
     const int32_t len = p.lens[b];
     it.pages = p.pages + (int64_t)b * p.ld_pages;
@@ -130,7 +136,7 @@ __device__ __forceinline__ bool att_own_item(const AttendParams &p, int32_t id, 
     it.first = (tile - p.tiles_own[b]) * ROWS;
     it.own = len < 0 ? 0 : (len < p.max_len ? len : p.max_len);
     const int32_t last = it.first + ROWS < it.rows ? it.first + ROWS - 1 : it.rows - 1;               // the tile's last row sees the most keys
-    const int32_t end = it.own + last / p.group + 1 < p.max_len ? it.own + last / p.group + 1 : p.max_len;
+    const int32_t end = it.own + p.by_group(last) + 1 < p.max_len ? it.own + p.by_group(last) + 1 : p.max_len;
     it.begin = chunk * p.chunk_own;
     it.end = it.begin + p.chunk_own < end ? it.begin + p.chunk_own : end;
     it.split = p.chunks_prefix + chunk;

@@ -284,6 +284,39 @@ __device__ __forceinline__ void att_add_infinite(const AttendParams &p, const At
     }
 }
 
+// Where a row's sums of a chunk lie
+__device__ __forceinline__ int64_t att_slot(const AttendParams &p, const AttendItem &it, int32_t row)
+{
+    const int32_t token = p.by_group(row), head = it.hk * p.group + row - token * p.group;
+    return ((int64_t)(it.token0 + token) * p.n_heads + head) * (p.chunks_prefix + p.chunks_own) + it.split;
+}
+
+// Features d .. d + 7 of a row: the sums themselves for the join, or the output
+template <bool BF16, bool FULL>
+__device__ __forceinline__ void att_store8(const AttendParams &p, const AttendItem &it, int32_t row, int d, float (&x)[8], float l)
+{
+    if (!FULL && d >= p.dim)
+        return;
+    if (p.part) {
+        float *at = p.part + att_slot(p, it, row) * p.dim + d;
+        *(float4 *)at = make_float4(x[0], x[1], x[2], x[3]);
+        *(float4 *)(at + 4) = make_float4(x[4], x[5], x[6], x[7]);
+        return;
+    }
+    const float f = l == 0.0f ? 0.0f : 1.0f / l;           // a row without keys: zeros
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        x[j] *= f;
+    const int32_t token = p.by_group(row), head = it.hk * p.group + row - token * p.group;
+    char *at = (char *)p.out + ((int64_t)(it.token0 + token) * p.ldo + (int64_t)head * p.hso + d) * (BF16 ? 2 : 4);
+    if (BF16)
+        *(uint4 *)at = make_uint4(f32x2_to_bf16x2(x[0], x[1]), f32x2_to_bf16x2(x[2], x[3]), f32x2_to_bf16x2(x[4], x[5]), f32x2_to_bf16x2(x[6], x[7]));
+    else {
+        *(float4 *)at = make_float4(x[0], x[1], x[2], x[3]);
+        *(float4 *)(at + 16) = make_float4(x[4], x[5], x[6], x[7]);
+    }
+}
+
 // The item's rows first .. first + 16 NT - 1, by the WAVES wavefronts of a workgroup (in turn, a step each) or by one alone
 template <bool BF16, int DB, bool FULL, int NT, int WAVES>
 __device__ __forceinline__ void attend_rows(const AttendParams &p, float *lds, const AttendItem &it)
@@ -296,22 +329,20 @@ __device__ __forceinline__ void attend_rows(const AttendParams &p, float *lds, c
     AttStage<BF16, DB, FULL> in(p, hk, lane);
     in.look_up(p, it, key0);
     AttRows<BF16, DB, NT> r;
-    int32_t token[NT], head[NT];
     int32_t least = end;                                   // keys that all rows see
-    if (own >= 0 && own + first / p.group + 1 < end)
-        least = own + first / p.group + 1;
+    if (own >= 0 && own + p.by_group(first) + 1 < end)
+        least = own + p.by_group(first) + 1;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         int32_t row = first + 16 * n + (lane & 15);
         row = row < rows ? row : rows - 1;                 // rows behind the last repeat it and are not stored
-        token[n] = it.token0 + row / p.group;
-        head[n] = hk * p.group + row % p.group;
+        const int32_t token = p.by_group(row), head = hk * p.group + row - token * p.group;
         r.end[n] = end;
         if (own >= 0) {
-            const int32_t sees = own + row / p.group + 1;
+            const int32_t sees = own + token + 1;
             r.end[n] = sees < end ? sees : end;
         }
-        const char *at = (const char *)p.q + ((int64_t)token[n] * p.ldq + (int64_t)head[n] * p.hsq) * ES + (lane >> 4) * 16;
+        const char *at = (const char *)p.q + ((int64_t)(it.token0 + token) * p.ldq + (int64_t)head * p.hsq) * ES + (lane >> 4) * 16;
 #pragma unroll
         for (int s = 0; s < S::NQ; ++s) {
             if (FULL || (s * 4 + (lane >> 4)) * S::E < p.dim)
@@ -357,69 +388,82 @@ __device__ __forceinline__ void attend_rows(const AttendParams &p, float *lds, c
         for (key0 = begin + wave * S::KS; key0 < end; key0 += WAVES * S::KS)
             if (key0 + S::KS > least)
                 att_add_infinite<BF16, DB, FULL, NT>(p, it, r, key0);
-    // the four wavefronts' sums come together in two steps (2 and 3 to 0 and 1, then 1 to 0), lane by lane
-    float *mine = lds + (wave & 1) * (S::NO * 4 + 2) * 64;
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
+    for (int n = 0; n < NT; ++n)
         r.l[n] = lane_groups_sum(r.l[n]);
+    if constexpr (WAVES == 1) {
 #pragma unroll
-        for (int step = WAVES / 2; step >= 1; step >>= 1) {
-            __syncthreads();
-            if (wave >= step && wave < 2 * step) {
+        for (int n = 0; n < NT; ++n) {
+            const int32_t row = first + 16 * n + (lane & 15);
+            if (row >= rows)
+                continue;
+            if (p.part && lane < 16)
+                p.part_ml[att_slot(p, it, row)] = make_float2(r.m[n], r.l[n]);
 #pragma unroll
-                for (int c = 0; c < S::NO; ++c)
-                    *(att_f32x4 *)(mine + c * 256 + lane * 4) = r.o[n][c];
-                mine[S::NO * 256 + lane] = r.m[n];
-                mine[S::NO * 256 + 64 + lane] = r.l[n];
-            }
-            __syncthreads();
-            if (wave < step) {
-                const float *from = lds + ((wave + step) & 1) * (S::NO * 4 + 2) * 64;
-                const float m2 = from[S::NO * 256 + lane], m = fmaxf(r.m[n], m2), base = m == -INFINITY ? 0.0f : m;
-                const float f1 = exp2f(r.m[n] - base), f2 = exp2f(m2 - base);
-                r.m[n] = m;
-                r.l[n] = r.l[n] * f1 + from[S::NO * 256 + 64 + lane] * f2;
+            for (int c = 0; c < S::NC; ++c)
 #pragma unroll
-                for (int c = 0; c < S::NO; ++c)
-                    r.o[n][c] = r.o[n][c] * f1 + *(const att_f32x4 *)(from + c * 256 + lane * 4) * f2;
-            }
+                for (int h = 0; h < S::VD / 2; ++h) {      // eight consecutive features of the lane's run of 4 VD
+                    float x[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        x[j] = r.o[n][c * S::VD + (h * 8 + j) % S::VD][(h * 8 + j) / S::VD];
+                    att_store8<BF16, FULL>(p, it, row, (c * 16 + (lane >> 4) * 4) * S::VD + h * 8, x, r.l[n]);
+                }
         }
-    }
-    if (wave != 0)
         return;
+    }
+    // The wavefronts' sums come together in LDS, up to 128 features of 16 rows at a time; then every thread joins and stores eight features of a row.
+    constexpr int W = DB < 128 ? DB : 128, CW = W / (16 * S::VD);          // features, and runs of a lane, at a time
+    float *ml = lds + WAVES * 16 * (W + 4);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        if (first + 16 * n + (lane & 15) >= rows)
-            continue;
-        const int64_t slot = ((int64_t)token[n] * p.n_heads + head[n]) * (p.chunks_prefix + p.chunks_own) + it.split;
-        const float f = p.part ? 1.0f : (r.l[n] == 0.0f ? 0.0f : 1.0f / r.l[n]);        // a row without keys: zeros
-        if (p.part && lane < 16)
-            p.part_ml[slot] = make_float2(r.m[n], r.l[n]);
+        const int here = rows - first - 16 * n < 16 ? rows - first - 16 * n : 16;
+        if (here <= 0)
+            break;
 #pragma unroll
-        for (int c = 0; c < S::NC; ++c)
+        for (int part = 0; part < S::NC / CW; ++part) {
+            if (n > 0 || part > 0)
+                __syncthreads();
+            if ((lane & 15) < here) {
+                float *mine = lds + (wave * 16 + (lane & 15)) * (W + 4);
 #pragma unroll
-            for (int h = 0; h < S::VD / 2; ++h) {          // eight consecutive features of the lane's run of 4 VD
-                const int d = (c * 16 + (lane >> 4) * 4) * S::VD + h * 8;
-                if (!FULL && d >= p.dim)
-                    continue;
-                float x[8];
+                for (int c = 0; c < CW; ++c)
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    x[j] = r.o[n][c * S::VD + (h * 8 + j) % S::VD][(h * 8 + j) / S::VD] * f;
-                if (p.part) {
-                    *(float4 *)(p.part + slot * p.dim + d) = make_float4(x[0], x[1], x[2], x[3]);
-                    *(float4 *)(p.part + slot * p.dim + d + 4) = make_float4(x[4], x[5], x[6], x[7]);
-                } else {
-                    char *at = (char *)p.out + ((int64_t)token[n] * p.ldo + (int64_t)head[n] * p.hso + d) * ES;
-                    if (BF16)
-                        *(uint4 *)at = make_uint4(f32x2_to_bf16x2(x[0], x[1]), f32x2_to_bf16x2(x[2], x[3]), f32x2_to_bf16x2(x[4], x[5]),
-                                                  f32x2_to_bf16x2(x[6], x[7]));
-                    else {
-                        *(float4 *)at = make_float4(x[0], x[1], x[2], x[3]);
-                        *(float4 *)(at + 16) = make_float4(x[4], x[5], x[6], x[7]);
+                    for (int h = 0; h < S::VD; ++h) {      // four consecutive features
+                        att_f32x4 x;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            x[j] = r.o[n][(part * CW + c) * S::VD + (h * 4 + j) % S::VD][(h * 4 + j) / S::VD];
+                        *(att_f32x4 *)(mine + (c * 16 + (lane >> 4) * 4) * S::VD + h * 4) = x;
                     }
+                if (lane < 16) {
+                    ml[wave * 32 + lane] = r.m[n];
+                    ml[wave * 32 + 16 + lane] = r.l[n];
                 }
             }
+            __syncthreads();
+            for (int item = threadIdx.x; item < here * (W / 8); item += WAVES * 64) {
+                const int at = item / (W / 8), d = item % (W / 8) * 8;
+                float m = -INFINITY, l = 0, x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w)
+                    m = fmaxf(m, ml[w * 32 + at]);
+                const float base = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) {
+                    const float f = __builtin_amdgcn_exp2f(ml[w * 32 + at] - base);
+                    const float *from = lds + (w * 16 + at) * (W + 4) + d;
+                    l += ml[w * 32 + 16 + at] * f;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        x[j] += from[j] * f;
+                }
+                const int32_t row = first + 16 * n + at;
+                if (p.part && part == 0 && d == 0)
+                    p.part_ml[att_slot(p, it, row)] = make_float2(m, l);
+                att_store8<BF16, FULL>(p, it, row, part * W + d, x, l);
+            }
+        }
     }
 }
 
@@ -427,7 +471,7 @@ __device__ __forceinline__ void attend_rows(const AttendParams &p, float *lds, c
 template <bool BF16, int DB, bool FULL, int NTP, int NTO, bool LONE>
 __global__ __launch_bounds__(ATT_WAVES * 64, DB > 128 || (!BF16 && DB > 64 && NTP > 1) ? 1 : 2) void attend_rows_kernel(AttendParams p)
 {
-    __shared__ float lds[2 * (AttShape<BF16, DB>::NO * 4 + 2) * 64];
+    __shared__ __align__(16) float lds[ATT_WAVES * 16 * ((DB < 128 ? DB : 128) + 4) + ATT_WAVES * 32];
     AttendItem it;
     if ((int32_t)blockIdx.x < p.wgs_prefix) {
         att_prefix_item<16 * NTP>(p, blockIdx.x, it);
@@ -452,60 +496,81 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendParams p)
     constexpr int LANES = DB / 4, PAR = 64 / LANES;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = lane / LANES, d = lane % LANES * 4;
     const int64_t row = (int64_t)blockIdx.x * (4 / WPR) + (WPR == 1 ? wave : 0);
-    if (WPR == 1 && row >= (int64_t)p.seqs.cu[p.seqs.n] * p.n_heads)
+    if (WPR == 1 && row >= (int64_t)p.tokens * p.n_heads)
         return;
-    const int32_t token = __builtin_amdgcn_readfirstlane((int32_t)(row / p.n_heads)), head = __builtin_amdgcn_readfirstlane((int32_t)(row % p.n_heads));
+    const int32_t token = __builtin_amdgcn_readfirstlane(p.by_heads((int32_t)row)), head = __builtin_amdgcn_readfirstlane((int32_t)row - token * p.n_heads);
     const int b = att_sequence(token, p.each, p.seqs.cu, p.seqs.n);
     const int32_t held = p.lens[b] < 0 ? 0 : (p.lens[b] < p.max_len ? p.lens[b] : p.max_len);
     const int32_t seen = held + token - p.seqs.cu[b] + 1 < p.max_len ? held + token - p.seqs.cu[b] + 1 : p.max_len;
     const int chunks = p.chunks_prefix + (seen + p.chunk_own - 1) / p.chunk_own;
     const int64_t slot0 = row * (p.chunks_prefix + p.chunks_own);
-    float m = -INFINITY;
-    for (int c = lane; c < chunks; c += 64)
-        m = fmaxf(m, p.part_ml[slot0 + c].x);
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1)
-        m = fmaxf(m, __shfl_xor(m, off));
-    const float base = m == -INFINITY ? 0.0f : m;
-    float l = 0;
+    // chunks c, c + WPR PAR, ... with a running maximum of their own, U on their way at a time
+    constexpr int U = 8;
+    float m = -INFINITY, l = 0;
     att_f32x4 o = {0, 0, 0, 0};
-    const bool in = d < p.dim;
-#pragma unroll 8
-    for (int c = (WPR == 1 ? 0 : wave * PAR) + sub; c < chunks; c += WPR * PAR) {
-        const float2 ml = p.part_ml[slot0 + c];
-        const float f = exp2f(ml.x - base);
-        l += ml.y * f;
-        if (in)
-            o += *(const att_f32x4 *)(p.part + (slot0 + c) * p.dim + d) * f;
+    const int d_in = d < p.dim ? d : 0;
+    for (int c = (WPR == 1 ? 0 : wave * PAR) + sub; c < chunks; c += U * WPR * PAR) {
+        float2 ml[U];
+        att_f32x4 x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int at = c + u * WPR * PAR < chunks ? c + u * WPR * PAR : c;
+            ml[u] = p.part_ml[slot0 + at];
+            x[u] = *(const att_f32x4 *)(p.part + (slot0 + at) * p.dim + d_in);
+        }
+        float top = m;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            top = fmaxf(top, ml[u].x);
+        const float base = top == -INFINITY ? 0.0f : top, f = __builtin_amdgcn_exp2f(m - base);
+        m = top;
+        l *= f;
+        o *= f;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (c + u * WPR * PAR < chunks) {
+                const float g = __builtin_amdgcn_exp2f(ml[u].x - base);
+                l += ml[u].y * g;
+                o += x[u] * g;
+            }
     }
 #pragma unroll
     for (int off = LANES; off < 64; off <<= 1) {
-        l += __shfl_xor(l, off);
+        const float m2 = __shfl_xor(m, off), l2 = __shfl_xor(l, off), top = fmaxf(m, m2), base = top == -INFINITY ? 0.0f : top;
+        const float f = __builtin_amdgcn_exp2f(m - base), f2 = __builtin_amdgcn_exp2f(m2 - base);
+        m = top;
+        l = l * f + l2 * f2;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            o[e] += __shfl_xor(o[e], off);
+            o[e] = o[e] * f + __shfl_xor(o[e], off) * f2;
     }
     if (WPR > 1) {
-        __shared__ float lds[WPR][LANES * 4 + 1];
+        __shared__ __align__(16) float lds[WPR][LANES * 4 + 4];
         if (sub == 0) {
-            *(float *)&lds[wave][0] = l;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                lds[wave][1 + d + e] = o[e];
+            *(att_f32x4 *)&lds[wave][d] = o;
+            if (d == 0) {
+                lds[wave][LANES * 4] = m;
+                lds[wave][LANES * 4 + 1] = l;
+            }
         }
         __syncthreads();
         if (wave != 0)
             return;
+        m = -INFINITY;
         l = 0;
         o = att_f32x4{0, 0, 0, 0};
-        for (int w = 0; w < WPR; ++w) {
-            l += lds[w][0];
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                o[e] += lds[w][1 + d + e];
+        for (int w = 0; w < WPR; ++w)
+            m = fmaxf(m, lds[w][LANES * 4]);
+        const float base = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+        for (int w = 0; w < WPR; ++w) {
+            const float f = __builtin_amdgcn_exp2f(lds[w][LANES * 4] - base);
+            l += lds[w][LANES * 4 + 1] * f;
+            o += *(const att_f32x4 *)&lds[w][d] * f;
         }
     }
-    if (sub != 0 || !in)
+    if (sub != 0 || d >= p.dim)
         return;
     const float f = l == 0.0f ? 0.0f : 1.0f / l;
     const int64_t at = (int64_t)token * p.ldo + (int64_t)head * p.hso + d;
@@ -553,8 +618,8 @@ static AttPlan attend_plan(const griffin_kv_cache &C, const griffin_kv_batch &B,
     const int64_t step = ATT_WAVES * (bf16 ? 32 : 16);
     const int64_t work_prefix = C.kv_heads * (int64_t)pl.tiles_prefix * B.n_prefix, work_own = C.kv_heads * tiles * B.max_len;
     const auto chunk = [&](bool tile, int64_t work) {
-        const int64_t quantum = tile ? ATT_TILE_KEYS : step;
-        return (int32_t)((std::max(work / (tile ? 256 : 512), (int64_t)1) + quantum - 1) / quantum * quantum);
+        const int64_t quantum = tile ? ATT_TILE_KEYS : step, wgs = tile || pl.lone || C.dim > 128 ? 256 : 1024;
+        return (int32_t)((std::max((work + wgs - 1) / wgs, (int64_t)1) + quantum - 1) / quantum * quantum);
     };
     const bool together = pl.tile_prefix == pl.tile_own && !pl.lone;
     pl.chunk_prefix = chunk(pl.tile_prefix, together ? work_prefix + work_own : work_prefix);
@@ -632,13 +697,18 @@ static int attend_width(AttendParams &p, const AttPlan &pl, hipStream_t st)
     return p.dim <= 128 ? attend_typed<BF16, 128>(p, pl, st) : attend_typed<BF16, 256>(p, pl, st);
 }
 
+static AttDiv divide_by(int32_t d) { return {(uint32_t)d, d > 1 ? (uint32_t)(((uint64_t)1 << 32) / d) + 1 : 0}; }
+
 int launch_attend(const AttendJob &job, const SeqTable &seqs, hipStream_t st)
 {
     const griffin_kv_cache &C = job.C;
     const griffin_kv_batch &B = job.B;
     const AttPlan pl = attend_plan(C, B, seqs, job.n_heads);
     const int64_t wgs = (int64_t)C.kv_heads * ((int64_t)pl.tiles_prefix * pl.chunks_prefix + (int64_t)pl.tiles_own * pl.chunks_own);
-    if (wgs >= 1 << 23 || (int64_t)seqs.cu[seqs.n] * job.n_heads >= 1 << 24)      // a launch holds fewer than 2^32 threads
+    // a launch holds fewer than 2^32 threads, and quotients are exact while dividend times divisor is below 2^32
+    const int64_t rows = (int64_t)seqs.cu[seqs.n] * job.n_heads, limit = (int64_t)1 << 32;
+    if (wgs >= 1 << 23 || rows >= 1 << 24 || wgs * C.kv_heads >= limit || wgs * std::max(pl.chunks_prefix, pl.chunks_own) >= limit ||
+        rows * job.n_heads >= limit)
         return GRIFFIN_EUNSUPPORTED;
     AttendParams p = {};
     p.q = job.q; p.K = C.K; p.V = C.V; p.out = job.out;
@@ -651,6 +721,7 @@ int launch_attend(const AttendJob &job, const SeqTable &seqs, hipStream_t st)
     p.page_stride = C.page_stride; p.head_stride = C.head_stride; p.token_stride = C.token_stride; p.ld_pages = B.ld_pages;
     p.page_stride16 = (uint32_t)(C.page_stride / (C.dtype == GRIFFIN_BF16 ? 8 : 4));
     p.scale2 = job.scale * 1.4426950408889634f;
+    p.tokens = seqs.cu[seqs.n];
     p.n_heads = job.n_heads; p.kv_heads = C.kv_heads; p.group = job.n_heads / C.kv_heads; p.dim = C.dim;
     p.page_shift = __builtin_ctz(C.page_size);
     p.last_page = (int32_t)(C.n_pages - 1);
@@ -660,12 +731,15 @@ int launch_attend(const AttendJob &job, const SeqTable &seqs, hipStream_t st)
     p.seqs = seqs;
     for (int b = 0; b < GRIFFIN_MAX_SEQS; ++b)
         p.tiles_own[b + 1] = p.tiles_own[b] + (int32_t)(((int64_t)(seqs.cu[b + 1] - seqs.cu[b]) * p.group + pl.rows_own - 1) / pl.rows_own);
-    p.each = seqs.cu[1];
-    p.tiles_each = p.tiles_own[1];
+    int32_t each = seqs.n > 1 ? seqs.cu[1] : 0, tiles_each = seqs.n > 1 ? p.tiles_own[1] : 0;
     for (int b = 1; b < seqs.n; ++b) {
-        p.each = seqs.cu[b + 1] - seqs.cu[b] == seqs.cu[1] ? p.each : 0;
-        p.tiles_each = p.tiles_own[b + 1] - p.tiles_own[b] == p.tiles_own[1] ? p.tiles_each : 0;
+        each = seqs.cu[b + 1] - seqs.cu[b] == seqs.cu[1] ? each : 0;
+        tiles_each = p.tiles_own[b + 1] - p.tiles_own[b] == p.tiles_own[1] ? tiles_each : 0;
     }
+    p.each = divide_by((int64_t)p.tokens * each < (int64_t)1 << 32 ? each : 0);
+    p.tiles_each = divide_by((int64_t)pl.tiles_own * tiles_each < (int64_t)1 << 32 ? tiles_each : 0);
+    p.by_heads = divide_by(p.n_heads); p.by_kv_heads = divide_by(p.kv_heads); p.by_group = divide_by(p.group);
+    p.by_chunks_prefix = divide_by(pl.chunks_prefix > 0 ? pl.chunks_prefix : 1); p.by_chunks_own = divide_by(pl.chunks_own);
     return C.dtype == GRIFFIN_BF16 ? attend_width<true>(p, pl, st) : attend_width<false>(p, pl, st);
 }
 

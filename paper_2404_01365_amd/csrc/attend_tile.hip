@@ -310,7 +310,7 @@ __global__ __launch_bounds__(64 * ATT_TILE_WAVES) void attend_tile_kernel(Attend
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int32_t first = it.first + wave * 16 * S::NT;
     const auto sees = [&](int32_t row) {                      // where the keys that a row sees end
-        const int32_t to = it.own + row / p.group + 1;
+        const int32_t to = it.own + p.by_group(row) + 1;
         return it.own < 0 || to > it.end ? it.end : to;
     };
     // rows behind the last repeat it and are not stored
@@ -320,7 +320,8 @@ __global__ __launch_bounds__(64 * ATT_TILE_WAVES) void attend_tile_kernel(Attend
     for (int n = 0; n < S::NT; ++n) {
         const int32_t row = of(n);
         r.end[n] = sees(row);
-        const char *at = (const char *)p.q + ((int64_t)(it.token0 + row / p.group) * p.ldq + (int64_t)(it.hk * p.group + row % p.group) * p.hsq) * 2 +
+        const int32_t token = p.by_group(row), head = it.hk * p.group + row - token * p.group;
+        const char *at = (const char *)p.q + ((int64_t)(it.token0 + token) * p.ldq + (int64_t)head * p.hsq) * 2 +
                          (lane >> 4) * 16;
 #pragma unroll
         for (int s = 0; s < S::NQ; ++s) {
@@ -377,7 +378,7 @@ __global__ __launch_bounds__(64 * ATT_TILE_WAVES) void attend_tile_kernel(Attend
         const float l = lane_groups_sum(r.l[n]);
         if (first + 16 * n + (lane & 15) >= it.rows)
             continue;
-        const int32_t row = of(n), token = it.token0 + row / p.group, head = it.hk * p.group + row % p.group;
+        const int32_t row = of(n), of_group = p.by_group(row), token = it.token0 + of_group, head = it.hk * p.group + row - of_group * p.group;
         if (p.part) {
             const int64_t slot = ((int64_t)token * p.n_heads + head) * (p.chunks_prefix + p.chunks_own) + it.split;
             if (lane < 16)
