@@ -341,22 +341,19 @@ __global__ __launch_bounds__(64 * ATT_TILE_WAVES) void attend_tile_kernel(Attend
     const int32_t most = first < it.rows ? sees(first + 16 * S::NT < it.rows ? first + 16 * S::NT - 1 : it.rows - 1) : it.begin;
     // steps from the one that begins at `clear` on have keys that some row of the workgroup does not see
     const int32_t clear = it.begin + (sees(it.first) - it.begin) / ATT_TILE_KEYS * ATT_TILE_KEYS;
-    TileStage<DB, FULL> in(p, it, wave, lane);
+    // Loads are two steps ahead of their use: a step's work is shorter than a read from memory under load takes.  Two stages take turns; step i
+    // loads step i + 2's, looks up i + 4's pages, and stores i + 1's in the other room.  Behind the last step they are some keys that nobody reads.
+    TileStage<DB, FULL> even(p, it, wave, lane), odds(p, it, wave, lane);
     bool odd = false;
-    in.look_up(p, it, it.begin, wave);
-    in.place(p, it.begin, wave);
-    in.load(p, wave, lane);
-    in.look_up(p, it, it.begin + ATT_TILE_KEYS, wave);
-    if (it.begin >= clear)
-        odd |= in.clear(it.begin, it.end, wave, lane);
-    in.store(lds, lds + 2 * S::BYTES, wave, lane);
-    in.place(p, it.begin + ATT_TILE_KEYS, wave);
-    __syncthreads();
     uint32_t room = 0;
-    for (int32_t key0 = it.begin; key0 < it.end; key0 += ATT_TILE_KEYS) {
-        // the next step's loads; behind the last step some keys that nobody reads
-        in.load(p, wave, lane);
-        in.look_up(p, it, key0 + 2 * ATT_TILE_KEYS, wave);
+    const auto store = [&](TileStage<DB, FULL> &in, int32_t key0) {
+        if (key0 >= clear)
+            odd |= in.clear(key0, it.end, wave, lane);
+        in.store(lds + room, lds + 2 * S::BYTES + room, wave, lane);
+    };
+    const auto step = [&](TileStage<DB, FULL> &now, TileStage<DB, FULL> &other, int32_t key0) {
+        now.load(p, wave, lane);
+        now.look_up(p, it, key0 + 4 * ATT_TILE_KEYS, wave);
         if (key0 < most) {
             TileScores<DB> s;
             att_u32x4 w[S::NT][S::KT / 2];
@@ -365,11 +362,26 @@ __global__ __launch_bounds__(64 * ATT_TILE_WAVES) void attend_tile_kernel(Attend
             tile_weigh<DB>(tile_vals_at<DB>(lds + 2 * S::BYTES + room), w, r);
         }
         room ^= S::BYTES;
-        if (key0 + ATT_TILE_KEYS >= clear)
-            odd |= in.clear(key0 + ATT_TILE_KEYS, it.end, wave, lane);
-        in.store(lds + room, lds + 2 * S::BYTES + room, wave, lane);
-        in.place(p, key0 + 2 * ATT_TILE_KEYS, wave);
+        store(other, key0 + ATT_TILE_KEYS);
+        other.place(p, key0 + 3 * ATT_TILE_KEYS, wave);
         __syncthreads();
+    };
+    even.look_up(p, it, it.begin, wave);
+    odds.look_up(p, it, it.begin + ATT_TILE_KEYS, wave);
+    even.place(p, it.begin, wave);
+    odds.place(p, it.begin + ATT_TILE_KEYS, wave);
+    even.load(p, wave, lane);
+    even.look_up(p, it, it.begin + 2 * ATT_TILE_KEYS, wave);
+    odds.load(p, wave, lane);
+    odds.look_up(p, it, it.begin + 3 * ATT_TILE_KEYS, wave);
+    store(even, it.begin);
+    even.place(p, it.begin + 2 * ATT_TILE_KEYS, wave);
+    __syncthreads();
+    for (int32_t key0 = it.begin; key0 < it.end; key0 += 2 * ATT_TILE_KEYS) {
+        step(even, odds, key0);
+        if (key0 + ATT_TILE_KEYS >= it.end)
+            break;
+        step(odds, even, key0 + ATT_TILE_KEYS);
     }
     if (__syncthreads_or(odd))
         tile_add_infinite<DB, FULL>(p, it, r, clear, most);
