@@ -38,7 +38,8 @@ struct AttendParams {
     int32_t items_own;       // own items of this launch
     AttDiv each, tiles_each;                                  // new tokens, and tiles of rows, of every sequence where they are equally many, else by 0
     SeqTable seqs;
-    int32_t tiles_own[GRIFFIN_MAX_SEQS + 1];                  // tiles of rows of the sequences before
+    int32_t tiles_own[GRIFFIN_MAX_SEQS + 1];                  // tiles of rows of the sequences before; where attend_tile.hip takes own parts:
+    uint8_t order[GRIFFIN_MAX_SEQS];                          // ... in this order, the sequences with most tiles first
 };
 
 // A workgroup's share: rows first .. of the `rows` rows whose tokens begin at token0 (row = token * group + member of the group), against keys
@@ -120,20 +121,42 @@ __device__ __forceinline__ void att_prefix_item(const AttendParams &p, int32_t i
     it.split = chunk;
 }
 
-// Own item `id` of [tile of ROWS rows][chunk][kv head]; TOP: from the last tile to the first, those that see the most keys ahead.  false: no row needs it.
+// Tiles of rows in falling order of their number within a sequence, so that those that see the most keys are begun first: the `id`-th one.  With tiles
+// T_0 >= T_1 >= .. of the sequences in p.order and S_m = T_0 + .. + T_(m-1), m sequences have a tile t for t in [T_m, T_(m-1)), and S_m - m t
+// tiles have number t or more.
+__device__ __forceinline__ void att_top_tile(const AttendParams &p, int32_t id, int &b, int32_t &tile)
+{
+    int lo = 1, hi = p.seqs.n;                                // the least m with id < S_m - m T_m (T_n = 0)
+    while (lo < hi) {
+        const int mid = (lo + hi) / 2;
+        const int32_t below = mid < p.seqs.n ? p.tiles_own[mid + 1] - p.tiles_own[mid] : 0;
+        if (id < p.tiles_own[mid] - mid * below) hi = mid;
+        else lo = mid + 1;
+    }
+    tile = (p.tiles_own[lo] - 1 - id) / lo;
+    b = p.order[id - (p.tiles_own[lo] - lo * (tile + 1))];
+}
+
+// Own item `id` of [tile of ROWS rows][chunk][kv head]; TOP: tiles as att_top_tile has them.  false: no row needs it.
 template <int ROWS, bool TOP>
 __device__ __forceinline__ bool att_own_item(const AttendParams &p, int32_t id, AttendItem &it)
 {
     const int32_t of_heads = p.by_kv_heads(id), of_chunks = p.by_chunks_own(of_heads), chunk = of_heads - of_chunks * p.chunks_own;
-    const int32_t tile = TOP ? p.tiles_own[p.seqs.n] - 1 - of_chunks : of_chunks;
+    int b;
+    int32_t tile;
+    if (TOP)
+        att_top_tile(p, of_chunks, b, tile);
+    else {
+        b = att_sequence(of_chunks, p.tiles_each, p.tiles_own, p.seqs.n);
+        tile = of_chunks - p.tiles_own[b];
+    }
     it.hk = id - of_heads * p.kv_heads;
-    const int b = att_sequence(tile, p.tiles_each, p.tiles_own, p.seqs.n);
     const int32_t len = p.lens[b];
     it.pages = p.pages + (int64_t)b * p.ld_pages;
     it.last_entry = (p.max_len - 1) >> p.page_shift;
     it.token0 = p.seqs.cu[b];
     it.rows = (p.seqs.cu[b + 1] - p.seqs.cu[b]) * p.group;
-    it.first = (tile - p.tiles_own[b]) * ROWS;
+    it.first = tile * ROWS;
     it.own = len < 0 ? 0 : (len < p.max_len ? len : p.max_len);
     const int32_t last = it.first + ROWS < it.rows ? it.first + ROWS - 1 : it.rows - 1;               // the tile's last row sees the most keys
     const int32_t end = it.own + p.by_group(last) + 1 < p.max_len ? it.own + p.by_group(last) + 1 : p.max_len;

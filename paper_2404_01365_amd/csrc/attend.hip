@@ -14,6 +14,8 @@
 // feature 8 r + e) and turns it with 32 byte permutes.
 //
 // Long key ranges are cut into chunks for as many workgroups as fill the chip; each leaves its rows' o, m and l, and a second kernel joins them.
+#include <algorithm>
+
 #include "attend.h"
 
 namespace griffin {
@@ -729,8 +731,13 @@ int launch_attend(const AttendJob &job, const SeqTable &seqs, hipStream_t st)
     p.chunk_prefix = pl.chunk_prefix; p.chunk_own = pl.chunk_own;
     p.chunks_prefix = pl.chunks_prefix; p.chunks_own = pl.chunks_own; p.tiles_prefix = pl.tiles_prefix;
     p.seqs = seqs;
-    for (int b = 0; b < GRIFFIN_MAX_SEQS; ++b)
-        p.tiles_own[b + 1] = p.tiles_own[b] + (int32_t)(((int64_t)(seqs.cu[b + 1] - seqs.cu[b]) * p.group + pl.rows_own - 1) / pl.rows_own);
+    const auto tiles_of = [&](int b) { return (int32_t)(((int64_t)(seqs.cu[b + 1] - seqs.cu[b]) * p.group + pl.rows_own - 1) / pl.rows_own); };
+    for (int b = 0; b < seqs.n; ++b)
+        p.order[b] = (uint8_t)b;
+    if (pl.tile_own)
+        std::stable_sort(p.order, p.order + seqs.n, [&](uint8_t a, uint8_t b) { return tiles_of(a) > tiles_of(b); });
+    for (int b = 0; b < seqs.n; ++b)
+        p.tiles_own[b + 1] = p.tiles_own[b] + tiles_of(p.order[b]);
     int32_t each = seqs.n > 1 ? seqs.cu[1] : 0, tiles_each = seqs.n > 1 ? p.tiles_own[1] : 0;
     for (int b = 1; b < seqs.n; ++b) {
         each = seqs.cu[b + 1] - seqs.cu[b] == seqs.cu[1] ? each : 0;
