@@ -59,7 +59,7 @@ struct AttVals {
 template <bool BF16, int DB, int NT>
 using AttScores = att_f32x4[NT][AttShape<BF16, DB>::KT];
 
-// A step's tiles of 16 keys: their pages' numbers (looked up a step ahead of their use) and places, and the lane's place in a tile
+// A step's tiles of 16 keys: their pages' numbers (looked up a step ahead of their use) and places, and the lane's place in a tile.
 template <bool BF16, int DB, bool FULL>
 struct AttStage {
     using S = AttShape<BF16, DB>;
@@ -328,6 +328,7 @@ __device__ __forceinline__ void attend_rows(const AttendParams &p, float *lds, c
     const int32_t begin = it.begin, end = it.end, own = it.own, rows = it.rows, first = it.first, hk = it.hk;
     const int lane = threadIdx.x & 63, wave = WAVES == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int32_t key0 = begin + wave * S::KS;
+    constexpr int STRIDE = WAVES * S::KS;
     AttStage<BF16, DB, FULL> in(p, hk, lane);
     in.look_up(p, it, key0);
     AttRows<BF16, DB, NT> r;
@@ -364,17 +365,20 @@ __device__ __forceinline__ void attend_rows(const AttendParams &p, float *lds, c
         AttVals<BF16, DB> fv;
         in.place(p, key0);
         in.load_keys(fk, p, lane);
-        in.look_up(p, it, key0 + WAVES * S::KS);
         in.load_vals(fv, p, lane);
-        for (; key0 < end; key0 += WAVES * S::KS) {
-            // the next step's keys leave as soon as this step's scores have taken the registers' old content, its values after the second product;
-            // behind the last step they are some that nobody looks at
+        in.look_up(p, it, key0 + STRIDE);
+        for (; key0 < end; key0 += STRIDE) {
+            // the next step's keys leave as soon as this step's scores have taken the registers' old content, its values after the second product.  Two
+            // steps on their way (222 registers instead of 177) are 1 to 6 % slower: most parts are a step or two a wavefront.
             att_f32x4 s[NT][S::KT];
             att_scores<BF16, DB, NT>(s, fk, r);
             __builtin_amdgcn_sched_barrier(0);
-            in.place(p, key0 + WAVES * S::KS);
-            in.load_keys(fk, p, lane);
-            in.look_up(p, it, key0 + 2 * WAVES * S::KS);
+            const bool more = key0 + STRIDE < end;
+            if (more) {
+                in.place(p, key0 + STRIDE);
+                in.load_keys(fk, p, lane);
+                in.look_up(p, it, key0 + 2 * STRIDE);
+            }
             __builtin_amdgcn_sched_barrier(0);
             if (key0 + S::KS > least) {
                 att_mask<BF16, DB, NT>(s, r, key0, lane);
@@ -383,7 +387,8 @@ __device__ __forceinline__ void attend_rows(const AttendParams &p, float *lds, c
             att_softmax<BF16, DB, NT>(s, r, p.scale2);
             att_weigh<BF16, DB, NT>(s, fv, r);
             __builtin_amdgcn_sched_barrier(0);
-            in.load_vals(fv, p, lane);
+            if (more)
+                in.load_vals(fv, p, lane);
         }
     }
     if (odd)

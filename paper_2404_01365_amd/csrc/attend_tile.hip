@@ -342,7 +342,7 @@ __global__ __launch_bounds__(64 * ATT_TILE_WAVES) void attend_tile_kernel(Attend
     // steps from the one that begins at `clear` on have keys that some row of the workgroup does not see
     const int32_t clear = it.begin + (sees(it.first) - it.begin) / ATT_TILE_KEYS * ATT_TILE_KEYS;
     // Loads are two steps ahead of their use: a step's work is shorter than a read from memory under load takes.  Two stages take turns; step i
-    // loads step i + 2's, looks up i + 4's pages, and stores i + 1's in the other room.  Behind the last step they are some keys that nobody reads.
+    // loads step i + 2's, looks up i + 4's pages, and stores i + 1's in the other room.
     TileStage<DB, FULL> even(p, it, wave, lane), odds(p, it, wave, lane);
     bool odd = false;
     uint32_t room = 0;
@@ -352,8 +352,10 @@ __global__ __launch_bounds__(64 * ATT_TILE_WAVES) void attend_tile_kernel(Attend
         in.store(lds + room, lds + 2 * S::BYTES + room, wave, lane);
     };
     const auto step = [&](TileStage<DB, FULL> &now, TileStage<DB, FULL> &other, int32_t key0) {
-        now.load(p, wave, lane);
-        now.look_up(p, it, key0 + 4 * ATT_TILE_KEYS, wave);
+        if (key0 + 2 * ATT_TILE_KEYS < it.end) {
+            now.load(p, wave, lane);
+            now.look_up(p, it, key0 + 4 * ATT_TILE_KEYS, wave);
+        }
         if (key0 < most) {
             TileScores<DB> s;
             att_u32x4 w[S::NT][S::KT / 2];
@@ -362,8 +364,10 @@ __global__ __launch_bounds__(64 * ATT_TILE_WAVES) void attend_tile_kernel(Attend
             tile_weigh<DB>(tile_vals_at<DB>(lds + 2 * S::BYTES + room), w, r);
         }
         room ^= S::BYTES;
-        store(other, key0 + ATT_TILE_KEYS);
-        other.place(p, key0 + 3 * ATT_TILE_KEYS, wave);
+        if (key0 + ATT_TILE_KEYS < it.end) {
+            store(other, key0 + ATT_TILE_KEYS);
+            other.place(p, key0 + 3 * ATT_TILE_KEYS, wave);
+        }
         __syncthreads();
     };
     even.look_up(p, it, it.begin, wave);
@@ -372,7 +376,8 @@ __global__ __launch_bounds__(64 * ATT_TILE_WAVES) void attend_tile_kernel(Attend
     odds.place(p, it.begin + ATT_TILE_KEYS, wave);
     even.load(p, wave, lane);
     even.look_up(p, it, it.begin + 2 * ATT_TILE_KEYS, wave);
-    odds.load(p, wave, lane);
+    if (it.begin + ATT_TILE_KEYS < it.end)
+        odds.load(p, wave, lane);
     odds.look_up(p, it, it.begin + 3 * ATT_TILE_KEYS, wave);
     store(even, it.begin);
     even.place(p, it.begin + 2 * ATT_TILE_KEYS, wave);
