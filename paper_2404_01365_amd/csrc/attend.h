@@ -12,7 +12,7 @@ typedef __attribute__((ext_vector_type(4))) uint32_t att_u32x4;
 
 constexpr int ATT_WAVES = 4;            // of a workgroup of attend.hip
 constexpr int ATT_TILE_WAVES = 8;       // ... of attend_tile.hip
-constexpr int ATT_TILE_KEYS = 64;       // its step
+constexpr int att_tile_keys(int32_t dim) { return dim > 128 ? 32 : 64; }      // its step
 
 // Division by a number that the host knows, exact while the dividend times it is below 2^32
 struct AttDiv {

@@ -599,6 +599,7 @@ struct AttPlan {
 static AttPlan attend_plan(const griffin_kv_cache &C, const griffin_kv_batch &B, const SeqTable &seqs, int32_t n_heads)
 {
     AttPlan pl;
+    const int32_t tile_keys = att_tile_keys(C.dim);
     const bool bf16 = C.dtype == GRIFFIN_BF16;
     const int widest = C.dim > 128 ? 1 : 2;                // what the registers hold beside a step's keys and values
     const int32_t group = n_heads / C.kv_heads;
@@ -625,7 +626,7 @@ static AttPlan attend_plan(const griffin_kv_cache &C, const griffin_kv_batch &B,
     const int64_t step = ATT_WAVES * (bf16 ? 32 : 16);
     const int64_t work_prefix = C.kv_heads * (int64_t)pl.tiles_prefix * B.n_prefix, work_own = C.kv_heads * tiles * B.max_len;
     const auto chunk = [&](bool tile, int64_t work) {
-        const int64_t quantum = tile ? ATT_TILE_KEYS : step, wgs = tile || pl.lone || C.dim > 128 ? 256 : 1024;
+        const int64_t quantum = tile ? tile_keys : step, wgs = tile || pl.lone || C.dim > 128 ? 256 : 1024;
         return (int32_t)((std::max((work + wgs - 1) / wgs, (int64_t)1) + quantum - 1) / quantum * quantum);
     };
     const bool together = pl.tile_prefix == pl.tile_own && !pl.lone;

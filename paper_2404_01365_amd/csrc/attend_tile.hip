@@ -1,6 +1,6 @@
 // Attention of many rows (bf16): prompts, and a prefix that more than 64 rows share.  The mathematics and the arrangement of scores
 // and sums are those of attend.hip; here eight wavefronts of 32 rows each (16 of heads wider than 128) take the same keys, which go through LDS
-// 64 at a time, two steps' worth of room, so that a step's loads travel while the step before is computed.
+// 64 at a time (32 of the wider heads), two steps' worth of room, so that a step's loads travel while the step before is computed.
 //
 // Keys lie in LDS in the order of the A operands (a lane's 16 bytes side by side: reads without bank conflicts).  Values lie as in memory, a row a
 // key; V^T's operand is read with ds_read_b64_tr_b16, by which 16 lanes fetch four rows' 16 features and get a feature's four keys each.  The 32-byte
@@ -20,10 +20,11 @@ template <int DB>
 struct TileShape {
     static constexpr int NQ = DB / 32;                        // 32-feature pieces of a key
     static constexpr int NO = DB / 16;                        // tiles of 16 features of the output
-    static constexpr int KT = ATT_TILE_KEYS / 16;             // tiles of 16 keys of a step
+    static constexpr int KEYS = att_tile_keys(DB);            // of a step
+    static constexpr int KT = KEYS / 16;                      // tiles of 16 keys of a step
     static constexpr int NT = DB > 128 ? 1 : 2;               // tiles of 16 rows of a wavefront
     static constexpr int ROW = DB * 2;                        // bytes of a value's row
-    static constexpr int BYTES = ATT_TILE_KEYS * ROW;         // of a step's keys, and of its values
+    static constexpr int BYTES = KEYS * ROW;            // of a step's keys, and of its values
     static constexpr int PIECES = BYTES / (16 * 64 * ATT_TILE_WAVES);      // 16-byte pieces of either that a thread brings in
 };
 
@@ -340,7 +341,7 @@ __global__ __launch_bounds__(64 * ATT_TILE_WAVES) void attend_tile_kernel(Attend
     const int32_t least = first < it.rows ? sees(first) : it.begin;
     const int32_t most = first < it.rows ? sees(first + 16 * S::NT < it.rows ? first + 16 * S::NT - 1 : it.rows - 1) : it.begin;
     // steps from the one that begins at `clear` on have keys that some row of the workgroup does not see
-    const int32_t clear = it.begin + (sees(it.first) - it.begin) / ATT_TILE_KEYS * ATT_TILE_KEYS;
+    const int32_t clear = it.begin + (sees(it.first) - it.begin) / S::KEYS * S::KEYS;
     // Loads are two steps ahead of their use: a step's work is shorter than a read from memory under load takes.  Two stages take turns; step i
     // loads step i + 2's, looks up i + 4's pages, and stores i + 1's in the other room.
     TileStage<DB, FULL> even(p, it, wave, lane), odds(p, it, wave, lane);
@@ -352,41 +353,41 @@ __global__ __launch_bounds__(64 * ATT_TILE_WAVES) void attend_tile_kernel(Attend
         in.store(lds + room, lds + 2 * S::BYTES + room, wave, lane);
     };
     const auto step = [&](TileStage<DB, FULL> &now, TileStage<DB, FULL> &other, int32_t key0) {
-        if (key0 + 2 * ATT_TILE_KEYS < it.end) {
+        if (key0 + 2 * S::KEYS < it.end) {
             now.load(p, wave, lane);
-            now.look_up(p, it, key0 + 4 * ATT_TILE_KEYS, wave);
+            now.look_up(p, it, key0 + 4 * S::KEYS, wave);
         }
         if (key0 < most) {
             TileScores<DB> s;
             att_u32x4 w[S::NT][S::KT / 2];
             tile_scores<DB>(lds + room, s, r);
-            tile_softmax<DB>(key0 + ATT_TILE_KEYS > least, s, w, r, p.scale2, key0);
+            tile_softmax<DB>(key0 + S::KEYS > least, s, w, r, p.scale2, key0);
             tile_weigh<DB>(tile_vals_at<DB>(lds + 2 * S::BYTES + room), w, r);
         }
         room ^= S::BYTES;
-        if (key0 + ATT_TILE_KEYS < it.end) {
-            store(other, key0 + ATT_TILE_KEYS);
-            other.place(p, key0 + 3 * ATT_TILE_KEYS, wave);
+        if (key0 + S::KEYS < it.end) {
+            store(other, key0 + S::KEYS);
+            other.place(p, key0 + 3 * S::KEYS, wave);
         }
         __syncthreads();
     };
     even.look_up(p, it, it.begin, wave);
-    odds.look_up(p, it, it.begin + ATT_TILE_KEYS, wave);
+    odds.look_up(p, it, it.begin + S::KEYS, wave);
     even.place(p, it.begin, wave);
-    odds.place(p, it.begin + ATT_TILE_KEYS, wave);
+    odds.place(p, it.begin + S::KEYS, wave);
     even.load(p, wave, lane);
-    even.look_up(p, it, it.begin + 2 * ATT_TILE_KEYS, wave);
-    if (it.begin + ATT_TILE_KEYS < it.end)
+    even.look_up(p, it, it.begin + 2 * S::KEYS, wave);
+    if (it.begin + S::KEYS < it.end)
         odds.load(p, wave, lane);
-    odds.look_up(p, it, it.begin + 3 * ATT_TILE_KEYS, wave);
+    odds.look_up(p, it, it.begin + 3 * S::KEYS, wave);
     store(even, it.begin);
-    even.place(p, it.begin + 2 * ATT_TILE_KEYS, wave);
+    even.place(p, it.begin + 2 * S::KEYS, wave);
     __syncthreads();
-    for (int32_t key0 = it.begin; key0 < it.end; key0 += 2 * ATT_TILE_KEYS) {
+    for (int32_t key0 = it.begin; key0 < it.end; key0 += 2 * S::KEYS) {
         step(even, odds, key0);
-        if (key0 + ATT_TILE_KEYS >= it.end)
+        if (key0 + S::KEYS >= it.end)
             break;
-        step(odds, even, key0 + ATT_TILE_KEYS);
+        step(odds, even, key0 + S::KEYS);
     }
     if (__syncthreads_or(odd))
         tile_add_infinite<DB, FULL>(p, it, r, clear, most);

@@ -416,3 +416,36 @@ def test_results_do_not_depend_on_the_run():
     first = run_attention(c)
     for _ in range(3):
         assert np.array_equal(run_attention(c), first)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_attention_of_own_parts_a_wavefront_each(dtype):
+    """Enough sequences and heads that own parts are not shared between wavefronts: with a prefix and without, one chunk and several, a few new tokens."""
+    rng = np.random.default_rng(12)
+    check_attention(91, heads=8, kv_heads=8, dim=64, page=16, prefix=0, held=rng.integers(0, 33, 200).tolist(), new=[1] * 200, dtype=dtype, max_len=128)
+    check_attention(92, heads=16, kv_heads=8, dim=64, page=32, prefix=45, held=rng.integers(0, 300, 64).tolist(), new=rng.integers(0, 3, 64).tolist(),
+                    dtype=dtype, order="thd")
+    check_attention(93, heads=16, kv_heads=16, dim=128, page=16, prefix=3, held=rng.integers(0, 150, 64).tolist(), new=[1] * 64, dtype=dtype)
+    check_attention(94, heads=8, kv_heads=8, dim=256, page=16, prefix=20, held=rng.integers(0, 150, 120).tolist(), new=[1] * 120, dtype=dtype)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_attention_of_ragged_prompts(dtype, dim):
+    """Packed prompts of no, one and several tiles of rows, in no order of their lengths, behind own tokens and a prefix."""
+    rng = np.random.default_rng(13)
+    new = [0, 1, 300, 64, 0, 129, 5, 65, 257, 30, 128, 2]
+    check_attention(95, heads=4, kv_heads=2, dim=dim, page=16, prefix=70, held=rng.integers(0, 90, len(new)).tolist(), new=new, dtype=dtype)
+    check_attention(96, heads=2, kv_heads=2, dim=dim, page=64, prefix=0, held=[0] * len(new), new=new, dtype=dtype, order="thd")
+
+
+def test_attention_of_a_prompt_alone_and_row_by_row():
+    """Tokens of a prompt in one call and one a call give the same within their roundings: every row sees the same keys either way."""
+    c = plain.Case(97, heads=4, kv_heads=2, dim=128, page=16, prefix=33, held=[20], new=[90], dtype=BF16)
+    whole = run_attention(c)
+    ref, size = c.attention(128 ** -0.5)
+    attention_close(whole, ref, size, BF16)
+    for i in (0, 1, 31, 63, 89):
+        one = plain.Case(97, heads=4, kv_heads=2, dim=128, page=16, prefix=33, held=[20], new=[90], dtype=BF16)
+        one.q, one.lens, one.new, one.cu = c.q[i:i + 1], [20 + i], [1], [0, 1]
+        attention_close(run_attention(one), ref[i:i + 1], size[i:i + 1], BF16)
