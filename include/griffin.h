@@ -368,7 +368,7 @@ typedef struct {
     const int32_t *lens;           /* device [n_seqs], below 0 counts as 0 */
     const int32_t *pages;          /* device [n_seqs][ld_pages]: the pages of a sequence's own tokens */
     int64_t ld_pages;              /* >= ceil(max_len / page_size) */
-    int32_t n_prefix;              /* tokens shared by all sequences, 0 or more */
+    int32_t n_prefix;              /* tokens shared by all sequences, 0 or more; n_prefix + max_len <= 2^30 */
     const int32_t *prefix_pages;   /* device [ceil(n_prefix / page_size)], NULL without a prefix */
 } griffin_kv_batch;                /* page numbers outside [0, n_pages) are clamped instead of faulting */
 

@@ -11,6 +11,7 @@ typedef __attribute__((ext_vector_type(8))) __bf16 att_bf16x8;
 typedef __attribute__((ext_vector_type(4))) uint32_t att_u32x4;
 
 constexpr int ATT_WAVES = 4;            // of a workgroup of attend.hip
+constexpr int ATT_FEW_WAVES = 8;        // ... of its attend_few_kernel
 constexpr int ATT_TILE_WAVES = 8;       // ... of attend_tile.hip
 constexpr int att_tile_keys(int32_t dim) { return dim > 128 ? 32 : 64; }      // its step
 
@@ -34,6 +35,7 @@ struct AttendParams {
     AttDiv by_heads, by_kv_heads, by_group, by_chunks_prefix, by_chunks_own;
     // keys a chunk (a multiple of a workgroup's step), chunks, and tiles of rows of the prefix
     int32_t chunk_prefix, chunk_own, chunks_prefix, chunks_own, tiles_prefix;
+    int32_t ahead;           // tokens of the prefix that own items take ahead of their own: all (then there are no items of the prefix) or 0
     int32_t wgs_prefix;      // workgroups of this launch that take the prefix, ahead of those that take own parts
     int32_t items_own;       // own items of this launch
     AttDiv each, tiles_each;                                  // new tokens, and tiles of rows, of every sequence where they are equally many, else by 0
@@ -48,6 +50,12 @@ struct AttendItem {
     const int32_t *pages;
     int32_t last_entry;      // of the list that may be read
     int32_t begin, end, own, hk, token0, rows, first, split;
+    // Where own items take the prefix, too, they count its keys first and their own from the next multiple of 16 on: keys from hole to hole_end are none,
+    // and `own`, `begin` and `end` are counted like that.  Else both are 0.
+    int32_t hole, hole_end;
+
+    __device__ __forceinline__ bool missing(int32_t key) const { return key >= hole && key < hole_end; }
+    __device__ __forceinline__ bool touches_hole(int32_t key0, int32_t keys) const { return hole < hole_end && key0 < hole_end && key0 + keys > hole; }
 };
 
 // maximum over the lanes l, l ^ 16, l ^ 32, l ^ 48
@@ -68,16 +76,19 @@ __device__ __forceinline__ uint32_t att_page(int32_t page, int32_t last_page) { 
 // that is asked of LDS behind it, too.
 __device__ __forceinline__ int32_t att_look_up(const AttendParams &p, const AttendItem &it, int32_t key)
 {
-    int32_t at = key >> p.page_shift;
-    at = at < it.last_entry ? at : it.last_entry;
+    const bool ahead = key < it.hole_end;
+    const int32_t last = ahead ? (it.hole - 1) >> p.page_shift : it.last_entry;
+    int32_t at = (ahead ? key : key - it.hole_end) >> p.page_shift;
+    at = at < last ? at : last;
     asm volatile("" : "+v"(at));
-    return it.pages[at];
+    return (ahead ? p.prefix_pages : it.pages)[at];
 }
 
 // where that tile begins, in bytes from the kv head's begin
 template <int ES>
-__device__ __forceinline__ uint64_t att_place(const AttendParams &p, int32_t page, int32_t key)
+__device__ __forceinline__ uint64_t att_place(const AttendParams &p, const AttendItem &it, int32_t page, int32_t key)
 {
+    key -= key < it.hole_end ? 0 : it.hole_end;
     return (uint64_t)att_page(__builtin_amdgcn_readfirstlane(page), p.last_page) * p.page_stride16 * 16 +
            (uint64_t)(uint32_t)(key & ((1 << p.page_shift) - 1)) * ((uint32_t)p.token_stride * ES);
 }
@@ -119,6 +130,7 @@ __device__ __forceinline__ void att_prefix_item(const AttendParams &p, int32_t i
     it.rows = p.tokens * p.group;
     it.first = tile * ROWS;
     it.split = chunk;
+    it.hole = it.hole_end = 0;
 }
 
 // Tiles of rows in falling order of their number within a sequence, so that those that see the most keys are begun first: the `id`-th one.  With tiles
@@ -159,7 +171,10 @@ __device__ __forceinline__ bool att_own_item(const AttendParams &p, int32_t id, 
     it.first = tile * ROWS;
     it.own = len < 0 ? 0 : (len < p.max_len ? len : p.max_len);
     const int32_t last = it.first + ROWS < it.rows ? it.first + ROWS - 1 : it.rows - 1;               // the tile's last row sees the most keys
-    const int32_t end = it.own + p.by_group(last) + 1 < p.max_len ? it.own + p.by_group(last) + 1 : p.max_len;
+    it.hole = p.ahead;
+    it.hole_end = (p.ahead + 15) & ~15;
+    const int32_t end = it.hole_end + (it.own + p.by_group(last) + 1 < p.max_len ? it.own + p.by_group(last) + 1 : p.max_len);
+    it.own += it.hole_end;
     it.begin = chunk * p.chunk_own;
     it.end = it.begin + p.chunk_own < end ? it.begin + p.chunk_own : end;
     it.split = p.chunks_prefix + chunk;

@@ -89,11 +89,11 @@ struct AttStage {
             page[i] = att_look_up(p, it, key0 + 16 * i);
     }
 
-    __device__ __forceinline__ void place(const AttendParams &p, int32_t key0)
+    __device__ __forceinline__ void place(const AttendParams &p, const AttendItem &it, int32_t key0)
     {
 #pragma unroll
         for (int i = 0; i < S::KT; ++i)
-            base[i] = att_place<ES>(p, page[i], key0 + 16 * i);
+            base[i] = att_place<ES>(p, it, page[i], key0 + 16 * i);
     }
 
     __device__ __forceinline__ void load_keys(AttKeys<BF16, DB> &f, const AttendParams &p, int lane) const
@@ -184,17 +184,19 @@ __device__ __forceinline__ void att_softmax(AttScores<BF16, DB, NT> &s, AttRows<
     }
 }
 
-// Keys from r.end on out of the scores
+// Keys from r.end on, and those in the hole, out of the scores
 template <bool BF16, int DB, int NT>
-__device__ __forceinline__ void att_mask(AttScores<BF16, DB, NT> &s, const AttRows<BF16, DB, NT> &r, int32_t key0, int lane)
+__device__ __forceinline__ void att_mask(AttScores<BF16, DB, NT> &s, const AttRows<BF16, DB, NT> &r, const AttendItem &it, int32_t key0, int lane)
 {
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int i = 0; i < AttShape<BF16, DB>::KT; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                s[n][i][e] = key0 + 16 * i + (lane >> 4) * 4 + e < r.end[n] ? s[n][i][e] : -INFINITY;
+            for (int e = 0; e < 4; ++e) {
+                const int32_t key = key0 + 16 * i + (lane >> 4) * 4 + e;
+                s[n][i][e] = key < r.end[n] && !it.missing(key) ? s[n][i][e] : -INFINITY;
+            }
 }
 
 // O^T += V^T P^T
@@ -241,13 +243,14 @@ __device__ __forceinline__ void att_weigh(const AttScores<BF16, DB, NT> &s, cons
 // key are made zero, and so are infinite and NaN ones; if there were any of these (`true`), they are added to the rows that do see them at the end
 // (att_add_infinite).
 template <bool BF16, int DB>
-__device__ __forceinline__ bool att_clear_infinite(AttVals<BF16, DB> &f, int32_t key0, int32_t end, int lane)
+__device__ __forceinline__ bool att_clear_infinite(AttVals<BF16, DB> &f, const AttendItem &it, int32_t key0, int lane)
 {
     using S = AttShape<BF16, DB>;
     uint32_t odd = 0;
 #pragma unroll
     for (int j = 0; j < S::VK; ++j) {
-        const uint32_t in = key0 + 16 * (j >> 2) + (lane >> 4) * 4 + (j & 3) < end ? ~0u : 0;
+        const int32_t key = key0 + 16 * (j >> 2) + (lane >> 4) * 4 + (j & 3);
+        const uint32_t in = key < it.end && !it.missing(key) ? ~0u : 0;
 #pragma unroll
         for (int c = 0; c < S::NC; ++c)
 #pragma unroll
@@ -267,7 +270,7 @@ __device__ __forceinline__ void att_add_infinite(const AttendParams &p, const At
     using S = AttShape<BF16, DB>;
     const int32_t stop = key + S::KS < it.end ? key + S::KS : it.end;
     for (; key < stop; ++key) {
-        const char *at = (const char *)p.V + it.hk * p.head_stride * (BF16 ? 2 : 4) + att_place<BF16 ? 2 : 4>(p, att_look_up(p, it, key), key);
+        const char *at = (const char *)p.V + it.hk * p.head_stride * (BF16 ? 2 : 4) + att_place<BF16 ? 2 : 4>(p, it, att_look_up(p, it, key), key);
 #pragma unroll
         for (int c = 0; c < S::NC; ++c)
 #pragma unroll
@@ -280,7 +283,7 @@ __device__ __forceinline__ void att_add_infinite(const AttendParams &p, const At
                     const bool odd = (__float_as_uint(x) & 0x7F800000u) == 0x7F800000u;
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
-                        r.o[n][c * S::VD + e][i] += odd && key < r.end[n] ? x : 0.0f;
+                        r.o[n][c * S::VD + e][i] += odd && key < r.end[n] && !it.missing(key) ? x : 0.0f;
                 }
             }
     }
@@ -363,7 +366,7 @@ __device__ __forceinline__ void attend_rows(const AttendParams &p, float *lds, c
     if (key0 < end) {
         AttKeys<BF16, DB> fk;
         AttVals<BF16, DB> fv;
-        in.place(p, key0);
+        in.place(p, it, key0);
         in.load_keys(fk, p, lane);
         in.load_vals(fv, p, lane);
         in.look_up(p, it, key0 + STRIDE);
@@ -375,14 +378,14 @@ __device__ __forceinline__ void attend_rows(const AttendParams &p, float *lds, c
             __builtin_amdgcn_sched_barrier(0);
             const bool more = key0 + STRIDE < end;
             if (more) {
-                in.place(p, key0 + STRIDE);
+                in.place(p, it, key0 + STRIDE);
                 in.load_keys(fk, p, lane);
                 in.look_up(p, it, key0 + 2 * STRIDE);
             }
             __builtin_amdgcn_sched_barrier(0);
-            if (key0 + S::KS > least) {
-                att_mask<BF16, DB, NT>(s, r, key0, lane);
-                odd |= att_clear_infinite<BF16, DB>(fv, key0, end, lane);
+            if (key0 + S::KS > least || it.touches_hole(key0, S::KS)) {
+                att_mask<BF16, DB, NT>(s, r, it, key0, lane);
+                odd |= att_clear_infinite<BF16, DB>(fv, it, key0, lane);
             }
             att_softmax<BF16, DB, NT>(s, r, p.scale2);
             att_weigh<BF16, DB, NT>(s, fv, r);
@@ -393,7 +396,7 @@ __device__ __forceinline__ void attend_rows(const AttendParams &p, float *lds, c
     }
     if (odd)
         for (key0 = begin + wave * S::KS; key0 < end; key0 += WAVES * S::KS)
-            if (key0 + S::KS > least)
+            if (key0 + S::KS > least || it.touches_hole(key0, S::KS))
                 att_add_infinite<BF16, DB, FULL, NT>(p, it, r, key0);
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -474,11 +477,15 @@ __device__ __forceinline__ void attend_rows(const AttendParams &p, float *lds, c
     }
 }
 
+// floats of LDS in which WAVES wavefronts' sums come together
+template <int DB, int WAVES>
+constexpr int att_lds_floats() { return WAVES * 16 * ((DB < 128 ? DB : 128) + 4) + WAVES * 32; }
+
 // LONE: own items go a wavefront each
 template <bool BF16, int DB, bool FULL, int NTP, int NTO, bool LONE>
 __global__ __launch_bounds__(ATT_WAVES * 64, DB > 128 || (!BF16 && DB > 64 && NTP > 1) ? 1 : 2) void attend_rows_kernel(AttendParams p)
 {
-    __shared__ __align__(16) float lds[ATT_WAVES * 16 * ((DB < 128 ? DB : 128) + 4) + ATT_WAVES * 32];
+    __shared__ __align__(16) float lds[att_lds_floats<DB, ATT_WAVES>()];
     AttendItem it;
     if ((int32_t)blockIdx.x < p.wgs_prefix) {
         att_prefix_item<16 * NTP>(p, blockIdx.x, it);
@@ -493,6 +500,16 @@ __global__ __launch_bounds__(ATT_WAVES * 64, DB > 128 || (!BF16 && DB > 64 && NT
     }
     if (att_own_item<16 * NTO, false>(p, id, it))
         attend_rows<BF16, DB, FULL, NTO, LONE ? 1 : ATT_WAVES>(p, lds, it);
+}
+
+// Parts so short and few that one launch does them: twice as many wavefronts an item instead of chunks, nothing to join
+template <bool BF16, int DB, bool FULL>
+__global__ __launch_bounds__(ATT_FEW_WAVES * 64) void attend_few_kernel(AttendParams p)
+{
+    extern __shared__ __align__(16) float few_lds[];
+    AttendItem it;
+    if (att_own_item<16, false>(p, blockIdx.x, it))
+        attend_rows<BF16, DB, FULL, 1, ATT_FEW_WAVES>(p, few_lds, it);
 }
 
 // Joins a row's chunks: with M = max m_c, o = sum o_c 2^(m_c - M) / sum l_c 2^(m_c - M).  A row per WPR wavefronts; a wavefront takes
@@ -591,6 +608,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendParams p)
 struct AttPlan {
     bool tile_prefix, tile_own;         // many rows: attend_tile.hip
     bool lone;                          // own items of a few rows go a wavefront each
+    bool ahead, few;                    // own items take the prefix, too; all of it in one launch of attend_few_kernel
     int ntp, nto;                       // else tiles of 16 rows that a wavefront takes
     int32_t rows_prefix, rows_own;      // rows of a workgroup
     int32_t chunk_prefix, chunk_own, chunks_prefix, chunks_own, tiles_prefix, tiles_own;
@@ -632,10 +650,23 @@ static AttPlan attend_plan(const griffin_kv_cache &C, const griffin_kv_batch &B,
     const bool together = pl.tile_prefix == pl.tile_own && !pl.lone;
     pl.chunk_prefix = chunk(pl.tile_prefix, together ? work_prefix + work_own : work_prefix);
     pl.chunk_own = chunk(pl.tile_own, together ? work_prefix + work_own : work_own);
-    if (pl.lone || (pl.tile_own && C.kv_heads * tiles >= 256))
+    if (pl.lone || (pl.tile_own && C.kv_heads * tiles > 128))
         pl.chunk_own = (int32_t)((B.max_len + step - 1) / step * step);
-    pl.chunks_prefix = (B.n_prefix + pl.chunk_prefix - 1) / pl.chunk_prefix;
-    pl.chunks_own = (B.max_len + pl.chunk_own - 1) / pl.chunk_own;
+    // (Own parts of many rows, whole / cut so that 256 workgroups share them: 3000 tokens of 16 heads, 192 tiles of rows, 95 / 113 us; 1000 of 40 heads on 8, 160
+    // tiles, 42 / 61; 2048 of 16 on 8, 128 tiles, 71 / 63.  3400 tokens of 32 on 8 behind a prefix of 300: 79 with the prefix ahead, 141 joined.)
+    // Own items take the prefix ahead of their own keys where that costs less than to join two parts: prompts that fill the chip (their rows' sums would go
+    // through memory in fp32), and parts so few and short that a step of twice as many wavefronts is cheaper than a second launch (some 5 us), prefix or not.  At
+    // two steps it is no longer: 513 keys of 32 heads of 128 take 10.4 us in one launch of 32 workgroups, 10.3 cut into chunks and joined (caches cold: 15.9,
+    // 14.4).
+    const int64_t all = (int64_t)B.n_prefix + B.max_len, items = C.kv_heads * tiles;
+    pl.few = longest <= 32 && !pl.tile_prefix && items <= 512 && all <= ATT_FEW_WAVES / ATT_WAVES * step && C.dim <= 128;
+    pl.ahead = B.n_prefix > 0 && (pl.few || (pl.tile_own && items > 128));
+    if (pl.ahead)
+        pl.tiles_prefix = 0;
+    if (pl.ahead || pl.few)
+        pl.chunk_own = (int32_t)((all + 15 + step - 1) / step * step);
+    pl.chunks_prefix = pl.ahead ? 0 : (B.n_prefix + pl.chunk_prefix - 1) / pl.chunk_prefix;
+    pl.chunks_own = pl.ahead ? 1 : (B.max_len + pl.chunk_own - 1) / pl.chunk_own;
     return pl;
 }
 
@@ -655,6 +686,15 @@ static int go_rows(const AttendParams &p, hipStream_t st)
     else
         hipLaunchKernelGGL((attend_rows_kernel<BF16, DB, false, NTP, NTO, LONE>), dim3(wgs), dim3(ATT_WAVES * 64), 0, st, p);
     return check_launch("attend_rows_kernel");
+}
+
+template <bool BF16, int DB, bool FULL>
+static int go_few(const AttendParams &p, hipStream_t st)
+{
+    constexpr int bytes = att_lds_floats<DB, ATT_FEW_WAVES>() * sizeof(float);
+    RAISE_LDS_LIMIT((attend_few_kernel<BF16, DB, FULL>), bytes);
+    hipLaunchKernelGGL((attend_few_kernel<BF16, DB, FULL>), dim3(p.items_own), dim3(ATT_FEW_WAVES * 64), bytes, st, p);
+    return check_launch("attend_few_kernel");
 }
 
 template <bool BF16, int DB, bool LONE>
@@ -684,6 +724,9 @@ static int attend_typed(AttendParams &p, const AttPlan &pl, hipStream_t st)
         p.wgs_prefix = pl.tile_prefix ? 0 : wgs_prefix;
         p.items_own = pl.tile_own ? 0 : wgs_own;
         const int ntp = p.wgs_prefix > 0 ? pl.ntp : 1, nto = p.items_own > 0 ? pl.nto : 1;
+        if constexpr (DB <= 128)
+            if (pl.few)
+                return p.dim == DB ? go_few<BF16, DB, true>(p, st) : go_few<BF16, DB, false>(p, st);
         rc = pl.lone ? launch_rows<BF16, DB, true>(p, ntp, nto, st) : launch_rows<BF16, DB, false>(p, ntp, nto, st);
     }
     if (rc != GRIFFIN_OK || !p.part)
@@ -734,6 +777,7 @@ int launch_attend(const AttendJob &job, const SeqTable &seqs, hipStream_t st)
     p.page_shift = __builtin_ctz(C.page_size);
     p.last_page = (int32_t)(C.n_pages - 1);
     p.max_len = B.max_len; p.n_prefix = B.n_prefix;
+    p.ahead = pl.ahead ? B.n_prefix : 0;
     p.chunk_prefix = pl.chunk_prefix; p.chunk_own = pl.chunk_own;
     p.chunks_prefix = pl.chunks_prefix; p.chunks_own = pl.chunks_own; p.tiles_prefix = pl.tiles_prefix;
     p.seqs = seqs;
@@ -741,7 +785,7 @@ int launch_attend(const AttendJob &job, const SeqTable &seqs, hipStream_t st)
     for (int b = 0; b < seqs.n; ++b)
         p.order[b] = (uint8_t)b;
     if (pl.tile_own)
-        std::stable_sort(p.order, p.order + seqs.n, [&](uint8_t a, uint8_t b) { return tiles_of(a) > tiles_of(b); });
+        std::sort(p.order, p.order + seqs.n, [&](uint8_t a, uint8_t b) { return tiles_of(a) != tiles_of(b) ? tiles_of(a) > tiles_of(b) : a < b; });
     for (int b = 0; b < seqs.n; ++b)
         p.tiles_own[b + 1] = p.tiles_own[b] + tiles_of(p.order[b]);
     int32_t each = seqs.n > 1 ? seqs.cu[1] : 0, tiles_each = seqs.n > 1 ? p.tiles_own[1] : 0;

@@ -72,11 +72,11 @@ struct TileStage {
             page[i] = att_look_up(p, it, key0 + 16 * tile_of(wave, i));
     }
 
-    __device__ __forceinline__ void place(const AttendParams &p, int32_t key0, int wave)
+    __device__ __forceinline__ void place(const AttendParams &p, const AttendItem &it, int32_t key0, int wave)
     {
 #pragma unroll
         for (int i = 0; i < S::PIECES; ++i)
-            base[i] = att_place<2>(p, page[i], key0 + 16 * tile_of(wave, i));
+            base[i] = att_place<2>(p, it, page[i], key0 + 16 * tile_of(wave, i));
     }
 
     __device__ __forceinline__ void load(const AttendParams &p, int wave, int lane)
@@ -97,13 +97,14 @@ struct TileStage {
     }
     static_assert(ATT_TILE_WAVES % S::NQ == 0, "a wavefront's pieces of keys have the same features");
 
-    // values behind the last key, and infinite and NaN ones, as zeros; true if there were any of these
-    __device__ __forceinline__ bool clear(int32_t key0, int32_t end, int wave, int lane)
+    // values behind the last key or in the hole, and infinite and NaN ones, as zeros; true if there were any of these
+    __device__ __forceinline__ bool clear(const AttendItem &it, int32_t key0, int wave, int lane)
     {
         uint32_t kept = ~0u;
 #pragma unroll
         for (int i = 0; i < S::PIECES; ++i) {
-            const bool in = key0 + 16 * tile_of(wave, i) + row_of(wave, lane) < end;
+            const int32_t key = key0 + 16 * tile_of(wave, i) + row_of(wave, lane);
+            const bool in = key < it.end && !it.missing(key);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const uint32_t m = att_finite_mask(v[i][j]);
@@ -160,7 +161,7 @@ __device__ __forceinline__ void tile_add_infinite(const AttendParams &p, const A
     const int d = (threadIdx.x >> 4 & 3) * 4;
     for (; key < most; ++key) {
         const uint16_t *at = (const uint16_t *)((const char *)((const uint16_t *)p.V + it.hk * p.head_stride) +
-                                                att_place<2>(p, att_look_up(p, it, key), key)) + d;
+                                                att_place<2>(p, it, att_look_up(p, it, key), key)) + d;
 #pragma unroll
         for (int e = 0; e < S::NO; ++e) {
             __builtin_amdgcn_sched_barrier(0);
@@ -170,7 +171,7 @@ __device__ __forceinline__ void tile_add_infinite(const AttendParams &p, const A
             for (int n = 0; n < S::NT; ++n)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    r.o[n][e][i] += key < r.end[n] ? (i & 1 ? bf16_hi(odd[i / 2]) : bf16_lo(odd[i / 2])) : 0.0f;
+                    r.o[n][e][i] += key < r.end[n] && !it.missing(key) ? (i & 1 ? bf16_hi(odd[i / 2]) : bf16_lo(odd[i / 2])) : 0.0f;
         }
     }
 }
@@ -245,7 +246,7 @@ __device__ __forceinline__ void tile_scores(uint32_t keys, TileScores<DB> &s, co
 // Scores to weights in bf16; the rows' reference and sum carried on, o scaled when the reference moves
 template <int DB>
 __device__ __forceinline__ void tile_softmax(bool masked, TileScores<DB> &s, att_u32x4 (&w)[TileShape<DB>::NT][TileShape<DB>::KT / 2], TileRows<DB> &r,
-                                             float scale2, int32_t key0)
+                                             float scale2, const AttendItem &it, int32_t key0)
 {
     using S = TileShape<DB>;
     const int lane = threadIdx.x & 63;
@@ -255,8 +256,10 @@ __device__ __forceinline__ void tile_softmax(bool masked, TileScores<DB> &s, att
 #pragma unroll
             for (int t = 0; t < S::KT; ++t)
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    s[n][t][e] = key0 + 16 * t + (lane >> 4) * 4 + e >= r.end[n] ? -INFINITY : s[n][t][e];
+                for (int e = 0; e < 4; ++e) {
+                    const int32_t key = key0 + 16 * t + (lane >> 4) * 4 + e;
+                    s[n][t][e] = key < r.end[n] && !it.missing(key) ? s[n][t][e] : -INFINITY;
+                }
     float top[S::NT];
     bool grown = false;
 #pragma unroll
@@ -348,8 +351,8 @@ __global__ __launch_bounds__(64 * ATT_TILE_WAVES) void attend_tile_kernel(Attend
     bool odd = false;
     uint32_t room = 0;
     const auto store = [&](TileStage<DB, FULL> &in, int32_t key0) {
-        if (key0 >= clear)
-            odd |= in.clear(key0, it.end, wave, lane);
+        if (key0 >= clear || it.touches_hole(key0, S::KEYS))
+            odd |= in.clear(it, key0, wave, lane);
         in.store(lds + room, lds + 2 * S::BYTES + room, wave, lane);
     };
     const auto step = [&](TileStage<DB, FULL> &now, TileStage<DB, FULL> &other, int32_t key0) {
@@ -361,27 +364,27 @@ __global__ __launch_bounds__(64 * ATT_TILE_WAVES) void attend_tile_kernel(Attend
             TileScores<DB> s;
             att_u32x4 w[S::NT][S::KT / 2];
             tile_scores<DB>(lds + room, s, r);
-            tile_softmax<DB>(key0 + S::KEYS > least, s, w, r, p.scale2, key0);
+            tile_softmax<DB>(key0 + S::KEYS > least || it.touches_hole(key0, S::KEYS), s, w, r, p.scale2, it, key0);
             tile_weigh<DB>(tile_vals_at<DB>(lds + 2 * S::BYTES + room), w, r);
         }
         room ^= S::BYTES;
         if (key0 + S::KEYS < it.end) {
             store(other, key0 + S::KEYS);
-            other.place(p, key0 + 3 * S::KEYS, wave);
+            other.place(p, it, key0 + 3 * S::KEYS, wave);
         }
         __syncthreads();
     };
     even.look_up(p, it, it.begin, wave);
     odds.look_up(p, it, it.begin + S::KEYS, wave);
-    even.place(p, it.begin, wave);
-    odds.place(p, it.begin + S::KEYS, wave);
+    even.place(p, it, it.begin, wave);
+    odds.place(p, it, it.begin + S::KEYS, wave);
     even.load(p, wave, lane);
     even.look_up(p, it, it.begin + 2 * S::KEYS, wave);
     if (it.begin + S::KEYS < it.end)
         odds.load(p, wave, lane);
     odds.look_up(p, it, it.begin + 3 * S::KEYS, wave);
     store(even, it.begin);
-    even.place(p, it.begin + 2 * S::KEYS, wave);
+    even.place(p, it, it.begin + 2 * S::KEYS, wave);
     __syncthreads();
     for (int32_t key0 = it.begin; key0 < it.end; key0 += 2 * S::KEYS) {
         step(even, odds, key0);
@@ -389,8 +392,12 @@ __global__ __launch_bounds__(64 * ATT_TILE_WAVES) void attend_tile_kernel(Attend
             break;
         step(odds, even, key0 + S::KEYS);
     }
-    if (__syncthreads_or(odd))
+    if (__syncthreads_or(odd)) {
+        const int32_t at_hole = it.hole / S::KEYS * S::KEYS;                 // the step with the hole, if it comes before
+        if (it.touches_hole(at_hole, S::KEYS) && at_hole < clear)
+            tile_add_infinite<DB, FULL>(p, it, r, at_hole, at_hole + S::KEYS < it.end ? at_hole + S::KEYS : it.end);
         tile_add_infinite<DB, FULL>(p, it, r, clear, most);
+    }
 #pragma unroll
     for (int n = 0; n < S::NT; ++n) {
         const float l = lane_groups_sum(r.l[n]);

@@ -31,7 +31,7 @@ static int check_batch(const griffin_kv_cache &C, const griffin_kv_batch *B, Seq
         return GRIFFIN_EUNSUPPORTED;
     if (!sizes_only && (!B->lens || !B->pages || (B->n_prefix > 0 && !B->prefix_pages)))
         return GRIFFIN_EINVAL;
-    if (B->max_len > (1 << 30) || B->n_prefix > (1 << 30))
+    if ((int64_t)B->max_len + B->n_prefix > (1 << 30))
         return GRIFFIN_ESHAPE;
     if (!sizes_only && B->ld_pages < (B->max_len + C.page_size - 1) / C.page_size)
         return GRIFFIN_ESHAPE;
@@ -73,6 +73,8 @@ int griffin_norm_residual(const griffin_norm *N, int64_t rows, const void *h, in
     for (const void *p : {h, y, gate, (const void *)h_out, (const void *)x, N->w_pre, N->b_pre, N->w_post, N->b_post})
         if (!aligned16(p))
             return GRIFFIN_ESHAPE;
+    if (x && x == h_out)
+        return GRIFFIN_EINVAL;
     if ((h_out == h && ldo != ldh) || (x && x == y && ldx != ldy))
         return GRIFFIN_ESHAPE;
     if (N->d > 32768)

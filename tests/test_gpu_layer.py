@@ -449,3 +449,26 @@ def test_attention_of_a_prompt_alone_and_row_by_row():
         one = plain.Case(97, heads=4, kv_heads=2, dim=128, page=16, prefix=33, held=[20], new=[90], dtype=BF16)
         one.q, one.lens, one.new, one.cu = c.q[i:i + 1], [20 + i], [1], [0, 1]
         attention_close(run_attention(one), ref[i:i + 1], size[i:i + 1], BF16)
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("prefix", [1, 64, 70])
+def test_attention_of_prompts_that_fill_the_chip_behind_a_prefix(dim, prefix):
+    """Enough tiles of rows that each takes the prefix ahead of its own keys (bf16), the prefix ending in a tile of 16 keys and at its end."""
+    check_attention(98 + dim, heads=32, kv_heads=32, dim=dim, page=16, prefix=prefix, held=[0, 17, 3, 0], new=[260, 300, 70, 259] if dim <= 128 else [130, 150, 70, 129],
+                    dtype=BF16)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("heads,kv_heads,new", [(4, 2, [1, 3]), (32, 32, [260, 257])])
+def test_attention_of_infinities_beside_the_prefix_end(dtype, heads, kv_heads, new):
+    """An infinite value in the 16 keys in which the prefix ends, and NaN behind its last token: one reaches everybody, the other nobody."""
+    c = plain.Case(99, heads=heads, kv_heads=kv_heads, dim=64, page=32, prefix=37, held=[2, 9], new=new, dtype=dtype)
+    ref, size = c.attention(0.125)
+    assert np.isnan(c.V[c.prefix_pages[1], 0, 5]).all()
+    c.V[c.prefix_pages[1], 1, 3, 7] = -np.inf
+    got = run_attention(c, scale=0.125)
+    group = heads // kv_heads
+    assert np.all(got[:, group:2 * group, 7] == -np.inf)
+    got[:, group:2 * group, 7], ref[:, group:2 * group, 7] = 0, 0
+    attention_close(got, ref, size, dtype)

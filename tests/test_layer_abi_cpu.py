@@ -43,7 +43,7 @@ def call_norm(N, rows=4, h=FAKE, ldh=512, h_dtype=G.BF16, y=FAKE, ldy=512, gate=
     (G.ESHAPE, dict(d=516), dict(ldh=520, ldy=520, ldo=520, ldx=520)), (G.ESHAPE, {}, dict(ldh=504)), (G.ESHAPE, {}, dict(ldy=516)),
     (G.ESHAPE, {}, dict(gate=FAKE, ldg=504)), (G.ESHAPE, {}, dict(ldx=0)), (G.ESHAPE, {}, dict(h=FAKE + 8, h_out=None)),
     (G.ESHAPE, {}, dict(x=FAKE + 2)), (G.ESHAPE, dict(w_post=FAKE + 4), {}), (G.ESHAPE, {}, dict(ldo=520)),        # in place with another stride
-    (G.ESHAPE, {}, dict(x=FAKE, h_out=None, ldx=520)), (G.ESHAPE, {}, dict(rows=2 ** 30 + 1)),
+    (G.ESHAPE, {}, dict(x=FAKE, h_out=None, ldx=520)), (G.EINVAL, {}, dict(x=FAKE)), (G.ESHAPE, {}, dict(rows=2 ** 30 + 1)),
     (G.EUNSUPPORTED, dict(d=32776), dict(ldh=32776, ldy=32776, ldo=32776, ldx=32776)),
     (G.EUNSUPPORTED, dict(dtype=G.F32), {}),                     # a bf16 stream beside fp32 blocks
     (G.OK, {}, dict(rows=0, h=None, x=None, h_out=None)),
@@ -96,7 +96,7 @@ def attend(C, B, q=FAKE, ldq=4096, hsq=128, out=FAKE + 4096, ldo=4096, hso=128, 
     (G.EINVAL, {}, dict(cu_seqlens=None)), (G.EINVAL, {}, dict(n_seqs=0)), (G.EINVAL, {}, dict(max_len=0)), (G.EINVAL, {}, dict(n_prefix=-1)),
     (G.EINVAL, {}, dict(lens=None)), (G.EINVAL, {}, dict(pages=None)), (G.EINVAL, {}, dict(prefix_pages=None)),
     (G.ESHAPE, {}, dict(ld_pages=3)), (G.ESHAPE, {}, dict(cu=(1, 2))), (G.ESHAPE, {}, dict(cu=(0, 3, 2))),
-    (G.ESHAPE, {}, dict(max_len=2 ** 30 + 1, ld_pages=2 ** 40)), (G.ESHAPE, {}, dict(n_prefix=2 ** 30 + 1)),
+    (G.ESHAPE, {}, dict(max_len=2 ** 30 + 1, ld_pages=2 ** 40)), (G.ESHAPE, {}, dict(n_prefix=2 ** 30 + 1)), (G.ESHAPE, {}, dict(n_prefix=2 ** 30 - 63)),
     (G.EUNSUPPORTED, {}, dict(cu=tuple(range(G.MAX_SEQS + 2)))), (G.EUNSUPPORTED, {}, dict(cu=(0, 2 ** 20 + 1))),
     (G.OK, {}, dict(cu=(0, 0, 0))),
 ])
@@ -129,16 +129,16 @@ def test_append_refuses(status, kw):
     (G.EWORKSPACE, dict(ws=None)), (G.EWORKSPACE, dict(ws=FAKE + 16)), (G.EWORKSPACE, dict(ws_bytes=64)),
 ])
 def test_attention_refuses(status, kw):
-    assert attend(mk_cache(), mk_batch(), **kw) == status
+    assert attend(mk_cache(), mk_batch(n_prefix=2000), **kw) == status
 
 
 def test_attention_workspace_is_enough_and_needed():
-    C, B = mk_cache(), mk_batch()
+    C, B = mk_cache(), mk_batch(n_prefix=2000)
     need = G.griffin_attention_workspace_bytes(C, B, 32)
     assert need > 0 and attend(C, B, ws_bytes=need - 1) == G.EWORKSPACE
     assert G.griffin_attention_workspace_bytes(C, B, 30) == 0 and G.griffin_attention_workspace_bytes(C, B, 1032) == 0
     # device pointers and strides do not enter
-    assert G.griffin_attention_workspace_bytes(C, mk_batch(lens=None, pages=None, prefix_pages=None, ld_pages=0), 32) == need
+    assert G.griffin_attention_workspace_bytes(C, mk_batch(n_prefix=2000, lens=None, pages=None, prefix_pages=None, ld_pages=0), 32) == need
     # one chunk of keys and nothing shared: written at once
     assert G.griffin_attention_workspace_bytes(mk_cache(), mk_batch(n_prefix=0, max_len=1), 32) == 0
 
@@ -201,11 +201,12 @@ for dtype in (G.F32, G.BF16):
     calls['one chunk %d' % dtype] = lambda C=C: T.attend(C, T.mk_batch(n_prefix=0, max_len=1))
     calls['a token each %d' % dtype] = lambda C=C: T.attend(C, T.mk_batch(n_prefix=2000))
     calls['prompt %d' % dtype] = lambda C=C: T.attend(C, T.mk_batch(cu=(0, 500, 1500), n_prefix=2000, max_len=2000, ld_pages=125))
+    calls['short prompt in chunks %d' % dtype] = lambda C=C: T.attend(C, T.mk_batch(cu=(0, 100, 200), n_prefix=2000, max_len=200, ld_pages=13))
 for name, call in calls.items():
     shim.shim_fail_at(-1)
     assert call() == G.OK, name
     launches = shim.shim_launches()
-    assert launches >= (3 if 'many' in name else 2 if 'each' in name or 'prompt' in name else 1), (name, launches)
+    assert launches >= (3 if 'many' in name else 2 if 'each' in name or 'chunks' in name else 1), (name, launches)
     for i in range(launches):
         shim.shim_fail_at(i)
         assert call() == G.EHIP, (name, i)

@@ -58,16 +58,18 @@ def step(heads, kv_heads, dim, new, max_len, prefix=0, bf16=True):
 
 # a step and its launches: rows<rows of the prefix / 16, of own parts / 16, own parts a wavefront each>, tiles of many rows, the join
 ROUTES = [
-    (step(32, 32, 128, [1], 100), ["rows 1 1"]),                                             # one chunk: written at once
-    (step(32, 32, 128, [1], 513), ["rows 1 1", "join"]),
+    (step(32, 32, 128, [1], 100), ["few"]),                                                  # a few steps are cheaper than a second launch
+    (step(32, 32, 128, [1], 257), ["rows 1 1", "join"]),
+    (step(8, 4, 64, [1, 1], 100, 150), ["few"]),                                        # ... the prefix ahead of own keys
+    (step(32, 8, 128, [2048, 1117, 604, 381], 2048, 300), ["tile"]),
     (step(32, 8, 128, [1] * 16, 201, 2048), ["rows 2 1", "join"]),
     (step(40, 40, 128, [1] * 64, 121, 1024), ["rows 2 1 alone", "join"]),
     (step(32, 8, 128, [1] * 48, 701, 32768), ["tile", "rows 1 1", "join"]),                  # 192 rows share the prefix
     (step(16, 16, 256, [1] * 5, 91, 1999), ["rows 1 1", "join"]),                            # wide heads go sixteen rows at a time
     (step(32, 8, 128, [2048, 1117, 604, 381], 2048), ["tile"]),
     (step(32, 8, 128, [20, 10], 40, 64), ["tile", "join"]),                                  # 80 rows: own parts and prefix in one launch
-    (step(32, 8, 128, [8, 8], 40, 64), ["rows 2 1", "join"]),                                # 32 rows a sequence, 64 in all
-    (step(4, 2, 64, [20, 10], 40, 64, bf16=False), ["rows 2 2", "join"]),
+    (step(32, 8, 128, [8, 8], 40, 640), ["rows 2 1", "join"]),                               # 32 rows a sequence, 64 in all
+    (step(4, 2, 64, [20, 10], 40, 640, bf16=False), ["rows 2 2", "join"]),
     (step(8, 4, 64, [500, 9], 600, 0, bf16=False), ["rows 2 2", "join"]),
     (step(32, 32, 64, [1500, 9], 1600, 0, bf16=False), ["rows 2 2 alone"]),
 ]
@@ -82,7 +84,7 @@ def test_routes_of_an_attention(record):
                 assert m[1] == str(int(call["bf16"])) and m[3] == "1"
                 names.append("rows %s %s%s" % (m[4], m[5], " alone" if m[6] == "1" else ""))
             else:
-                names.append("tile" if "attend_tile_kernel" in name else "join" if "attend_join_kernel" in name else name)
+                names.append(next((k for k in ("tile", "join", "few") if "attend_%s_kernel" % k in name), name))
         assert names == want, (call, names)
 
 
