@@ -625,8 +625,12 @@ static AttPlan attend_plan(const griffin_kv_cache &C, const griffin_kv_batch &B,
     int64_t longest = 0;
     for (int b = 0; b < seqs.n; ++b)
         longest = std::max(longest, (int64_t)(seqs.cu[b + 1] - seqs.cu[b]) * group);
+    // Own parts of more than 64 rows go through LDS, 256 rows a workgroup.  (16 sequences of 2000 keys, us there / here: 48 rows 38 / 36, 80 rows 42 / 58, 128 rows
+    // 46 / 62; one sequence of 64 rows 16.6 / 14.2.)  So does a prefix of more rows than that where there is enough to multiply: its workgroups are fewer and
+    // larger, and another launch if own parts do not go there, too.  (8 kv heads of 128, us there / here: 80 rows of 8192 keys 26.7 / 21.7, of 32768 42.7 / 43.0; 192
+    // rows of 2048 keys 33 / 21, of 8192 34.6 / 33.2, of 32768 57 / 81; 448 rows of 2048 keys 37 / 27, of 8192 45 / 54.)
     pl.tile_own = bf16 && longest > 64;
-    pl.tile_prefix = bf16 && rows > 64;
+    pl.tile_prefix = bf16 && (pl.tile_own || (rows > 64 && (double)rows * B.n_prefix * C.kv_heads * C.dim >= 0x1p31));
     pl.nto = longest <= 32 ? 1 : widest;
     pl.ntp = rows <= 16 ? 1 : widest;
     if (!pl.tile_own && !pl.tile_prefix && pl.nto == widest)        // compiled pairs: (1, 1), (2, 1), (2, 2)
@@ -638,13 +642,17 @@ static AttPlan attend_plan(const griffin_kv_cache &C, const griffin_kv_batch &B,
         tiles += ((int64_t)(seqs.cu[b + 1] - seqs.cu[b]) * group + pl.rows_own - 1) / pl.rows_own;
     pl.tiles_own = (int32_t)tiles;
     pl.tiles_prefix = B.n_prefix > 0 ? (int32_t)((rows + pl.rows_prefix - 1) / pl.rows_prefix) : 0;
-    // own parts that fill the chip as they are, a wavefront each, are not cut
-    pl.lone = !pl.tile_own && C.kv_heads * tiles >= 1024;
-    // as many keys a chunk as leave a workgroup a CU, or two of the smaller ones; own parts of many rows are one chunk if they fill the chip
+    // Own parts that fill the chip as they are, a wavefront each, are not cut, unless the longest may keep the others waiting.  (2560 parts of up to 60 keys, a
+    // wavefront each / a workgroup each: 11.7 / 12.8 us, caches cold 20.6 / 20.2; 2048 of up to 200: 27 / 28.5, 62 / 60; 1280 of up to 500: 41 / 36, 93 / 87;
+    // 768 of up to 500: 29 / 25, 58 / 55; two fp32 prompts of 1500 and 9 tokens, 32 heads of 64: 161 / 113.)
+    pl.lone = !pl.tile_own && C.kv_heads * tiles >= 1024 && B.max_len <= 256;
+    // As many keys a chunk as leave a workgroup a CU, or two of the smaller ones, which a CU holds at a time.  (More of them, us for 512 / 1024 / 2048: 48 rows of 16384
+    // keys 23 / 30 / 32, 32 rows of 30000 31 / 35 / 41; fewer, 256, the same within 3 %.  Tiles, 256 / 512: 192 rows of 32768 keys 71 / 85, a prompt of 2048 63 / 70;
+    // heads of 256, 256 / 512: 15.7 / 18.4.)  Own parts of many rows are one chunk if they fill the chip.
     const int64_t step = ATT_WAVES * (bf16 ? 32 : 16);
     const int64_t work_prefix = C.kv_heads * (int64_t)pl.tiles_prefix * B.n_prefix, work_own = C.kv_heads * tiles * B.max_len;
     const auto chunk = [&](bool tile, int64_t work) {
-        const int64_t quantum = tile ? tile_keys : step, wgs = tile || pl.lone || C.dim > 128 ? 256 : 1024;
+        const int64_t quantum = tile ? tile_keys : step, wgs = tile || pl.lone || C.dim > 128 ? 256 : 512;
         return (int32_t)((std::max((work + wgs - 1) / wgs, (int64_t)1) + quantum - 1) / quantum * quantum);
     };
     const bool together = pl.tile_prefix == pl.tile_own && !pl.lone;
@@ -732,8 +740,9 @@ static int attend_typed(AttendParams &p, const AttPlan &pl, hipStream_t st)
     if (rc != GRIFFIN_OK || !p.part)
         return rc;
     const int64_t rows = (int64_t)p.seqs.cu[p.seqs.n] * p.n_heads;
-    // few rows of many chunks: four wavefronts a row
-    if (rows <= 2048 && pl.chunks_prefix + pl.chunks_own > 8)
+    // A wavefront has 16 chunks of features on their way at a time (dim 128); of few rows with more, four share a row.  (One / four wavefronts a row, the whole call:
+    // 256 rows of 60 chunks 34.4 / 31.4 us, 512 of 33 21.3 / 20.1, 32 of 32 10.3 / 9.9; 512 of 18 13.2 / 14.1, 1280 of 33 28.7 / 31.6.)
+    if (rows <= 512 && pl.chunks_prefix + pl.chunks_own > 24)
         hipLaunchKernelGGL((attend_join_kernel<BF16, DB, 4>), dim3((uint32_t)rows), dim3(256), 0, st, p);
     else
         hipLaunchKernelGGL((attend_join_kernel<BF16, DB, 1>), dim3((uint32_t)((rows + 3) / 4)), dim3(256), 0, st, p);

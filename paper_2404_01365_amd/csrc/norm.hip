@@ -166,8 +166,8 @@ static int launch_typed(const NormParams &p, hipStream_t st)
                        dim3(WAVES == 1 ? 256 : WAVES * 64), 0, st, p)
     if (lanes <= 1) NORM_GO(1, 1);
     else if (lanes <= 4) NORM_GO(4, 1);
-    else if (lanes <= 8) NORM_GO(4, 2);
-    else if (lanes <= 16) NORM_GO(8, 2);
+    else if (lanes <= 8) NORM_GO(8, 1);
+    else if (lanes <= 16) NORM_GO(16, 1);
     else if (lanes <= 32) NORM_GO(16, 2);
     else NORM_GO(16, 4);
 #undef NORM_GO

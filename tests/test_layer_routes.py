@@ -71,7 +71,10 @@ ROUTES = [
     (step(32, 8, 128, [8, 8], 40, 640), ["rows 2 1", "join"]),                               # 32 rows a sequence, 64 in all
     (step(4, 2, 64, [20, 10], 40, 640, bf16=False), ["rows 2 2", "join"]),
     (step(8, 4, 64, [500, 9], 600, 0, bf16=False), ["rows 2 2", "join"]),
-    (step(32, 32, 64, [1500, 9], 1600, 0, bf16=False), ["rows 2 2 alone"]),
+    (step(32, 32, 64, [1500, 9], 1600, 0, bf16=False), ["rows 2 2"]),                        # long ones wait for each other: a workgroup each
+    (step(32, 32, 64, [40] * 16, 250, 0, bf16=False), ["rows 2 2 alone"]),
+    (step(32, 8, 128, [1] * 20, 60, 8000), ["rows 2 1", "join"]),                            # 80 rows: a prefix with too little for tiles ...
+    (step(32, 8, 128, [1] * 20, 60, 30000), ["tile", "rows 1 1", "join"]),                   # ... and one with enough
 ]
 
 
