@@ -648,7 +648,8 @@ static AttPlan attend_plan(const griffin_kv_cache &C, const griffin_kv_batch &B,
     pl.lone = !pl.tile_own && C.kv_heads * tiles >= 1024 && B.max_len <= 256;
     // As many keys a chunk as leave a workgroup a CU, or two of the smaller ones, which a CU holds at a time.  (More of them, us for 512 / 1024 / 2048: 48 rows of 16384
     // keys 23 / 30 / 32, 32 rows of 30000 31 / 35 / 41; fewer, 256, the same within 3 %.  Tiles, 256 / 512: 192 rows of 32768 keys 71 / 85, a prompt of 2048 63 / 70;
-    // heads of 256, 256 / 512: 15.7 / 18.4.)  Own parts of many rows are one chunk if they fill the chip.
+    // heads of 256, 256 / 512: 15.7 / 18.4.)  Own parts that have a launch for themselves behind tiles of the prefix are cut finer: the longest is known here, most are shorter, and
+    // nothing else runs beside it (48 of 5 to 700 keys, 512 / 1024 / 2048 workgroups: 75 / 70 / 68 us).  Own parts of many rows are one chunk if they fill the chip.
     const int64_t step = ATT_WAVES * (bf16 ? 32 : 16);
     const int64_t work_prefix = C.kv_heads * (int64_t)pl.tiles_prefix * B.n_prefix, work_own = C.kv_heads * tiles * B.max_len;
     const auto chunk = [&](bool tile, int64_t work) {
@@ -657,7 +658,7 @@ static AttPlan attend_plan(const griffin_kv_cache &C, const griffin_kv_batch &B,
     };
     const bool together = pl.tile_prefix == pl.tile_own && !pl.lone;
     pl.chunk_prefix = chunk(pl.tile_prefix, together ? work_prefix + work_own : work_prefix);
-    pl.chunk_own = chunk(pl.tile_own, together ? work_prefix + work_own : work_own);
+    pl.chunk_own = chunk(pl.tile_own, together ? work_prefix + work_own : pl.lone ? work_own : work_own / 4);
     if (pl.lone || (pl.tile_own && C.kv_heads * tiles > 128))
         pl.chunk_own = (int32_t)((B.max_len + step - 1) / step * step);
     // (Own parts of many rows, whole / cut so that 256 workgroups share them: 3000 tokens of 16 heads, 192 tiles of rows, 95 / 113 us; 1000 of 40 heads on 8, 160
