@@ -394,8 +394,8 @@ int griffin_kv_append(const griffin_kv_cache *C, const griffin_kv_batch *B, cons
 /*
  * Attention of a step's new tokens, which griffin_kv_append has put into the cache:
  *   out[t][h] = sum_k softmax_k(scale * q[t][h] . K_k) V_k      over the keys that token t sees, kv head h / (n_heads / kv_heads)
- * (zeros where all scores are -inf).  The prefix's keys and values are read
- * once for up to 64 rows (tokens times heads of a group) or more, whichever sequences they belong to.  Scores, the softmax's maximum and sum and the
+ * (zeros where all scores are -inf).  The prefix's keys and values are read once for up to 16 to 256 rows (tokens
+ * times heads of a group) by what there is to do, whichever sequences the rows belong to.  Scores, the softmax's maximum and sum and the
  * weighted sum are fp32; bf16 caches take the weights rounded to bf16 into the second product (2^-8 each).  Keys that a token does not
  * see do not reach its output, whatever they hold.
  *   q, out     [tokens][n_heads][dim], token and head strides (ldq, hsq; ldo, hso), multiples of 8, 16-byte aligned; out is not q

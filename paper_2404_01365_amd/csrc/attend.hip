@@ -14,6 +14,11 @@
 // feature 8 r + e) and turns it with 32 byte permutes.
 //
 // Long key ranges are cut into chunks for as many workgroups as fill the chip; each leaves its rows' o, m and l, and a second kernel joins them.
+//
+// Bound by bytes while few rows share a key, with the latency of a step's loads on top: a part that one step covers is two launches' latency, 4.5 us of it the join's.
+// Measured: 64 continuations of 1024 shared tokens and 1 to 120 of their own, 40 heads of 128, 102 MB, 32 us warm = 3.2 TB/s; 8 sequences behind 30000 shared
+// keys of 8 heads of 128, four query heads each, 125 MB, 31 us = 4.0 TB/s; one row of 513 keys of 32 heads 8.3 us and the join.
+// The products of 16 rows a key are a twentieth of the matrix cores' rate when keys arrive at a copy's, of 64 rows a quarter: the arrangement is made for loads.
 #include <algorithm>
 
 #include "attend.h"
