@@ -1,4 +1,4 @@
-// What the two attention kernels share: attend.hip (a few rows, keys straight into registers) and attend_tile.hip (many rows,
+// What the attention's kernels share: those of a few rows (attend_rows.h, keys straight into registers) and of many (attend_tile.hip,
 // keys through LDS).
 #pragma once
 
@@ -11,7 +11,7 @@ typedef __attribute__((ext_vector_type(8))) __bf16 att_bf16x8;
 typedef __attribute__((ext_vector_type(4))) uint32_t att_u32x4;
 
 constexpr int ATT_WAVES = 4;            // of a workgroup of attend.hip
-constexpr int ATT_FEW_WAVES = 8;        // ... of its attend_few_kernel
+constexpr int ATT_FEW_WAVES = 8;        // ... of its attend_few_kernel, and of own parts beside tiles
 constexpr int ATT_TILE_WAVES = 8;       // ... of attend_tile.hip
 constexpr int att_tile_keys(int32_t dim) { return dim > 128 ? 32 : 64; }      // its step
 
@@ -181,8 +181,9 @@ __device__ __forceinline__ bool att_own_item(const AttendParams &p, int32_t id, 
     return it.begin < it.end;                                 // else no row reads this chunk's partial sums
 }
 
-// launches the `wgs` workgroups of p on tiles of att_tile_rows(dim) rows; bf16 only
-int launch_attend_tiles(const AttendParams &p, int32_t wgs, hipStream_t st);
+// launches the `wgs` workgroups of p on tiles of att_tile_rows(dim) rows, and behind them p.items_own own items of 16 rows, a workgroup each or, `each`, a
+// wavefront each (dim <= 128); bf16 only
+int launch_attend_tiles(const AttendParams &p, int32_t wgs, bool each, hipStream_t st);
 constexpr int att_tile_rows(int32_t dim) { return 16 * ATT_TILE_WAVES * (dim > 128 ? 1 : 2); }
 
 }  // namespace griffin

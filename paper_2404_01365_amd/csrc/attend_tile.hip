@@ -1,5 +1,5 @@
 // Attention of many rows (bf16): prompts, and a prefix that more than 64 rows share.  The mathematics and the arrangement of scores
-// and sums are those of attend.hip; here eight wavefronts of 32 rows each (16 of heads wider than 128) take the same keys, which go through LDS
+// and sums are those of attend_rows.h; here eight wavefronts of 32 rows each (16 of heads wider than 128) take the same keys, which go through LDS
 // 64 at a time (32 of the wider heads), two steps' worth of room, so that a step's loads travel while the step before is computed.
 //
 // Keys lie in LDS in the order of the A operands (a lane's 16 bytes side by side: reads without bank conflicts).  Values lie as in memory, a row a
@@ -15,7 +15,7 @@
 // 1.56 us is what this arrangement can reach, and 2.03 is measured: prompts of 2048, 1117, 604 and 381 tokens of 32 heads on 8, 49 GFLOP that are seen, 72 us = 675
 // TFLOP/s of them.  Tried and slower on these, 88 to 117 us: the halves of a workgroup in turn, one multiplying while the other forms weights; products and
 // weights of neighbouring tiles interleaved within a wavefront; four wavefronts of 64 rows.
-#include "attend.h"
+#include "attend_rows.h"
 
 namespace griffin {
 
@@ -307,7 +307,11 @@ __device__ __forceinline__ void tile_softmax(bool masked, TileScores<DB> &s, att
     }
 }
 
-template <int DB, bool FULL>
+// OWN: who takes own parts.  TILES: they are tiles, too.  ROWS, EACH: they are of a few rows, and a workgroup, or each wavefront, takes one as attend_rows.h has it
+// behind the tiles, which saves a launch.
+enum TileOwn { OWN_TILES, OWN_ROWS, OWN_EACH };
+
+template <int DB, bool FULL, TileOwn OWN>
 __global__ __launch_bounds__(64 * ATT_TILE_WAVES) void attend_tile_kernel(AttendParams p)
 {
     using S = TileShape<DB>;
@@ -316,8 +320,17 @@ __global__ __launch_bounds__(64 * ATT_TILE_WAVES) void attend_tile_kernel(Attend
     AttendItem it;
     if ((int32_t)blockIdx.x < p.wgs_prefix)
         att_prefix_item<att_tile_rows(DB)>(p, blockIdx.x, it);
-    else if (!att_own_item<att_tile_rows(DB), true>(p, blockIdx.x - p.wgs_prefix, it))
+    else if constexpr (OWN == OWN_TILES) {
+        if (!att_own_item<att_tile_rows(DB), true>(p, blockIdx.x - p.wgs_prefix, it))
+            return;
+    } else {
+        int32_t id = blockIdx.x - p.wgs_prefix;
+        if (OWN == OWN_EACH)
+            id = id * ATT_TILE_WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        if (id < p.items_own && att_own_item<16, false>(p, id, it))
+            attend_rows<true, DB, FULL, 1, OWN == OWN_EACH ? 1 : ATT_TILE_WAVES>(p, (float *)tile_lds, it);
         return;
+    }
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int32_t first = it.first + wave * 16 * S::NT;
     const auto sees = [&](int32_t row) {                      // where the keys that a row sees end
@@ -432,25 +445,33 @@ __global__ __launch_bounds__(64 * ATT_TILE_WAVES) void attend_tile_kernel(Attend
     }
 }
 
-template <int DB>
+template <int DB, TileOwn OWN>
 static int go_tiles(const AttendParams &p, int32_t wgs, hipStream_t st)
 {
-    constexpr int bytes = 4 * TileShape<DB>::BYTES;
+    constexpr int rooms = 4 * TileShape<DB>::BYTES, sums = OWN == OWN_ROWS ? att_lds_floats<DB, ATT_TILE_WAVES>() * 4 : 0, bytes = rooms > sums ? rooms : sums;
     if (p.dim == DB) {
-        RAISE_LDS_LIMIT((attend_tile_kernel<DB, true>), bytes);
-        hipLaunchKernelGGL((attend_tile_kernel<DB, true>), dim3(wgs), dim3(64 * ATT_TILE_WAVES), bytes, st, p);
+        RAISE_LDS_LIMIT((attend_tile_kernel<DB, true, OWN>), bytes);
+        hipLaunchKernelGGL((attend_tile_kernel<DB, true, OWN>), dim3(wgs), dim3(64 * ATT_TILE_WAVES), bytes, st, p);
     } else {
-        RAISE_LDS_LIMIT((attend_tile_kernel<DB, false>), bytes);
-        hipLaunchKernelGGL((attend_tile_kernel<DB, false>), dim3(wgs), dim3(64 * ATT_TILE_WAVES), bytes, st, p);
+        RAISE_LDS_LIMIT((attend_tile_kernel<DB, false, OWN>), bytes);
+        hipLaunchKernelGGL((attend_tile_kernel<DB, false, OWN>), dim3(wgs), dim3(64 * ATT_TILE_WAVES), bytes, st, p);
     }
     return check_launch("attend_tile_kernel");
 }
 
-int launch_attend_tiles(const AttendParams &p, int32_t wgs, hipStream_t st)
+template <int DB>
+static int go_tiles_and_rows(const AttendParams &p, int32_t wgs, bool each, hipStream_t st)
+{
+    if (each)
+        return go_tiles<DB, OWN_EACH>(p, wgs + (p.items_own + ATT_TILE_WAVES - 1) / ATT_TILE_WAVES, st);
+    return p.items_own > 0 ? go_tiles<DB, OWN_ROWS>(p, wgs + p.items_own, st) : go_tiles<DB, OWN_TILES>(p, wgs, st);
+}
+
+int launch_attend_tiles(const AttendParams &p, int32_t wgs, bool each, hipStream_t st)
 {
     if (p.dim <= 64)
-        return go_tiles<64>(p, wgs, st);
-    return p.dim <= 128 ? go_tiles<128>(p, wgs, st) : go_tiles<256>(p, wgs, st);
+        return go_tiles_and_rows<64>(p, wgs, each, st);
+    return p.dim <= 128 ? go_tiles_and_rows<128>(p, wgs, each, st) : go_tiles<256, OWN_TILES>(p, wgs, st);
 }
 
 }  // namespace griffin

@@ -472,3 +472,15 @@ def test_attention_of_infinities_beside_the_prefix_end(dtype, heads, kv_heads, n
     assert np.all(got[:, group:2 * group, 7] == -np.inf)
     got[:, group:2 * group, 7], ref[:, group:2 * group, 7] = 0, 0
     attention_close(got, ref, size, dtype)
+
+
+@pytest.mark.parametrize("heads,kv_heads,dim,prefix,held,new,order", [
+    (128, 4, 80, 23500, [0, 600, 33, 270, 5, 9, 256, 1, 300], [1] * 9, "thd"),        # a workgroup each, two tiles of rows, several chunks of own parts
+    (64, 2, 128, 43700, [700, 0, 250], [1, 3, 2], "htd"),                             # ... of up to 96 rows: own parts are tiles, too
+    (64, 2, 128, 43700, [700, 0, 250, 3, 31], [1, 1, 1, 2, 1], "htd"),                # ... of up to 64
+    (128, 16, 64, 4200, list(range(0, 192, 3)), [1] * 64, "htd"),                     # a wavefront each
+])
+def test_attention_of_own_parts_beside_tiles_of_the_prefix(heads, kv_heads, dim, prefix, held, new, order):
+    """bf16: a prefix with so much to multiply that its rows go in tiles, own parts of a few rows behind them."""
+    assert sum(new) * heads * dim * prefix >= 2 ** 31
+    check_attention(111, order, heads=heads, kv_heads=kv_heads, dim=dim, page=64, prefix=prefix, held=held, new=new, dtype=BF16)

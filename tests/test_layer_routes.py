@@ -64,7 +64,7 @@ ROUTES = [
     (step(32, 8, 128, [2048, 1117, 604, 381], 2048, 300), ["tile"]),
     (step(32, 8, 128, [1] * 16, 201, 2048), ["rows 2 1", "join"]),
     (step(40, 40, 128, [1] * 64, 121, 1024), ["rows 2 1 alone", "join"]),
-    (step(32, 8, 128, [1] * 48, 701, 32768), ["tile", "rows 1 1", "join"]),                  # 192 rows share the prefix
+    (step(32, 8, 128, [1] * 48, 701, 32768), ["tile and rows", "join"]),                  # 192 rows share the prefix
     (step(16, 16, 256, [1] * 5, 91, 1999), ["rows 1 1", "join"]),                            # wide heads go sixteen rows at a time
     (step(32, 8, 128, [2048, 1117, 604, 381], 2048), ["tile"]),
     (step(32, 8, 128, [20, 10], 40, 64), ["tile", "join"]),                                  # 80 rows: own parts and prefix in one launch
@@ -74,7 +74,9 @@ ROUTES = [
     (step(32, 32, 64, [1500, 9], 1600, 0, bf16=False), ["rows 2 2"]),                        # long ones wait for each other: a workgroup each
     (step(32, 32, 64, [40] * 16, 250, 0, bf16=False), ["rows 2 2 alone"]),
     (step(32, 8, 128, [1] * 20, 60, 8000), ["rows 2 1", "join"]),                            # 80 rows: a prefix with too little for tiles ...
-    (step(32, 8, 128, [1] * 20, 60, 30000), ["tile", "rows 1 1", "join"]),                   # ... and one with enough
+    (step(32, 8, 128, [1] * 20, 60, 30000), ["tile and rows", "join"]),                      # ... and one with enough
+    (step(40, 20, 128, [1] * 64, 121, 8192), ["tile and rows alone", "join"]),
+    (step(80, 10, 256, [1] * 9, 60, 30000), ["tile", "rows 1 1", "join"]),                   # heads whose rows need more registers than tiles leave
 ]
 
 
@@ -86,8 +88,10 @@ def test_routes_of_an_attention(record):
             if m:
                 assert m[1] == str(int(call["bf16"])) and m[3] == "1"
                 names.append("rows %s %s%s" % (m[4], m[5], " alone" if m[6] == "1" else ""))
+            elif "attend_tile_kernel" in name:
+                names.append(("tile", "tile and rows", "tile and rows alone")[int(re.search(r"TileOwnE(\d)E", name)[1])])
             else:
-                names.append(next((k for k in ("tile", "join", "few") if "attend_%s_kernel" % k in name), name))
+                names.append(next((k for k in ("join", "few") if "attend_%s_kernel" % k in name), name))
         assert names == want, (call, names)
 
 
