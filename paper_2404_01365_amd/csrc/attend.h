@@ -10,8 +10,8 @@ typedef __attribute__((ext_vector_type(4))) float att_f32x4;
 typedef __attribute__((ext_vector_type(8))) __bf16 att_bf16x8;
 typedef __attribute__((ext_vector_type(4))) uint32_t att_u32x4;
 
-constexpr int ATT_WAVES = 4;            // of a workgroup of attend.hip
-constexpr int ATT_FEW_WAVES = 8;        // ... of its attend_few_kernel, and of own parts beside tiles
+constexpr int ATT_WAVES = 4;            // of a workgroup of attend_rows_kernel
+constexpr int ATT_FEW_WAVES = 8;        // ... of attend_few_kernel, and of own parts beside tiles
 constexpr int ATT_TILE_WAVES = 8;       // ... of attend_tile.hip
 constexpr int att_tile_keys(int32_t dim) { return dim > 128 ? 32 : 64; }      // its step
 
