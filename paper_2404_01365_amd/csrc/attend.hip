@@ -174,6 +174,9 @@ static AttPlan attend_plan(const griffin_kv_cache &C, const griffin_kv_batch &B,
     // Own parts of a few rows go in the launch of those tiles, if the tiles' share of registers is enough for them.  (In a launch of their own, 48 of 5 to 700 keys
     // behind 32768: 74 us, not 67; 20 of 50: 43, not 40.)
     pl.beside = pl.tile_prefix && !pl.tile_own && C.dim <= 128;
+    // Where a wavefront has the registers it takes two tiles of 16 rows, and so reads keys half as often.  (Own parts, two / one: 16 of 48 rows and 2000 keys 35 / 57 us, 16
+    // of 64 rows and 1000 keys 26.8 / 25.6, one of 64 rows and 4000 keys 17.6 / 14.4; up to 32 rows the same.  A prefix: 64 rows of 30000 keys 34 / 47, 48 of 16384 23 / 28, 64
+    // of 2048 12.7 / 14.0, 80 of 2048 15.1 / 13.6.)
     pl.nto = longest <= 32 || pl.beside ? 1 : widest;
     pl.ntp = rows <= 16 ? 1 : widest;
     if (!pl.tile_own && !pl.tile_prefix && pl.nto == widest)        // compiled pairs: (1, 1), (2, 1), (2, 2)
