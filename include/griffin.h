@@ -396,7 +396,7 @@ int griffin_kv_append(const griffin_kv_cache *C, const griffin_kv_batch *B, cons
  *   out[t][h] = sum_k softmax_k(scale * q[t][h] . K_k) V_k      over the keys that token t sees, kv head h / (n_heads / kv_heads)
  * (zeros where all scores are -inf).  The prefix's keys and values are read once for up to 16 to 256 rows (tokens
  * times heads of a group) by what there is to do, whichever sequences the rows belong to.  Scores, the softmax's maximum and sum and the
- * weighted sum are fp32; bf16 caches take the weights rounded to bf16 into the second product (2^-8 each).  Keys that a token does not
+ * weighted sum are fp32; bf16 caches take the weights rounded to bf16 (2^-8 each) into the second product and into the sum, so that they add up to one.  Keys that a token does not
  * see do not reach its output, whatever they hold.
  *   q, out     [tokens][n_heads][dim], token and head strides (ldq, hsq; ldo, hso), multiples of 8, 16-byte aligned; out is not q
  *   n_heads    a multiple of C->kv_heads, at most 1024; tokens * n_heads^2 < 2^32

@@ -33,7 +33,8 @@ struct AttRows {
     using S = AttShape<BF16, DB>;
     att_u32x4 q[NT][S::NQ];
     int32_t end[NT];             // keys from here on are not seen by the lane's row
-    float m[NT], l[NT];
+    float m[NT];
+    att_f32x4 l[NT];             // bf16: the row's sum in every element (att_add_weights); fp32: element 0, of the lane's own keys
     att_f32x4 o[NT][S::NO];
 };
 
@@ -136,8 +137,7 @@ __device__ __forceinline__ void att_scores(AttScores<BF16, DB, NT> &s, const Att
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 if constexpr (BF16)
-                    s[n][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(att_bf16x8, f.k[i][c]), __builtin_bit_cast(att_bf16x8, r.q[n][c]),
-                                                                      s[n][i], 0, 0, 0);
+                    s[n][i] = att_mfma(f.k[i][c], r.q[n][c], s[n][i]);
                 else
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
@@ -145,7 +145,7 @@ __device__ __forceinline__ void att_scores(AttScores<BF16, DB, NT> &s, const Att
             }
 }
 
-// Scores to weights: the rows' maximum and sum carried on, o scaled to the new maximum
+// Scores to weights: the rows' maximum carried on, sum and o scaled to the new one, the sum carried on in fp32 (bf16: with the second product)
 template <bool BF16, int DB, int NT>
 __device__ __forceinline__ void att_softmax(AttScores<BF16, DB, NT> &s, AttRows<BF16, DB, NT> &r, float scale2)
 {
@@ -170,7 +170,10 @@ __device__ __forceinline__ void att_softmax(AttScores<BF16, DB, NT> &s, AttRows<
                 s[n][i][e] = __builtin_amdgcn_exp2f(s[n][i][e] * scale2 - base);
                 l += s[n][i][e];
             }
-        r.l[n] = r.l[n] * f + l;
+        if constexpr (BF16)
+            r.l[n] *= f;
+        else
+            r.l[n][0] = r.l[n][0] * f + l;
 #pragma unroll
         for (int c = 0; c < S::NO; ++c)
             r.o[n][c] *= f;
@@ -207,6 +210,9 @@ __device__ __forceinline__ void att_weigh(const AttScores<BF16, DB, NT> &s, cons
                 w[n][2 * i + 1] = f32x2_to_bf16x2(s[n][i][2], s[n][i][3]);
             }
 #pragma unroll
+        for (int n = 0; n < NT; ++n)
+            att_add_weights(r.l[n], w[n]);
+#pragma unroll
         for (int c = 0; c < S::NC; ++c)
 #pragma unroll
             for (int e = 0; e < S::VD; ++e) {
@@ -216,8 +222,7 @@ __device__ __forceinline__ void att_weigh(const AttScores<BF16, DB, NT> &s, cons
                     a[h] = __builtin_amdgcn_perm(f.v[2 * h + 1][c][e / 2], f.v[2 * h][c][e / 2], e & 1 ? 0x07060302 : 0x05040100);
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
-                    r.o[n][c * S::VD + e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(att_bf16x8, a), __builtin_bit_cast(att_bf16x8, w[n]),
-                                                                                   r.o[n][c * S::VD + e], 0, 0, 0);
+                    r.o[n][c * S::VD + e] = att_mfma(a, w[n], r.o[n][c * S::VD + e]);
             }
     } else {
 #pragma unroll
@@ -350,7 +355,7 @@ __device__ __forceinline__ void attend_rows(const AttendParams &p, float *lds, c
                 r.q[n][s] = att_u32x4{0, 0, 0, 0};
         }
         r.m[n] = -INFINITY;
-        r.l[n] = 0;
+        r.l[n] = att_f32x4{0, 0, 0, 0};
 #pragma unroll
         for (int c = 0; c < S::NO; ++c)
             r.o[n][c] = att_f32x4{0, 0, 0, 0};
@@ -391,9 +396,10 @@ __device__ __forceinline__ void attend_rows(const AttendParams &p, float *lds, c
         for (key0 = begin + wave * S::KS; key0 < end; key0 += WAVES * S::KS)
             if (key0 + S::KS > least || it.touches_hole(key0, S::KS))
                 att_add_infinite<BF16, DB, FULL, NT>(p, it, r, key0);
+    float sum[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n)
-        r.l[n] = lane_groups_sum(r.l[n]);
+        sum[n] = BF16 ? r.l[n][0] : lane_groups_sum(r.l[n][0]);
     if constexpr (WAVES == 1) {
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -401,7 +407,7 @@ __device__ __forceinline__ void attend_rows(const AttendParams &p, float *lds, c
             if (row >= rows)
                 continue;
             if (p.part && lane < 16)
-                p.part_ml[att_slot(p, it, row)] = make_float2(r.m[n], r.l[n]);
+                p.part_ml[att_slot(p, it, row)] = make_float2(r.m[n], sum[n]);
 #pragma unroll
             for (int c = 0; c < S::NC; ++c)
 #pragma unroll
@@ -410,7 +416,7 @@ __device__ __forceinline__ void attend_rows(const AttendParams &p, float *lds, c
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
                         x[j] = r.o[n][c * S::VD + (h * 8 + j) % S::VD][(h * 8 + j) / S::VD];
-                    att_store8<BF16, FULL>(p, it, row, (c * 16 + (lane >> 4) * 4) * S::VD + h * 8, x, r.l[n]);
+                    att_store8<BF16, FULL>(p, it, row, (c * 16 + (lane >> 4) * 4) * S::VD + h * 8, x, sum[n]);
                 }
         }
         return;
@@ -441,7 +447,7 @@ __device__ __forceinline__ void attend_rows(const AttendParams &p, float *lds, c
                     }
                 if (lane < 16) {
                     ml[wave * 32 + lane] = r.m[n];
-                    ml[wave * 32 + 16 + lane] = r.l[n];
+                    ml[wave * 32 + 16 + lane] = sum[n];
                 }
             }
             __syncthreads();

@@ -7,7 +7,7 @@
 // pieces of a row are exchanged by the row's number so that those rows fall into different banks.
 //
 // The rows' reference maximum moves only when scores outgrow it by more than 8 (base 2): weights then are up to 2^8 (their rounding to bf16 is
-// relative), and o is scaled a few times instead of at every step.
+// relative, and cancels from what a dominating one weighs, as the sum is of rounded ones, too), and o is scaled a few times instead of at every step.
 //
 // Bound by the matrix cores and what stands between the two products.  A step of 64 keys for 32 rows of 128 features is 64 products of 16x16x32 a wavefront, two
 // wavefronts a SIMD: at 8.25 ns each when they are fed without a pause 1.06 us, and some 0.5 us of weights (exponentials, maxima, rounding) for both.  The two
@@ -40,7 +40,8 @@ struct TileRows {
     using S = TileShape<DB>;
     att_u32x4 q[S::NT][S::NQ];
     int32_t end[S::NT];
-    float m[S::NT], l[S::NT];
+    float m[S::NT];
+    att_f32x4 l[S::NT];                                       // the row's sum in every element (att_add_weights)
     att_f32x4 o[S::NT][S::NO];
 };
 
@@ -154,11 +155,6 @@ __device__ __forceinline__ att_u32x4 tile_vals(uint32_t at, int e, int h)
     return att_u32x4{lo.x, lo.y, hi.x, hi.y};
 }
 
-__device__ __forceinline__ att_f32x4 att_mfma(att_u32x4 a, att_u32x4 b, att_f32x4 c)
-{
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(att_bf16x8, a), __builtin_bit_cast(att_bf16x8, b), c, 0, 0, 0);
-}
-
 // In steps in which rows differ in the keys that they see, or in which keys end, infinite and NaN values of keys that a row does not see must not reach
 // it, as 0 x Inf would: there they are stored as zeros, and what was made zero is added at the end to the rows that do see it.
 template <int DB, bool FULL>
@@ -193,6 +189,11 @@ __device__ __forceinline__ void tile_weigh(uint32_t vals, const att_u32x4 (&w)[T
 #pragma unroll
     for (int i = 0; i < 4; ++i)
         a[0][i] = tile_vals<DB>(vals, i % G, i / G);
+#pragma unroll
+    for (int h = 0; h < H; ++h)                               // while the first operands are on their way
+#pragma unroll
+        for (int n = 0; n < S::NT; ++n)
+            att_add_weights(r.l[n], w[n][h]);
 #pragma unroll
     for (int e = 0; e < S::NO; e += G) {
         const int now = e / G & 1;
@@ -250,7 +251,7 @@ __device__ __forceinline__ void tile_scores(uint32_t keys, TileScores<DB> &s, co
     __builtin_amdgcn_sched_barrier(0);
 }
 
-// Scores to weights in bf16; the rows' reference and sum carried on, o scaled when the reference moves
+// Scores to weights in bf16; the rows' reference carried on, sum and o scaled when it moves
 template <int DB>
 __device__ __forceinline__ void tile_softmax(bool masked, TileScores<DB> &s, att_u32x4 (&w)[TileShape<DB>::NT][TileShape<DB>::KT / 2], TileRows<DB> &r,
                                              float scale2, const AttendItem &it, int32_t key0)
@@ -300,7 +301,6 @@ __device__ __forceinline__ void tile_softmax(bool masked, TileScores<DB> &s, att
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 x[e] = __builtin_amdgcn_exp2f(s[n][t][e] * scale2 - base);
-            r.l[n] += (x[0] + x[1]) + (x[2] + x[3]);
             w[n][t / 2][t % 2 * 2] = f32x2_to_bf16x2(x[0], x[1]);
             w[n][t / 2][t % 2 * 2 + 1] = f32x2_to_bf16x2(x[2], x[3]);
         }
@@ -355,7 +355,7 @@ __global__ __launch_bounds__(64 * ATT_TILE_WAVES) void attend_tile_kernel(Attend
                 r.q[n][s] = att_u32x4{0, 0, 0, 0};
         }
         r.m[n] = -INFINITY;
-        r.l[n] = 0;
+        r.l[n] = att_f32x4{0, 0, 0, 0};
 #pragma unroll
         for (int e = 0; e < S::NO; ++e)
             r.o[n][e] = att_f32x4{0, 0, 0, 0};
@@ -420,7 +420,7 @@ __global__ __launch_bounds__(64 * ATT_TILE_WAVES) void attend_tile_kernel(Attend
     }
 #pragma unroll
     for (int n = 0; n < S::NT; ++n) {
-        const float l = lane_groups_sum(r.l[n]);
+        const float l = r.l[n][0];
         if (first + 16 * n + (lane & 15) >= it.rows)
             continue;
         const int32_t row = of(n), of_group = p.by_group(row), token = it.token0 + of_group, head = it.hk * p.group + row - of_group * p.group;
