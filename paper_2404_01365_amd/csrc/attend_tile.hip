@@ -363,8 +363,10 @@ __global__ __launch_bounds__(64 * ATT_TILE_WAVES) void attend_tile_kernel(Attend
     // keys that all rows of the wavefront see, and that any sees (none: it has no rows)
     const int32_t least = first < it.rows ? sees(first) : it.begin;
     const int32_t most = first < it.rows ? sees(first + 16 * S::NT < it.rows ? first + 16 * S::NT - 1 : it.rows - 1) : it.begin;
-    // steps from the one that begins at `clear` on have keys that some row of the workgroup does not see
-    const int32_t clear = it.begin + (sees(it.first) - it.begin) / S::KEYS * S::KEYS;
+    // steps from the one that begins at `clear` on have keys that some row of the workgroup does not see.  A first row that ends before this chunk begins: all of
+    // its steps, and none of the chunk before, whose workgroup adds what is infinite there.
+    const int32_t alike = sees(it.first) > it.begin ? sees(it.first) - it.begin : 0;
+    const int32_t clear = it.begin + alike / S::KEYS * S::KEYS;
     // Loads are two steps ahead of their use: a step's work is shorter than a read from memory under load takes.  Two stages take turns; step i
     // loads step i + 2's, looks up i + 4's pages, and stores i + 1's in the other room.
     TileStage<DB, FULL> even(p, it, wave, lane), odds(p, it, wave, lane);

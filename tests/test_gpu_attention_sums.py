@@ -41,3 +41,19 @@ def test_the_mean_of_equal_values_is_that_value(dtype, heads, kv_heads, dim, pre
     c.V[~np.isnan(c.V)] = value
     got = run_attention(c, scale=-np.log(0.5 * (1 + 0.98 * 2.0 ** -8)))
     assert np.all(got == value) if dtype == BF16 else np.abs(got - value).max() <= 2e-5
+
+
+@pytest.mark.parametrize("dim,early", [(64, 100), (128, 100), (256, 170)])
+def test_an_infinite_value_is_added_by_its_own_chunk(dim, early):
+    """A prompt in chunks of 64 keys (32 of wide heads), nearly all of whose weight lies on one key with an infinite feature.  A chunk behind that key's, which has an infinite
+    value of its own, has sums that the join scales by 2^-288: it must not add the early key's once more (0 x Inf)."""
+    c = plain.Case(6, heads=1, kv_heads=1, dim=dim, page=256, prefix=0, held=[0], new=[256], dtype=BF16)
+    set_scores(c, lambda slot: np.where(slot == early, 200.0, 0.0))
+    ref, size = c.attention(1.0)
+    page = c.pages[0, 0]
+    c.V[page, 0, early, 7], c.V[page, 0, 200, 9] = np.inf, np.inf
+    got = run_attention(c, scale=1.0)
+    assert np.all(got[early:, :, 7] == np.inf) and np.isfinite(got[:early]).all()
+    assert not np.isfinite(got[200:, :, 9]).any()
+    got[early:, :, 7], got[200:, :, 9] = ref[early:, :, 7], ref[200:, :, 9]
+    attention_close(got, ref, size, BF16)
