@@ -198,13 +198,14 @@ static AttPlan attend_plan(const griffin_kv_cache &C, const griffin_kv_batch &B,
     // (48 of 5 to 700 keys, 512 / 1024 / 2048 workgroups of four wavefronts' keys: 68 / 73 / 67 us).  Own parts of many rows are one chunk if they fill the chip.
     const int64_t step = ATT_WAVES * (bf16 ? 32 : 16);
     const int64_t work_prefix = C.kv_heads * (int64_t)pl.tiles_prefix * B.n_prefix, work_own = C.kv_heads * tiles * B.max_len;
-    const auto chunk = [&](bool tile, int64_t work) {
+    const auto chunk = [&](bool tile, int64_t work, int32_t keys) {        // no longer than the part: up to 2^30 keys and a quantum
         const int64_t quantum = tile ? tile_keys : pl.beside ? ATT_FEW_WAVES / ATT_WAVES * step : step, wgs = tile || pl.lone || C.dim > 128 ? 256 : 512;
-        return (int32_t)((std::max((work + wgs - 1) / wgs, (int64_t)1) + quantum - 1) / quantum * quantum);
+        const int64_t even = std::min((work + wgs - 1) / wgs, (int64_t)keys);
+        return (int32_t)((std::max(even, (int64_t)1) + quantum - 1) / quantum * quantum);
     };
     const bool together = pl.tile_prefix == pl.tile_own && !pl.lone;
-    pl.chunk_prefix = chunk(pl.tile_prefix, together ? work_prefix + work_own : work_prefix);
-    pl.chunk_own = chunk(pl.tile_own, together ? work_prefix + work_own : pl.lone ? work_own : work_own / 4);
+    pl.chunk_prefix = chunk(pl.tile_prefix, together ? work_prefix + work_own : work_prefix, B.n_prefix);
+    pl.chunk_own = chunk(pl.tile_own, together ? work_prefix + work_own : pl.lone ? work_own : work_own / 4, B.max_len);
     if (pl.lone || (pl.tile_own && C.kv_heads * tiles > 128))
         pl.chunk_own = (int32_t)((B.max_len + step - 1) / step * step);
     // (Own parts of many rows, whole / cut so that 256 workgroups share them: 3000 tokens of 16 heads, 192 tiles of rows, 95 / 113 us; 1000 of 40 heads on 8, 160
@@ -225,8 +226,18 @@ static AttPlan attend_plan(const griffin_kv_cache &C, const griffin_kv_batch &B,
     return pl;
 }
 
+// Rows that are planned for: a launch holds fewer than 2^32 threads, and quotients are exact while dividend times divisor is below 2^32.  With at most 2^30 keys the
+// plan's products then stay below 2^52.
+static bool attend_takes(const SeqTable &seqs, int32_t n_heads)
+{
+    const int64_t rows = (int64_t)seqs.cu[seqs.n] * n_heads;
+    return rows < 1 << 24 && rows * n_heads < (int64_t)1 << 32;
+}
+
 size_t attend_floats(const griffin_kv_cache &C, const griffin_kv_batch &B, const SeqTable &seqs, int32_t n_heads)
 {
+    if (!attend_takes(seqs, n_heads))
+        return 0;
     const AttPlan pl = attend_plan(C, B, seqs, n_heads);
     const size_t slots = (size_t)seqs.cu[seqs.n] * n_heads * (pl.chunks_prefix + pl.chunks_own);
     return pl.chunks_prefix + pl.chunks_own < 2 ? 0 : slots * (C.dim + 2);
@@ -311,12 +322,11 @@ int launch_attend(const AttendJob &job, const SeqTable &seqs, hipStream_t st)
 {
     const griffin_kv_cache &C = job.C;
     const griffin_kv_batch &B = job.B;
+    if (!attend_takes(seqs, job.n_heads))
+        return GRIFFIN_EUNSUPPORTED;
     const AttPlan pl = attend_plan(C, B, seqs, job.n_heads);
-    const int64_t wgs = (int64_t)C.kv_heads * ((int64_t)pl.tiles_prefix * pl.chunks_prefix + (int64_t)pl.tiles_own * pl.chunks_own);
-    // a launch holds fewer than 2^32 threads, and quotients are exact while dividend times divisor is below 2^32
-    const int64_t rows = (int64_t)seqs.cu[seqs.n] * job.n_heads, limit = (int64_t)1 << 32;
-    if (wgs >= 1 << 23 || rows >= 1 << 24 || wgs * C.kv_heads >= limit || wgs * std::max(pl.chunks_prefix, pl.chunks_own) >= limit ||
-        rows * job.n_heads >= limit)
+    const int64_t wgs = (int64_t)C.kv_heads * ((int64_t)pl.tiles_prefix * pl.chunks_prefix + (int64_t)pl.tiles_own * pl.chunks_own), limit = (int64_t)1 << 32;
+    if (wgs >= 1 << 23 || wgs * C.kv_heads >= limit || wgs * std::max(pl.chunks_prefix, pl.chunks_own) >= limit)
         return GRIFFIN_EUNSUPPORTED;
     AttendParams p = {};
     p.q = job.q; p.K = C.K; p.V = C.V; p.out = job.out;

@@ -1,0 +1,96 @@
+"""Sizes at the ends of what an attention takes, without a GPU: every call either launches work for all its rows and keys or is refused."""
+import json
+import os
+import subprocess
+import sys
+
+import pytest
+
+import launches
+import paper_2404_01365_amd as G
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+CHILD = """
+import ctypes, json, sys
+shim = ctypes.CDLL(sys.argv[1])
+sys.path.insert(0, sys.argv[2])
+import launches
+import paper_2404_01365_amd as G
+import test_layer_abi_cpu as T
+notes = (launches._Note * 64)()
+for c in json.load(sys.stdin):
+    seqs, new, dim, kvh, heads = c['seqs'], c['new'], c['dim'], c['kv_heads'], c['heads']
+    C = T.mk_cache(dtype=c['dtype'], kv_heads=kvh, dim=dim, page_size=65536, page_stride=kvh * 65536 * dim, head_stride=65536 * dim, token_stride=dim)
+    B = T.mk_batch(cu=[new * b for b in range(seqs + 1)], n_prefix=c['prefix'], max_len=c['max_len'], ld_pages=1 << 20)
+    print(json.dumps(c), file=sys.stderr, flush=True)
+    need = G.griffin_attention_workspace_bytes(C, B, heads)
+    shim.shim_take(notes)
+    rc = T.attend(C, B, heads=heads, ldq=dim, hsq=dim, ldo=dim, hso=dim, ws_bytes=need)
+    print(json.dumps([rc, need, [(notes[i].name.decode(), notes[i].grid[0]) for i in range(shim.shim_take(notes))]]), flush=True)
+"""
+
+
+@pytest.fixture(scope="module")
+def record(tmp_path_factory):
+    tmp = tmp_path_factory.mktemp("shim")
+    src, so = str(tmp / "shim.c"), str(tmp / "shim.so")
+    open(src, "w").write(launches._SHIM)
+    subprocess.check_call(["gcc", "-shared", "-fPIC", "-O1", src, "-o", so, "-ldl"])
+
+    def run(calls):
+        env = dict(os.environ, LD_PRELOAD=":".join(filter(None, [so, os.environ.get("LD_PRELOAD")])), PYTHONPATH=ROOT)
+        r = subprocess.run([sys.executable, "-c", CHILD, so, os.path.join(ROOT, "tests")], input=json.dumps(calls), env=env, capture_output=True,
+                           text=True, timeout=120)
+        assert r.returncode == 0, (r.returncode, r.stderr.strip().splitlines()[-1])
+        return [json.loads(line) for line in r.stdout.splitlines()]
+    return run
+
+
+def step(seqs, new, max_len, *, prefix=0, heads=32, kv_heads=8, dim=128, dtype=G.BF16):
+    return dict(seqs=seqs, new=new, max_len=max_len, prefix=prefix, heads=heads, kv_heads=kv_heads, dim=dim, dtype=dtype)
+
+
+def check(c, rc, need, got):
+    """What a call that is taken launches: workgroups for every row, and a join of as many parts as the workspace holds."""
+    assert rc == G.OK and got, (c, rc, got)
+    rows = c["seqs"] * c["new"] * c["heads"]
+    parts = need // (4 * rows * (c["dim"] + 2))
+    assert need == parts * 4 * rows * (c["dim"] + 2) and parts != 1, (c, need)
+    assert ("attend_join_kernel" in got[-1][0]) == (parts > 1), (c, got)
+    work = [g for n, g in got if "join" not in n]
+    # a workgroup takes no more than 256 rows, or eight items of 16
+    assert work and min(work) > 0 and sum(work) * 256 >= rows * max(parts - 1, 1) and sum(work) < 1 << 23, (c, got)
+
+
+EXTREME = [
+    step(1, 2 ** 17, 2 ** 23, dtype=G.F32), step(1, 2 ** 18, 2 ** 22, dtype=G.F32), step(1, 2 ** 18, 2 ** 23, dtype=G.F32),
+    step(1, 2 ** 18, 2 ** 18, prefix=2 ** 22, dtype=G.F32), step(1, 2 ** 18, 2 ** 30),
+    step(32, 1, 2 ** 30, kv_heads=32), step(64, 1, 2 ** 30, kv_heads=32), step(256, 1, 2 ** 29), step(256, 1, 2 ** 30, kv_heads=32, dtype=G.F32),
+    step(256, 20, 2 ** 30, kv_heads=32), step(256, 1, 2 ** 29, prefix=2 ** 29, kv_heads=32), step(1, 1, 1, prefix=2 ** 30 - 1),
+    step(1, 1, 2 ** 30, heads=1, kv_heads=1, dim=8), step(256, 1, 16, prefix=2 ** 30 - 16, heads=1024, kv_heads=1024, dim=64),
+    step(1, 2 ** 20 - 1, 2 ** 30, heads=8, kv_heads=8, dim=256), step(8, 2 ** 17, 2 ** 30, heads=1, kv_heads=1, dtype=G.F32),
+    step(256, 8, 2 ** 30, heads=1024, kv_heads=1024, dim=8, dtype=G.F32),
+]
+
+
+def test_long_parts_of_many_rows_are_planned_in_64_bits(record):
+    for c, (rc, need, got) in zip(EXTREME, record(EXTREME)):
+        check(c, rc, need, got)
+
+
+def test_a_query_of_sizes_that_are_not_taken_ends(record):
+    calls = [step(1, 2 ** 20, 2 ** 21, dtype=G.F32), step(1, 2 ** 20, 2 ** 30, heads=1024, kv_heads=1024), step(256, 4096, 2 ** 30, heads=64, kv_heads=64)]
+    for c, (rc, need, got) in zip(calls, record(calls)):
+        assert rc == G.EUNSUPPORTED and not got, c
+
+
+def test_a_longer_prefix_takes_no_more_workspace(record):
+    """... nor more workgroups, up to the longest there is; every step launches something."""
+    calls = [step(16, 1, 201, prefix=p) for p in (4096, 65536, 1 << 20, 1 << 25, (1 << 30) - 201)]
+    found = record(calls)
+    for c, one in zip(calls, found):
+        check(c, *one)
+    assert max(need for _, need, _ in found) <= 2 * min(need for _, need, _ in found)
+    grids = [sum(g for n, g in got if "join" not in n) for _, _, got in found]
+    assert max(grids) <= 2 * min(grids)
