@@ -399,10 +399,11 @@ int griffin_kv_append(const griffin_kv_cache *C, const griffin_kv_batch *B, cons
  * weighted sum are fp32; bf16 caches take the weights rounded to bf16 (2^-8 each) into the second product and into the sum, so that they add up to one.  Keys that a token does not
  * see do not reach its output, whatever they hold.
  *   q, out     [tokens][n_heads][dim], token and head strides (ldq, hsq; ldo, hso), multiples of 8, 16-byte aligned; out is not q
- *   n_heads    a multiple of C->kv_heads, at most 1024; tokens * n_heads^2 < 2^32
+ *   n_heads    a multiple of C->kv_heads, at most 1024; tokens * n_heads < 2^24 and tokens * n_heads^2 < 2^32, else GRIFFIN_EUNSUPPORTED (a
+ *              longer step is given as several, of fewer sequences or of a sequence's tokens one part after the other)
  *   scale      > 0 and finite
  *   workspace  griffin_attention_workspace_bytes(C, B, n_heads) bytes or more (may be 0), 256-byte aligned.  The query depends on sizes
- *              alone: kv_heads, dim, dtype, page_size, cu_seqlens, max_len, n_prefix
+ *              alone: kv_heads, dim, dtype, page_size, cu_seqlens, max_len, n_prefix.  It gives 0 for what a call refuses, too.
  */
 size_t griffin_attention_workspace_bytes(const griffin_kv_cache *C, const griffin_kv_batch *B, int32_t n_heads);
 int griffin_attention(const griffin_kv_cache *C, const griffin_kv_batch *B, const void *q, int64_t ldq, int64_t hsq, void *out, int64_t ldo,

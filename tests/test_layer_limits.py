@@ -94,3 +94,22 @@ def test_a_longer_prefix_takes_no_more_workspace(record):
     assert max(need for _, need, _ in found) <= 2 * min(need for _, need, _ in found)
     grids = [sum(g for n, g in got if "join" not in n) for _, _, got in found]
     assert max(grids) <= 2 * min(grids)
+
+
+@pytest.mark.parametrize("dtype", [G.F32, G.BF16])
+def test_rows_at_the_limits_of_an_attention(record, dtype):
+    """tokens * n_heads < 2^24 and tokens * n_heads^2 < 2^32, as the header says; a query of more gives 0."""
+    inside = [step(1, 2 ** 19 - 1, 2 ** 20, dtype=dtype), step(1, 2 ** 20, 2 ** 20, heads=15, kv_heads=15, dtype=dtype), step(256, 2047, 4096, dtype=dtype),
+              step(5, 819, 1000, heads=1024, kv_heads=1024, dim=64, dtype=dtype), step(1, 4095, 2 ** 14, heads=1024, kv_heads=8, prefix=99, dtype=dtype)]
+    outside = [step(1, 2 ** 19, 2 ** 20, dtype=dtype), step(1, 2 ** 20, 2 ** 20, heads=16, kv_heads=16, dtype=dtype), step(256, 2048, 4096, dtype=dtype),
+               step(4, 1024, 1024, heads=1024, kv_heads=1024, dim=64, dtype=dtype), step(1, 4096, 2 ** 14, heads=1024, kv_heads=8, prefix=99, dtype=dtype)]
+    found = record(inside + outside)
+    for c, one in zip(inside, found):
+        check(c, *one)
+    for c, one in zip(outside, found[len(inside):]):
+        assert one == [G.EUNSUPPORTED, 0, []], c
+
+
+def test_the_header_names_these_limits():
+    text = open(os.path.join(ROOT, "include", "griffin.h")).read()
+    assert "tokens * n_heads < 2^24 and tokens * n_heads^2 < 2^32" in text
