@@ -16,6 +16,7 @@ struct AppendParams {
     int64_t n_pos;
     int32_t n_heads, kv_heads, dim, half, pieces, page_shift, last_page, max_len, n_prefix;
     int32_t items, items_rot, items_copy, blocks;     // a token's work; of a rotated and of a copied head; workgroups a token
+    int32_t token0;                                   // this launch's first token
     int32_t each;                                     // new tokens of every sequence where they are equally many, else 0
     SeqTable seqs;
 };
@@ -65,7 +66,7 @@ __device__ __forceinline__ void store_n(void *p, int64_t i, const float (&v)[N])
 template <bool BF16, bool PAIRS, int N>
 __global__ __launch_bounds__(256) void kv_append_kernel(AppendParams p)
 {
-    const int token = blockIdx.x / p.blocks;
+    const int token = p.token0 + blockIdx.x / p.blocks;
     const int item = (blockIdx.x % p.blocks) * 256 + threadIdx.x;
     int b = 0;
     if (p.each > 0)
@@ -155,10 +156,15 @@ static int launch_form(AppendParams &p, hipStream_t st)
     p.items_copy = p.dim / 8;
     p.items = (p.n_heads + p.kv_heads) * p.items_rot + p.kv_heads * p.items_copy;
     p.blocks = (p.items + 255) / 256;
-    if ((int64_t)p.seqs.cu[p.seqs.n] * p.blocks >= 1 << 24)        // a launch holds fewer than 2^32 threads
-        return GRIFFIN_EUNSUPPORTED;
-    hipLaunchKernelGGL((kv_append_kernel<BF16, PAIRS, N>), dim3((uint32_t)p.seqs.cu[p.seqs.n] * p.blocks), dim3(256), 0, st, p);
-    return check_launch("kv_append_kernel");
+    const int32_t tokens = p.seqs.cu[p.seqs.n], most = ((1 << 24) - 1) / p.blocks;        // a launch holds fewer than 2^32 threads
+    for (p.token0 = 0; p.token0 < tokens; p.token0 += most) {
+        const int32_t now = tokens - p.token0 < most ? tokens - p.token0 : most;
+        hipLaunchKernelGGL((kv_append_kernel<BF16, PAIRS, N>), dim3((uint32_t)now * p.blocks), dim3(256), 0, st, p);
+        const int rc = check_launch("kv_append_kernel");
+        if (rc != GRIFFIN_OK)
+            return rc;
+    }
+    return GRIFFIN_OK;
 }
 
 template <bool BF16>

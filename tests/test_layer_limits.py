@@ -38,9 +38,9 @@ def record(tmp_path_factory):
     open(src, "w").write(launches._SHIM)
     subprocess.check_call(["gcc", "-shared", "-fPIC", "-O1", src, "-o", so, "-ldl"])
 
-    def run(calls):
+    def run(calls, child=CHILD):
         env = dict(os.environ, LD_PRELOAD=":".join(filter(None, [so, os.environ.get("LD_PRELOAD")])), PYTHONPATH=ROOT)
-        r = subprocess.run([sys.executable, "-c", CHILD, so, os.path.join(ROOT, "tests")], input=json.dumps(calls), env=env, capture_output=True,
+        r = subprocess.run([sys.executable, "-c", child, so, os.path.join(ROOT, "tests")], input=json.dumps(calls), env=env, capture_output=True,
                            text=True, timeout=120)
         assert r.returncode == 0, (r.returncode, r.stderr.strip().splitlines()[-1])
         return [json.loads(line) for line in r.stdout.splitlines()]
@@ -113,3 +113,33 @@ def test_rows_at_the_limits_of_an_attention(record, dtype):
 def test_the_header_names_these_limits():
     text = open(os.path.join(ROOT, "include", "griffin.h")).read()
     assert "tokens * n_heads < 2^24 and tokens * n_heads^2 < 2^32" in text
+
+
+APPEND = """
+import ctypes, json, sys
+shim = ctypes.CDLL(sys.argv[1])
+sys.path.insert(0, sys.argv[2])
+import launches
+import paper_2404_01365_amd as G
+import test_layer_abi_cpu as T
+notes = (launches._Note * 64)()
+for c in json.load(sys.stdin):
+    C = T.mk_cache(dtype=c['dtype'], kv_heads=c['kv_heads'], dim=c['dim'], page_stride=c['kv_heads'] * 16 * c['dim'], head_stride=16 * c['dim'], token_stride=c['dim'])
+    B = T.mk_batch(cu=c['cu'], max_len=1 << 20, ld_pages=1 << 16)
+    shim.shim_take(notes)
+    d = c['dim']
+    rc = T.append(C, B, ldk=d, hsk=d, ldv=d, hsv=d, ldq=d, hsq=d, ldo=d, hso=d, heads=c['heads'], rot=c['rot'], style=c['style'])
+    print(json.dumps([rc, 0, [(notes[i].name.decode(), notes[i].grid[0]) for i in range(shim.shim_take(notes))]]), flush=True)
+"""
+
+
+def test_an_append_of_any_step_is_taken(record):
+    """2^20 tokens and 1024 heads are all that limits a step: one that would need 2^24 workgroups or more is launched in parts."""
+    form = lambda cu, heads, kv_heads, dim, rot, style, dtype=G.BF16: dict(cu=cu, heads=heads, kv_heads=kv_heads, dim=dim, rot=rot, style=style, dtype=dtype)  # noqa: E731
+    calls = [form([0, 2 ** 19], 128, 128, 256, 256, 0), form([0, 2 ** 19], 1024, 1024, 256, 254, 0), form([0, 2 ** 18, 2 ** 19], 1024, 1024, 256, 2, 1, G.F32),
+             form([0, 5, 2 ** 20], 32, 8, 128, 128, 0), form([0, 1], 1024, 1024, 256, 256, 0)]
+    # items of a token: pieces of rotated heads (8, 1 and 2 features, both halves of a pair together) and of values, 256 a workgroup
+    items = [256 * 16 + 128 * 32, 2048 * (127 + 2) + 1024 * 32, 2048 * 128 + 1024 * 32, 40 * 8 + 8 * 16, 2048 * 16 + 1024 * 32]
+    for c, n, (rc, _, got) in zip(calls, items, record(calls, APPEND)):
+        assert rc == G.OK and sum(g for _, g in got) == c["cu"][-1] * -(-n // 256), (c, rc, got)
+        assert all("kv_append_kernel" in name and 0 < g < 1 << 24 for name, g in got) and len(got) < 60, got
