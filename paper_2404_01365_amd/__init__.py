@@ -350,63 +350,72 @@ def griffin_ff_prompt_out(Z, W2p, Y, *, b2=None, dtype: Optional[int] = None, wo
 
 
 # ------------------------------------------------------------------ around the block
-# These calls are a few microseconds of work for one token, so their arguments are looked at once: every tensor's shape, type and
-# strides in one helper.
-_TORCH_TYPE = {}
+# These calls are a few microseconds of work for one token, so their arguments are looked at once: every tensor's shape, type, strides
+# and card in one helper.  Descriptors of tensors on the host can be made, and are refused by the calls.
+_TORCH_TYPE, _NUMBER = {}, {}
 
 
 def _torch_type(dtype: int):
     if not _TORCH_TYPE:
         import torch
         _TORCH_TYPE.update({F32: torch.float32, BF16: torch.bfloat16})
+        _NUMBER.update({torch.float32: F32, torch.bfloat16: BF16})
     return _TORCH_TYPE[dtype]
 
 
 def _dtype_of(t) -> int:
-    for dtype in (BF16, F32):
-        if t.dtype is _torch_type(dtype):
-            return dtype
-    raise TypeError("%s is neither float32 nor bfloat16" % t.dtype)
+    if not _NUMBER:
+        _torch_type(F32)
+    dtype = _NUMBER.get(t.dtype)
+    if dtype is None:
+        raise TypeError("%s is neither float32 nor bfloat16" % t.dtype)
+    return dtype
 
 
-def _refuse(what: str, t, shape, dtype) -> None:
+def _refuse(what: str, t, shape, dtype, device=None) -> None:
     if dtype is not None and t.dtype is not dtype:
         raise TypeError("%s is %s, not %s" % (what, t.dtype, dtype))
+    if t.shape == shape and device is not None and t.get_device() != device:
+        raise ValueError("%s is on %s, other tensors of the call on %s" % (what, _place(t.get_device()), _place(device)))
     raise ValueError("%s has shape %s and strides %s; shape %s with a dense last axis is needed"
                      % (what, tuple(t.shape), t.stride(), tuple(shape)))
+
+
+def _place(device: int) -> str:
+    return "the host" if device < 0 else "cuda:%d" % device
 
 
 def _dense(width: int) -> int:
     return -(-width // 8) * 8
 
 
-def _row(what: str, t, width: int, dtype):
+def _row(what: str, t, width: int, dtype, device: int):
     """Address of a vector, or None."""
     if t is None:
         return None
-    if t.shape != (width,) or t.dtype is not dtype or (t.stride(0) != 1 and width > 1):
-        _refuse(what, t, (width,), dtype)
+    if t.shape != (width,) or t.dtype is not dtype or t.get_device() != device or (t.stride(0) != 1 and width > 1):
+        _refuse(what, t, (width,), dtype, device)
     return t.data_ptr()
 
 
-def _mat(what: str, t, shape, dtype):
+def _mat(what: str, t, shape, dtype, device: int):
     """Address and row stride of a matrix, or of None.  A single row has whatever stride it was made with: a dense one is taken."""
     if t is None:
         return None, 0
-    if t.shape != shape or t.dtype is not dtype:
-        _refuse(what, t, shape, dtype)
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != device:
+        _refuse(what, t, shape, dtype, device)
     ld, one = t.stride()
     if one != 1 and shape[1] > 1:
         _refuse(what, t, shape, dtype)
     return t.data_ptr(), ld if shape[0] > 1 else _dense(shape[1])
 
 
-def _heads(what: str, t, shape, dtype):
+def _heads(what: str, t, shape, dtype, device: int):
     """Address, token stride and head stride of [tokens][heads][features], or of None."""
     if t is None:
         return None, 0, 0
-    if t.shape != shape or t.dtype is not dtype:
-        _refuse(what, t, shape, dtype)
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != device:
+        _refuse(what, t, shape, dtype, device)
     ld, hs, one = t.stride()
     if one != 1 and shape[2] > 1:
         _refuse(what, t, shape, dtype)
@@ -420,27 +429,29 @@ def norm(w_pre=None, *, b_pre=None, w_post=None, b_post=None, eps: float, w_offs
     N = griffin_norm()
     N.d = some.shape[0] if d is None else d
     N.dtype = _dtype_of(some) if dtype is None else dtype
-    N._type = _torch_type(N.dtype)
+    N._type, N._device = _torch_type(N.dtype), None if some is None else some.get_device()
     N.kind, N.eps, N.w_offset, N.h_scale, N.y_scale = kind, eps, w_offset, h_scale, y_scale
     for name, t in (("w_pre", w_pre), ("b_pre", b_pre), ("w_post", w_post), ("b_post", b_post)):
-        setattr(N, name, _row("norm: " + name, t, N.d, N._type))
+        setattr(N, name, _row("norm: " + name, t, N.d, N._type, N._device))
     N._keep = (w_pre, b_pre, w_post, b_post)
     return N
 
 
 def griffin_norm_residual(N: griffin_norm, h, y=None, h_out=None, x=None, *, gate=None, stream=None) -> None:
     """h_out = h_scale h + y_scale gate N_post(y), x = N_pre(h_out); [rows][d] tensors, gate [d] or [rows][d]."""
-    shape, htype, dtype = (h.shape[0], N.d), h.dtype, N._type
+    shape, htype, dtype, device = (h.shape[0], N.d), h.dtype, N._type, h.get_device() if N._device is None else N._device
     if gate is None:
         at_g, ldg = None, 0
     elif gate.dim() == 2:
-        at_g, ldg = _mat("griffin_norm_residual: gate", gate, shape, dtype)
+        at_g, ldg = _mat("griffin_norm_residual: gate", gate, shape, dtype, device)
     else:
-        at_g, ldg = _row("griffin_norm_residual: gate", gate, N.d, dtype), 0
-    at_h, ldh = _mat("griffin_norm_residual: h", h, shape, htype)
-    at_y, ldy = _mat("griffin_norm_residual: y", y, shape, dtype)
-    at_o, ldo = _mat("griffin_norm_residual: h_out", h_out, shape, htype)
-    at_x, ldx = _mat("griffin_norm_residual: x", x, shape, dtype)
+        at_g, ldg = _row("griffin_norm_residual: gate", gate, N.d, dtype, device), 0
+    at_h, ldh = _mat("griffin_norm_residual: h", h, shape, htype, device)
+    at_y, ldy = _mat("griffin_norm_residual: y", y, shape, dtype, device)
+    at_o, ldo = _mat("griffin_norm_residual: h_out", h_out, shape, htype, device)
+    at_x, ldx = _mat("griffin_norm_residual: x", x, shape, dtype, device)
+    if device < 0:
+        raise ValueError("griffin_norm_residual: the tensors lie on the host")
     _check(lib.griffin_norm_residual(N, shape[0], at_h, ldh, _dtype_of(h), at_y, ldy, at_g, ldg, at_o, ldo, at_x, ldx, _stream(stream)),
            "griffin_norm_residual")
 
@@ -450,11 +461,11 @@ def kv_cache(K, V) -> griffin_kv_cache:
     [page][token][kv head][feature] is given as pool.transpose(1, 2))."""
     C = griffin_kv_cache()
     C.dtype = _dtype_of(K)
-    C._type = _torch_type(C.dtype)
+    C._type, C._device = _torch_type(C.dtype), K.get_device()
     if K.dim() != 4 or (K.stride(3) != 1 and K.shape[3] > 1):
         _refuse("kv_cache: K", K, (0, 0, 0, 0), None)
-    if V.shape != K.shape or V.dtype is not C._type or V.stride() != K.stride():
-        _refuse("kv_cache: V", V, K.shape, C._type)
+    if V.shape != K.shape or V.dtype is not C._type or V.stride() != K.stride() or V.get_device() != C._device:
+        _refuse("kv_cache: V", V, K.shape, C._type, C._device)
     C.K, C.V = _ptr(K), _ptr(V)
     C.n_pages, C.kv_heads, C.page_size, C.dim = K.shape
     C.page_stride, C.head_stride, C.token_stride = (st if n > 1 else _dense(C.dim) for n, st in zip(K.shape, K.stride()[:3]))
@@ -471,15 +482,16 @@ def kv_batch(cu_seqlens: Sequence[int], lens, pages, max_len: int, *, prefix_pag
     B.n_seqs = n = len(cu_seqlens) - 1
     arr = _cu_array(cu_seqlens)
     B.cu_seqlens = ctypes.cast(arr, _IP)
-    B.lens = _row("kv_batch: lens", lens, n, torch.int32)
-    B.pages, B.ld_pages = _mat("kv_batch: pages", pages, (n, pages.shape[-1]), torch.int32)
+    B._device = device = lens.get_device()
+    B.lens = _row("kv_batch: lens", lens, n, torch.int32, device)
+    B.pages, B.ld_pages = _mat("kv_batch: pages", pages, (n, pages.shape[-1]), torch.int32, device)
     if n == 1:
         B.ld_pages = pages.shape[1]
     if pages.shape[1] > B.ld_pages:
         raise ValueError("kv_batch: rows of pages overlap")
     B.max_len, B.n_prefix = max_len, n_prefix
     if n_prefix > 0 and prefix_pages is not None:
-        B.prefix_pages = _row("kv_batch: prefix_pages", prefix_pages, prefix_pages.numel(), torch.int32)
+        B.prefix_pages = _row("kv_batch: prefix_pages", prefix_pages, prefix_pages.numel(), torch.int32, device)
     # what a call compares with a cache's page size
     B._total, B._pages, B._max_len = int(cu_seqlens[-1]), pages.shape[1], max_len
     B._prefix_pages, B._n_prefix = 0 if prefix_pages is None else prefix_pages.numel(), n_prefix
@@ -491,27 +503,30 @@ def _check_room(where: str, C: griffin_kv_cache, B: griffin_kv_batch) -> None:
     size = C.page_size
     if B._pages * size < B._max_len or B._prefix_pages * size < B._n_prefix:
         raise ValueError("%s: fewer pages than max_len or n_prefix need" % where)
+    if C._device != B._device or C._device < 0:
+        raise ValueError("%s: the cache is on %s, lens and pages lie on %s" % (where, _place(C._device), _place(B._device)))
 
 
 def griffin_kv_append(C: griffin_kv_cache, B: griffin_kv_batch, k, v, *, q=None, q_out=None, cos=None, sin=None,
                       style: int = ROT_HALF, stream=None) -> None:
     """New keys (rotated) and values [tokens][kv_heads][dim] into their pages; queries [tokens][n_heads][dim] rotated into q_out.
     cos, sin: fp32 [positions][rot / 2], None: nothing is rotated."""
-    dtype, tokens, dim = C._type, B._total, C._dim
+    dtype, tokens, dim, device = C._type, B._total, C._dim, C._device
     kv, heads = (tokens, C._heads, dim), 0 if q is None else q.shape[1]
-    at_k, ldk, hsk = _heads("griffin_kv_append: k", k, kv, dtype)
-    at_v, ldv, hsv = _heads("griffin_kv_append: v", v, kv, dtype)
-    at_q, ldq, hsq = _heads("griffin_kv_append: q", q, (tokens, heads, dim), dtype)
-    at_o, ldo, hso = _heads("griffin_kv_append: q_out", q_out, (tokens, heads, dim), dtype)
-    _check_room("griffin_kv_append", C, B)
+    at_k, ldk, hsk = _heads("griffin_kv_append: k", k, kv, dtype, device)
+    at_v, ldv, hsv = _heads("griffin_kv_append: v", v, kv, dtype, device)
+    at_q, ldq, hsq = _heads("griffin_kv_append: q", q, (tokens, heads, dim), dtype, device)
+    at_o, ldo, hso = _heads("griffin_kv_append: q_out", q_out, (tokens, heads, dim), dtype, device)
     n_pos = half = 0
     at_c = at_s = None
     if cos is not None:
         n_pos, half = shape = cos.shape
-        at_c, ldc = _mat("griffin_kv_append: cos", cos, shape, _torch_type(F32))
-        at_s, lds = _mat("griffin_kv_append: sin", sin, shape, _torch_type(F32))
+        f32 = _torch_type(F32)
+        at_c, ldc = _mat("griffin_kv_append: cos", cos, shape, f32, device)
+        at_s, lds = _mat("griffin_kv_append: sin", sin, shape, f32, device)
         if n_pos > 1 and (ldc != half or lds != half):
             raise ValueError("griffin_kv_append: rows of cos and sin are not dense")
+    _check_room("griffin_kv_append", C, B)
     _check(lib.griffin_kv_append(C, B, at_k, ldk, hsk, at_v, ldv, hsv, at_q, ldq, hsq, at_o, ldo, hso, heads, at_c, at_s, n_pos, 2 * half,
                                  style, _stream(stream)), "griffin_kv_append")
 
@@ -522,9 +537,11 @@ def griffin_attention_workspace_bytes(C: griffin_kv_cache, B: griffin_kv_batch, 
 
 def griffin_attention(C: griffin_kv_cache, B: griffin_kv_batch, q, out, *, scale: Optional[float] = None, workspace=None, stream=None) -> None:
     """out = softmax(scale q K^T) V over the shared prefix and the sequences' own tokens; q, out [tokens][n_heads][dim]."""
-    shape, dtype = (B._total, q.shape[1], C._dim), C._type
-    at_q, ldq, hsq = _heads("griffin_attention: q", q, shape, dtype)
-    at_o, ldo, hso = _heads("griffin_attention: out", out, shape, dtype)
+    shape, dtype, device = (B._total, q.shape[1], C._dim), C._type, C._device
+    at_q, ldq, hsq = _heads("griffin_attention: q", q, shape, dtype, device)
+    at_o, ldo, hso = _heads("griffin_attention: out", out, shape, dtype, device)
+    if workspace is not None and workspace.get_device() != device:
+        _refuse("griffin_attention: workspace", workspace, workspace.shape, None, device)
     _check_room("griffin_attention", C, B)
     _check(lib.griffin_attention(C, B, at_q, ldq, hsq, at_o, ldo, hso, shape[1], shape[2] ** -0.5 if scale is None else scale, _ptr(workspace),
                                  _nbytes(workspace), _stream(stream)), "griffin_attention")
