@@ -540,7 +540,7 @@ def griffin_attention(C: griffin_kv_cache, B: griffin_kv_batch, q, out, *, scale
     shape, dtype, device = (B._total, q.shape[1], C._dim), C._type, C._device
     at_q, ldq, hsq = _heads("griffin_attention: q", q, shape, dtype, device)
     at_o, ldo, hso = _heads("griffin_attention: out", out, shape, dtype, device)
-    if workspace is not None and workspace.get_device() != device:
+    if workspace is not None and (workspace.get_device() != device or not workspace.is_contiguous()):
         _refuse("griffin_attention: workspace", workspace, workspace.shape, None, device)
     _check_room("griffin_attention", C, B)
     _check(lib.griffin_attention(C, B, at_q, ldq, hsq, at_o, ldo, hso, shape[1], shape[2] ** -0.5 if scale is None else scale, _ptr(workspace),

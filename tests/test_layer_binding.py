@@ -98,3 +98,13 @@ def test_a_residual_sum_without_norms(calls):
     with pytest.raises(ValueError):
         G.griffin_norm_residual(N, t(2, 64), t(2, 64), t(2, 64), stream=1)
     assert len(calls) == 1
+
+
+def test_a_workspace_has_no_gaps(calls):
+    """Its size is what its elements take, so one element that is repeated is not a workspace."""
+    C, B, q = cache(), batch(), OnCard(t(1, 4, 64))
+    with pytest.raises(ValueError):
+        G.griffin_attention(C, B, q, OnCard(t(1, 4, 64)), workspace=OnCard(t(1, dtype=torch.uint8).expand(4096)), stream=1)
+    with pytest.raises(ValueError):
+        G.griffin_attention(C, B, q, OnCard(t(1, 4, 64)), workspace=OnCard(t(4096, dtype=torch.uint8)[::2]), stream=1)
+    assert not calls
