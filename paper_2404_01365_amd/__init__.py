@@ -41,7 +41,10 @@ class griffin_layer(ctypes.Structure):
     ]
 
 
+# Of the three descriptors around the block, the functions that make them from tensors note beside the fields which card these lie on (None: filled in by hand,
+# any), how many tokens a step has and how many pages a table holds.
 class griffin_norm(ctypes.Structure):
+    _device = None
     _fields_ = [
         ("d", ctypes.c_int32), ("dtype", ctypes.c_int32), ("kind", ctypes.c_int32), ("eps", ctypes.c_float),
         ("w_offset", ctypes.c_float), ("h_scale", ctypes.c_float), ("y_scale", ctypes.c_float),
@@ -50,6 +53,7 @@ class griffin_norm(ctypes.Structure):
 
 
 class griffin_kv_cache(ctypes.Structure):
+    _device = None
     _fields_ = [
         ("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("dtype", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
         ("dim", ctypes.c_int32), ("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int64),
@@ -58,6 +62,7 @@ class griffin_kv_cache(ctypes.Structure):
 
 
 class griffin_kv_batch(ctypes.Structure):
+    _device = _total = _pages = _prefix_pages = None
     _fields_ = [
         ("cu_seqlens", ctypes.POINTER(ctypes.c_int32)), ("n_seqs", ctypes.c_int32), ("max_len", ctypes.c_int32),
         ("lens", ctypes.c_void_p), ("pages", ctypes.c_void_p), ("ld_pages", ctypes.c_int64),
@@ -352,24 +357,19 @@ def griffin_ff_prompt_out(Z, W2p, Y, *, b2=None, dtype: Optional[int] = None, wo
 # ------------------------------------------------------------------ around the block
 # These calls are a few microseconds of work for one token, so their arguments are looked at once: every tensor's shape, type, strides
 # and card in one helper.  Descriptors of tensors on the host can be made, and are refused by the calls.
-_TORCH_TYPE, _NUMBER = {}, {}
+class _Types(dict):
+    """PyTorch's type for a griffin_dtype and the other way round; filled when first asked, as the library works without PyTorch."""
 
-
-def _torch_type(dtype: int):
-    if not _TORCH_TYPE:
+    def __missing__(self, key):
         import torch
-        _TORCH_TYPE.update({F32: torch.float32, BF16: torch.bfloat16})
-        _NUMBER.update({torch.float32: F32, torch.bfloat16: BF16})
-    return _TORCH_TYPE[dtype]
+        if not self:
+            self.update({F32: torch.float32, BF16: torch.bfloat16, torch.float32: F32, torch.bfloat16: BF16})
+        if key not in self:
+            raise TypeError("%s is neither float32 nor bfloat16" % key)
+        return self[key]
 
 
-def _dtype_of(t) -> int:
-    if not _NUMBER:
-        _torch_type(F32)
-    dtype = _NUMBER.get(t.dtype)
-    if dtype is None:
-        raise TypeError("%s is neither float32 nor bfloat16" % t.dtype)
-    return dtype
+_TYPE = _Types()
 
 
 def _refuse(what: str, t, shape, dtype, device=None) -> None:
@@ -428,18 +428,18 @@ def norm(w_pre=None, *, b_pre=None, w_post=None, b_post=None, eps: float, w_offs
     some = w_pre if w_pre is not None else w_post
     N = griffin_norm()
     N.d = some.shape[0] if d is None else d
-    N.dtype = _dtype_of(some) if dtype is None else dtype
-    N._type, N._device = _torch_type(N.dtype), None if some is None else some.get_device()
+    N.dtype = _TYPE[some.dtype] if dtype is None else dtype
+    N._device = None if some is None else some.get_device()
     N.kind, N.eps, N.w_offset, N.h_scale, N.y_scale = kind, eps, w_offset, h_scale, y_scale
     for name, t in (("w_pre", w_pre), ("b_pre", b_pre), ("w_post", w_post), ("b_post", b_post)):
-        setattr(N, name, _row("norm: " + name, t, N.d, N._type, N._device))
+        setattr(N, name, _row("norm: " + name, t, N.d, _TYPE[N.dtype], N._device))
     N._keep = (w_pre, b_pre, w_post, b_post)
     return N
 
 
 def griffin_norm_residual(N: griffin_norm, h, y=None, h_out=None, x=None, *, gate=None, stream=None) -> None:
     """h_out = h_scale h + y_scale gate N_post(y), x = N_pre(h_out); [rows][d] tensors, gate [d] or [rows][d]."""
-    shape, htype, dtype, device = (h.shape[0], N.d), h.dtype, N._type, h.get_device() if N._device is None else N._device
+    shape, htype, dtype, device = (h.shape[0], N.d), h.dtype, _TYPE[N.dtype], h.get_device() if N._device is None else N._device
     if gate is None:
         at_g, ldg = None, 0
     elif gate.dim() == 2:
@@ -452,7 +452,7 @@ def griffin_norm_residual(N: griffin_norm, h, y=None, h_out=None, x=None, *, gat
     at_x, ldx = _mat("griffin_norm_residual: x", x, shape, dtype, device)
     if device < 0:
         raise ValueError("griffin_norm_residual: the tensors lie on the host")
-    _check(lib.griffin_norm_residual(N, shape[0], at_h, ldh, _dtype_of(h), at_y, ldy, at_g, ldg, at_o, ldo, at_x, ldx, _stream(stream)),
+    _check(lib.griffin_norm_residual(N, shape[0], at_h, ldh, _TYPE[htype], at_y, ldy, at_g, ldg, at_o, ldo, at_x, ldx, _stream(stream)),
            "griffin_norm_residual")
 
 
@@ -460,16 +460,15 @@ def kv_cache(K, V) -> griffin_kv_cache:
     """Describe pools of pages, K and V indexed [page][kv head][token][feature] with the same strides (a pool that holds
     [page][token][kv head][feature] is given as pool.transpose(1, 2))."""
     C = griffin_kv_cache()
-    C.dtype = _dtype_of(K)
-    C._type, C._device = _torch_type(C.dtype), K.get_device()
+    C.dtype = _TYPE[K.dtype]
+    C._device, dtype = K.get_device(), _TYPE[C.dtype]
     if K.dim() != 4 or (K.stride(3) != 1 and K.shape[3] > 1):
         _refuse("kv_cache: K", K, (0, 0, 0, 0), None)
-    if V.shape != K.shape or V.dtype is not C._type or V.stride() != K.stride() or V.get_device() != C._device:
-        _refuse("kv_cache: V", V, K.shape, C._type, C._device)
+    if V.shape != K.shape or V.dtype is not dtype or V.stride() != K.stride() or V.get_device() != C._device:
+        _refuse("kv_cache: V", V, K.shape, dtype, C._device)
     C.K, C.V = _ptr(K), _ptr(V)
     C.n_pages, C.kv_heads, C.page_size, C.dim = K.shape
     C.page_stride, C.head_stride, C.token_stride = (st if n > 1 else _dense(C.dim) for n, st in zip(K.shape, K.stride()[:3]))
-    C._heads, C._dim = C.kv_heads, C.dim
     C._keep = (K, V)
     return C
 
@@ -492,27 +491,33 @@ def kv_batch(cu_seqlens: Sequence[int], lens, pages, max_len: int, *, prefix_pag
     B.max_len, B.n_prefix = max_len, n_prefix
     if n_prefix > 0 and prefix_pages is not None:
         B.prefix_pages = _row("kv_batch: prefix_pages", prefix_pages, prefix_pages.numel(), torch.int32, device)
-    # what a call compares with a cache's page size
-    B._total, B._pages, B._max_len = int(cu_seqlens[-1]), pages.shape[1], max_len
-    B._prefix_pages, B._n_prefix = 0 if prefix_pages is None else prefix_pages.numel(), n_prefix
+    # what a call compares with max_len and n_prefix, by the cache's page size
+    B._total, B._pages, B._prefix_pages = arr[n], pages.shape[1], 0 if prefix_pages is None else prefix_pages.numel()
     B._keep = (arr, lens, pages, prefix_pages)
     return B
 
 
-def _check_room(where: str, C: griffin_kv_cache, B: griffin_kv_batch) -> None:
-    size = C.page_size
-    if B._pages * size < B._max_len or B._prefix_pages * size < B._n_prefix:
-        raise ValueError("%s: fewer pages than max_len or n_prefix need" % where)
-    if C._device != B._device or C._device < 0:
-        raise ValueError("%s: the cache is on %s, lens and pages lie on %s" % (where, _place(C._device), _place(B._device)))
+def _check_room(where: str, C: griffin_kv_cache, B: griffin_kv_batch, device: int) -> None:
+    """`device`: the card of the call's tensors."""
+    table = B._device
+    if table is not None:
+        size = C.page_size
+        if B._pages * size < B.max_len or B._prefix_pages * size < B.n_prefix:
+            raise ValueError("%s: fewer pages than max_len or n_prefix need" % where)
+    if device < 0 or (table != device and table is not None):
+        raise ValueError("%s: cache and tensors lie on %s, lens and pages on %s" % (where, _place(device), _place(device if table is None else table)))
 
 
 def griffin_kv_append(C: griffin_kv_cache, B: griffin_kv_batch, k, v, *, q=None, q_out=None, cos=None, sin=None,
                       style: int = ROT_HALF, stream=None) -> None:
     """New keys (rotated) and values [tokens][kv_heads][dim] into their pages; queries [tokens][n_heads][dim] rotated into q_out.
     cos, sin: fp32 [positions][rot / 2], None: nothing is rotated."""
-    dtype, tokens, dim, device = C._type, B._total, C._dim, C._device
-    kv, heads = (tokens, C._heads, dim), 0 if q is None else q.shape[1]
+    dtype, tokens, dim, device = _TYPE[C.dtype], B._total, C.dim, C._device
+    if tokens is None:
+        tokens = B.cu_seqlens[B.n_seqs]
+    if device is None:
+        device = k.get_device()
+    kv, heads = (tokens, C.kv_heads, dim), 0 if q is None else q.shape[1]
     at_k, ldk, hsk = _heads("griffin_kv_append: k", k, kv, dtype, device)
     at_v, ldv, hsv = _heads("griffin_kv_append: v", v, kv, dtype, device)
     at_q, ldq, hsq = _heads("griffin_kv_append: q", q, (tokens, heads, dim), dtype, device)
@@ -521,12 +526,12 @@ def griffin_kv_append(C: griffin_kv_cache, B: griffin_kv_batch, k, v, *, q=None,
     at_c = at_s = None
     if cos is not None:
         n_pos, half = shape = cos.shape
-        f32 = _torch_type(F32)
+        f32 = _TYPE[F32]
         at_c, ldc = _mat("griffin_kv_append: cos", cos, shape, f32, device)
         at_s, lds = _mat("griffin_kv_append: sin", sin, shape, f32, device)
         if n_pos > 1 and (ldc != half or lds != half):
             raise ValueError("griffin_kv_append: rows of cos and sin are not dense")
-    _check_room("griffin_kv_append", C, B)
+    _check_room("griffin_kv_append", C, B, device)
     _check(lib.griffin_kv_append(C, B, at_k, ldk, hsk, at_v, ldv, hsv, at_q, ldq, hsq, at_o, ldo, hso, heads, at_c, at_s, n_pos, 2 * half,
                                  style, _stream(stream)), "griffin_kv_append")
 
@@ -537,11 +542,16 @@ def griffin_attention_workspace_bytes(C: griffin_kv_cache, B: griffin_kv_batch, 
 
 def griffin_attention(C: griffin_kv_cache, B: griffin_kv_batch, q, out, *, scale: Optional[float] = None, workspace=None, stream=None) -> None:
     """out = softmax(scale q K^T) V over the shared prefix and the sequences' own tokens; q, out [tokens][n_heads][dim]."""
-    shape, dtype, device = (B._total, q.shape[1], C._dim), C._type, C._device
+    tokens, dtype, device = B._total, _TYPE[C.dtype], C._device
+    if tokens is None:
+        tokens = B.cu_seqlens[B.n_seqs]
+    if device is None:
+        device = q.get_device()
+    shape = (tokens, q.shape[1], C.dim)
     at_q, ldq, hsq = _heads("griffin_attention: q", q, shape, dtype, device)
     at_o, ldo, hso = _heads("griffin_attention: out", out, shape, dtype, device)
     if workspace is not None and (workspace.get_device() != device or not workspace.is_contiguous()):
         _refuse("griffin_attention: workspace", workspace, workspace.shape, None, device)
-    _check_room("griffin_attention", C, B)
+    _check_room("griffin_attention", C, B, device)
     _check(lib.griffin_attention(C, B, at_q, ldq, hsq, at_o, ldo, hso, shape[1], shape[2] ** -0.5 if scale is None else scale, _ptr(workspace),
                                  _nbytes(workspace), _stream(stream)), "griffin_attention")

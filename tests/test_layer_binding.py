@@ -108,3 +108,49 @@ def test_a_workspace_has_no_gaps(calls):
     with pytest.raises(ValueError):
         G.griffin_attention(C, B, q, OnCard(t(1, 4, 64)), workspace=OnCard(t(4096, dtype=torch.uint8)[::2]), stream=1)
     assert not calls
+
+
+def test_a_step_whose_bounds_were_raised_is_looked_at_as_it_is(calls):
+    """max_len and n_prefix belong to the descriptor and may change from step to step: calls compare what is in it with the tables of pages."""
+    q, ws = OnCard(t(1, 4, 64)), OnCard(t(4096, dtype=torch.uint8))
+    C, B = cache(), batch()                                      # two pages of 16 tokens, one of the prefix
+    run = (lambda: G.griffin_attention(C, B, q, OnCard(t(1, 4, 64)), workspace=ws, stream=1),
+           lambda: G.griffin_kv_append(C, B, OnCard(t(1, 2, 64)), OnCard(t(1, 2, 64)), stream=1))
+    for field, fits, too_many in (("max_len", (1, 32), 33), ("n_prefix", (0, 16), 17)):
+        for call in run:
+            for value in fits:
+                setattr(B, field, value)
+                call()
+            setattr(B, field, too_many)
+            with pytest.raises(ValueError, match="fewer pages"):
+                call()
+            setattr(B, field, fits[-1])
+    assert len(calls) == 8
+    C.dtype = G.BF16
+    for call in run:
+        with pytest.raises(TypeError):
+            call()
+
+
+def test_descriptors_that_are_filled_in_by_hand(calls):
+    """Structures as the C header has them; tensors are then held against their fields."""
+    N = G.griffin_norm()
+    N.d, N.dtype, N.kind, N.eps, N.h_scale, N.y_scale, N.w_pre = 64, G.F32, G.NORM_RMS, 1e-5, 1.0, 1.0, 0x7F0000001000
+    h = OnCard(t(2, 64))
+    G.griffin_norm_residual(N, h, OnCard(t(2, 64)), h, OnCard(t(2, 64)), stream=1)
+    with pytest.raises(ValueError):
+        G.griffin_norm_residual(N, h, OnCard(t(2, 32)), h, OnCard(t(2, 64)), stream=1)
+    with pytest.raises(TypeError):
+        G.griffin_norm_residual(N, h, OnCard(t(2, 64).bfloat16()), h, OnCard(t(2, 64)), stream=1)
+    C, B, made, step = G.griffin_kv_cache(), G.griffin_kv_batch(), cache(), batch()
+    for mine, theirs in ((C, made), (B, step)):
+        for name, _ in mine._fields_:
+            setattr(mine, name, getattr(theirs, name))
+    for c, b in ((C, B), (made, B), (C, step)):
+        G.griffin_attention(c, b, OnCard(t(1, 4, 64)), OnCard(t(1, 4, 64)), workspace=OnCard(t(4096, dtype=torch.uint8)), stream=1)
+        G.griffin_kv_append(c, b, OnCard(t(1, 2, 64)), OnCard(t(1, 2, 64)), stream=1)
+        with pytest.raises(ValueError):
+            G.griffin_attention(c, b, OnCard(t(2, 4, 64)), OnCard(t(2, 4, 64)), stream=1)
+        with pytest.raises(ValueError):
+            G.griffin_attention(c, b, OnCard(t(1, 4, 64), -1), OnCard(t(1, 4, 64), -1), stream=1)
+    assert len(calls) == 7
