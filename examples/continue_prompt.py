@@ -85,8 +85,11 @@ class Continuations:
         return x @ self.w["embed"].t()
 
     def prompt(self, tokens):
-        """The prompt through the full blocks; fills the shared pages and selects and copies the neurons that generation keeps."""
+        """The prompt through the full blocks; fills the shared pages and selects and copies the neurons that generation keeps.  What an earlier prompt
+        left, its blocks and its continuations' tokens, is dropped."""
         n = self.prompt_len
+        self.compact, self.kept = [], []
+        self.lens.zero_()
         batch = G.kv_batch([0, n], torch.zeros(1, dtype=torch.int32, device="cuda"), self.prefix_pages[None], n)
         need = G.griffin_attention_workspace_bytes(self.caches[0], batch, self.heads)
         ws_attention = torch.empty(max(need, 256), dtype=torch.uint8, device="cuda")
