@@ -39,6 +39,7 @@ def weights(layers, d, d_ff, heads, kv_heads, dim, vocab, dtype, seed=0):
 class Continuations:
     def __init__(self, w, heads, kv_heads, dim, rows, prompt_len, steps, keep=0.5):
         self.w, self.heads, self.kv_heads, self.dim, self.rows, self.prompt_len = w, heads, kv_heads, dim, rows, prompt_len
+        self.steps, self.done = steps, 0                      # that there is room for; since the prompt
         dtype, dev = w["embed"].dtype, "cuda"
         self.d, d_ff = w["embed"].shape[1], w["layers"][0]["W1"].shape[0]
         self.k = G.griffin_k_from_fraction(d_ff, keep)
@@ -90,6 +91,7 @@ class Continuations:
         n = self.prompt_len
         self.compact, self.kept = [], []
         self.lens.zero_()
+        self.done = 0
         batch = G.kv_batch([0, n], torch.zeros(1, dtype=torch.int32, device="cuda"), self.prefix_pages[None], n)
         need = G.griffin_attention_workspace_bytes(self.caches[0], batch, self.heads)
         ws_attention = torch.empty(max(need, 256), dtype=torch.uint8, device="cuda")
@@ -110,6 +112,8 @@ class Continuations:
 
     def generate(self, tokens):
         """One token of every row in, the logits of the next out."""
+        if self.done >= self.steps:
+            raise ValueError("generate: the cache holds %d tokens a row" % self.steps)
         def block(i, x):
             y = torch.empty_like(x)
             G.griffin_ff_decode(self.compact[i], x, y, self.rows, workspace=self.ws_block)
@@ -117,6 +121,7 @@ class Continuations:
 
         logits = self._stack(tokens, self.step, self.ws_attention, block)
         self.lens.add_(1)
+        self.done += 1
         return logits
 
 

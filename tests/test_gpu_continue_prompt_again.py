@@ -31,3 +31,16 @@ def test_a_second_prompt_is_continued_as_by_a_new_object(dtype):
     for i in range(3):
         assert torch.equal(run.generate(tokens(20 + i, 3)), other.generate(tokens(20 + i, 3))), i
     assert run.lens.tolist() == [3, 3, 3]
+
+
+def test_more_steps_than_there_is_room_for_are_refused():
+    """The pages and tables hold `steps` tokens of a row; one more would be seen by nobody."""
+    ex = example()
+    run = fresh(ex, ex.weights(2, 256, 512, 4, 2, 64, 128, torch.float32, seed=3), steps=2)
+    for _ in range(2):
+        run.prompt(tokens(1, 70))
+        for i in range(2):
+            run.generate(tokens(i, 3))
+        with pytest.raises(ValueError):
+            run.generate(tokens(2, 3))
+        assert run.lens.tolist() == [2, 2, 2]
