@@ -209,14 +209,21 @@ static AttPlan attend_plan(const griffin_kv_cache &C, const griffin_kv_batch &B,
     if (pl.lone || (pl.tile_own && C.kv_heads * tiles > 128))
         pl.chunk_own = (int32_t)((B.max_len + step - 1) / step * step);
     // (Own parts of many rows, whole / cut so that 256 workgroups share them: 3000 tokens of 16 heads, 192 tiles of rows, 95 / 113 us; 1000 of 40 heads on 8, 160
-    // tiles, 42 / 61; 2048 of 16 on 8, 128 tiles, 71 / 63.  3400 tokens of 32 on 8 behind a prefix of 300: 79 with the prefix ahead, 141 joined.)
-    // Own items take the prefix ahead of their own keys where that costs less than to join two parts: prompts that fill the chip (their rows' sums would go
-    // through memory in fp32), and parts so few and short that a step of twice as many wavefronts is cheaper than a second launch (some 5 us), prefix or not.  At
-    // two steps it is no longer: 513 keys of 32 heads of 128 take 10.4 us in one launch of 32 workgroups, 10.3 cut into chunks and joined (caches cold: 15.9,
-    // 14.4).
+    // tiles, 42 / 61; 2048 of 16 on 8, 128 tiles, 71 / 63.  Behind own tokens in the cache: 1100 of 32 on 8 behind 1000 73 / 106, behind 30000 898 / 1043;
+    // three times 400 behind 8000, 8000 and 0 251 / 216.)
+    // Own items take the prefix ahead of their own keys where that costs less than to join two parts: parts so few and short that a step of twice as many
+    // wavefronts is cheaper than a second launch (some 5 us), prefix or not, and own tiles that fill the chip (their rows' sums would go through memory in fp32),
+    // unless the prefix is read much oftener for it: tiles of a sequence's rows are not full, those of the prefix are.  With three of four tiles' rows there it pays
+    // whatever the prefix, else up to 16384 keys more in all.  (Prefix ahead / joined, 32 heads on 8.  3400 tokens behind 300, 2048, 8192 and 32768: 131 / 193, 224 /
+    // 277, 578 / 601, 1996 / 1975; four times 300 behind 32768: 970 / 1168.  20 times 20 behind 300, 1024, 2048, 32768: 18 / 32, 33 / 41, 55 / 47, 698 / 295; 47 times a
+    // token and one of 17 tokens behind 64, 300, 1024, 32768: 37 / 39, 48 / 40, 75 / 45, 1366 / 84.  64 heads on 8, 17 times 9 behind 300, 1024, 8192: 19 / 28, 33 / 32, 181 /
+    // 71.)
+    // At two steps one launch is no longer cheaper: 513 keys of 32 heads of 128 take 10.4 us in one launch of 32 workgroups, 10.3 cut into chunks and joined (caches
+    // cold: 15.9, 14.4).
     const int64_t all = (int64_t)B.n_prefix + B.max_len, items = C.kv_heads * tiles;
     pl.few = longest <= 32 && !pl.tile_prefix && items <= 512 && all <= ATT_FEW_WAVES / ATT_WAVES * step && C.dim <= 128;
-    pl.ahead = B.n_prefix > 0 && (pl.few || (pl.tile_own && items > 128));
+    const int64_t beyond = tiles - (rows + pl.rows_own - 1) / pl.rows_own;      // tiles more than all rows in a row would take
+    pl.ahead = B.n_prefix > 0 && (pl.few || (pl.tile_own && items > 128 && (4 * beyond <= tiles || beyond * B.n_prefix <= 16384)));
     if (pl.ahead)
         pl.tiles_prefix = 0;
     if (pl.ahead || pl.few)
