@@ -11,8 +11,8 @@
 // Long key ranges are cut into chunks for as many workgroups as fill the chip; each leaves its rows' o, m and l, and a second kernel joins them.
 //
 // Bound by bytes while few rows share a key, with the latency of a step's loads on top: a part that one step covers is two launches' latency, 4.5 us of it the join's.
-// Measured: 64 continuations of 1024 shared tokens and 1 to 120 of their own, 40 heads of 128, 102 MB, 32 us warm = 3.2 TB/s; 8 sequences behind 30000 shared
-// keys of 8 heads of 128, four query heads each, 125 MB, 31 us = 4.0 TB/s; one row of 513 keys of 32 heads 8.3 us and the join.
+// Measured: 64 continuations of 1024 shared tokens and 1 to 120 of their own, 40 heads of 128, 102 MB, 32 us warm = 3.2 TB/s, caches cold 57 us = 1.8; 8 sequences behind 30000 shared
+// keys of 8 heads of 128, four query heads each, 125 MB, 31 us = 4.0 TB/s, cold 64 = 2.0; one row of 513 keys of 32 heads 8.3 us and the join.
 // The products of 16 rows a key are a twentieth of the matrix cores' rate when keys arrive at a copy's, of 64 rows a quarter: the arrangement is made for loads.
 #include <algorithm>
 
@@ -166,8 +166,8 @@ static AttPlan attend_plan(const griffin_kv_cache &C, const griffin_kv_batch &B,
     for (int b = 0; b < seqs.n; ++b)
         longest = std::max(longest, (int64_t)(seqs.cu[b + 1] - seqs.cu[b]) * group);
     // Own parts of more than 64 rows go through LDS, 256 rows a workgroup.  (16 sequences of 2000 keys, us there / here: 48 rows 38 / 36, 80 rows 42 / 58, 128 rows
-    // 46 / 62; one sequence of 64 rows 16.6 / 14.2.)  So does a prefix of more rows than that where there is enough to multiply: its workgroups are fewer and
-    // larger.  (8 kv heads of 128, us there / here: 80 rows of 8192 keys 24.4 / 21.2, of 32768 40.0 / 43.0; 192 rows of 2048 keys 28 / 18, of 8192 34.8 / 31.4, of 32768
+    // 46 / 62; one sequence of 64 rows 16.6 / 14.2.)  So does a prefix beside them, in their launch (2 x 100 tokens of 32 heads on 8 behind 300 shared 23 / 35, behind 2048 31 / 51; 5 x 1 and
+    // 33 tokens 15 / 22, 19 / 27), and one of more rows than that where there is enough to multiply: its workgroups are fewer and larger.  (8 kv heads of 128, us there / here: 80 rows of 8192 keys 24.4 / 21.2, of 32768 40.0 / 43.0; 192 rows of 2048 keys 28 / 18, of 8192 34.8 / 31.4, of 32768
     // 55 / 81; 448 rows of 2048 keys 34 / 26, of 8192 43 / 54.)
     pl.tile_own = bf16 && longest > 64;
     pl.tile_prefix = bf16 && (pl.tile_own || (rows > 64 && (double)rows * B.n_prefix * C.kv_heads * C.dim >= 0x1p31));

@@ -9,11 +9,11 @@
 // The rows' reference maximum moves only when scores outgrow it by more than 8 (base 2): weights then are up to 2^8 (their rounding to bf16 is
 // relative, and cancels from what a dominating one weighs, as the sum is of rounded ones, too), and o is scaled a few times instead of at every step.
 //
-// Bound by the matrix cores and what stands between the two products.  A step of 64 keys for 32 rows of 128 features is 64 products of 16x16x32 a wavefront, two
-// wavefronts a SIMD: at 8.25 ns each when they are fed without a pause 1.06 us, and some 0.5 us of weights (exponentials, maxima, rounding) for both.  The two
-// hardly overlap, though they come from different wavefronts: two products and eight multiply-adds of two wavefronts take 49 ns together, 33 and 20 apart.  So
-// 1.56 us is what this arrangement can reach, and 2.03 is measured: prompts of 2048, 1117, 604 and 381 tokens of 32 heads on 8, 49 GFLOP that are seen, 74 us = 660
-// TFLOP/s of them.  Tried and slower on these, 88 to 117 us: the halves of a workgroup in turn, one multiplying while the other forms weights; products and
+// Bound by the matrix cores and what stands between the two products.  A step of 64 keys for 32 rows of 128 features is 64 products of 16x16x32 a wavefront and four with ones
+// for the sums, two wavefronts a SIMD: at 8.25 ns each when they are fed without a pause 1.12 us, and some 0.5 us of weights (exponentials, maxima, rounding) for
+// both.  The two hardly overlap, though they come from different wavefronts: two products and eight multiply-adds of two wavefronts take 49 ns together, 33 and 20
+// apart.  So some 1.6 us is what this arrangement can reach, and 2.0 is measured; what the rest goes into is not known.  Prompts of 2048, 1117, 604 and 381 tokens of 32
+// heads on 8, 49 GFLOP that are seen: 74 us = 660 TFLOP/s of them, caches cold 89.  Tried and slower on these, 88 to 117 us: the halves of a workgroup in turn, one multiplying while the other forms weights; products and
 // weights of neighbouring tiles interleaved within a wavefront; four wavefronts of 64 rows.
 #include "attend_rows.h"
 

@@ -1,8 +1,8 @@
 // A step's keys and values into their pages, the keys rotated on the way, the queries rotated beside them (griffin_kv_append).
 // Moves every element once: bytes bound for prompts, one launch's latency for a token a sequence.  A thread takes eight features where their alignment
 // lets it, with both halves of the rotated pairs, so that nothing is read twice; sines and cosines come from tables (they are a program's own, and exact for any
-// position).  Measured: 4150 packed prompt tokens of 32 heads, q, k and v, 205 MB, 45 us = 4.5 TB/s (a large copy reaches 4.9); a token for each of 16
-// sequences 4.7 us, a launch's own.
+// position).  Measured: 4150 packed prompt tokens of 32 heads, q, k and v, 205 MB, 45 us = 4.5 TB/s, caches cold 54 us = 3.8 (a large copy reaches
+// 4.9); a token for each of 16 sequences 4.7 us, a launch's own.
 #include "layer.h"
 
 namespace griffin {

@@ -1,8 +1,8 @@
 // Norms around a block (griffin_norm_residual): u = N(y) behind it, h' = h_scale h + y_scale gate u, x = N(h') before the next.
 // Bound by bytes from some hundreds of rows on (h, y and a gate are read once, h' and x written once), by latency below.  A row is
 // held in registers from its first load to its last store, so the second norm's statistics cost no second pass.
-// Measured: 1024 rows of 5120, fp32 stream, 63 MB, 13.1 us = 4.8 TB/s (a large copy reaches 4.9); 8191 rows of 4096 with a gate
-// for each, layer norm, 335 MB, 61 us = 5.5 TB/s, part of it cached; one row of 4096 4.1 us, a launch's own.
+// Measured (a large copy reaches 4.9 TB/s; pass behind pass, part of the rows in the caches / caches cold): 1024 rows of 5120, fp32 stream, 63 MB, 13.1 us =
+// 4.8 TB/s / 20.6 us = 3.1; 8191 rows of 4096 with a gate for each, layer norm, 335 MB, 61 us = 5.5 TB/s / 84 us = 4.0; one row of 4096 4.1 us, a launch's own.
 #include "layer.h"
 
 namespace griffin {
