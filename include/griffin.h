@@ -412,6 +412,84 @@ int griffin_attention(const griffin_kv_cache *C, const griffin_kv_batch *B, cons
                       int64_t hso, int32_t n_heads, float scale, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * ---------------------------------------------------------------- a cache in 4 bits
+ * Keys and values of long contexts in a little more than a quarter of the bytes of bf16: quantised as they are written, read back, and attended to as
+ * they lie.  The features of a token and kv head go in groups of `group`, the last of fewer where dim is no multiple.  With lo and hi the least and
+ * greatest of a group's values (cut to +-32768), a scale s = (hi - lo) / 15 and a middle m = lo + 8 s, each rounded to fp32 and then to fp16, a value x is held as the code
+ * c = round((x - m) / s), ties to even, in -8 .. 7 (0 where s is 0), and stands for m + s c, rounded to fp16: at most s / 2 off, and what the roundings of
+ * s, m and the value to fp16 add (2^-11 of the group's largest value in all).  A group with a value that is infinite or NaN has s = NaN and m = 0, and stands
+ * for NaN throughout.  s, m and c are taken from x in 64 bits, rotated in 64 bits: none hangs on the rounding of a sum.
+ */
+typedef struct {
+    void *K, *V;             /* device, 16-byte aligned; n_pages pages of griffin_kv_q4_page_bytes() bytes each.  A page holds, for every kv head in turn,
+                                page_size rows of 16 ceil(dim / 32) bytes, c + 8 of feature f in the low (f even) or high half of byte f / 2, then
+                                page_size rows of ceil(dim / group) pairs (s, m) of fp16 */
+    int32_t dtype;           /* griffin_dtype of keys, values, queries and outputs outside the cache */
+    int32_t kv_heads;
+    int32_t dim;             /* features of a head: a multiple of 8, at most 256 */
+    int32_t page_size;       /* tokens in a page: a power of two from 16 to 65536 */
+    int32_t group;           /* features that share a scale: 32 or 64 */
+    int64_t n_pages;         /* pages in the pools, at most 2^31 - 1 */
+} griffin_kv_cache_q4;
+
+/* bytes of a page of K, or of V; 0 for sizes that the calls refuse */
+size_t griffin_kv_q4_page_bytes(int32_t kv_heads, int32_t dim, int32_t page_size, int32_t group);
+
+/*
+ * griffin_kv_append into such a cache: same batch, same rotation, same places; the keys are rotated in 64 bits and quantised from there, the queries
+ * are rotated in fp32 and rounded once.  Arguments as there.  Nothing of the pools is written but the rows and pairs of the step's tokens.
+ */
+int griffin_kv_append_q4(const griffin_kv_cache_q4 *C, const griffin_kv_batch *B, const void *k, int64_t ldk, int64_t hsk, const void *v,
+                         int64_t ldv, int64_t hsv, const void *q, int64_t ldq, int64_t hsq, void *q_out, int64_t ldo, int64_t hso,
+                         int32_t n_heads, const float *cos, const float *sin, int64_t n_pos, int32_t rot, int32_t style, void *stream);
+
+/*
+ * What a cache's tokens stand for: rows cu[b] + i of k and v receive token lens[b] + i of sequence b's own pages, i < cu[b+1] - cu[b], which are
+ * the rows that griffin_kv_append_q4 writes with the same batch.  (A prefix is read as one sequence of length 0 whose pages are the prefix's.)  Rows whose
+ * token lies at max_len or beyond are left as they were.
+ *   k, v       [tokens][kv_heads][dim], token and head strides in elements (ldk, hsk; ldv, hsv), multiples of 8, C->dtype; one of them may be NULL
+ */
+int griffin_kv_read_q4(const griffin_kv_cache_q4 *C, const griffin_kv_batch *B, void *k, int64_t ldk, int64_t hsk, void *v, int64_t ldv, int64_t hsv,
+                       void *stream);
+
+/*
+ * griffin_attention over such a cache: out[t][h] = sum_k softmax_k(scale * q[t][h] . K_k) V_k with the values that the cache stands for.  Products are of
+ * fp16 on the matrix cores, exact for keys and values; a row of queries is scaled by a power of two and rounded to fp16 (bf16 caches: features down to 2^-24 of
+ * the largest keep all their bits, below that 2^-32 of it is lost at most; fp32: to a pair of fp16, 2^-23), weights are cut to fp16 (2^-10; fp32: to a pair, 2^-20) for product
+ * and sum alike.  Scores, maximum, sum and weighted sum are fp32.  Tokens that a row does not see do not reach its output, whatever their places hold; those that
+ * it sees hold what griffin_kv_append_q4 has written.
+ * Arguments, limits and workspace as in griffin_attention.
+ */
+size_t griffin_attention_q4_workspace_bytes(const griffin_kv_cache_q4 *C, const griffin_kv_batch *B, int32_t n_heads);
+int griffin_attention_q4(const griffin_kv_cache_q4 *C, const griffin_kv_batch *B, const void *q, int64_t ldq, int64_t hsq, void *out, int64_t ldo,
+                         int64_t hso, int32_t n_heads, float scale, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Verification of drafted tokens.  A block pruned by its prompt drafts a few tokens a sequence, the full block computes the probabilities behind each of
+ * them in one step (several new tokens a sequence in griffin_kv_append and griffin_attention), and as many are kept as leave the target's distribution
+ * as it is: sequence b owns rows cu[b] .. cu[b+1]-1, row r holding the target's probabilities p_r of the token behind it, and d_r = drafted[r] is what the
+ * draft put there, by its probabilities q_r (the last row has none: its entry is not looked at).  From the first row on, d_r is kept if
+ * accept_u[r] * q_r(d_r) < p_r(d_r), product and comparison in fp32.  At the first row that is not kept a token is drawn with weights max(p_r - q_r, 0) (fp32),
+ * at the last row, if all were kept, with weights p_r: the first token j with w_0 + .. + w_j > draw_u[b] * (w_0 + .. + w_(V-1)), sums in 64 bits.  Weights
+ * that are all zero are replaced by p_r, and where those are, too, or the product is no less than the sum, the last token of the vocabulary comes out.
+ *   p               [cu[n_seqs]][vocab] fp32, row stride ldp; >= 0 and finite
+ *   draft_p         [cu[n_seqs]][vocab] fp32, row stride ldq, a sequence's last row is not read; NULL: every draft had all its probability on d_r
+ *   drafted         [cu[n_seqs]] int32; one outside 0 .. vocab-1 is no draft: its sequence ends there, with weights p_r
+ *   cu_seqlens_host HOST int32 [n_seqs+1] as in griffin_prefill_select; n_seqs <= GRIFFIN_MAX_SEQS.  Read before the call returns.
+ *   accept_u        [cu[n_seqs]] fp32, draw_u [n_seqs] fp32: random numbers, uniform in [0, 1) (the library draws none)
+ *   tokens_out      [cu[n_seqs]] int32: row by row the kept tokens of a sequence, the drawn one, then -1.  Not `drafted` itself.
+ *   accepted        [n_seqs] int32: tokens kept
+ *   lens, lens_out  [n_seqs] int32 or both NULL: lens_out[b] = lens[b] + accepted[b] + 1, the tokens in the cache that count (rows of the step that are dropped
+ *                   are overwritten by the next one).  lens_out may be lens itself.
+ *   workspace       griffin_verify_workspace_bytes(n_seqs, vocab) bytes, 256-byte aligned (may be 0)
+ * A sequence without rows keeps 0 and its length.  vocab <= 2^24; rows of any alignment.
+ */
+size_t griffin_verify_workspace_bytes(int32_t n_seqs, int32_t vocab);
+int griffin_verify_drafts(const float *p, int64_t ldp, const float *draft_p, int64_t ldq, const int32_t *drafted, const int32_t *cu_seqlens_host,
+                          int32_t n_seqs, int32_t vocab, const float *accept_u, const float *draw_u, int32_t *tokens_out, int32_t *accepted,
+                          const int32_t *lens, int32_t *lens_out, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * MEASUREMENT ONLY -- not part of the method's interface and the one entry point that keeps state
  * between calls (a one-shot, per-thread note of three event handles; every other entry point is
  * stateless, apart from addresses and kernel attributes looked up once per device).  It exists so that a benchmark can time the kernels of a decode call on the stream

@@ -41,7 +41,7 @@ class griffin_layer(ctypes.Structure):
     ]
 
 
-# Of the three descriptors around the block, the functions that make them from tensors note beside the fields which card these lie on (None: filled in by hand,
+# Of the four descriptors around the block, the functions that make them from tensors note beside the fields which card these lie on (None: filled in by hand,
 # any), how many tokens a step has and how many pages a table holds.
 class griffin_norm(ctypes.Structure):
     _device = None
@@ -58,6 +58,14 @@ class griffin_kv_cache(ctypes.Structure):
         ("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("dtype", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
         ("dim", ctypes.c_int32), ("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int64),
         ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64),
+    ]
+
+
+class griffin_kv_cache_q4(ctypes.Structure):
+    _device = None
+    _fields_ = [
+        ("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("dtype", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+        ("dim", ctypes.c_int32), ("page_size", ctypes.c_int32), ("group", ctypes.c_int32), ("n_pages", ctypes.c_int64),
     ]
 
 
@@ -88,6 +96,7 @@ _vp, _i32, _i64, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c
 _LP = ctypes.POINTER(griffin_layer)
 _IP = ctypes.POINTER(ctypes.c_int32)
 _NP, _CP, _BP = (ctypes.POINTER(t) for t in (griffin_norm, griffin_kv_cache, griffin_kv_batch))
+_QP = ctypes.POINTER(griffin_kv_cache_q4)
 _f32 = ctypes.c_float
 
 _SIGS = {
@@ -122,6 +131,13 @@ _SIGS = {
     "griffin_kv_append": (ctypes.c_int, [_CP, _BP] + 4 * [_vp, _i64, _i64] + [_i32, _vp, _vp, _i64, _i32, _i32, _vp]),
     "griffin_attention_workspace_bytes": (_sz, [_CP, _BP, _i32]),
     "griffin_attention": (ctypes.c_int, [_CP, _BP, _vp, _i64, _i64, _vp, _i64, _i64, _i32, _f32, _vp, _sz, _vp]),
+    "griffin_kv_q4_page_bytes": (_sz, [_i32, _i32, _i32, _i32]),
+    "griffin_kv_append_q4": (ctypes.c_int, [_QP, _BP] + 4 * [_vp, _i64, _i64] + [_i32, _vp, _vp, _i64, _i32, _i32, _vp]),
+    "griffin_kv_read_q4": (ctypes.c_int, [_QP, _BP] + 2 * [_vp, _i64, _i64] + [_vp]),
+    "griffin_attention_q4_workspace_bytes": (_sz, [_QP, _BP, _i32]),
+    "griffin_attention_q4": (ctypes.c_int, [_QP, _BP, _vp, _i64, _i64, _vp, _i64, _i64, _i32, _f32, _vp, _sz, _vp]),
+    "griffin_verify_workspace_bytes": (_sz, [_i32, _i32]),
+    "griffin_verify_drafts": (ctypes.c_int, [_vp, _i64, _vp, _i64, _vp, _IP, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
 }
 for _name, (_res, _args) in _SIGS.items():
     _fn = getattr(lib, _name)
@@ -508,50 +524,145 @@ def _check_room(where: str, C: griffin_kv_cache, B: griffin_kv_batch, device: in
         raise ValueError("%s: cache and tensors lie on %s, lens and pages on %s" % (where, _place(device), _place(device if table is None else table)))
 
 
-def griffin_kv_append(C: griffin_kv_cache, B: griffin_kv_batch, k, v, *, q=None, q_out=None, cos=None, sin=None,
-                      style: int = ROT_HALF, stream=None) -> None:
-    """New keys (rotated) and values [tokens][kv_heads][dim] into their pages; queries [tokens][n_heads][dim] rotated into q_out.
-    cos, sin: fp32 [positions][rot / 2], None: nothing is rotated."""
+def _append(where: str, call, C, B: griffin_kv_batch, k, v, q, q_out, cos, sin, style: int, stream) -> None:
     dtype, tokens, dim, device = _TYPE[C.dtype], B._total, C.dim, C._device
     if tokens is None:
         tokens = B.cu_seqlens[B.n_seqs]
     if device is None:
         device = k.get_device()
     kv, heads = (tokens, C.kv_heads, dim), 0 if q is None else q.shape[1]
-    at_k, ldk, hsk = _heads("griffin_kv_append: k", k, kv, dtype, device)
-    at_v, ldv, hsv = _heads("griffin_kv_append: v", v, kv, dtype, device)
-    at_q, ldq, hsq = _heads("griffin_kv_append: q", q, (tokens, heads, dim), dtype, device)
-    at_o, ldo, hso = _heads("griffin_kv_append: q_out", q_out, (tokens, heads, dim), dtype, device)
+    at_k, ldk, hsk = _heads(where + ": k", k, kv, dtype, device)
+    at_v, ldv, hsv = _heads(where + ": v", v, kv, dtype, device)
+    at_q, ldq, hsq = _heads(where + ": q", q, (tokens, heads, dim), dtype, device)
+    at_o, ldo, hso = _heads(where + ": q_out", q_out, (tokens, heads, dim), dtype, device)
     n_pos = half = 0
     at_c = at_s = None
     if cos is not None:
         n_pos, half = shape = cos.shape
         f32 = _TYPE[F32]
-        at_c, ldc = _mat("griffin_kv_append: cos", cos, shape, f32, device)
-        at_s, lds = _mat("griffin_kv_append: sin", sin, shape, f32, device)
+        at_c, ldc = _mat(where + ": cos", cos, shape, f32, device)
+        at_s, lds = _mat(where + ": sin", sin, shape, f32, device)
         if n_pos > 1 and (ldc != half or lds != half):
-            raise ValueError("griffin_kv_append: rows of cos and sin are not dense")
-    _check_room("griffin_kv_append", C, B, device)
-    _check(lib.griffin_kv_append(C, B, at_k, ldk, hsk, at_v, ldv, hsv, at_q, ldq, hsq, at_o, ldo, hso, heads, at_c, at_s, n_pos, 2 * half,
-                                 style, _stream(stream)), "griffin_kv_append")
+            raise ValueError("%s: rows of cos and sin are not dense" % where)
+    _check_room(where, C, B, device)
+    _check(call(C, B, at_k, ldk, hsk, at_v, ldv, hsv, at_q, ldq, hsq, at_o, ldo, hso, heads, at_c, at_s, n_pos, 2 * half, style, _stream(stream)), where)
+
+
+def griffin_kv_append(C: griffin_kv_cache, B: griffin_kv_batch, k, v, *, q=None, q_out=None, cos=None, sin=None,
+                      style: int = ROT_HALF, stream=None) -> None:
+    """New keys (rotated) and values [tokens][kv_heads][dim] into their pages; queries [tokens][n_heads][dim] rotated into q_out.
+    cos, sin: fp32 [positions][rot / 2], None: nothing is rotated."""
+    _append("griffin_kv_append", lib.griffin_kv_append, C, B, k, v, q, q_out, cos, sin, style, stream)
 
 
 def griffin_attention_workspace_bytes(C: griffin_kv_cache, B: griffin_kv_batch, n_heads: int) -> int:
     return int(lib.griffin_attention_workspace_bytes(ctypes.byref(C), ctypes.byref(B), n_heads))
 
 
-def griffin_attention(C: griffin_kv_cache, B: griffin_kv_batch, q, out, *, scale: Optional[float] = None, workspace=None, stream=None) -> None:
-    """out = softmax(scale q K^T) V over the shared prefix and the sequences' own tokens; q, out [tokens][n_heads][dim]."""
+def _attention(where: str, call, C, B: griffin_kv_batch, q, out, scale, workspace, stream) -> None:
     tokens, dtype, device = B._total, _TYPE[C.dtype], C._device
     if tokens is None:
         tokens = B.cu_seqlens[B.n_seqs]
     if device is None:
         device = q.get_device()
     shape = (tokens, q.shape[1], C.dim)
-    at_q, ldq, hsq = _heads("griffin_attention: q", q, shape, dtype, device)
-    at_o, ldo, hso = _heads("griffin_attention: out", out, shape, dtype, device)
+    at_q, ldq, hsq = _heads(where + ": q", q, shape, dtype, device)
+    at_o, ldo, hso = _heads(where + ": out", out, shape, dtype, device)
     if workspace is not None and (workspace.get_device() != device or not workspace.is_contiguous()):
-        _refuse("griffin_attention: workspace", workspace, workspace.shape, None, device)
-    _check_room("griffin_attention", C, B, device)
-    _check(lib.griffin_attention(C, B, at_q, ldq, hsq, at_o, ldo, hso, shape[1], shape[2] ** -0.5 if scale is None else scale, _ptr(workspace),
-                                 _nbytes(workspace), _stream(stream)), "griffin_attention")
+        _refuse(where + ": workspace", workspace, workspace.shape, None, device)
+    _check_room(where, C, B, device)
+    _check(call(C, B, at_q, ldq, hsq, at_o, ldo, hso, shape[1], shape[2] ** -0.5 if scale is None else scale, _ptr(workspace), _nbytes(workspace),
+                _stream(stream)), where)
+
+
+def griffin_attention(C: griffin_kv_cache, B: griffin_kv_batch, q, out, *, scale: Optional[float] = None, workspace=None, stream=None) -> None:
+    """out = softmax(scale q K^T) V over the shared prefix and the sequences' own tokens; q, out [tokens][n_heads][dim]."""
+    _attention("griffin_attention", lib.griffin_attention, C, B, q, out, scale, workspace, stream)
+
+
+# ------------------------------------------------------------------ a cache in 4 bits
+def griffin_kv_q4_page_bytes(kv_heads: int, dim: int, page_size: int, group: int = 32) -> int:
+    return int(lib.griffin_kv_q4_page_bytes(kv_heads, dim, page_size, group))
+
+
+def kv_cache_q4(K, V, *, kv_heads: int, dim: int, page_size: int, group: int = 32, dtype) -> griffin_kv_cache_q4:
+    """Describe pools of pages in 4 bits, K and V uint8 [page][griffin_kv_q4_page_bytes(..)]; dtype: PyTorch's type of keys, values, queries and
+    outputs outside the cache."""
+    import torch
+    C = griffin_kv_cache_q4()
+    C.dtype, C.kv_heads, C.dim, C.page_size, C.group = _TYPE[dtype], kv_heads, dim, page_size, group
+    size = griffin_kv_q4_page_bytes(kv_heads, dim, page_size, group)
+    if size == 0:
+        raise ValueError("kv_cache_q4: no pages of %d heads of %d features, %d tokens, groups of %d" % (kv_heads, dim, page_size, group))
+    C._device, shape = K.get_device(), (K.shape[0], size)
+    for what, t in (("K", K), ("V", V)):
+        if t.shape != shape or t.dtype is not torch.uint8 or t.get_device() != C._device or not t.is_contiguous():
+            _refuse("kv_cache_q4: " + what, t, shape, torch.uint8, C._device)
+    C.K, C.V, C.n_pages = K.data_ptr(), V.data_ptr(), shape[0]
+    C._keep = (K, V)
+    return C
+
+
+def griffin_kv_append_q4(C: griffin_kv_cache_q4, B: griffin_kv_batch, k, v, *, q=None, q_out=None, cos=None, sin=None,
+                         style: int = ROT_HALF, stream=None) -> None:
+    """griffin_kv_append into a cache in 4 bits."""
+    _append("griffin_kv_append_q4", lib.griffin_kv_append_q4, C, B, k, v, q, q_out, cos, sin, style, stream)
+
+
+def griffin_kv_read_q4(C: griffin_kv_cache_q4, B: griffin_kv_batch, k=None, v=None, *, stream=None) -> None:
+    """What the tokens that griffin_kv_append_q4 writes with this batch stand for, into k and v [tokens][kv_heads][dim] (or one of them)."""
+    tokens, device = B._total, C._device
+    if tokens is None:
+        tokens = B.cu_seqlens[B.n_seqs]
+    if device is None:
+        device = (v if k is None else k).get_device()
+    shape, dtype = (tokens, C.kv_heads, C.dim), _TYPE[C.dtype]
+    at_k, ldk, hsk = _heads("griffin_kv_read_q4: k", k, shape, dtype, device)
+    at_v, ldv, hsv = _heads("griffin_kv_read_q4: v", v, shape, dtype, device)
+    _check_room("griffin_kv_read_q4", C, B, device)
+    _check(lib.griffin_kv_read_q4(C, B, at_k, ldk, hsk, at_v, ldv, hsv, _stream(stream)), "griffin_kv_read_q4")
+
+
+def griffin_attention_q4_workspace_bytes(C: griffin_kv_cache_q4, B: griffin_kv_batch, n_heads: int) -> int:
+    return int(lib.griffin_attention_q4_workspace_bytes(ctypes.byref(C), ctypes.byref(B), n_heads))
+
+
+def griffin_attention_q4(C: griffin_kv_cache_q4, B: griffin_kv_batch, q, out, *, scale: Optional[float] = None, workspace=None, stream=None) -> None:
+    """griffin_attention over a cache in 4 bits."""
+    _attention("griffin_attention_q4", lib.griffin_attention_q4, C, B, q, out, scale, workspace, stream)
+
+
+# ------------------------------------------------------------------ drafted tokens
+def cu_seqlens(values: Sequence[int]):
+    """A batch's host array of sequence ends, made once where a call is made many times."""
+    return _cu_array(values)
+
+
+def griffin_verify_workspace_bytes(n_seqs: int, vocab: int) -> int:
+    return int(lib.griffin_verify_workspace_bytes(n_seqs, vocab))
+
+
+def griffin_verify_drafts(cu_seqlens, p, drafted, accept_u, draw_u, tokens_out, accepted, *, draft_p=None, lens=None, lens_out=None, workspace=None,
+                          stream=None) -> None:
+    """Keeps the drafted tokens that the target's probabilities p [rows][vocab] allow and draws the one behind them.  cu_seqlens: a sequence of ints or
+    what cu_seqlens() made of one; drafted, accept_u, tokens_out [rows]; draw_u, accepted, lens, lens_out [sequences]."""
+    import torch
+    cu = cu_seqlens if isinstance(cu_seqlens, ctypes.Array) else _cu_array(cu_seqlens)
+    n, device, where = len(cu) - 1, p.get_device(), "griffin_verify_drafts: "
+    if n < 1:
+        raise ValueError(where + "no sequences")
+    rows, f32, i32 = cu[n], torch.float32, torch.int32
+    shape = (rows, p.shape[-1])
+    at_p, ldp = _mat(where + "p", p, shape, f32, device)
+    at_q, ldq = _mat(where + "draft_p", draft_p, shape, f32, device)
+    if rows == 1:
+        ldp = ldq = shape[1]
+    addresses = [_row(where + name, t, width, dtype, device) for name, t, width, dtype in (
+        ("drafted", drafted, rows, i32), ("accept_u", accept_u, rows, f32), ("draw_u", draw_u, n, f32), ("tokens_out", tokens_out, rows, i32),
+        ("accepted", accepted, n, i32), ("lens", lens, n, i32), ("lens_out", lens_out, n, i32))]
+    if workspace is not None and (workspace.get_device() != device or not workspace.is_contiguous()):
+        _refuse(where + "workspace", workspace, workspace.shape, None, device)
+    if device < 0:
+        raise ValueError(where + "the tensors lie on the host")
+    _check(lib.griffin_verify_drafts(at_p, ldp, at_q, ldq, addresses[0], cu, n, shape[1], *addresses[1:], _ptr(workspace), _nbytes(workspace),
+                                     _stream(stream)), "griffin_verify_drafts")

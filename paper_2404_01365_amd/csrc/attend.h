@@ -196,6 +196,24 @@ __device__ __forceinline__ bool att_own_item(const AttendParams &p, int32_t id, 
     return it.begin < it.end;                                 // else no row reads this chunk's partial sums
 }
 
+struct AttPlan {
+    bool tile_prefix, tile_own;         // many rows: attend_tile.hip
+    bool lone;                          // own items of a few rows go a wavefront each
+    bool beside;                        // ... in the launch of the prefix's tiles
+    bool ahead, few;                    // own items take the prefix, too; all of it in one launch of attend_few_kernel
+    int ntp, nto;                       // else tiles of 16 rows that a wavefront takes
+    int32_t rows_prefix, rows_own;      // rows of a workgroup
+    int32_t chunk_prefix, chunk_own, chunks_prefix, chunks_own, tiles_prefix, tiles_own;
+};
+
+// Host side that both kinds of cache share (attend.hip).  What a plan's sizes have to fit into; the fields of p that come from a batch and a plan; the join of a
+// row's chunks.
+bool attend_takes(const SeqTable &seqs, int32_t n_heads);
+bool att_launch_fits(const AttPlan &pl, int32_t kv_heads);
+void att_set_up(AttendParams &p, const AttPlan &pl, const griffin_kv_batch &B, const SeqTable &seqs, int32_t n_heads, int32_t kv_heads, int32_t dim,
+                int32_t page_size, int64_t n_pages, float scale, float *ws);
+int launch_attend_join(const AttendParams &p, bool bf16, hipStream_t st);
+
 // launches the `wgs` workgroups of p on tiles of att_tile_rows(dim) rows, and behind them p.items_own own items of 16 rows, a workgroup each or, `each`, a
 // wavefront each (dim <= 128); bf16 only
 int launch_attend_tiles(const AttendParams &p, int32_t wgs, bool each, hipStream_t st);

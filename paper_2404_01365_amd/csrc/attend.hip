@@ -144,16 +144,6 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendParams p)
 }
 
 // ------------------------------------------------------------------ host side
-struct AttPlan {
-    bool tile_prefix, tile_own;         // many rows: attend_tile.hip
-    bool lone;                          // own items of a few rows go a wavefront each
-    bool beside;                        // ... in the launch of the prefix's tiles
-    bool ahead, few;                    // own items take the prefix, too; all of it in one launch of attend_few_kernel
-    int ntp, nto;                       // else tiles of 16 rows that a wavefront takes
-    int32_t rows_prefix, rows_own;      // rows of a workgroup
-    int32_t chunk_prefix, chunk_own, chunks_prefix, chunks_own, tiles_prefix, tiles_own;
-};
-
 static AttPlan attend_plan(const griffin_kv_cache &C, const griffin_kv_batch &B, const SeqTable &seqs, int32_t n_heads)
 {
     AttPlan pl;
@@ -235,7 +225,7 @@ static AttPlan attend_plan(const griffin_kv_cache &C, const griffin_kv_batch &B,
 
 // Rows that are planned for: a launch holds fewer than 2^32 threads, and quotients are exact while dividend times divisor is below 2^32.  With at most 2^30 keys the
 // plan's products then stay below 2^52.
-static bool attend_takes(const SeqTable &seqs, int32_t n_heads)
+bool attend_takes(const SeqTable &seqs, int32_t n_heads)
 {
     const int64_t rows = (int64_t)seqs.cu[seqs.n] * n_heads;
     return rows < 1 << 24 && rows * n_heads < (int64_t)1 << 32;
@@ -283,6 +273,28 @@ static int launch_rows(const AttendParams &p, int ntp, int nto, hipStream_t st)
 }
 
 template <bool BF16, int DB>
+static int go_join(const AttendParams &p, hipStream_t st)
+{
+    const int64_t rows = (int64_t)p.tokens * p.n_heads;
+    // A wavefront has 16 chunks of features on their way at a time (dim 128); of few rows with more, four share a row.  (One / four wavefronts a row, the whole call:
+    // 256 rows of 60 chunks 34.4 / 31.4 us, 512 of 33 21.3 / 20.1, 32 of 32 10.3 / 9.9; 512 of 18 13.2 / 14.1, 1280 of 33 28.7 / 31.6.)
+    if (rows <= 512 && p.chunks_prefix + p.chunks_own > 24)
+        hipLaunchKernelGGL((attend_join_kernel<BF16, DB, 4>), dim3((uint32_t)rows), dim3(256), 0, st, p);
+    else
+        hipLaunchKernelGGL((attend_join_kernel<BF16, DB, 1>), dim3((uint32_t)((rows + 3) / 4)), dim3(256), 0, st, p);
+    return check_launch("attend_join_kernel");
+}
+
+int launch_attend_join(const AttendParams &p, bool bf16, hipStream_t st)
+{
+    if (p.dim <= 64)
+        return bf16 ? go_join<true, 64>(p, st) : go_join<false, 64>(p, st);
+    if (p.dim <= 128)
+        return bf16 ? go_join<true, 128>(p, st) : go_join<false, 128>(p, st);
+    return bf16 ? go_join<true, 256>(p, st) : go_join<false, 256>(p, st);
+}
+
+template <bool BF16, int DB>
 static int attend_typed(AttendParams &p, const AttPlan &pl, hipStream_t st)
 {
     int rc = GRIFFIN_OK;
@@ -303,16 +315,7 @@ static int attend_typed(AttendParams &p, const AttPlan &pl, hipStream_t st)
                 return p.dim == DB ? go_few<BF16, DB, true>(p, st) : go_few<BF16, DB, false>(p, st);
         rc = pl.lone ? launch_rows<BF16, DB, true>(p, ntp, nto, st) : launch_rows<BF16, DB, false>(p, ntp, nto, st);
     }
-    if (rc != GRIFFIN_OK || !p.part)
-        return rc;
-    const int64_t rows = (int64_t)p.seqs.cu[p.seqs.n] * p.n_heads;
-    // A wavefront has 16 chunks of features on their way at a time (dim 128); of few rows with more, four share a row.  (One / four wavefronts a row, the whole call:
-    // 256 rows of 60 chunks 34.4 / 31.4 us, 512 of 33 21.3 / 20.1, 32 of 32 10.3 / 9.9; 512 of 18 13.2 / 14.1, 1280 of 33 28.7 / 31.6.)
-    if (rows <= 512 && pl.chunks_prefix + pl.chunks_own > 24)
-        hipLaunchKernelGGL((attend_join_kernel<BF16, DB, 4>), dim3((uint32_t)rows), dim3(256), 0, st, p);
-    else
-        hipLaunchKernelGGL((attend_join_kernel<BF16, DB, 1>), dim3((uint32_t)((rows + 3) / 4)), dim3(256), 0, st, p);
-    return check_launch("attend_join_kernel");
+    return rc == GRIFFIN_OK && p.part ? launch_attend_join(p, BF16, st) : rc;
 }
 
 template <bool BF16>
@@ -325,31 +328,25 @@ static int attend_width(AttendParams &p, const AttPlan &pl, hipStream_t st)
 
 static AttDiv divide_by(int32_t d) { return {(uint32_t)d, d > 1 ? (uint32_t)(((uint64_t)1 << 32) / d) + 1 : 0}; }
 
-int launch_attend(const AttendJob &job, const SeqTable &seqs, hipStream_t st)
+bool att_launch_fits(const AttPlan &pl, int32_t kv_heads)
 {
-    const griffin_kv_cache &C = job.C;
-    const griffin_kv_batch &B = job.B;
-    if (!attend_takes(seqs, job.n_heads))
-        return GRIFFIN_EUNSUPPORTED;
-    const AttPlan pl = attend_plan(C, B, seqs, job.n_heads);
-    const int64_t wgs = (int64_t)C.kv_heads * ((int64_t)pl.tiles_prefix * pl.chunks_prefix + (int64_t)pl.tiles_own * pl.chunks_own), limit = (int64_t)1 << 32;
-    if (wgs >= 1 << 23 || wgs * C.kv_heads >= limit || wgs * std::max(pl.chunks_prefix, pl.chunks_own) >= limit)
-        return GRIFFIN_EUNSUPPORTED;
-    AttendParams p = {};
-    p.q = job.q; p.K = C.K; p.V = C.V; p.out = job.out;
+    const int64_t wgs = (int64_t)kv_heads * ((int64_t)pl.tiles_prefix * pl.chunks_prefix + (int64_t)pl.tiles_own * pl.chunks_own), limit = (int64_t)1 << 32;
+    return wgs < 1 << 23 && wgs * kv_heads < limit && wgs * std::max(pl.chunks_prefix, pl.chunks_own) < limit;
+}
+
+void att_set_up(AttendParams &p, const AttPlan &pl, const griffin_kv_batch &B, const SeqTable &seqs, int32_t n_heads, int32_t kv_heads, int32_t dim,
+                int32_t page_size, int64_t n_pages, float scale, float *ws)
+{
     if (pl.chunks_prefix + pl.chunks_own > 1) {
-        p.part = job.ws;
-        p.part_ml = (float2 *)(job.ws + (size_t)seqs.cu[seqs.n] * job.n_heads * (pl.chunks_prefix + pl.chunks_own) * C.dim);
+        p.part = ws;
+        p.part_ml = (float2 *)(ws + (size_t)seqs.cu[seqs.n] * n_heads * (pl.chunks_prefix + pl.chunks_own) * dim);
     }
-    p.lens = B.lens; p.pages = B.pages; p.prefix_pages = B.prefix_pages;
-    p.ldq = job.ldq; p.hsq = job.hsq; p.ldo = job.ldo; p.hso = job.hso;
-    p.page_stride = C.page_stride; p.head_stride = C.head_stride; p.token_stride = C.token_stride; p.ld_pages = B.ld_pages;
-    p.page_stride16 = (uint32_t)(C.page_stride / (C.dtype == GRIFFIN_BF16 ? 8 : 4));
-    p.scale2 = job.scale * 1.4426950408889634f;
+    p.lens = B.lens; p.pages = B.pages; p.prefix_pages = B.prefix_pages; p.ld_pages = B.ld_pages;
+    p.scale2 = scale * 1.4426950408889634f;
     p.tokens = seqs.cu[seqs.n];
-    p.n_heads = job.n_heads; p.kv_heads = C.kv_heads; p.group = job.n_heads / C.kv_heads; p.dim = C.dim;
-    p.page_shift = __builtin_ctz(C.page_size);
-    p.last_page = (int32_t)(C.n_pages - 1);
+    p.n_heads = n_heads; p.kv_heads = kv_heads; p.group = n_heads / kv_heads; p.dim = dim;
+    p.page_shift = __builtin_ctz(page_size);
+    p.last_page = (int32_t)(n_pages - 1);
     p.max_len = B.max_len; p.n_prefix = B.n_prefix;
     p.ahead = pl.ahead ? B.n_prefix : 0;
     p.chunk_prefix = pl.chunk_prefix; p.chunk_own = pl.chunk_own;
@@ -371,6 +368,22 @@ int launch_attend(const AttendJob &job, const SeqTable &seqs, hipStream_t st)
     p.tiles_each = divide_by((int64_t)pl.tiles_own * tiles_each < (int64_t)1 << 32 ? tiles_each : 0);
     p.by_heads = divide_by(p.n_heads); p.by_kv_heads = divide_by(p.kv_heads); p.by_group = divide_by(p.group);
     p.by_chunks_prefix = divide_by(pl.chunks_prefix > 0 ? pl.chunks_prefix : 1); p.by_chunks_own = divide_by(pl.chunks_own);
+}
+
+int launch_attend(const AttendJob &job, const SeqTable &seqs, hipStream_t st)
+{
+    const griffin_kv_cache &C = job.C;
+    if (!attend_takes(seqs, job.n_heads))
+        return GRIFFIN_EUNSUPPORTED;
+    const AttPlan pl = attend_plan(C, job.B, seqs, job.n_heads);
+    if (!att_launch_fits(pl, C.kv_heads))
+        return GRIFFIN_EUNSUPPORTED;
+    AttendParams p = {};
+    p.q = job.q; p.K = C.K; p.V = C.V; p.out = job.out;
+    p.ldq = job.ldq; p.hsq = job.hsq; p.ldo = job.ldo; p.hso = job.hso;
+    p.page_stride = C.page_stride; p.head_stride = C.head_stride; p.token_stride = C.token_stride;
+    p.page_stride16 = (uint32_t)(C.page_stride / (C.dtype == GRIFFIN_BF16 ? 8 : 4));
+    att_set_up(p, pl, job.B, seqs, job.n_heads, C.kv_heads, C.dim, C.page_size, C.n_pages, job.scale, job.ws);
     return C.dtype == GRIFFIN_BF16 ? attend_width<true>(p, pl, st) : attend_width<false>(p, pl, st);
 }
 

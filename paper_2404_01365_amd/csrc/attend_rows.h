@@ -320,6 +320,90 @@ __device__ __forceinline__ void att_store8(const AttendParams &p, const AttendIt
     }
 }
 
+// What the wavefronts have summed comes together and is stored.  S says which features a lane's sums are: element i of o[n][c S::VD + e] is feature
+// (c 16 + 4 (lane >> 4) + i) S::VD + e of row 16 n + (lane & 15).
+template <bool BF16, class S, int DB, bool FULL, int NT, int WAVES>
+__device__ __forceinline__ void att_finish(const AttendParams &p, float *lds, const AttendItem &it, const float (&m_of)[NT], const float (&sum)[NT],
+                                           const att_f32x4 (&o)[NT][S::NO])
+{
+    const int32_t rows = it.rows, first = it.first;
+    const int lane = threadIdx.x & 63, wave = WAVES == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if constexpr (WAVES == 1) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int32_t row = first + 16 * n + (lane & 15);
+            if (row >= rows)
+                continue;
+            if (p.part && lane < 16)
+                p.part_ml[att_slot(p, it, row)] = make_float2(m_of[n], sum[n]);
+#pragma unroll
+            for (int c = 0; c < S::NC; ++c)
+#pragma unroll
+                for (int h = 0; h < S::VD / 2; ++h) {      // eight consecutive features of the lane's run of 4 VD
+                    float x[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        x[j] = o[n][c * S::VD + (h * 8 + j) % S::VD][(h * 8 + j) / S::VD];
+                    att_store8<BF16, FULL>(p, it, row, (c * 16 + (lane >> 4) * 4) * S::VD + h * 8, x, sum[n]);
+                }
+        }
+        return;
+    }
+    // The wavefronts' sums come together in LDS, up to 128 features of 16 rows at a time; then every thread joins and stores eight features of a row.
+    constexpr int W = DB < 128 ? DB : 128, CW = W / (16 * S::VD);          // features, and runs of a lane, at a time
+    float *ml = lds + WAVES * 16 * (W + 4);
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int here = rows - first - 16 * n < 16 ? rows - first - 16 * n : 16;
+        if (here <= 0)
+            break;
+#pragma unroll
+        for (int part = 0; part < S::NC / CW; ++part) {
+            if (n > 0 || part > 0)
+                __syncthreads();
+            if ((lane & 15) < here) {
+                float *mine = lds + (wave * 16 + (lane & 15)) * (W + 4);
+#pragma unroll
+                for (int c = 0; c < CW; ++c)
+#pragma unroll
+                    for (int h = 0; h < S::VD; ++h) {      // four consecutive features
+                        att_f32x4 x;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            x[j] = o[n][(part * CW + c) * S::VD + (h * 4 + j) % S::VD][(h * 4 + j) / S::VD];
+                        *(att_f32x4 *)(mine + (c * 16 + (lane >> 4) * 4) * S::VD + h * 4) = x;
+                    }
+                if (lane < 16) {
+                    ml[wave * 32 + lane] = m_of[n];
+                    ml[wave * 32 + 16 + lane] = sum[n];
+                }
+            }
+            __syncthreads();
+            for (int item = threadIdx.x; item < here * (W / 8); item += WAVES * 64) {
+                const int at = item / (W / 8), d = item % (W / 8) * 8;
+                float m = -INFINITY, l = 0, x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w)
+                    m = fmaxf(m, ml[w * 32 + at]);
+                const float base = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) {
+                    const float f = __builtin_amdgcn_exp2f(ml[w * 32 + at] - base);
+                    const float *from = lds + (w * 16 + at) * (W + 4) + d;
+                    l += ml[w * 32 + 16 + at] * f;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        x[j] += from[j] * f;
+                }
+                const int32_t row = first + 16 * n + at;
+                if (p.part && part == 0 && d == 0)
+                    p.part_ml[att_slot(p, it, row)] = make_float2(m, l);
+                att_store8<BF16, FULL>(p, it, row, part * W + d, x, l);
+            }
+        }
+    }
+}
+
 // The item's rows first .. first + 16 NT - 1, by the WAVES wavefronts of a workgroup (in turn, a step each) or by one alone
 template <bool BF16, int DB, bool FULL, int NT, int WAVES>
 __device__ __forceinline__ void attend_rows(const AttendParams &p, float *lds, const AttendItem &it)
@@ -400,80 +484,7 @@ __device__ __forceinline__ void attend_rows(const AttendParams &p, float *lds, c
 #pragma unroll
     for (int n = 0; n < NT; ++n)
         sum[n] = BF16 ? r.l[n][0] : lane_groups_sum(r.l[n][0]);
-    if constexpr (WAVES == 1) {
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const int32_t row = first + 16 * n + (lane & 15);
-            if (row >= rows)
-                continue;
-            if (p.part && lane < 16)
-                p.part_ml[att_slot(p, it, row)] = make_float2(r.m[n], sum[n]);
-#pragma unroll
-            for (int c = 0; c < S::NC; ++c)
-#pragma unroll
-                for (int h = 0; h < S::VD / 2; ++h) {      // eight consecutive features of the lane's run of 4 VD
-                    float x[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        x[j] = r.o[n][c * S::VD + (h * 8 + j) % S::VD][(h * 8 + j) / S::VD];
-                    att_store8<BF16, FULL>(p, it, row, (c * 16 + (lane >> 4) * 4) * S::VD + h * 8, x, sum[n]);
-                }
-        }
-        return;
-    }
-    // The wavefronts' sums come together in LDS, up to 128 features of 16 rows at a time; then every thread joins and stores eight features of a row.
-    constexpr int W = DB < 128 ? DB : 128, CW = W / (16 * S::VD);          // features, and runs of a lane, at a time
-    float *ml = lds + WAVES * 16 * (W + 4);
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const int here = rows - first - 16 * n < 16 ? rows - first - 16 * n : 16;
-        if (here <= 0)
-            break;
-#pragma unroll
-        for (int part = 0; part < S::NC / CW; ++part) {
-            if (n > 0 || part > 0)
-                __syncthreads();
-            if ((lane & 15) < here) {
-                float *mine = lds + (wave * 16 + (lane & 15)) * (W + 4);
-#pragma unroll
-                for (int c = 0; c < CW; ++c)
-#pragma unroll
-                    for (int h = 0; h < S::VD; ++h) {      // four consecutive features
-                        att_f32x4 x;
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            x[j] = r.o[n][(part * CW + c) * S::VD + (h * 4 + j) % S::VD][(h * 4 + j) / S::VD];
-                        *(att_f32x4 *)(mine + (c * 16 + (lane >> 4) * 4) * S::VD + h * 4) = x;
-                    }
-                if (lane < 16) {
-                    ml[wave * 32 + lane] = r.m[n];
-                    ml[wave * 32 + 16 + lane] = sum[n];
-                }
-            }
-            __syncthreads();
-            for (int item = threadIdx.x; item < here * (W / 8); item += WAVES * 64) {
-                const int at = item / (W / 8), d = item % (W / 8) * 8;
-                float m = -INFINITY, l = 0, x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-#pragma unroll
-                for (int w = 0; w < WAVES; ++w)
-                    m = fmaxf(m, ml[w * 32 + at]);
-                const float base = m == -INFINITY ? 0.0f : m;
-#pragma unroll
-                for (int w = 0; w < WAVES; ++w) {
-                    const float f = __builtin_amdgcn_exp2f(ml[w * 32 + at] - base);
-                    const float *from = lds + (w * 16 + at) * (W + 4) + d;
-                    l += ml[w * 32 + 16 + at] * f;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        x[j] += from[j] * f;
-                }
-                const int32_t row = first + 16 * n + at;
-                if (p.part && part == 0 && d == 0)
-                    p.part_ml[att_slot(p, it, row)] = make_float2(m, l);
-                att_store8<BF16, FULL>(p, it, row, part * W + d, x, l);
-            }
-        }
-    }
+    att_finish<BF16, S, DB, FULL, NT, WAVES>(p, lds, it, r.m, sum, r.o);
 }
 
 // floats of LDS in which WAVES wavefronts' sums come together

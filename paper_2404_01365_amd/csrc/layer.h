@@ -40,6 +40,53 @@ struct AttendJob {
 size_t attend_floats(const griffin_kv_cache &C, const griffin_kv_batch &B, const SeqTable &seqs, int32_t n_heads);
 int launch_attend(const AttendJob &job, const SeqTable &seqs, hipStream_t st);
 
+struct AppendQ4Job {
+    griffin_kv_cache_q4 C;
+    griffin_kv_batch B;
+    const void *k, *v, *q;
+    void *q_out;
+    int64_t ldk, hsk, ldv, hsv, ldq, hsq, ldo, hso;
+    int32_t n_heads, rot, style;
+    const float *cos, *sin;
+    int64_t n_pos;
+};
+int launch_kv_append_q4(const AppendQ4Job &job, const SeqTable &seqs, hipStream_t st);
+
+struct ReadQ4Job {
+    griffin_kv_cache_q4 C;
+    griffin_kv_batch B;
+    void *k, *v;
+    int64_t ldk, hsk, ldv, hsv;
+};
+int launch_kv_read_q4(const ReadQ4Job &job, const SeqTable &seqs, hipStream_t st);
+
+struct AttendQ4Job {
+    griffin_kv_cache_q4 C;
+    griffin_kv_batch B;
+    const void *q;
+    void *out;
+    int64_t ldq, hsq, ldo, hso;
+    int32_t n_heads;
+    float scale;
+    float *ws;
+};
+size_t attend_q4_floats(const griffin_kv_cache_q4 &C, const griffin_kv_batch &B, const SeqTable &seqs, int32_t n_heads);
+int launch_attend_q4(const AttendQ4Job &job, const SeqTable &seqs, hipStream_t st);
+
+struct VerifyJob {
+    const float *p, *q;
+    int64_t ldp, ldq;
+    const int32_t *drafted;
+    int32_t vocab;
+    const float *accept_u, *draw_u;
+    int32_t *tokens_out, *accepted;
+    const int32_t *lens;
+    int32_t *lens_out;
+    double *ws;
+};
+size_t verify_bytes(int32_t n_seqs, int32_t vocab);
+int launch_verify(const VerifyJob &job, const SeqTable &seqs, hipStream_t st);
+
 // The page of a token, clamped into the pools; `at` is the same for the whole wavefront.
 __device__ __forceinline__ int64_t page_of(const int32_t *pages, int32_t at, int32_t last_page)
 {
