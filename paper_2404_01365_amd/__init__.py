@@ -388,6 +388,11 @@ class _Types(dict):
 _TYPE = _Types()
 
 
+def _int32():
+    import torch
+    return torch.int32
+
+
 def _refuse(what: str, t, shape, dtype, device=None) -> None:
     if dtype is not None and t.dtype is not dtype:
         raise TypeError("%s is %s, not %s" % (what, t.dtype, dtype))
@@ -646,23 +651,26 @@ def griffin_verify_drafts(cu_seqlens, p, drafted, accept_u, draw_u, tokens_out, 
                           stream=None) -> None:
     """Keeps the drafted tokens that the target's probabilities p [rows][vocab] allow and draws the one behind them.  cu_seqlens: a sequence of ints or
     what cu_seqlens() made of one; drafted, accept_u, tokens_out [rows]; draw_u, accepted, lens, lens_out [sequences]."""
-    import torch
     cu = cu_seqlens if isinstance(cu_seqlens, ctypes.Array) else _cu_array(cu_seqlens)
-    n, device, where = len(cu) - 1, p.get_device(), "griffin_verify_drafts: "
+    n, device, f32, i32 = len(cu) - 1, p.get_device(), _TYPE[F32], _int32()
     if n < 1:
-        raise ValueError(where + "no sequences")
-    rows, f32, i32 = cu[n], torch.float32, torch.int32
+        raise ValueError("griffin_verify_drafts: no sequences")
+    rows = cu[n]
     shape = (rows, p.shape[-1])
-    at_p, ldp = _mat(where + "p", p, shape, f32, device)
-    at_q, ldq = _mat(where + "draft_p", draft_p, shape, f32, device)
+    at_p, ldp = _mat("griffin_verify_drafts: p", p, shape, f32, device)
+    at_q, ldq = _mat("griffin_verify_drafts: draft_p", draft_p, shape, f32, device)
     if rows == 1:
         ldp = ldq = shape[1]
-    addresses = [_row(where + name, t, width, dtype, device) for name, t, width, dtype in (
-        ("drafted", drafted, rows, i32), ("accept_u", accept_u, rows, f32), ("draw_u", draw_u, n, f32), ("tokens_out", tokens_out, rows, i32),
-        ("accepted", accepted, n, i32), ("lens", lens, n, i32), ("lens_out", lens_out, n, i32))]
+    at_d = _row("griffin_verify_drafts: drafted", drafted, rows, i32, device)
+    at_u = _row("griffin_verify_drafts: accept_u", accept_u, rows, f32, device)
+    at_r = _row("griffin_verify_drafts: draw_u", draw_u, n, f32, device)
+    at_t = _row("griffin_verify_drafts: tokens_out", tokens_out, rows, i32, device)
+    at_a = _row("griffin_verify_drafts: accepted", accepted, n, i32, device)
+    at_l = _row("griffin_verify_drafts: lens", lens, n, i32, device)
+    at_o = _row("griffin_verify_drafts: lens_out", lens_out, n, i32, device)
     if workspace is not None and (workspace.get_device() != device or not workspace.is_contiguous()):
-        _refuse(where + "workspace", workspace, workspace.shape, None, device)
+        _refuse("griffin_verify_drafts: workspace", workspace, workspace.shape, None, device)
     if device < 0:
-        raise ValueError(where + "the tensors lie on the host")
-    _check(lib.griffin_verify_drafts(at_p, ldp, at_q, ldq, addresses[0], cu, n, shape[1], *addresses[1:], _ptr(workspace), _nbytes(workspace),
+        raise ValueError("griffin_verify_drafts: the tensors lie on the host")
+    _check(lib.griffin_verify_drafts(at_p, ldp, at_q, ldq, at_d, cu, n, shape[1], at_u, at_r, at_t, at_a, at_l, at_o, _ptr(workspace), _nbytes(workspace),
                                      _stream(stream)), "griffin_verify_drafts")

@@ -1,0 +1,468 @@
+// A few rows of an attention over a cache in 4 bits, by the wavefronts of a workgroup or by one alone (attend_q4.hip, and attend_q4_tile.hip for own parts beside a
+// prefix that it takes).  The mathematics and the arrangement of scores and sums are those of attend_rows.h; a wavefront streams codes from memory into its registers, makes
+// fp16 values of them there, and feeds the matrix cores with those.
+//
+// A code is four bits of a word: masked into the last bits of an fp16 it is an integer, and one multiply-add makes the value of it, two at a time.
+// Keys (A operand of S^T = K Q^T): lane & 15 is the key, lane >> 4 says which quarter of its features the lane holds; the order of a word's features in the
+// operand is that in which they come out, and queries are laid out alike.  Values (A operand of O^T = V^T P^T): the lane holds the codes of eight keys for VD
+// neighbouring features; a byte permute puts two keys' codes of two features side by side, so the turn from rows of features to pairs of keys costs nothing beside
+// the unpacking.
+#pragma once
+
+#include "attend_rows.h"
+#include "q4.h"
+
+namespace griffin {
+
+typedef __attribute__((ext_vector_type(8))) _Float16 q4_f16x8;
+typedef __attribute__((ext_vector_type(2))) uint32_t q4_u32x2;
+
+__device__ __forceinline__ att_f32x4 q4_mfma(att_u32x4 a, att_u32x4 b, att_f32x4 c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(q4_f16x8, a), __builtin_bit_cast(q4_f16x8, b), c, 0, 0, 0);
+}
+
+constexpr uint32_t Q4_ONES = 0x3C003C00u;    // two fp16
+
+struct AttendQ4Params : AttendParams {
+    Q4Shape s;
+};
+
+template <bool F32, int DB>
+struct Q4Att {
+    static constexpr int KS = 32;                          // keys a step, two tiles of 16
+    static constexpr int NW = DB / 32;                     // words of codes of a key that a lane holds (four lanes share a key)
+    static constexpr int NP = NW > 4 ? 2 : 1;              // ... and (scale, middle) pairs
+    static constexpr int VD = DB / 16 < 8 ? DB / 16 : 8;   // consecutive features of a value that a lane holds
+    static constexpr int NC = DB / (16 * VD);              // ... and how many such runs, 16 VD apart
+    static constexpr int NO = NC * VD;                     // tiles of 16 features of the output
+    static constexpr int NF = F32 ? 2 : 1;                 // fp16 that make up a query's feature, and a weight
+};
+
+template <bool F32, int DB, int NT>
+struct Q4Rows {
+    using S = Q4Att<F32, DB>;
+    att_u32x4 q[NT][S::NF][S::NW];
+    int32_t end[NT];             // keys from here on are not seen by the lane's row
+    float scale2[NT];            // of the row's scores: the queries were scaled by a power of two
+    float m[NT];
+    att_f32x4 l[NT];             // the row's sum in every element
+    att_f32x4 o[NT][S::NO];
+};
+
+template <bool F32, int DB>
+struct Q4Keys {
+    using S = Q4Att<F32, DB>;
+    uint32_t k[2][S::NW], pair[2][S::NP];
+};
+template <bool F32, int DB>
+struct Q4Vals {
+    using S = Q4Att<F32, DB>;
+    uint32_t v[8][S::NC], pair[8][S::NC];
+};
+
+// A tile of 16 keys: its page's number, and where it lies.  A page's part of a kv head is one buffer, so that a load takes all that is the same for the wavefront from
+// scalar registers and 32 bits from the lane: with addresses of 64 bits every load of four bytes has an addition before it.
+struct Q4Tile {
+    int32_t page;
+    __amdgpu_buffer_rsrc_t K, V;
+    int32_t codes, pairs;
+
+    __device__ __forceinline__ void look_up(const AttendQ4Params &p, const AttendItem &it, int32_t key) { page = att_look_up(p, it, key); }
+
+    __device__ __forceinline__ void set(const AttendQ4Params &p, const AttendItem &it, int32_t key)
+    {
+        key -= key < it.hole_end ? 0 : it.hole_end;
+        const uint32_t in = key & ((1 << p.page_shift) - 1);
+        const uint64_t block = ((uint64_t)att_page(__builtin_amdgcn_readfirstlane(page), p.last_page) * (uint32_t)p.kv_heads + it.hk) * p.s.head_bytes;
+        K = __builtin_amdgcn_make_buffer_rsrc((char *)p.K + block, 0, p.s.head_bytes, 0x00020000);
+        V = __builtin_amdgcn_make_buffer_rsrc((char *)p.V + block, 0, p.s.head_bytes, 0x00020000);
+        codes = in * p.s.row_bytes;
+        pairs = p.s.pairs_at + in * p.s.groups * 4;
+    }
+};
+
+// the lane's place in a tile
+template <bool F32, int DB>
+struct Q4Stage {
+    using S = Q4Att<F32, DB>;
+    uint32_t at_k, at_kp[S::NP], at_v[4][S::NC], at_vp[4][S::NC];       // of values: keys 4 (lane >> 4) + j
+    __device__ __forceinline__ Q4Stage(const AttendQ4Params &p, int lane)
+    {
+        // features from dim on meet queries that are zero, or end in outputs that are not stored: some of the row's own will do
+        const int f = (lane >> 4) * S::NW * 8 < p.dim ? (lane >> 4) * S::NW * 8 : 0;
+        at_k = (lane & 15) * p.s.row_bytes + f / 2;
+#pragma unroll
+        for (int j = 0; j < S::NP; ++j) {
+            const uint32_t g = (uint32_t)(f + 32 * j) >> p.s.group_shift;
+            at_kp[j] = ((lane & 15) * p.s.groups + (g < p.s.groups ? g : p.s.groups - 1)) * 4;
+        }
+#pragma unroll
+        for (int c = 0; c < S::NC; ++c) {
+            const int d = (c * 16 + (lane & 15)) * S::VD < p.dim ? (c * 16 + (lane & 15)) * S::VD : 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                at_v[j][c] = ((lane >> 4) * 4 + j) * p.s.row_bytes + d / 2;
+                at_vp[j][c] = (((lane >> 4) * 4 + j) * p.s.groups + (d >> p.s.group_shift)) * 4;
+            }
+        }
+    }
+
+    __device__ __forceinline__ void load_keys(Q4Keys<F32, DB> &f, const Q4Tile (&of)[2]) const
+    {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            if constexpr (S::NW == 2)
+                *(q4_u32x2 *)f.k[i] = __builtin_amdgcn_raw_buffer_load_b64(of[i].K, at_k, of[i].codes, 0);
+            else
+#pragma unroll
+                for (int w = 0; w < S::NW; w += 4)
+                    *(att_u32x4 *)(f.k[i] + w) = __builtin_amdgcn_raw_buffer_load_b128(of[i].K, at_k + w * 4, of[i].codes, 0);
+#pragma unroll
+            for (int j = 0; j < S::NP; ++j)
+                f.pair[i][j] = __builtin_amdgcn_raw_buffer_load_b32(of[i].K, at_kp[j], of[i].pairs, 0);
+        }
+    }
+
+    __device__ __forceinline__ void load_vals(Q4Vals<F32, DB> &f, const Q4Tile (&of)[2]) const
+    {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int c = 0; c < S::NC; ++c) {
+                if constexpr (S::VD == 4)
+                    f.v[j][c] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(of[j >> 2].V, at_v[j & 3][c], of[j >> 2].codes, 0);
+                else
+                    f.v[j][c] = __builtin_amdgcn_raw_buffer_load_b32(of[j >> 2].V, at_v[j & 3][c], of[j >> 2].codes, 0);
+                f.pair[j][c] = __builtin_amdgcn_raw_buffer_load_b32(of[j >> 2].V, at_vp[j & 3][c], of[j >> 2].pairs, 0);
+            }
+    }
+};
+
+template <bool F32, int DB, int NT>
+using Q4Scores = att_f32x4[NT][2];
+
+__device__ __forceinline__ uint32_t q4_word(q4_pair v) { return __builtin_bit_cast(uint32_t, v); }
+
+template <bool F32, int DB, int NT>
+__device__ __forceinline__ void q4_scores(Q4Scores<F32, DB, NT> &s, const Q4Keys<F32, DB> &f, const Q4Rows<F32, DB, NT> &r)
+{
+    using S = Q4Att<F32, DB>;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int w = 0; w < S::NW; ++w) {
+            const q4_pair scale = q4_scales(f.pair[i][w / 4]), middle = q4_middles(f.pair[i][w / 4]);
+            att_u32x4 a;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                a[j] = q4_word(q4_value_pair(f.k[i][w] >> 4 * j, scale, middle));
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int h = 0; h < S::NF; ++h)
+                    s[n][i] = q4_mfma(a, r.q[n][h][w], w == 0 && h == 0 ? att_f32x4{0, 0, 0, 0} : s[n][i]);
+        }
+}
+
+// Keys from r.end on, and those in the hole, out of the scores
+template <bool F32, int DB, int NT>
+__device__ __forceinline__ void q4_mask(Q4Scores<F32, DB, NT> &s, const Q4Rows<F32, DB, NT> &r, const AttendItem &it, int32_t key0, int lane)
+{
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int32_t key = key0 + 16 * i + (lane >> 4) * 4 + e;
+                s[n][i][e] = key < r.end[n] && !it.missing(key) ? s[n][i][e] : -INFINITY;
+            }
+}
+
+// Scores to weights, cut to fp16 (fp32: and what that leaves, once more): the rows' reference carried on, moved only when scores outgrow it by more than 8 (base 2), so
+// that weights are up to 2^8 times its.  Sums are of the weights as they are multiplied, by a product with ones: what cutting takes off all of them cancels.
+template <bool F32, int DB, int NT>
+__device__ __forceinline__ void q4_softmax(Q4Scores<F32, DB, NT> &s, att_u32x4 (&w)[NT][Q4Att<F32, DB>::NF], Q4Rows<F32, DB, NT> &r)
+{
+    using S = Q4Att<F32, DB>;
+    float top[NT];
+    bool grown = false;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        top[n] = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                top[n] = fmaxf(top[n], s[n][i][e]);
+        top[n] *= r.scale2[n];
+        grown |= top[n] > r.m[n] + 8.0f;
+    }
+    if (__any(grown))
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const float m = fmaxf(r.m[n], lane_groups_max(top[n]));
+            const float f = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(r.m[n] - m);        // nothing seen yet: nothing to scale
+            r.m[n] = m;
+            r.l[n] *= f;
+#pragma unroll
+            for (int e = 0; e < S::NO; ++e)
+                r.o[n][e] *= f;
+        }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        // 2^7 times the weights, up to 2^15: fp16 keeps their bits down to 2^-21 of the reference's, and 2^-31 of it below.  The quotient does not see it.
+        const float base = r.m[n] == -INFINITY ? -7.0f : r.m[n] - 7.0f;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            float x[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                x[e] = __builtin_amdgcn_exp2f(s[n][i][e] * r.scale2[n] - base);
+#pragma unroll
+            for (int e = 0; e < 4; e += 2) {
+                const q4_pair v = __builtin_bit_cast(q4_pair, __builtin_amdgcn_cvt_pkrtz(x[e], x[e + 1]));
+                w[n][0][2 * i + e / 2] = q4_word(v);
+                if constexpr (F32)
+                    w[n][1][2 * i + e / 2] = q4_word(__builtin_bit_cast(q4_pair, __builtin_amdgcn_cvt_pkrtz(x[e] - (float)v[0], x[e + 1] - (float)v[1])));
+            }
+        }
+#pragma unroll
+        for (int h = 0; h < S::NF; ++h)
+            r.l[n] = q4_mfma(att_u32x4{Q4_ONES, Q4_ONES, Q4_ONES, Q4_ONES}, w[n][h], r.l[n]);
+    }
+}
+
+// O^T += V^T P^T
+template <bool F32, int DB, int NT>
+__device__ __forceinline__ void q4_weigh(const att_u32x4 (&w)[NT][Q4Att<F32, DB>::NF], const Q4Vals<F32, DB> &f, Q4Rows<F32, DB, NT> &r)
+{
+    using S = Q4Att<F32, DB>;
+#pragma unroll
+    for (int c = 0; c < S::NC; ++c) {
+        q4_pair scale[4], middle[4];                       // of keys 2h and 2h + 1
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            scale[h] = __builtin_bit_cast(q4_pair, __builtin_amdgcn_perm(f.pair[2 * h + 1][c], f.pair[2 * h][c], 0x05040100));
+            middle[h] = __builtin_bit_cast(q4_pair, __builtin_amdgcn_perm(f.pair[2 * h + 1][c], f.pair[2 * h][c], 0x07060302));
+        }
+#pragma unroll
+        for (int e = 0; e < S::VD; e += 2) {               // features e and e + 1: a byte
+            att_u32x4 a[2];
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+                const uint32_t x = __builtin_amdgcn_perm(f.v[2 * h + 1][c], f.v[2 * h][c], 0x0C000C00u | (4 + e / 2) << 16 | e / 2);
+                a[0][h] = q4_word(q4_value_pair(x, scale[h], middle[h]));
+                a[1][h] = q4_word(q4_value_pair(x >> 4, scale[h], middle[h]));
+            }
+#pragma unroll
+            for (int g = 0; g < 2; ++g)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int h = 0; h < S::NF; ++h)
+                        r.o[n][c * S::VD + e + g] = q4_mfma(a[g], w[n][h], r.o[n][c * S::VD + e + g]);
+        }
+    }
+}
+
+// whether either of a (scale, middle) word is infinite or NaN
+__device__ __forceinline__ bool q4_odd(uint32_t pair) { return (pair & 0x7C00u) == 0x7C00u || (pair & 0x7C000000u) == 0x7C000000u; }
+
+// Before a masked step's second product: what stands behind the last key, or in the hole, is any memory's content and becomes zero, and so do groups of NaN,
+// which must not reach the rows that do not see them, as 0 x NaN would; true if there were any of these: they are added at the end to those that do.
+template <bool F32, int DB>
+__device__ __forceinline__ bool q4_clear(Q4Vals<F32, DB> &f, const AttendItem &it, int32_t key0, int lane)
+{
+    using S = Q4Att<F32, DB>;
+    bool odd = false;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int32_t key = key0 + 16 * (j >> 2) + (lane >> 4) * 4 + (j & 3);
+        const bool in = key < it.end && !it.missing(key);
+#pragma unroll
+        for (int c = 0; c < S::NC; ++c) {
+            const bool bad = q4_odd(f.pair[j][c]);
+            odd |= in && bad;
+            f.pair[j][c] = in && !bad ? f.pair[j][c] : 0;
+        }
+    }
+    return __any(odd);
+}
+
+// where a key's (scale, middle) words lie in a pool
+__device__ __forceinline__ uint64_t q4_pairs_of(const AttendQ4Params &p, const AttendItem &it, int32_t key)
+{
+    const uint32_t page = att_page(__builtin_amdgcn_readfirstlane(att_look_up(p, it, key)), p.last_page);
+    const uint32_t in = (key - (key < it.hole_end ? 0 : it.hole_end)) & ((1 << p.page_shift) - 1);
+    return ((uint64_t)page * (uint32_t)p.kv_heads + it.hk) * p.s.head_bytes + p.s.pairs_at + in * p.s.groups * 4;
+}
+
+// ... of the keys from `key` on of one step
+template <bool F32, int DB, int NT>
+__device__ __forceinline__ void q4_add_odd(const AttendQ4Params &p, const AttendItem &it, Q4Rows<F32, DB, NT> &r, int32_t key)
+{
+    using S = Q4Att<F32, DB>;
+    const int32_t stop = key + S::KS < it.end ? key + S::KS : it.end;
+    for (; key < stop; ++key) {
+        const char *at = (const char *)p.V + q4_pairs_of(p, it, key);
+#pragma unroll
+        for (int c = 0; c < S::NC; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {                  // elements i of the lane's sums: features (c 16 + (lane >> 4) 4 + i) VD + e
+                const int d = (c * 16 + (threadIdx.x >> 4 & 3) * 4 + i) * S::VD;
+                const bool odd = d < p.dim && q4_odd(*(const uint32_t *)(at + (d < p.dim ? d >> p.s.group_shift : 0) * 4));
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < S::VD; ++e)
+                        r.o[n][c * S::VD + e][i] = odd && key < r.end[n] && !it.missing(key) ? __builtin_nanf("") : r.o[n][c * S::VD + e][i];
+            }
+    }
+}
+
+// A row's queries in the order of the codes' pairs, scaled so that the largest lies in [128, 256); returns what its scores are to be multiplied by
+template <bool F32, int NW>
+__device__ __forceinline__ float q4_load_row(const AttendQ4Params &p, att_u32x4 (&q)[F32 ? 2 : 1][NW], int64_t at, int lane)
+{
+    float x[NW][8], top = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+        const int d = ((lane >> 4) * NW + w) * 8;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            x[w][j] = 0;
+        if (d < p.dim) {
+            if (F32) {
+                *(float4 *)x[w] = *(const float4 *)((const float *)p.q + at + d);
+                *(float4 *)(x[w] + 4) = *(const float4 *)((const float *)p.q + at + d + 4);
+            } else {
+                const uint4 b = *(const uint4 *)((const uint16_t *)p.q + at + d);
+                x[w][0] = bf16_lo(b.x); x[w][1] = bf16_hi(b.x); x[w][2] = bf16_lo(b.y); x[w][3] = bf16_hi(b.y);
+                x[w][4] = bf16_lo(b.z); x[w][5] = bf16_hi(b.z); x[w][6] = bf16_lo(b.w); x[w][7] = bf16_hi(b.w);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            top = fmaxf(top, fabsf(x[w][j]));
+    }
+    const int up = 8 - __builtin_amdgcn_frexp_expf(lane_groups_max(top));      // infinite: frexp gives 0, and the queries stay infinite
+#pragma unroll
+    for (int w = 0; w < NW; ++w)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float a = ldexpf(x[w][j], up), b = ldexpf(x[w][j + 4], up);
+            const q4_pair v = {(_Float16)a, (_Float16)b};
+            q[0][w][j] = q4_word(v);
+            if constexpr (F32) {
+                const q4_pair rest = {(_Float16)(a - (float)v[0]), (_Float16)(b - (float)v[1])};
+                q[1][w][j] = q4_word(rest);
+            }
+        }
+    return ldexpf(p.scale2, -up);
+}
+
+// The item's rows first .. first + 16 NT - 1, by the WAVES wavefronts of a workgroup (in turn, a step each) or by one alone
+template <bool F32, int DB, int NT, int WAVES>
+__device__ __forceinline__ void attend_q4(const AttendQ4Params &p, float *lds, const AttendItem &it)
+{
+    using S = Q4Att<F32, DB>;
+    const int32_t begin = it.begin, end = it.end, own = it.own, rows = it.rows, first = it.first;
+    const int lane = threadIdx.x & 63, wave = WAVES == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int32_t key0 = begin + wave * S::KS;
+    constexpr int STRIDE = WAVES * S::KS;
+    const Q4Stage<F32, DB> in(p, lane);
+    Q4Tile at[2][2];
+    const auto look_up = [&](Q4Tile (&of)[2], int32_t key) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            of[i].look_up(p, it, key + 16 * i);
+    };
+    const auto set = [&](Q4Tile (&of)[2], int32_t key) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            of[i].set(p, it, key + 16 * i);
+    };
+    look_up(at[0], key0);
+    look_up(at[1], key0 + STRIDE);
+    Q4Rows<F32, DB, NT> r;
+    int32_t least = end;                                   // keys that all rows see
+    if (own >= 0 && own + p.by_group(first) + 1 < end)
+        least = own + p.by_group(first) + 1;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        int32_t row = first + 16 * n + (lane & 15);
+        row = row < rows ? row : rows - 1;                 // rows behind the last repeat it and are not stored
+        const int32_t token = p.by_group(row), head = it.hk * p.group + row - token * p.group;
+        r.end[n] = end;
+        if (own >= 0) {
+            const int32_t sees = own + token + 1;
+            r.end[n] = sees < end ? sees : end;
+        }
+        r.scale2[n] = q4_load_row<F32, S::NW>(p, r.q[n], (int64_t)(it.token0 + token) * p.ldq + (int64_t)head * p.hsq, lane);
+        r.m[n] = -INFINITY;
+        r.l[n] = att_f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int c = 0; c < S::NO; ++c)
+            r.o[n][c] = att_f32x4{0, 0, 0, 0};
+    }
+    bool odd = false;
+    if (key0 < end) {
+        // Two steps are on their way while one is computed: step i's registers take step i + 2 as soon as they have been read, and i + 4's pages are looked up
+        Q4Keys<F32, DB> fk[2];
+        Q4Vals<F32, DB> fv[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (key0 + i * STRIDE < end) {
+                set(at[i], key0 + i * STRIDE);
+                in.load_keys(fk[i], at[i]);
+                in.load_vals(fv[i], at[i]);
+                look_up(at[i], key0 + (i + 2) * STRIDE);
+            }
+        while (true) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                att_f32x4 s[NT][2];
+                att_u32x4 w[NT][S::NF];
+                q4_scores<F32, DB, NT>(s, fk[i], r);
+                __builtin_amdgcn_sched_barrier(0);
+                const bool more = key0 + 2 * STRIDE < end;
+                if (more) {
+                    set(at[i], key0 + 2 * STRIDE);
+                    in.load_keys(fk[i], at[i]);
+                    look_up(at[i], key0 + 4 * STRIDE);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                if (key0 + S::KS > least || it.touches_hole(key0, S::KS)) {
+                    q4_mask<F32, DB, NT>(s, r, it, key0, lane);
+                    odd |= q4_clear<F32, DB>(fv[i], it, key0, lane);
+                }
+                q4_softmax<F32, DB, NT>(s, w, r);
+                q4_weigh<F32, DB, NT>(w, fv[i], r);
+                __builtin_amdgcn_sched_barrier(0);
+                if (more)
+                    in.load_vals(fv[i], at[i]);
+                key0 += STRIDE;
+                if (key0 >= end)
+                    goto done;
+            }
+        }
+    done:;
+    }
+    if (odd)
+        for (key0 = begin + wave * S::KS; key0 < end; key0 += WAVES * S::KS)
+            if (key0 + S::KS > least || it.touches_hole(key0, S::KS))
+                q4_add_odd<F32, DB, NT>(p, it, r, key0);
+    float sum[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+        sum[n] = r.l[n][0];
+    att_finish<!F32, S, DB, false, NT, WAVES>(p, lds, it, r.m, sum, r.o);
+}
+
+// launches the `wgs` workgroups of p on tiles of att_tile_rows(dim) rows, and behind them p.items_own own items of 16 rows, a workgroup each or, `each`, a
+// wavefront each (dim <= 128); bf16 outside the cache only
+int launch_attend_q4_tiles(const AttendQ4Params &p, int32_t wgs, bool each, hipStream_t st);
+
+}  // namespace griffin

@@ -29,9 +29,12 @@ inline Q4Shape q4_shape(const griffin_kv_cache_q4 &C)
 
 // Codes of features f .. f + 7 are one word.  With a code's four bits as the last of an fp16's whose unit is one, 1024 + (c + 8), taking away 1032 leaves c
 // exactly, two codes an instruction.  Features (0, 4), (1, 5), (2, 6), (3, 7) come out as pairs: those are four bits apart in both halves of the word.
+// One instruction takes both constants only if one of them is in a vector register, where the compiler would not put it by itself.
 __device__ __forceinline__ q4_pair q4_code_pair(uint32_t bits)       // codes in bits 0 .. 3 and 16 .. 19; others are cut away
 {
-    return __builtin_bit_cast(q4_pair, (bits & 0x000F000Fu) | 0x64006400u) - q4_pair{(_Float16)1032, (_Float16)1032};
+    uint32_t mask = 0x000F000Fu;
+    asm("" : "+v"(mask));
+    return __builtin_bit_cast(q4_pair, (bits & mask) | 0x64006400u) - q4_pair{(_Float16)1032, (_Float16)1032};
 }
 
 // middle + scale c, rounded once

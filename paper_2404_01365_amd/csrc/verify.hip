@@ -3,14 +3,22 @@
 // A sequence keeps its drafted tokens while u q(d) < p(d); where that ends a token is drawn from w = max(p - q, 0), or from p, by the inverse of the running
 // sum: the first j with w_0 + .. + w_j > r W.  Sums are in 64 bits, so that their order does not decide which token that is.
 //
-// Only the row where the kept tokens end is read whole.  Its sum is taken in chunks by many workgroups, each of which finds that row for itself (a few numbers a
-// drafted token); a second launch adds the chunks in order, finds the one that the sum falls into and goes through it again.
+// Only the row where the kept tokens end is read whole.  A wavefront adds up a piece of 1024 tokens of it, and finds that row for itself (a few numbers a drafted token); a
+// second launch adds the pieces in order, finds the one that the sum falls into and goes through it again.
+//
+// Bound by the two launches while there are few tokens (one sequence of 32000: 4.6 + 3.8 us), else by bytes: 64 sequences of 128001, p and q, 66 MB, 11.8 + 5.4 us.
 #include "layer.h"
 
 namespace griffin {
 
 constexpr int VERIFY_THREADS = 256;
-constexpr int VERIFY_CHUNK = 4096;           // tokens of the vocabulary a workgroup adds up
+constexpr int VERIFY_PIECE = 1024;           // tokens of the vocabulary a wavefront adds up
+
+// Where a sequence's kept tokens end: its row, and what w is there
+struct VerifyEnd {
+    int32_t kept, row, without;              // without: the token that w leaves out (a draft without probabilities), or -1
+    int32_t minus_q;
+};
 
 struct VerifyParams {
     const float *p, *q;
@@ -19,15 +27,11 @@ struct VerifyParams {
     const float *accept_u, *draw_u;
     int32_t *tokens_out, *accepted, *lens_out;
     const int32_t *lens;
-    double *sums;                            // [sequence][chunk] sums of w, then of p
-    int32_t vocab, chunks;
+    VerifyEnd *ends;                         // [sequence], left by the first launch
+    double *sums;                            // [sequence][piece] sums of w
+    int32_t vocab, pieces, blocks;           // workgroups a sequence
+    bool wide;                               // rows in 16 bytes
     SeqTable seqs;
-};
-
-// Where a sequence's kept tokens end: its row, and what w is there
-struct VerifyEnd {
-    int32_t kept, row, without;              // without: the token that w leaves out (a draft without probabilities), or -1
-    bool minus_q;
 };
 
 // by every wavefront for itself, 64 rows at a time
@@ -35,7 +39,7 @@ __device__ __forceinline__ VerifyEnd verify_end(const VerifyParams &p, int b)
 {
     const int lane = threadIdx.x & 63;
     const int32_t first = p.seqs.cu[b], last = p.seqs.cu[b + 1] - 1;
-    VerifyEnd e = {last - first, last, -1, false};
+    VerifyEnd e = {last - first, last, -1, 0};
     for (int32_t at = first; at < last; at += 64) {
         const int32_t row = at + lane;
         bool kept = true;
@@ -63,56 +67,136 @@ __device__ __forceinline__ VerifyEnd verify_end(const VerifyParams &p, int b)
     return e;
 }
 
-// w of token j, and p
-__device__ __forceinline__ float verify_weight(const VerifyParams &p, const VerifyEnd &e, int32_t j, float &whole)
+// w of N consecutive tokens from j on, zero behind the vocabulary's end
+template <int N>
+__device__ __forceinline__ void verify_weights(const VerifyParams &p, const VerifyEnd &e, int32_t j, float (&w)[N])
 {
-    whole = p.p[e.row * p.ldp + j];
-    if (e.minus_q)
-        return fmaxf(whole - p.q[e.row * p.ldq + j], 0.0f);
-    return j == e.without ? 0.0f : whole;
-}
-
-__device__ __forceinline__ double wave_sum64(double v)
-{
+    const float *at = p.p + e.row * p.ldp + j, *less = p.q + (e.minus_q ? e.row * p.ldq + j : 0);
+    float q[N];
+    if (N == 4 && p.wide && j + 4 <= p.vocab) {
+        *(float4 *)w = *(const float4 *)at;
+        if (e.minus_q)
+            *(float4 *)q = *(const float4 *)less;
+    } else
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1)
-        v += __shfl_xor(v, off);
-    return v;
+        for (int i = 0; i < N; ++i) {
+            w[i] = j + i < p.vocab ? at[i] : 0.0f;
+            if (e.minus_q)
+                q[i] = j + i < p.vocab ? less[i] : 0.0f;
+        }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if (e.minus_q)
+            w[i] = fmaxf(w[i] - q[i], 0.0f);
+        w[i] = j + i == e.without ? 0.0f : w[i];
+    }
 }
 
 __global__ __launch_bounds__(VERIFY_THREADS) void verify_sums_kernel(VerifyParams p)
 {
-    __shared__ double part[2][VERIFY_THREADS / 64];
-    const int b = blockIdx.x / p.chunks, chunk = blockIdx.x - b * p.chunks;
-    if (p.seqs.cu[b] == p.seqs.cu[b + 1])
+    const int b = blockIdx.x / p.blocks, lane = threadIdx.x & 63;
+    const int32_t piece = (blockIdx.x - b * p.blocks) * (VERIFY_THREADS / 64) + (threadIdx.x >> 6);
+    if (p.seqs.cu[b] == p.seqs.cu[b + 1] || piece >= p.pieces)
         return;
     const VerifyEnd e = verify_end(p, b);
-    double sum = 0, all = 0;
-    const int32_t begin = chunk * VERIFY_CHUNK, end = begin + VERIFY_CHUNK < p.vocab ? begin + VERIFY_CHUNK : p.vocab;
-    for (int32_t j = begin + threadIdx.x; j < end; j += VERIFY_THREADS) {
-        float whole;
-        sum += verify_weight(p, e, j, whole);
-        all += whole;
+    if (piece == 0 && lane == 0)
+        p.ends[b] = e;
+    double sum = 0;
+    const int32_t begin = piece * VERIFY_PIECE;
+    const auto add = [&](auto &w) {
+#pragma unroll
+        for (auto &v : w)
+#pragma unroll
+            for (float x : v)
+                sum += x;
+    };
+    if (p.wide) {
+        float w[VERIFY_PIECE / 256][4];
+#pragma unroll
+        for (int i = 0; i < VERIFY_PIECE / 256; ++i)
+            verify_weights(p, e, begin + (i * 64 + lane) * 4, w[i]);
+        add(w);
+    } else {
+        float w[VERIFY_PIECE / 64][1];
+#pragma unroll
+        for (int i = 0; i < VERIFY_PIECE / 64; ++i)
+            verify_weights(p, e, begin + i * 64 + lane, w[i]);
+        add(w);
     }
-    sum = wave_sum64(sum);
-    all = wave_sum64(all);
-    if ((threadIdx.x & 63) == 0) {
-        part[0][threadIdx.x >> 6] = sum;
-        part[1][threadIdx.x >> 6] = all;
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1)
+        sum += __shfl_xor(sum, off);
+    if (lane == 0)
+        p.sums[(int64_t)b * p.pieces + piece] = sum;
+}
+
+// The sum of what the threads before have, and of all; called by all threads of a workgroup
+__device__ __forceinline__ double verify_before(double v, double &all)
+{
+    __shared__ double totals[VERIFY_THREADS / 64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    double run = v;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const double other = __shfl_up(run, off);
+        run += lane >= off ? other : 0.0;
+    }
+    __syncthreads();                         // everyone has read what a call before left
+    if (lane == 63)
+        totals[wave] = run;
+    __syncthreads();
+    double before = 0;
+    all = 0;
+#pragma unroll
+    for (int w = 0; w < VERIFY_THREADS / 64; ++w) {
+        before += w < wave ? totals[w] : 0.0;
+        all += totals[w];
+    }
+    const double other = __shfl_up(run, 1);
+    return before + (lane > 0 ? other : 0.0);
+}
+
+// the least of the threads' numbers
+__device__ __forceinline__ int32_t verify_least(int32_t v)
+{
+    __shared__ int32_t least[VERIFY_THREADS / 64];
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) {
+        const int32_t other = __shfl_xor(v, off);
+        v = other < v ? other : v;
     }
     __syncthreads();
-    if (threadIdx.x < 2) {
-        double total = 0;
+    if ((threadIdx.x & 63) == 0)
+        least[threadIdx.x >> 6] = v;
+    __syncthreads();
 #pragma unroll
-        for (int w = 0; w < VERIFY_THREADS / 64; ++w)
-            total += part[threadIdx.x][w];
-        p.sums[((int64_t)b * p.chunks + chunk) * 2 + threadIdx.x] = total;
+    for (int w = 0; w < VERIFY_THREADS / 64; ++w)
+        v = least[w] < v ? least[w] : v;
+    return v;
+}
+
+// The first token of [begin, begin + 4 VERIFY_THREADS) whose running sum, with what comes before, passes the goal; INT32_MAX: none.  `before` is carried on.
+__device__ __forceinline__ int32_t verify_find(const VerifyParams &p, const VerifyEnd &e, int32_t begin, double goal, double &before)
+{
+    const int32_t j = begin + threadIdx.x * 4;
+    float w[4];
+    verify_weights(p, e, j, w);
+    double all, run = verify_before((double)w[0] + (double)w[1] + (double)w[2] + (double)w[3], all) + before;
+    int32_t found = INT32_MAX;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        run += w[i];
+        if (found == INT32_MAX && j + i < p.vocab && run > goal)
+            found = j + i;
     }
+    before += all;
+    return verify_least(found);
 }
 
 __global__ __launch_bounds__(VERIFY_THREADS) void verify_draw_kernel(VerifyParams p)
 {
-    const int b = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    static_assert(VERIFY_PIECE == 4 * VERIFY_THREADS, "verify_find goes through a piece");
+    const int b = blockIdx.x;
     const int32_t first = p.seqs.cu[b], rows = p.seqs.cu[b + 1] - first;
     if (rows == 0) {
         if (threadIdx.x == 0) {
@@ -122,64 +206,53 @@ __global__ __launch_bounds__(VERIFY_THREADS) void verify_draw_kernel(VerifyParam
         }
         return;
     }
-    VerifyEnd e = verify_end(p, b);
-    // the chunk that the goal falls into, by every thread alike
-    const double *sums = p.sums + (int64_t)b * p.chunks * 2;
-    double total = 0;
-    for (int c = 0; c < p.chunks; ++c)
-        total += sums[2 * c];
-    int which = 0;
-    if (!(total > 0)) {                      // nothing left over: the target's own probabilities
-        which = 1;
-        e.minus_q = false;
-        e.without = -1;
-        total = 0;
-        for (int c = 0; c < p.chunks; ++c)
-            total += sums[2 * c + 1];
-    }
-    const double goal = (double)p.draw_u[b] * total;
-    double before = 0;
-    int chunk = 0;
-    for (; chunk < p.chunks; ++chunk) {
-        if (before + sums[2 * chunk + which] > goal)
-            break;
-        before += sums[2 * chunk + which];
-    }
-    int32_t drawn = p.vocab - 1;
-    if (chunk < p.chunks) {
-        // 64 tokens a wavefront and 256 a workgroup at a time, sums carried on
-        __shared__ double totals[VERIFY_THREADS / 64];
-        __shared__ int32_t found;
-        if (threadIdx.x == 0)
-            found = INT32_MAX;
-        const int32_t begin = chunk * VERIFY_CHUNK, end = begin + VERIFY_CHUNK < p.vocab ? begin + VERIFY_CHUNK : p.vocab;
-        for (int32_t at = begin; at < end; at += VERIFY_THREADS) {
-            const int32_t j = at + threadIdx.x;
-            float whole;
-            double run = j < end ? verify_weight(p, e, j, whole) : 0.0f;
-#pragma unroll
-            for (int off = 1; off < 64; off <<= 1) {
-                const double other = __shfl_up(run, off);
-                run += lane >= off ? other : 0.0;
-            }
-            __syncthreads();                 // everyone has read what the round before left
-            if (lane == 63)
-                totals[wave] = run;
-            __syncthreads();
-            double here = before;
-            for (int w = 0; w < wave; ++w)
-                here += totals[w];
-            if (j < end && here + run > goal)
-                atomicMin(&found, j);
-            for (int w = 0; w < VERIFY_THREADS / 64; ++w)
-                before += totals[w];
-            __syncthreads();
-            if (found != INT32_MAX)
+    VerifyEnd e = p.ends[b];
+    const double u = p.draw_u[b];
+    // a thread takes as many pieces as its share is, one behind the other
+    const double *sums = p.sums + (int64_t)b * p.pieces;
+    const int32_t share = (p.pieces + VERIFY_THREADS - 1) / VERIFY_THREADS, from = threadIdx.x * share;
+    const int32_t to = from + share < p.pieces ? from + share : p.pieces;
+    double mine = 0, total;
+    for (int32_t i = from; i < to; ++i)
+        mine += sums[i];
+    double before = verify_before(mine, total);
+    int32_t drawn = INT32_MAX;
+    if (total > 0) {
+        const double goal = u * total;
+        int32_t piece = INT32_MAX;
+        double run = before;
+        for (int32_t i = from; i < to; ++i) {
+            if (run + sums[i] > goal) {
+                piece = i;
                 break;
+            }
+            run += sums[i];
         }
-        // where the chunk's sum passes the goal and the running one, rounded otherwise, does not: its last token
-        drawn = found != INT32_MAX ? found : end - 1;
+        __shared__ double start;
+        const int32_t least = verify_least(piece);
+        if (piece == least && piece != INT32_MAX)        // one thread's
+            start = run;
+        __syncthreads();
+        if (least != INT32_MAX) {
+            before = start;
+            drawn = verify_find(p, e, least * VERIFY_PIECE, goal, before);
+            // where the piece's sum passes the goal and the running one, rounded otherwise, does not: its last token
+            const int32_t last = (least + 1) * VERIFY_PIECE - 1;
+            drawn = drawn != INT32_MAX ? drawn : last < p.vocab ? last : p.vocab - 1;
+        }
+    } else {
+        // nothing left over: the target's own probabilities, by this workgroup alone
+        e.minus_q = 0;
+        e.without = -1;
+        before = 0;
+        for (int32_t at = 0; at < p.vocab; at += VERIFY_PIECE)
+            verify_find(p, e, at, INFINITY, before);
+        const double goal = u * before;
+        before = 0;
+        for (int32_t at = 0; at < p.vocab && drawn == INT32_MAX; at += VERIFY_PIECE)
+            drawn = verify_find(p, e, at, goal, before);
     }
+    drawn = drawn != INT32_MAX ? drawn : p.vocab - 1;
     for (int32_t i = threadIdx.x; i < rows; i += VERIFY_THREADS)
         p.tokens_out[first + i] = i < e.kept ? p.drafted[first + i] : i == e.kept ? drawn : -1;
     if (threadIdx.x == 0) {
@@ -189,20 +262,29 @@ __global__ __launch_bounds__(VERIFY_THREADS) void verify_draw_kernel(VerifyParam
     }
 }
 
-static int32_t verify_chunks(int32_t vocab) { return (vocab + VERIFY_CHUNK - 1) / VERIFY_CHUNK; }
+static int32_t verify_pieces(int32_t vocab) { return (vocab + VERIFY_PIECE - 1) / VERIFY_PIECE; }
 
-size_t verify_bytes(int32_t n_seqs, int32_t vocab) { return (size_t)n_seqs * verify_chunks(vocab) * 2 * sizeof(double); }
+size_t verify_bytes(int32_t n_seqs, int32_t vocab)
+{
+    static_assert(sizeof(VerifyEnd) == 2 * sizeof(double), "the sums behind the ends are aligned");
+    return (size_t)n_seqs * (verify_pieces(vocab) * sizeof(double) + sizeof(VerifyEnd));
+}
 
 int launch_verify(const VerifyJob &job, const SeqTable &seqs, hipStream_t st)
 {
     VerifyParams p = {};
     p.p = job.p; p.q = job.q; p.ldp = job.ldp; p.ldq = job.ldq; p.drafted = job.drafted;
     p.accept_u = job.accept_u; p.draw_u = job.draw_u; p.tokens_out = job.tokens_out; p.accepted = job.accepted;
-    p.lens = job.lens; p.lens_out = job.lens_out; p.sums = job.ws;
+    p.lens = job.lens; p.lens_out = job.lens_out;
+    p.ends = (VerifyEnd *)job.ws;
+    p.sums = job.ws + 2 * seqs.n;
     p.vocab = job.vocab;
-    p.chunks = verify_chunks(job.vocab);
+    p.pieces = verify_pieces(job.vocab);
+    p.blocks = (p.pieces + VERIFY_THREADS / 64 - 1) / (VERIFY_THREADS / 64);
+    const auto wide = [](const float *at, int64_t ld) { return !at || (((uintptr_t)at & 15) == 0 && ld % 4 == 0); };
+    p.wide = wide(job.p, job.ldp) && wide(job.q, job.ldq);
     p.seqs = seqs;
-    hipLaunchKernelGGL(verify_sums_kernel, dim3((uint32_t)seqs.n * p.chunks), dim3(VERIFY_THREADS), 0, st, p);
+    hipLaunchKernelGGL(verify_sums_kernel, dim3((uint32_t)seqs.n * p.blocks), dim3(VERIFY_THREADS), 0, st, p);
     const int rc = check_launch("verify_sums_kernel");
     if (rc != GRIFFIN_OK)
         return rc;
