@@ -68,6 +68,10 @@ struct AttendItem {
     // Where own items take the prefix, too, they count its keys first and their own from the next multiple of 16 on: keys from hole to hole_end are none,
     // and `own`, `begin` and `end` are counted like that.  Else both are 0.
     int32_t hole, hole_end;
+    // Where the sums of a part lie that the device has cut (attend_q4.h): from slot0 on, a slot a row; -1: where att_slot says.  alone: it is all that its rows see, and
+    // leaves outputs.
+    int64_t slot0;
+    bool alone;
 
     __device__ __forceinline__ bool missing(int32_t key) const { return key >= hole && key < hole_end; }
     __device__ __forceinline__ bool touches_hole(int32_t key0, int32_t keys) const { return hole < hole_end && key0 < hole_end && key0 + keys > hole; }
@@ -146,6 +150,8 @@ __device__ __forceinline__ void att_prefix_item(const AttendParams &p, int32_t i
     it.first = tile * ROWS;
     it.split = chunk;
     it.hole = it.hole_end = 0;
+    it.slot0 = -1;
+    it.alone = false;
 }
 
 // Tiles of rows in falling order of their number within a sequence, so that those that see the most keys are begun first: the `id`-th one.  With tiles
@@ -193,6 +199,8 @@ __device__ __forceinline__ bool att_own_item(const AttendParams &p, int32_t id, 
     it.begin = chunk * p.chunk_own;
     it.end = it.begin + p.chunk_own < end ? it.begin + p.chunk_own : end;
     it.split = p.chunks_prefix + chunk;
+    it.slot0 = -1;
+    it.alone = false;
     return it.begin < it.end;                                 // else no row reads this chunk's partial sums
 }
 
@@ -206,13 +214,11 @@ struct AttPlan {
     int32_t chunk_prefix, chunk_own, chunks_prefix, chunks_own, tiles_prefix, tiles_own;
 };
 
-// Host side that both kinds of cache share (attend.hip).  What a plan's sizes have to fit into; the fields of p that come from a batch and a plan; the join of a
-// row's chunks.
+// Host side that both kinds of cache share (attend.hip).  What a plan's sizes have to fit into, and the fields of p that come from a batch and a plan.
 bool attend_takes(const SeqTable &seqs, int32_t n_heads);
 bool att_launch_fits(const AttPlan &pl, int32_t kv_heads);
 void att_set_up(AttendParams &p, const AttPlan &pl, const griffin_kv_batch &B, const SeqTable &seqs, int32_t n_heads, int32_t kv_heads, int32_t dim,
                 int32_t page_size, int64_t n_pages, float scale, float *ws);
-int launch_attend_join(const AttendParams &p, bool bf16, hipStream_t st);
 
 // launches the `wgs` workgroups of p on tiles of att_tile_rows(dim) rows, and behind them p.items_own own items of 16 rows, a workgroup each or, `each`, a
 // wavefront each (dim <= 128); bf16 only

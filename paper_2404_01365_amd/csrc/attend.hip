@@ -16,6 +16,7 @@
 // The products of 16 rows a key are a twentieth of the matrix cores' rate when keys arrive at a copy's, of 64 rows a quarter: the arrangement is made for loads.
 #include <algorithm>
 
+#include "attend_join.h"
 #include "attend_rows.h"
 
 namespace griffin {
@@ -49,98 +50,6 @@ __global__ __launch_bounds__(ATT_FEW_WAVES * 64) void attend_few_kernel(AttendPa
     AttendItem it;
     if (att_own_item<16, false>(p, blockIdx.x, it))
         attend_rows<BF16, DB, FULL, 1, ATT_FEW_WAVES>(p, few_lds, it);
-}
-
-// Joins a row's chunks: with M = max m_c, o = sum o_c 2^(m_c - M) / sum l_c 2^(m_c - M).  A row per WPR wavefronts; a wavefront takes
-// 64 / (DB / 4) chunks at a time, four features a lane.
-template <bool BF16, int DB, int WPR>
-__global__ __launch_bounds__(256) void attend_join_kernel(AttendParams p)
-{
-    constexpr int LANES = DB / 4, PAR = 64 / LANES;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = lane / LANES, d = lane % LANES * 4;
-    const int64_t row = (int64_t)blockIdx.x * (4 / WPR) + (WPR == 1 ? wave : 0);
-    if (WPR == 1 && row >= (int64_t)p.tokens * p.n_heads)
-        return;
-    const int32_t token = __builtin_amdgcn_readfirstlane(p.by_heads((int32_t)row)), head = __builtin_amdgcn_readfirstlane((int32_t)row - token * p.n_heads);
-    const int b = att_sequence(token, p.each, p.seqs.cu, p.seqs.n);
-    const int32_t held = p.lens[b] < 0 ? 0 : (p.lens[b] < p.max_len ? p.lens[b] : p.max_len);
-    const int32_t seen = held + token - p.seqs.cu[b] + 1 < p.max_len ? held + token - p.seqs.cu[b] + 1 : p.max_len;
-    const int chunks = p.chunks_prefix + (seen + p.chunk_own - 1) / p.chunk_own;
-    const int64_t slot0 = row * (p.chunks_prefix + p.chunks_own);
-    // chunks c, c + WPR PAR, ... with a running maximum of their own, U on their way at a time
-    constexpr int U = 8;
-    float m = -INFINITY, l = 0;
-    att_f32x4 o = {0, 0, 0, 0};
-    const int d_in = d < p.dim ? d : 0;
-    for (int c = (WPR == 1 ? 0 : wave * PAR) + sub; c < chunks; c += U * WPR * PAR) {
-        float2 ml[U];
-        att_f32x4 x[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int at = c + u * WPR * PAR < chunks ? c + u * WPR * PAR : c;
-            ml[u] = p.part_ml[slot0 + at];
-            x[u] = *(const att_f32x4 *)(p.part + (slot0 + at) * p.dim + d_in);
-        }
-        float top = m;
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            top = fmaxf(top, ml[u].x);
-        const float base = top == -INFINITY ? 0.0f : top, f = __builtin_amdgcn_exp2f(m - base);
-        m = top;
-        l *= f;
-        o *= f;
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (c + u * WPR * PAR < chunks) {
-                const float g = __builtin_amdgcn_exp2f(ml[u].x - base);
-                l += ml[u].y * g;
-                o += x[u] * g;
-            }
-    }
-#pragma unroll
-    for (int off = LANES; off < 64; off <<= 1) {
-        const float m2 = __shfl_xor(m, off), l2 = __shfl_xor(l, off), top = fmaxf(m, m2), base = top == -INFINITY ? 0.0f : top;
-        const float f = __builtin_amdgcn_exp2f(m - base), f2 = __builtin_amdgcn_exp2f(m2 - base);
-        m = top;
-        l = l * f + l2 * f2;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            o[e] = o[e] * f + __shfl_xor(o[e], off) * f2;
-    }
-    if (WPR > 1) {
-        __shared__ __align__(16) float lds[WPR][LANES * 4 + 4];
-        if (sub == 0) {
-            *(att_f32x4 *)&lds[wave][d] = o;
-            if (d == 0) {
-                lds[wave][LANES * 4] = m;
-                lds[wave][LANES * 4 + 1] = l;
-            }
-        }
-        __syncthreads();
-        if (wave != 0)
-            return;
-        m = -INFINITY;
-        l = 0;
-        o = att_f32x4{0, 0, 0, 0};
-#pragma unroll
-        for (int w = 0; w < WPR; ++w)
-            m = fmaxf(m, lds[w][LANES * 4]);
-        const float base = m == -INFINITY ? 0.0f : m;
-#pragma unroll
-        for (int w = 0; w < WPR; ++w) {
-            const float f = __builtin_amdgcn_exp2f(lds[w][LANES * 4] - base);
-            l += lds[w][LANES * 4 + 1] * f;
-            o += *(const att_f32x4 *)&lds[w][d] * f;
-        }
-    }
-    if (sub != 0 || d >= p.dim)
-        return;
-    const float f = l == 0.0f ? 0.0f : 1.0f / l;
-    const int64_t at = (int64_t)token * p.ldo + (int64_t)head * p.hso + d;
-    if (BF16)
-        *(uint2 *)((uint16_t *)p.out + at) = make_uint2(f32x2_to_bf16x2(o[0] * f, o[1] * f), f32x2_to_bf16x2(o[2] * f, o[3] * f));
-    else
-        *(att_f32x4 *)((float *)p.out + at) = o * f;
 }
 
 // ------------------------------------------------------------------ host side
@@ -273,28 +182,6 @@ static int launch_rows(const AttendParams &p, int ntp, int nto, hipStream_t st)
 }
 
 template <bool BF16, int DB>
-static int go_join(const AttendParams &p, hipStream_t st)
-{
-    const int64_t rows = (int64_t)p.tokens * p.n_heads;
-    // A wavefront has 16 chunks of features on their way at a time (dim 128); of few rows with more, four share a row.  (One / four wavefronts a row, the whole call:
-    // 256 rows of 60 chunks 34.4 / 31.4 us, 512 of 33 21.3 / 20.1, 32 of 32 10.3 / 9.9; 512 of 18 13.2 / 14.1, 1280 of 33 28.7 / 31.6.)
-    if (rows <= 512 && p.chunks_prefix + p.chunks_own > 24)
-        hipLaunchKernelGGL((attend_join_kernel<BF16, DB, 4>), dim3((uint32_t)rows), dim3(256), 0, st, p);
-    else
-        hipLaunchKernelGGL((attend_join_kernel<BF16, DB, 1>), dim3((uint32_t)((rows + 3) / 4)), dim3(256), 0, st, p);
-    return check_launch("attend_join_kernel");
-}
-
-int launch_attend_join(const AttendParams &p, bool bf16, hipStream_t st)
-{
-    if (p.dim <= 64)
-        return bf16 ? go_join<true, 64>(p, st) : go_join<false, 64>(p, st);
-    if (p.dim <= 128)
-        return bf16 ? go_join<true, 128>(p, st) : go_join<false, 128>(p, st);
-    return bf16 ? go_join<true, 256>(p, st) : go_join<false, 256>(p, st);
-}
-
-template <bool BF16, int DB>
 static int attend_typed(AttendParams &p, const AttPlan &pl, hipStream_t st)
 {
     int rc = GRIFFIN_OK;
@@ -315,7 +202,7 @@ static int attend_typed(AttendParams &p, const AttPlan &pl, hipStream_t st)
                 return p.dim == DB ? go_few<BF16, DB, true>(p, st) : go_few<BF16, DB, false>(p, st);
         rc = pl.lone ? launch_rows<BF16, DB, true>(p, ntp, nto, st) : launch_rows<BF16, DB, false>(p, ntp, nto, st);
     }
-    return rc == GRIFFIN_OK && p.part ? launch_attend_join(p, BF16, st) : rc;
+    return rc == GRIFFIN_OK && p.part ? launch_attend_join(p, BF16, pl.chunks_prefix + pl.chunks_own, st) : rc;
 }
 
 template <bool BF16>
@@ -367,7 +254,7 @@ void att_set_up(AttendParams &p, const AttPlan &pl, const griffin_kv_batch &B, c
     p.each = divide_by((int64_t)p.tokens * each < (int64_t)1 << 32 ? each : 0);
     p.tiles_each = divide_by((int64_t)pl.tiles_own * tiles_each < (int64_t)1 << 32 ? tiles_each : 0);
     p.by_heads = divide_by(p.n_heads); p.by_kv_heads = divide_by(p.kv_heads); p.by_group = divide_by(p.group);
-    p.by_chunks_prefix = divide_by(pl.chunks_prefix > 0 ? pl.chunks_prefix : 1); p.by_chunks_own = divide_by(pl.chunks_own);
+    p.by_chunks_prefix = divide_by(pl.chunks_prefix > 0 ? pl.chunks_prefix : 1); p.by_chunks_own = divide_by(pl.chunks_own > 0 ? pl.chunks_own : 1);
 }
 
 int launch_attend(const AttendJob &job, const SeqTable &seqs, hipStream_t st)

@@ -26,7 +26,115 @@ constexpr uint32_t Q4_ONES = 0x3C003C00u;    // two fp16
 
 struct AttendQ4Params : AttendParams {
     Q4Shape s;
+    // Own parts that the device cuts, by the lengths that it has: into about 2^deal parts of all heads together, and no more than one more of every tile of rows.
+    // deal < 0: they are cut as the plan says.
+    int32_t deal;
+    int32_t quantum;         // keys a part is a multiple of, but for a sequence's last
+    int32_t rows_own;        // rows of a tile
+    int64_t slots_own;       // where the own parts' slots begin: [part][kv head][row of the tile]
+    int4 *cuts;              // [sequence] first part, parts of a tile of rows, keys of a part, for the join
 };
+
+// The sums of the lanes up to each one
+__device__ __forceinline__ uint32_t q4_wave_scan(uint32_t v)
+{
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, true);             // row_shr 1, 2, 4, 8: within 16 lanes
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);            // row_bcast 15: the first and third sixteen's sums to the second and fourth
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);            // row_bcast 31: the first half's to the second
+    return v;
+}
+
+// A part of a sequence's own keys: part number `part` of `parts` of tile `tile`'s, `keys` each; the sequence had `held` before the step
+struct Q4Cut {
+    int32_t b, tile, part, parts, keys, held;
+};
+
+// Own part j of a kv head, in the order of sequences, tiles of rows and keys.  With U quanta in all a part is c = ceil(U kv_heads / 2^deal) of them at most; a sequence of q is cut into
+// ceil(q / c) parts, as even as quanta allow.  Every wavefront counts for itself, a lane four sequences that are 64 apart.  The first of all notes the cuts for the join.
+__device__ __forceinline__ bool q4_deal(const AttendQ4Params &p, int32_t j, bool first_of_all, int lane, Q4Cut &cut)
+{
+    constexpr int TURNS = GRIFFIN_MAX_SEQS / 64;
+    int32_t held[TURNS];
+    uint32_t tiles[TURNS], quanta[TURNS], all = 0;
+#pragma unroll
+    for (int i = 0; i < TURNS; ++i) {
+        const int b = i * 64 + lane;
+        tiles[i] = quanta[i] = 0;
+        held[i] = 0;
+        if (i > 0 && p.seqs.n <= i * 64)
+            continue;
+        if (b < p.seqs.n) {
+            const int32_t tokens = p.each.by > 0 ? p.each.by : p.seqs.cu[b + 1] - p.seqs.cu[b], len = p.lens[b];
+            held[i] = len < 0 ? 0 : len < p.max_len ? len : p.max_len;
+            const int32_t keys = held[i] + tokens < p.max_len ? held[i] + tokens : p.max_len;
+            tiles[i] = (uint32_t)(tokens * p.group + p.rows_own - 1) / (uint32_t)p.rows_own;
+            quanta[i] = tokens > 0 ? (uint32_t)(keys + p.quantum - 1) / (uint32_t)p.quantum : 0;
+        }
+        all += tiles[i] * quanta[i];
+    }
+    const uint64_t whole = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(q4_wave_scan(all), 63) * (uint32_t)p.kv_heads;
+    const uint32_t most = (uint32_t)((whole + ((uint64_t)1 << p.deal) - 1) >> p.deal);        // below 2^31, as the sum is
+    uint32_t first = 0;                                    // parts of the sequences before these 64
+    bool found = false;
+#pragma unroll
+    for (int i = 0; i < TURNS; ++i) {
+        if (i > 0 && p.seqs.n <= i * 64)
+            break;
+        uint32_t n = (quanta[i] + most - 1) / (most > 0 ? most : 1);
+        const uint32_t each = n > 0 ? (quanta[i] + n - 1) / n : 1;
+        n = (quanta[i] + each - 1) / each;
+        const uint32_t mine = tiles[i] * n, run = q4_wave_scan(mine);
+        if (first_of_all && i * 64 + lane < p.seqs.n)
+            p.cuts[i * 64 + lane] = make_int4(first + run - mine, n, each * p.quantum, 0);
+        const uint64_t behind = __ballot(first + run > (uint32_t)j);
+        if (behind && !found) {
+            const int l = __builtin_ctzll(behind);
+            const uint32_t within = j - first - __builtin_amdgcn_readlane(run - mine, l);
+            cut.b = i * 64 + l;
+            cut.parts = __builtin_amdgcn_readlane(n, l);
+            cut.keys = __builtin_amdgcn_readlane(each, l) * p.quantum;
+            cut.held = __builtin_amdgcn_readlane(held[i], l);
+            cut.tile = within / (uint32_t)cut.parts;
+            cut.part = within - cut.tile * cut.parts;
+            found = true;
+            if (!first_of_all)
+                return true;
+        }
+        first += __builtin_amdgcn_readlane(run, 63);
+    }
+    return found;
+}
+
+// Own item `id` of [part][kv head], or as the plan has cut them; false: no row needs it
+template <int ROWS>
+__device__ __forceinline__ bool q4_own_item(const AttendQ4Params &p, int32_t id, AttendItem &it)
+{
+    if (p.deal < 0)
+        return att_own_item<ROWS, false>(p, id, it);
+    const int32_t j = p.by_kv_heads(id);
+    Q4Cut cut = {0, 0, 0, 1, 0, 0};
+    if (!q4_deal(p, j, id == 0 && __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) == 0, threadIdx.x & 63, cut))
+        return false;
+    it.hk = id - j * p.kv_heads;
+    it.pages = p.pages + (int64_t)cut.b * p.ld_pages;
+    it.last_entry = (p.max_len - 1) >> p.page_shift;
+    it.token0 = p.seqs.cu[cut.b];
+    it.rows = (p.seqs.cu[cut.b + 1] - p.seqs.cu[cut.b]) * p.group;
+    it.first = cut.tile * ROWS;
+    it.own = cut.held;
+    const int32_t last = it.first + ROWS < it.rows ? it.first + ROWS - 1 : it.rows - 1;               // the tile's last row sees the most keys
+    const int32_t end = it.own + p.by_group(last) + 1 < p.max_len ? it.own + p.by_group(last) + 1 : p.max_len;
+    it.hole = it.hole_end = 0;
+    it.begin = cut.part * cut.keys;
+    it.end = it.begin + cut.keys < end ? it.begin + cut.keys : end;
+    it.split = 0;
+    it.slot0 = p.slots_own + ((int64_t)j * p.kv_heads + it.hk) * p.rows_own;
+    it.alone = cut.parts == 1 && p.n_prefix == 0;
+    return it.begin < it.end;                              // else no row reads this part's sums
+}
 
 template <bool F32, int DB>
 struct Q4Att {

@@ -1,6 +1,7 @@
 // Attention over a cache in 4 bits (griffin_attention_q4): a few rows straight from memory (attend_q4.h), many through LDS (attend_q4_tile.hip).
 #include <algorithm>
 
+#include "attend_join.h"
 #include "attend_q4.h"
 
 namespace griffin {
@@ -22,7 +23,7 @@ __global__ __launch_bounds__(ATT_WAVES * 64, DB > 128 || F32 ? 1 : 2) void atten
         if (id >= p.items_own)
             return;
     }
-    if (att_own_item<16 * NTO, false>(p, id, it))
+    if (LONE ? att_own_item<16 * NTO, false>(p, id, it) : q4_own_item<16 * NTO>(p, id, it))
         attend_q4<F32, DB, NTO, LONE ? 1 : ATT_WAVES>(p, lds, it);
 }
 
@@ -36,22 +37,51 @@ __global__ __launch_bounds__(ATT_FEW_WAVES * 64) void attend_q4_few_kernel(Atten
         attend_q4<F32, DB, 1, ATT_FEW_WAVES>(p, q4_few_lds, it);
 }
 
-// ------------------------------------------------------------------ host side
-static int q4_widest(const griffin_kv_cache_q4 &C) { return C.dim > 128 || (C.dtype == GRIFFIN_F32 && C.dim > 64) ? 1 : 2; }
-
-static AttPlan attend_q4_plan(const griffin_kv_cache_q4 &C, const griffin_kv_batch &B, const SeqTable &seqs, int32_t n_heads)
+// where the join finds a row's chunks
+__device__ __forceinline__ AttParts att_parts(const AttendQ4Params &p, int32_t row, int32_t token, int32_t head)
 {
-    AttPlan pl = {};
+    if (p.deal < 0)
+        return att_parts((const AttendParams &)p, row, token, head);
+    const int b = att_sequence(token, p.each, p.seqs.cu, p.seqs.n);
+    const int32_t first = p.seqs.cu[b], held = p.lens[b] < 0 ? 0 : (p.lens[b] < p.max_len ? p.lens[b] : p.max_len);
+    const int32_t seen = held + token - first + 1 < p.max_len ? held + token - first + 1 : p.max_len;
+    const int4 cut = p.cuts[b];
+    if (p.chunks_prefix == 0 && cut.y == 1)                // the part's own workgroup has left the output
+        return {0, 0, 0, 0, 0};
+    const int32_t hk = p.by_group(head), in = (token - first) * p.group + head - hk * p.group, tile = in / p.rows_own;
+    const int64_t slot = ((int64_t)(cut.x + tile * cut.y) * p.kv_heads + hk) * p.rows_own + in - tile * p.rows_own;
+    return {(int64_t)row * p.chunks_prefix, p.slots_own + slot, p.chunks_prefix, (seen + cut.z - 1) / cut.z, p.kv_heads * p.rows_own};
+}
+
+// ------------------------------------------------------------------ host side
+struct Q4Plan : AttPlan {
+    int32_t deal;                       // as in AttendQ4Params
+    int64_t parts;                      // own parts of a kv head at most, where the device cuts them
+    int32_t quantum;
+    int64_t slots_own;                  // slots before theirs
+    size_t floats;                      // of workspace
+};
+
+// All rules go by sizes alone; figures are for 8 kv heads of 128 and four query heads each unless they say otherwise, us a call.
+static Q4Plan attend_q4_plan(const griffin_kv_cache_q4 &C, const griffin_kv_batch &B, const SeqTable &seqs, int32_t n_heads)
+{
+    Q4Plan pl = {};
     const bool bf16 = C.dtype == GRIFFIN_BF16;
-    const int widest = q4_widest(C);                       // tiles of 16 rows that the registers hold
+    const int widest = C.dim > 128 || (!bf16 && C.dim > 64) ? 1 : 2;         // tiles of 16 rows that the registers hold
     const int32_t group = n_heads / C.kv_heads;
     const int64_t rows = (int64_t)seqs.cu[seqs.n] * group;
     int64_t longest = 0;
     for (int b = 0; b < seqs.n; ++b)
         longest = std::max(longest, (int64_t)(seqs.cu[b + 1] - seqs.cu[b]) * group);
+    // Own parts of more than 64 rows go through LDS, 256 rows a workgroup.  (16 sequences of 200 to 2000 keys, there / here: 48 rows each 36 / 32, 80 rows 40 / 40, 128 rows 44 / 43, 192 rows 57 / 58,
+    // two of 3000 to 4000 keys and 48 to 192 rows the same within 3 %; 20 times 80 rows behind 300 shared keys, which they then take ahead of their own, 17 / 32.)  So does a
+    // prefix of more rows than that where there is enough to multiply.  (80 rows of 16384 keys 31 / 29, of 32768 42 / 45; 128 rows of 4096 26 / 17, of 32768 45 / 44; 320 rows of
+    // 1024 33 / 22, of 4096 38 / 32, of 32768 80 / 105.)
     pl.tile_own = bf16 && longest > 64;
     pl.tile_prefix = bf16 && (pl.tile_own || (rows > 64 && (double)rows * B.n_prefix * C.kv_heads * C.dim >= 0x1p31));
     pl.beside = pl.tile_prefix && !pl.tile_own && C.dim <= 128;
+    // A wavefront takes two tiles of 16 rows where it has the registers and the rows: codes are unpacked once for both.  (Own parts, two / one: 16 of 20 rows and 500 to 4000
+    // keys 26 / 32, 32 of 32 rows and 100 to 1000 keys 24.3 / 24.9; two of 48 rows and 4000 keys 18.9 / 17.6.)
     pl.nto = longest <= 16 || pl.beside ? 1 : widest;
     pl.ntp = rows <= 16 ? 1 : widest;
     if (!pl.tile_own && !pl.tile_prefix && pl.nto == widest)        // compiled pairs: (1, 1), (2, 1), (2, 2)
@@ -63,40 +93,56 @@ static AttPlan attend_q4_plan(const griffin_kv_cache_q4 &C, const griffin_kv_bat
         tiles += ((int64_t)(seqs.cu[b + 1] - seqs.cu[b]) * group + pl.rows_own - 1) / pl.rows_own;
     pl.tiles_own = (int32_t)tiles;
     pl.tiles_prefix = B.n_prefix > 0 ? (int32_t)((rows + pl.rows_prefix - 1) / pl.rows_prefix) : 0;
-    pl.lone = !pl.tile_own && C.kv_heads * tiles >= 1024 && B.max_len <= 256;
-    const int64_t step = ATT_WAVES * 32;
+    const int64_t step = ATT_WAVES * 32, all = (int64_t)B.n_prefix + B.max_len, items = C.kv_heads * tiles;
+    // Own parts that fill the chip as they are go a wavefront each, and parts so few and short that a step of twice as many wavefronts is cheaper than a second launch take the
+    // prefix, too, all in one launch: rules of the 16-bit cache (attend.hip), whose parts are as many steps long.
+    pl.lone = !pl.tile_own && items >= 1024 && B.max_len <= 256;
+    pl.few = longest <= 16 && !pl.tile_prefix && items <= 512 && all <= ATT_FEW_WAVES / ATT_WAVES * step && C.dim <= 128;
     const int64_t work_prefix = C.kv_heads * (int64_t)pl.tiles_prefix * B.n_prefix, work_own = C.kv_heads * tiles * B.max_len;
-    const auto chunk = [&](bool tile, int64_t work, int32_t keys, int64_t wgs) {   // no longer than the part: up to 2^30 keys and a quantum
-        const int64_t quantum = tile ? att_tile_keys(C.dim) : pl.beside ? ATT_FEW_WAVES / ATT_WAVES * step : step;
-        const int64_t even = std::min((work + wgs - 1) / wgs, (int64_t)keys);
+    const auto chunk = [&](int64_t quantum, int64_t work, int32_t keys) {    // for 256 workgroups; no longer than the part: up to 2^30 keys and a quantum
+        const int64_t even = std::min((work + 255) / 256, (int64_t)keys);
         return (int32_t)((std::max(even, (int64_t)1) + quantum - 1) / quantum * quantum);
     };
-    const bool together = pl.tile_prefix == pl.tile_own && !pl.lone;
-    const int64_t wgs_rows = C.dim > 128 ? 512 : 512;
-    pl.chunk_prefix = chunk(pl.tile_prefix, together && pl.tile_own ? work_prefix + work_own : work_prefix, B.n_prefix, pl.tile_prefix ? 256 : 512);
-    pl.chunk_own = chunk(pl.tile_own, together && pl.tile_own ? work_prefix + work_own : work_own, B.max_len, pl.tile_own ? 256 : pl.beside ? 1024 : wgs_rows);
-    if (pl.lone || (pl.tile_own && C.kv_heads * tiles > 128))
-        pl.chunk_own = (int32_t)((B.max_len + step - 1) / step * step);
-    const int64_t all = (int64_t)B.n_prefix + B.max_len, items = C.kv_heads * tiles;
-    pl.few = longest <= 16 && !pl.tile_prefix && items <= 512 && all <= ATT_FEW_WAVES / ATT_WAVES * step && C.dim <= 128;
-    const int64_t beyond = tiles - (rows + pl.rows_own - 1) / pl.rows_own;      // tiles more than all rows in a row would take
+    // The prefix: a workgroup a CU, two steps each at least of heads wider than 128.  (128 / 256 / 512 workgroups: 32 rows of 16384 keys 21 / 17 / 22, of 32768 31 / 22 / 25, 64 rows of 32768
+    // 48 / 32 / 31, 16 rows of 4096 11.8 / 13.3 / 13.0, 64 rows of 4096 16.0 / 15.5 / 19.8.  Through LDS, 256 / 512: 320 rows of 32768 84 / 96.  16 heads of 256, 5 rows of 1999: 15.9 /
+    // 22.0 / 21.7, which is two steps, one and one.)
+    pl.chunk_prefix = pl.tile_prefix ? chunk(att_tile_keys(C.dim), work_prefix + (pl.tile_own ? work_own : 0), B.n_prefix)
+                                     : chunk(C.dim > 128 ? 2 * step : step, work_prefix, B.n_prefix);
+    // Own items of many rows take the prefix ahead of their own keys where they fill the chip and it is not read much oftener for it, as there.
+    const int64_t beyond = tiles - (rows + pl.rows_own - 1) / pl.rows_own;   // tiles more than all rows in a row would take
     pl.ahead = B.n_prefix > 0 && (pl.few || (pl.tile_own && items > 128 && (4 * beyond <= tiles || beyond * B.n_prefix <= 16384)));
-    if (pl.ahead)
-        pl.tiles_prefix = 0;
     if (pl.ahead || pl.few)
         pl.chunk_own = (int32_t)((all + 15 + step - 1) / step * step);
+    else if (pl.tile_own && items <= 128)
+        pl.chunk_own = chunk(att_tile_keys(C.dim), work_prefix + work_own, B.max_len);
+    else
+        pl.chunk_own = (int32_t)((B.max_len + step - 1) / step * step);
+    if (pl.ahead)
+        pl.tiles_prefix = 0;
     pl.chunks_prefix = pl.ahead ? 0 : (B.n_prefix + pl.chunk_prefix - 1) / pl.chunk_prefix;
     pl.chunks_own = pl.ahead ? 1 : (B.max_len + pl.chunk_own - 1) / pl.chunk_own;
+    // Other own parts of a few rows, longer than a step, are cut by the device, which counts quanta in 32 bits: into 512 parts and more, behind tiles of the prefix 256.  (256 / 512 / 1024: 32
+    // sequences of 500 to 8000 keys 63 / 52 / 53, 64 of 100 to 4000 60 / 51 / 55, four of 500 to 30000 33 / 25 / 27, 16 of 20 rows and 500 to 4000 31 / 26 / 33, 8 of 100 to 4000 of 16 heads of 256 43 / 40 / 45;
+    // 48 of 5 to 700 behind 32768 66 / 66 / 69, 16 of five tokens there 79 / 81 / 82.  Cut by max_len instead, the best number of workgroups for each: 57, 58, 27, 33.)
+    pl.quantum = (int32_t)(pl.beside ? ATT_FEW_WAVES / ATT_WAVES * step : step);
+    pl.deal = -1;
+    if (!pl.tile_own && !pl.few && !pl.lone && B.max_len > pl.quantum && tiles * ((B.max_len + (int64_t)pl.quantum - 1) / pl.quantum) < (int64_t)1 << 31) {
+        pl.deal = pl.beside ? 8 : 9;
+        pl.parts = (((int64_t)1 << pl.deal) / C.kv_heads) + tiles;
+        pl.chunks_own = 0;
+    }
+    const int64_t row_heads = (int64_t)seqs.cu[seqs.n] * n_heads;
+    pl.slots_own = (row_heads * pl.chunks_prefix + 1) / 2 * 2;
+    if (pl.deal >= 0)
+        pl.floats = (size_t)(pl.slots_own + pl.parts * C.kv_heads * pl.rows_own) * (C.dim + 2) + 4 * seqs.n;
+    else if (pl.chunks_prefix + pl.chunks_own > 1)
+        pl.floats = (size_t)row_heads * (pl.chunks_prefix + pl.chunks_own) * (C.dim + 2);
     return pl;
 }
 
 size_t attend_q4_floats(const griffin_kv_cache_q4 &C, const griffin_kv_batch &B, const SeqTable &seqs, int32_t n_heads)
 {
-    if (!attend_takes(seqs, n_heads))
-        return 0;
-    const AttPlan pl = attend_q4_plan(C, B, seqs, n_heads);
-    const size_t slots = (size_t)seqs.cu[seqs.n] * n_heads * (pl.chunks_prefix + pl.chunks_own);
-    return pl.chunks_prefix + pl.chunks_own < 2 ? 0 : slots * (C.dim + 2);
+    return attend_takes(seqs, n_heads) ? attend_q4_plan(C, B, seqs, n_heads).floats : 0;
 }
 
 template <bool F32, int DB, int NTP, int NTO>
@@ -111,10 +157,10 @@ static int go_rows(const AttendQ4Params &p, bool lone, hipStream_t st)
 }
 
 template <bool F32, int DB>
-static int attend_typed(AttendQ4Params &p, const AttPlan &pl, hipStream_t st)
+static int attend_typed(AttendQ4Params &p, const Q4Plan &pl, hipStream_t st)
 {
     int rc = GRIFFIN_OK;
-    const int32_t wgs_prefix = p.kv_heads * pl.tiles_prefix * pl.chunks_prefix, wgs_own = p.kv_heads * pl.tiles_own * pl.chunks_own;
+    const int32_t wgs_prefix = p.kv_heads * pl.tiles_prefix * pl.chunks_prefix, wgs_own = p.kv_heads * (int32_t)(pl.deal < 0 ? (int64_t)pl.tiles_own * pl.chunks_own : pl.parts);
     const int32_t tiled = (pl.tile_prefix ? wgs_prefix : 0) + (pl.tile_own ? wgs_own : 0), others = wgs_prefix + wgs_own - tiled;
     if constexpr (!F32)
         if (tiled > 0) {
@@ -143,11 +189,11 @@ static int attend_typed(AttendQ4Params &p, const AttPlan &pl, hipStream_t st)
         } else
             rc = go_rows<F32, DB, 1, 1>(p, pl.lone, st);
     }
-    return rc == GRIFFIN_OK && p.part ? launch_attend_join(p, !F32, st) : rc;
+    return rc == GRIFFIN_OK && p.part ? launch_attend_join(p, !F32, pl.chunks_prefix + (pl.deal < 0 ? pl.chunks_own : (1 << pl.deal) / p.kv_heads / pl.tiles_own), st) : rc;
 }
 
 template <bool F32>
-static int attend_width(AttendQ4Params &p, const AttPlan &pl, hipStream_t st)
+static int attend_width(AttendQ4Params &p, const Q4Plan &pl, hipStream_t st)
 {
     if (p.dim <= 64)
         return attend_typed<F32, 64>(p, pl, st);
@@ -159,14 +205,21 @@ int launch_attend_q4(const AttendQ4Job &job, const SeqTable &seqs, hipStream_t s
     const griffin_kv_cache_q4 &C = job.C;
     if (!attend_takes(seqs, job.n_heads))
         return GRIFFIN_EUNSUPPORTED;
-    const AttPlan pl = attend_q4_plan(C, job.B, seqs, job.n_heads);
-    if (!att_launch_fits(pl, C.kv_heads))
+    const Q4Plan pl = attend_q4_plan(C, job.B, seqs, job.n_heads);
+    if (!att_launch_fits(pl, C.kv_heads) || (pl.deal >= 0 && (pl.parts * C.kv_heads >= 1 << 23 || pl.parts * C.kv_heads * C.kv_heads >= (int64_t)1 << 32)))
         return GRIFFIN_EUNSUPPORTED;
     AttendQ4Params p = {};
     p.q = job.q; p.K = C.K; p.V = C.V; p.out = job.out;
     p.ldq = job.ldq; p.hsq = job.hsq; p.ldo = job.ldo; p.hso = job.hso;
     att_set_up(p, pl, job.B, seqs, job.n_heads, C.kv_heads, C.dim, C.page_size, C.n_pages, job.scale, job.ws);
     p.s = q4_shape(C);
+    p.deal = pl.deal; p.quantum = pl.quantum; p.rows_own = pl.rows_own; p.slots_own = pl.slots_own;
+    if (pl.deal >= 0) {
+        const int64_t slots = pl.slots_own + pl.parts * C.kv_heads * pl.rows_own;
+        p.part = job.ws;
+        p.part_ml = (float2 *)(job.ws + slots * C.dim);
+        p.cuts = (int4 *)(p.part_ml + slots);              // an even number of slots: 16 bytes
+    }
     return C.dtype == GRIFFIN_BF16 ? attend_width<false>(p, pl, st) : attend_width<true>(p, pl, st);
 }
 

@@ -140,6 +140,7 @@ struct TileQ4 {
                 r.o[n][e] = first ? att_f32x4{v[0], v[2], a, b} : att_f32x4{a, b, v[1], v[3]};
             }
     }
+    static __device__ __forceinline__ bool own_item(const AttendQ4Params &p, int32_t id, AttendItem &it) { return q4_own_item<16>(p, id, it); }
     template <int WAVES>
     static __device__ __forceinline__ void own_rows(const AttendQ4Params &p, float *lds, const AttendItem &it)
     {

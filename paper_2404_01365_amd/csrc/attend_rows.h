@@ -290,6 +290,8 @@ __device__ __forceinline__ void att_add_infinite(const AttendParams &p, const At
 // Where a row's sums of a chunk lie
 __device__ __forceinline__ int64_t att_slot(const AttendParams &p, const AttendItem &it, int32_t row)
 {
+    if (it.slot0 >= 0)
+        return it.slot0 + row - it.first;
     const int32_t token = p.by_group(row), head = it.hk * p.group + row - token * p.group;
     return ((int64_t)(it.token0 + token) * p.n_heads + head) * (p.chunks_prefix + p.chunks_own) + it.split;
 }
@@ -300,7 +302,7 @@ __device__ __forceinline__ void att_store8(const AttendParams &p, const AttendIt
 {
     if (!FULL && d >= p.dim)
         return;
-    if (p.part) {
+    if (p.part && !it.alone) {
         float *at = p.part + att_slot(p, it, row) * p.dim + d;
         *(float4 *)at = make_float4(x[0], x[1], x[2], x[3]);
         *(float4 *)(at + 4) = make_float4(x[4], x[5], x[6], x[7]);
@@ -334,7 +336,7 @@ __device__ __forceinline__ void att_finish(const AttendParams &p, float *lds, co
             const int32_t row = first + 16 * n + (lane & 15);
             if (row >= rows)
                 continue;
-            if (p.part && lane < 16)
+            if (p.part && !it.alone && lane < 16)
                 p.part_ml[att_slot(p, it, row)] = make_float2(m_of[n], sum[n]);
 #pragma unroll
             for (int c = 0; c < S::NC; ++c)
@@ -396,7 +398,7 @@ __device__ __forceinline__ void att_finish(const AttendParams &p, float *lds, co
                         x[j] += from[j] * f;
                 }
                 const int32_t row = first + 16 * n + at;
-                if (p.part && part == 0 && d == 0)
+                if (p.part && !it.alone && part == 0 && d == 0)
                     p.part_ml[att_slot(p, it, row)] = make_float2(m, l);
                 att_store8<BF16, FULL>(p, it, row, part * W + d, x, l);
             }

@@ -7,7 +7,7 @@
 //   load_row                 a row's queries
 //   add_odd                  infinite and NaN values that were made zero in the steps of [key, most), added to the rows that see them
 //   order                    the features of o as they are stored: element i of o[n][e] is feature 16 e + 4 (lane >> 4) + i
-//   own_rows                 a few rows of an own part, by a workgroup or a wavefront
+//   own_item, own_rows       the id-th own part of a few rows (false: no row needs it), and the work on it, by a workgroup or a wavefront
 #pragma once
 
 #include "attend_rows.h"
@@ -214,7 +214,7 @@ __global__ __launch_bounds__(64 * ATT_TILE_WAVES) void attend_tile_kernel(typena
         int32_t id = blockIdx.x - p.wgs_prefix;
         if (OWN == OWN_EACH)
             id = id * ATT_TILE_WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        if (id < p.items_own && att_own_item<16, false>(p, id, it))
+        if (id < p.items_own && F::own_item(p, id, it))
             F::template own_rows<OWN == OWN_EACH ? 1 : ATT_TILE_WAVES>(p, (float *)tile_lds, it);
         return;
     }

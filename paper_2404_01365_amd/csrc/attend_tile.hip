@@ -156,6 +156,7 @@ struct TileBf16 {
         tile_add_infinite<DB, FULL>(p, it, r, key, most);
     }
     static __device__ __forceinline__ void order(Rows &) {}
+    static __device__ __forceinline__ bool own_item(const AttendParams &p, int32_t id, AttendItem &it) { return att_own_item<16, false>(p, id, it); }
     template <int WAVES>
     static __device__ __forceinline__ void own_rows(const AttendParams &p, float *lds, const AttendItem &it)
     {

@@ -1,9 +1,9 @@
 // A step's keys and values into a cache in 4 bits (griffin_kv_append_q4), and out of one (griffin_kv_read_q4).
 //
 // c = round((x - m) / s) with s = fp16((hi - lo) / 15), m = fp16(lo + 8 s) of a group's least and greatest value.  A thread takes eight features, a word of
-// codes; a group's threads are neighbouring lanes, which exchange lo and hi.  Keys are rotated in 64 bits, where products of two fp32 are exact, and a code is taken
-// from the quotient in 64 bits: a value next to the border of two codes falls to the side that the definition says, not to one that the order of fp32 operations
-// chooses.  Few are that near: a quotient in fp32 decides the others.
+// codes; a group's threads are neighbouring lanes, which exchange lo and hi.  By its definition all of it is computed in 64 bits: a value next to the border of two codes falls to
+// the side that the definition says, not to one that the order of fp32 operations chooses.  Few are that near, so everything is computed in fp32 with a bound on how far off it
+// is, and in 64 bits only by wavefronts where a rounding lies within that bound.
 #include "q4.h"
 
 namespace griffin {
@@ -63,17 +63,38 @@ __device__ __forceinline__ void q4_store8(void *p, int64_t i, const float (&x)[8
     }
 }
 
-// a value of the lane l ^ 1, 2 or 4 of a row of eight
+// a word, or a value, of the lane l ^ 1, 2 or 4 of a row of eight
+template <int STEP>
+__device__ __forceinline__ uint32_t q4_other(uint32_t w)
+{
+    // row_half_mirror exchanges lanes l and 7 - l: the four of each half have the same value by then
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w, STEP == 1 ? 0xB1 : STEP == 2 ? 0x4E : 0x141, 0xF, 0xF, true);
+}
+
+template <int STEP>
+__device__ __forceinline__ float q4_other(float v) { return __uint_as_float(q4_other<STEP>(__float_as_uint(v))); }
+
 template <int STEP>
 __device__ __forceinline__ double q4_other(double v)
 {
     const uint64_t b = __builtin_bit_cast(uint64_t, v);
-    const auto move = [](uint32_t w) {
-        // row_half_mirror exchanges lanes l and 7 - l: the four of each half have the same value by then
-        return (uint64_t)(uint32_t)__builtin_amdgcn_update_dpp(0, (int)w, STEP == 1 ? 0xB1 : STEP == 2 ? 0x4E : 0x141, 0xF, 0xF, true);
-    };
-    return __builtin_bit_cast(double, move((uint32_t)b) | move((uint32_t)(b >> 32)) << 32);
+    return __builtin_bit_cast(double, (uint64_t)q4_other<STEP>((uint32_t)b) | (uint64_t)q4_other<STEP>((uint32_t)(b >> 32)) << 32);
 }
+
+// the least, the greatest of a group's
+__device__ __forceinline__ float q4_min(float a, float b) { return fminf(a, b); }
+__device__ __forceinline__ double q4_min(double a, double b) { return fmin(a, b); }
+
+template <bool WIDE, class T>
+__device__ __forceinline__ T q4_group_min(T v)
+{
+    v = q4_min(v, q4_other<1>(v));
+    v = q4_min(v, q4_other<2>(v));
+    return WIDE ? q4_min(v, q4_other<4>(v)) : v;
+}
+
+template <bool WIDE, class T>
+__device__ __forceinline__ T q4_group_max(T v) { return -q4_group_min<WIDE>(-v); }
 
 // To fp16 by way of fp32, two instructions.  The compiler makes one rounding of it by some forty, which gives another result where fp32 falls between two fp16.
 __device__ __forceinline__ _Float16 q4_half(double v)
@@ -83,9 +104,19 @@ __device__ __forceinline__ _Float16 q4_half(double v)
     return (_Float16)f;
 }
 
-// Quantises a thread's eight features (zeros and `in` false behind the head's last) and stores their codes and, one thread a group, the scale and middle.
+// What a thread has of its head's codes: a word, and its group's (scale, middle) word
+struct Q4Out {
+    uint32_t codes, pair;
+};
+
+__device__ __forceinline__ uint32_t q4_pair_word(_Float16 scale, _Float16 middle)
+{
+    return (uint32_t)__builtin_bit_cast(uint16_t, scale) | (uint32_t)__builtin_bit_cast(uint16_t, middle) << 16;
+}
+
+// The definition, in 64 bits; `in`: the features are the head's
 template <bool WIDE>
-__device__ __forceinline__ void q4_store_codes(const Q4Shape &s, char *head, uint32_t slot, int i, bool in, bool store, const double (&x)[8])
+__device__ __forceinline__ Q4Out q4_quantise_exactly(const double (&x)[8], bool in)
 {
     double lo = 32768, hi = -32768;        // no value is outside
     bool odd = false;
@@ -96,44 +127,64 @@ __device__ __forceinline__ void q4_store_codes(const Q4Shape &s, char *head, uin
         lo = fmin(lo, c);
         hi = fmax(hi, c);
     }
-    if (!in) {
-        lo = 32768;
-        hi = -32768;
-        odd = false;
-    }
-    // a group that holds a value that is not finite is marked by a range no other has
-    hi = odd ? 1e9 : hi;
-    lo = fmin(lo, q4_other<1>(lo)); hi = fmax(hi, q4_other<1>(hi));
-    lo = fmin(lo, q4_other<2>(lo)); hi = fmax(hi, q4_other<2>(hi));
-    if (WIDE) {
-        lo = fmin(lo, q4_other<4>(lo)); hi = fmax(hi, q4_other<4>(hi));
-    }
+    lo = in ? lo : 32768.0;
+    hi = in ? odd ? 1e9 : hi : -32768.0;   // a group that holds a value that is not finite is marked by a range no other has
+    lo = q4_group_min<WIDE>(lo);
+    hi = q4_group_max<WIDE>(hi);
     odd = hi > 1e8;
     const _Float16 scale = q4_half((hi - lo) / 15.0);
     const double step = (double)(float)scale;
     const _Float16 middle = q4_half(lo + 8.0 * step);
     const double mid = (double)(float)middle;
-    const float inv = 1.0f / (float)step;
     const bool flat = odd || !(step > 0);
     uint32_t codes = 0;
-#pragma unroll
+#pragma unroll 1
     for (int j = 0; j < 8; ++j) {
         const double d = fmin(fmax(x[j], -32768.0), 32768.0) - mid;
-        const float t = (float)d * inv;    // at most 9 or so, off by less than 2e-6
-        float c = rintf(t);
-        if (!flat && 0.5f - fabsf(t - c) < 8e-6f)
-            c = (float)rint(d / step);
-        c = flat ? 0.0f : fminf(fmaxf(c, -8.0f), 7.0f);
+        const double c = flat ? 0.0 : fmin(fmax(rint(d / step), -8.0), 7.0);
         codes |= (uint32_t)((int)c + 8) << 4 * j;
     }
-    if (!store)
-        return;
-    if ((uint32_t)i * 4 < s.row_bytes)
-        *(uint32_t *)(head + slot * s.row_bytes + i * 4) = in ? codes : 0;
-    if (in && (i & (WIDE ? 7 : 3)) == 0) {
-        const uint32_t pair = odd ? 0x7E00u : (uint32_t)__builtin_bit_cast(uint16_t, scale) | (uint32_t)__builtin_bit_cast(uint16_t, middle) << 16;
-        *(uint32_t *)(head + s.pairs_at + (slot * s.groups + (i >> (WIDE ? 3 : 2))) * 4) = pair;
+    return {codes, odd ? 0x7E00u : q4_pair_word(scale, middle)};
+}
+
+// The same in fp32, from values that are up to `off` from the exact ones: false where a rounding to fp16, or a code, could be another, where values are cut to the
+// format's range or are not finite.
+template <bool WIDE>
+__device__ __forceinline__ bool q4_quantise_fast(const float (&x)[8], float off, bool in, Q4Out &out)
+{
+    float lo = INFINITY, hi = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        lo = fminf(lo, x[j]);
+        hi = fmaxf(hi, x[j]);
     }
+    lo = q4_group_min<WIDE>(in ? lo : INFINITY);
+    hi = q4_group_max<WIDE>(in ? hi : -INFINITY);
+    off = q4_group_max<WIDE>(off);
+    // s: the difference and the product are off by 2^-24 of themselves, 1 / 15 as well.  m: what the sum has lost is known, and often nothing: values of few bits, as bf16 are, would
+    // else be taken for ones next to a rounding's border whenever they lie on it.  t: the reciprocal is off by 2^-23 of itself, which counts for x and for the middle, at most as large
+    // as the greatest value and four steps, and each product and sum by 2^-24 of itself.  A little more is allowed for each.
+    const float size = fmaxf(fabsf(lo), fabsf(hi));
+    const float s = (hi - lo) * (1.0f / 15.0f), se = off * 0.14f + 0x1p-22f * fabsf(s);
+    const _Float16 scale = (_Float16)(s - se), above = (_Float16)(s + se);
+    const float step = (float)scale, m = lo + 8.0f * step, part = m - lo;
+    const float me = off + 1.01f * fabsf((lo - (m - part)) + (8.0f * step - part));
+    const _Float16 middle = (_Float16)(m - me), beyond = (_Float16)(m + me);
+    const float inv = __builtin_amdgcn_rcpf(step), shift = 8.0f - (float)middle * inv;
+    const float near = 0.5f - (1.01f * off * inv + 0x1p-21f * size * inv + 4e-6f);
+    bool sure = scale == above && middle == beyond && size + off <= 32768.0f && step > 0;      // infinities: not sure
+    // codes of even and of odd features in bytes, by a conversion that takes a number into a byte of a word
+    uint32_t even = 0, odd = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float t = x[j] * inv + shift, c = rintf(t);
+        sure &= fabsf(t - c) < near;                       // NaN: not sure
+        uint32_t &word = j & 1 ? odd : even;
+        word = __builtin_amdgcn_cvt_pk_u8_f32(fminf(c, 15.0f), j / 2, word);
+    }
+    const uint32_t codes = even | odd << 4;
+    out = {codes, q4_pair_word(scale, middle)};
+    return sure || !in;
 }
 
 // Heads of keys, of values, then of queries; a thread's item is eight features of one.  FAST: all of a thread's eight are rotated or none is, and cos and sin
@@ -145,46 +196,44 @@ __global__ __launch_bounds__(256) void kv_append_q4_kernel(AppendQ4Params p)
     const int item = (blockIdx.x % p.blocks) * 256 + threadIdx.x, head = item >> p.lanes_shift, i = item & ((1 << p.lanes_shift) - 1);
     if (head >= 2 * p.s.kv_heads + p.n_heads)
         return;                            // whole heads leave
-    const int b = q4_sequence(p.seqs, p.each, token);
-    const int32_t held = p.lens[b] < 0 ? 0 : p.lens[b];
-    const int64_t slot = (int64_t)held + token - p.seqs.cu[b];
-    const int64_t pos = slot + p.n_prefix < p.n_pos ? slot + p.n_prefix : p.n_pos - 1;
-    const bool room = slot < p.max_len;    // else no slot: only the query is of use
     const bool is_k = head < p.s.kv_heads, is_q = head >= 2 * p.s.kv_heads;
     const int h = is_k ? head : is_q ? head - 2 * p.s.kv_heads : head - p.s.kv_heads;
     const void *src = is_k ? p.k : is_q ? p.q : p.v;
     const int64_t from = is_k ? token * p.ldk + h * p.hsk : is_q ? token * p.ldq + h * p.hsq : token * p.ldv + h * p.hsv;
     const int f = i * 8;
     const bool in = f < p.dim;
-    float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (in)
-        q4_load8<BF16>(src, from + f, x);
-    double y[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-        y[j] = x[j];
-    if ((is_k || is_q) && in && f < 2 * p.half) {
-        // feature a of a pair becomes a cos - b sin, feature b becomes b cos + a sin: with the other one of a pair in z, x cos + z sin with sin's sign
-        float z[8], c[8], s[8];
+    float x[8], z[8], c[8], s[8];
+    q4_load8<BF16>(src, from + (in ? f : 0), x);
+    // places are looked up while that is on its way
+    const int b = q4_sequence(p.seqs, p.each, token);
+    const int32_t held = p.lens[b] < 0 ? 0 : p.lens[b];
+    const int64_t slot = (int64_t)held + token - p.seqs.cu[b];
+    const int64_t pos = slot + p.n_prefix < p.n_pos ? slot + p.n_prefix : p.n_pos - 1;
+    const bool room = slot < p.max_len;    // else no slot: only the query is of use
+    const int64_t page = room ? page_of(p.pages + (int64_t)b * p.ld_pages, (int32_t)(slot >> p.s.page_shift), p.s.last_page) : 0;
+    // feature a of a pair becomes a cos - b sin, feature b becomes b cos + a sin: with the other one of a pair in z, x cos + z sin with sin's sign
+    const bool rotated = (is_k || is_q) && in && f < 2 * p.half;
+    const auto turned = [&](int j) { return FAST || f + j < 2 * p.half; };     // else the feature stays as it is: z sin could be 0 x Inf
+    float y[8], off = 0;
+    if (rotated) {
         const float *cs = p.cos + pos * p.half, *sn = p.sin + pos * p.half;
         if constexpr (PAIRS) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                z[j] = x[j ^ 1];
+            float c4[4], s4[4];
             if (FAST) {
-                *(float4 *)c = *(const float4 *)(cs + f / 2);
-                *(float4 *)s = *(const float4 *)(sn + f / 2);
+                *(float4 *)c4 = *(const float4 *)(cs + f / 2);
+                *(float4 *)s4 = *(const float4 *)(sn + f / 2);
             } else
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const int e = f / 2 + j < p.half ? f / 2 + j : p.half - 1;
-                    c[j] = cs[e];
-                    s[j] = sn[e];
+                    c4[j] = cs[e];
+                    s4[j] = sn[e];
                 }
 #pragma unroll
-            for (int j = 7; j >= 0; --j) {
-                c[j] = f + j < 2 * p.half ? c[j / 2] : 1.0f;
-                s[j] = f + j < 2 * p.half ? (j & 1 ? s[j / 2] : -s[j / 2]) : 0.0f;
+            for (int j = 0; j < 8; ++j) {
+                z[j] = x[j ^ 1];
+                c[j] = c4[j / 2];
+                s[j] = j & 1 ? s4[j / 2] : -s4[j / 2];
             }
         } else if (FAST) {
             const bool first = f < p.half;
@@ -198,30 +247,48 @@ __global__ __launch_bounds__(256) void kv_append_q4_kernel(AppendQ4Params p)
         } else
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const bool turned = f + j < 2 * p.half, first = f + j < p.half;
-                const int e = turned ? (first ? f + j : f + j - p.half) : 0;
-                z[j] = turned ? load_scalar<BF16>(src, from + (first ? f + j + p.half : e)) : 0.0f;
-                c[j] = turned ? cs[e] : 1.0f;
-                s[j] = turned ? (first ? -sn[e] : sn[e]) : 0.0f;
+                const bool first = f + j < p.half;
+                const int e = turned(j) ? (first ? f + j : f + j - p.half) : 0;
+                z[j] = turned(j) ? load_scalar<BF16>(src, from + (first ? f + j + p.half : e)) : 0.0f;
+                c[j] = cs[e];
+                s[j] = first ? -sn[e] : sn[e];
             }
+        // off by half a last place of the second product, and of the sum
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const bool turned = FAST || f + j < 2 * p.half;          // 0 x Inf for those that stay as they are
-            if (is_q)
-                x[j] = turned ? x[j] * c[j] + z[j] * s[j] : x[j];
-            else
-                y[j] = turned ? (double)x[j] * (double)c[j] + (double)z[j] * (double)s[j] : y[j];
+            const float second = z[j] * s[j];
+            y[j] = turned(j) ? __builtin_fmaf(x[j], c[j], second) : x[j];
+            off = fmaxf(off, turned(j) ? fabsf(second) + fabsf(y[j]) : 0.0f);
         }
-    }
+        off *= 0x1.01p-24f;
+    } else
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            y[j] = x[j];
     if (is_q) {                            // q_out may be q: all of a head's threads have loaded by now, as they are of one wavefront
         if (in)
-            q4_store8<BF16>(p.q_out, token * p.ldo + h * p.hso + f, x);
+            q4_store8<BF16>(p.q_out, token * p.ldo + h * p.hso + f, y);
         return;
     }
-    char *at = is_k ? p.K : p.V;
-    if (room)
-        at += (page_of(p.pages + (int64_t)b * p.ld_pages, (int32_t)(slot >> p.s.page_shift), p.s.last_page) * p.s.kv_heads + h) * p.s.head_bytes;
-    q4_store_codes<WIDE>(p.s, at, (uint32_t)(slot & ((1 << p.s.page_shift) - 1)), i, in, room, y);
+    Q4Out out;
+    const bool sure = q4_quantise_fast<WIDE>(y, off, in, out);
+    if (__any(!sure)) {                    // one wavefront in ten or so, of keys
+        double exact[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            asm volatile("" : "+v"(x[j]), "+v"(z[j]), "+v"(c[j]), "+v"(s[j]));        // here, not ahead of the branch for everyone
+            exact[j] = rotated && turned(j) ? (double)x[j] * (double)c[j] + (double)z[j] * (double)s[j] : (double)x[j];
+        }
+        out = q4_quantise_exactly<WIDE>(exact, in);
+    }
+    if (!room)
+        return;
+    char *at = (is_k ? p.K : p.V) + (page * p.s.kv_heads + h) * p.s.head_bytes;
+    const uint32_t row = (uint32_t)(slot & ((1 << p.s.page_shift) - 1));
+    if ((uint32_t)i * 4 < p.s.row_bytes)
+        *(uint32_t *)(at + row * p.s.row_bytes + i * 4) = in ? out.codes : 0;
+    if (in && (i & (WIDE ? 7 : 3)) == 0)
+        *(uint32_t *)(at + p.s.pairs_at + (row * p.s.groups + (i >> (WIDE ? 3 : 2))) * 4) = out.pair;
 }
 
 template <bool BF16, bool PAIRS, bool FAST>
