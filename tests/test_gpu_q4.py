@@ -273,67 +273,6 @@ def test_attention_of_a_prompt_alone_and_row_by_row():
         one = plain.Case(15, heads=8, kv_heads=2, dim=128, page=16, prefix=0, held=[0], new=[90], dtype=BF16)
         one.q, one.cu, one.lens = c.q[i:i + 1], [0, 1], [i]
         alone = run_attention(one, K, V, 32)[0]
-        # weights are cut apart from each other (2^-10 each way) and rounded to bf16 twice
-        assert np.all(np.abs(alone - together[i]) <= 2.0 ** -7 * np.abs(alone) + 2.0 ** -8)
-
-
-@pytest.mark.parametrize("dim", [64, 128, 256])
-@pytest.mark.parametrize("prefix", [1, 64, 70])
-def test_attention_of_prompts_that_fill_the_chip_behind_a_prefix(dim, prefix):
-    check_attention(16, heads=22, kv_heads=22, dim=dim, page=16, prefix=prefix, held=[0, 20, 5], new=[130, 257, 270], dtype=BF16)
-
-
-@pytest.mark.parametrize("heads,kv_heads,dim,prefix,held,new", [
-    (16, 2, 128, 9000, [0, 300, 31, 5, 64, 200, 7, 90, 3], [1, 1, 1, 2, 1, 1, 1, 1, 2]),          # 88 rows a kv head, own parts a workgroup each
-    (16, 8, 64, 20000, [int(x) for x in np.random.default_rng(3).integers(0, 200, 130)], [1] * 130),     # ... a wavefront each
-    (40, 1, 96, 70000, [0, 9], [1, 1]),
-    (20, 1, 256, 40000, [30, 1], [3, 1])])
-def test_attention_of_own_parts_beside_tiles_of_the_prefix(heads, kv_heads, dim, prefix, held, new):
-    check_attention(17, heads=heads, kv_heads=kv_heads, dim=dim, page=64, prefix=prefix, held=held, new=new, dtype=BF16)
-
-
-@pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("dim", [64, 128, 256])
-def test_groups_of_nan_in_prompts_behind_a_prefix(dtype, dim):
-    """... in the prefix (everyone sees them), beside the place where it ends, and among a prompt's own keys"""
-    c = plain.Case(18, heads=32, kv_heads=32, dim=dim, page=16, prefix=21, held=[0, 6], new=[260, 40], dtype=dtype)
-    clean = q4_plain.pool_of(c.K, 32), q4_plain.pool_of(c.V, 32)
-    ref, size = reference(c, *clean, 32, None)
-    V = np.array(clean[1])
-    row, groups = q4_plain.sizes(dim, 32)
-
-    def spoil(page, slot, head, g):
-        V.reshape(V.shape[0], 32, -1)[page, head][16 * row:].view(np.float16).reshape(16, groups, 2)[slot, g] = np.float16(np.nan), np.float16(0)
-
-    spoil(c.prefix_pages[1], 4, 3, 0)                    # the prefix's last key
-    for i, head, g in ((0, 5, 1), (200, 7, 0), (259, 9, groups - 1)):
-        spoil(c.pages[0, i // 16], i % 16, head, g)
-    spoil(c.pages[1, (6 + 39) // 16], (6 + 39) % 16, 11, 0)
-    got = run_attention(c, clean[0], V, 32)
-    want = ref.copy()
-    want[:, 3, :32] = np.nan
-    want[0:260, 5, 32:64] = want[200:260, 7, :32] = want[259, 9, dim - 32:] = want[299, 11, :32] = np.nan
-    odd = np.isnan(want)
-    assert np.array_equal(np.isnan(got), odd)
-    attention_close(np.where(odd, 0, got), np.where(odd, 0, want), size, dtype)
-
-
-@pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("dim", [40, 64, 96, 128, 200, 256])
-def test_attention_of_ragged_prompts(dtype, dim):
-    check_attention(13, heads=10, kv_heads=2, dim=dim, page=16, prefix=0, held=[0, 3, 0, 40, 0, 9], new=[150, 70, 13, 64, 0, 129], dtype=dtype)
-    check_attention(14, heads=4, kv_heads=1, dim=dim, page=32, prefix=77, held=[0, 3, 0, 250], new=[160, 70, 33, 64], dtype=dtype, group=64)
-
-
-def test_attention_of_a_prompt_alone_and_row_by_row():
-    """The rows of a prompt in one call (through LDS) and one token a call (straight from memory)"""
-    c = plain.Case(15, heads=8, kv_heads=2, dim=128, page=16, prefix=0, held=[0], new=[90], dtype=BF16)
-    K, V = q4_plain.pool_of(c.K, 32), q4_plain.pool_of(c.V, 32)
-    together = run_attention(c, K, V, 32)
-    for i in (0, 1, 31, 32, 63, 64, 89):
-        one = plain.Case(15, heads=8, kv_heads=2, dim=128, page=16, prefix=0, held=[0], new=[90], dtype=BF16)
-        one.q, one.cu, one.lens = c.q[i:i + 1], [0, 1], [i]
-        alone = run_attention(one, K, V, 32)[0]
         # the output's rounding to bf16 twice, and weights that are cut apart from each other, 2^-10 of values below 5
         assert np.all(np.abs(alone - together[i]) <= 2.0 ** -7 * np.abs(alone) + 2.0 ** -10 * 2 * 5)
 
@@ -341,7 +280,7 @@ def test_attention_of_a_prompt_alone_and_row_by_row():
 @pytest.mark.parametrize("dim", [64, 128, 256])
 @pytest.mark.parametrize("prefix", [1, 64, 70])
 def test_attention_of_prompts_that_fill_the_chip_behind_a_prefix(dim, prefix):
-    check_attention(16, heads=22, kv_heads=22, dim=dim, page=16, prefix=prefix, held=[0, 20, 5], new=[130, 257, 270], dtype=BF16)
+    check_attention(16, heads=28, kv_heads=28, dim=dim, page=16, prefix=prefix, held=[0, 20, 5], new=[130, 257, 270], dtype=BF16)
 
 
 @pytest.mark.parametrize("heads,kv_heads,dim,prefix,held,new", [
