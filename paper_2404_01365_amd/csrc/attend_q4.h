@@ -569,7 +569,9 @@ __device__ __forceinline__ void attend_q4(const AttendQ4Params &p, float *lds, c
     att_finish<!F32, S, DB, false, NT, WAVES>(p, lds, it, r.m, sum, r.o);
 }
 
-// launches the `wgs` workgroups of p on tiles of att_tile_rows(dim) rows, and behind them p.items_own own items of 16 rows, a workgroup each or, `each`, a
+constexpr int Q4_TILE_WAVES = 4;         // of a workgroup of attend_q4_tile.hip
+constexpr int q4_tile_rows(int32_t dim) { return 16 * Q4_TILE_WAVES * (dim > 128 ? 1 : 2); }
+// launches the `wgs` workgroups of p on tiles of q4_tile_rows(dim) rows, and behind them p.items_own own items of 16 rows, a workgroup each or, `each`, a
 // wavefront each (dim <= 128); bf16 outside the cache only
 int launch_attend_q4_tiles(const AttendQ4Params &p, int32_t wgs, bool each, hipStream_t st);
 

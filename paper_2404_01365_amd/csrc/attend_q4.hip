@@ -73,12 +73,12 @@ static Q4Plan attend_q4_plan(const griffin_kv_cache_q4 &C, const griffin_kv_batc
     int64_t longest = 0;
     for (int b = 0; b < seqs.n; ++b)
         longest = std::max(longest, (int64_t)(seqs.cu[b + 1] - seqs.cu[b]) * group);
-    // Own parts of more than 64 rows go through LDS, 256 rows a workgroup.  (16 sequences of 200 to 2000 keys, there / here: 48 rows each 36 / 32, 80 rows 40 / 40, 128 rows 44 / 43, 192 rows 57 / 58,
-    // two of 3000 to 4000 keys and 48 to 192 rows the same within 3 %; 20 times 80 rows behind 300 shared keys, which they then take ahead of their own, 17 / 32.)  So does a
-    // prefix of more rows than that where there is enough to multiply.  (80 rows of 16384 keys 31 / 29, of 32768 42 / 45; 128 rows of 4096 26 / 17, of 32768 45 / 44; 320 rows of
-    // 1024 33 / 22, of 4096 38 / 32, of 32768 80 / 105.)
+    // Own parts of more than 64 rows go through LDS, 128 rows a workgroup.  (16 sequences of 200 to 2000 keys, there / here: 48 rows each 34 / 32, 80 rows 37 / 39, 128 rows 42 / 43, 192 rows 60 / 58,
+    // two of 3000 to 4000 keys and 64 to 192 rows the same within 6 %; 20 times 80 rows behind 300 shared keys, which they then take ahead of their own, 18 / 32.)  So does a
+    // prefix of more rows than that where there is enough to multiply.  (80 rows of 16384 keys 31 / 28, of 32768 37 / 46; 128 rows of 4096 28 / 18, of 16384 34 / 31, of 32768 44 / 44; 192 of 8192 32 / 34,
+    // of 16384 40 / 54; 320 rows of 1024 26 / 22, of 4096 30 / 32, of 8192 38 / 49.)
     pl.tile_own = bf16 && longest > 64;
-    pl.tile_prefix = bf16 && (pl.tile_own || (rows > 64 && (double)rows * B.n_prefix * C.kv_heads * C.dim >= 0x1p31));
+    pl.tile_prefix = bf16 && (pl.tile_own || (rows > 64 && (double)rows * B.n_prefix * C.kv_heads * C.dim > 0x1p31));
     pl.beside = pl.tile_prefix && !pl.tile_own && C.dim <= 128;
     // A wavefront takes two tiles of 16 rows where it has the registers and the rows: codes are unpacked once for both.  (Own parts, two / one: 16 of 20 rows and 500 to 4000
     // keys 26 / 32, 32 of 32 rows and 100 to 1000 keys 24.3 / 24.9; two of 48 rows and 4000 keys 18.9 / 17.6.)
@@ -86,8 +86,8 @@ static Q4Plan attend_q4_plan(const griffin_kv_cache_q4 &C, const griffin_kv_batc
     pl.ntp = rows <= 16 ? 1 : widest;
     if (!pl.tile_own && !pl.tile_prefix && pl.nto == widest)        // compiled pairs: (1, 1), (2, 1), (2, 2)
         pl.ntp = widest;
-    pl.rows_own = pl.tile_own ? att_tile_rows(C.dim) : 16 * pl.nto;
-    pl.rows_prefix = pl.tile_prefix ? att_tile_rows(C.dim) : 16 * pl.ntp;
+    pl.rows_own = pl.tile_own ? q4_tile_rows(C.dim) : 16 * pl.nto;
+    pl.rows_prefix = pl.tile_prefix ? q4_tile_rows(C.dim) : 16 * pl.ntp;
     int64_t tiles = 0;
     for (int b = 0; b < seqs.n; ++b)
         tiles += ((int64_t)(seqs.cu[b + 1] - seqs.cu[b]) * group + pl.rows_own - 1) / pl.rows_own;
@@ -98,23 +98,39 @@ static Q4Plan attend_q4_plan(const griffin_kv_cache_q4 &C, const griffin_kv_batc
     // prefix, too, all in one launch: rules of the 16-bit cache (attend.hip), whose parts are as many steps long.
     pl.lone = !pl.tile_own && items >= 1024 && B.max_len <= 256;
     pl.few = longest <= 16 && !pl.tile_prefix && items <= 512 && all <= ATT_FEW_WAVES / ATT_WAVES * step && C.dim <= 128;
-    const int64_t work_prefix = C.kv_heads * (int64_t)pl.tiles_prefix * B.n_prefix, work_own = C.kv_heads * tiles * B.max_len;
+    const int64_t work_prefix = C.kv_heads * (int64_t)pl.tiles_prefix * B.n_prefix;
     const auto chunk = [&](int64_t quantum, int64_t work, int32_t keys) {    // for 256 workgroups; no longer than the part: up to 2^30 keys and a quantum
         const int64_t even = std::min((work + 255) / 256, (int64_t)keys);
         return (int32_t)((std::max(even, (int64_t)1) + quantum - 1) / quantum * quantum);
     };
+    // Tiles' chunks, the least for which no more than 512 workgroups share the prefix and, of tiles, own parts: two a CU, and none in a second round.  (320 rows of 32768 keys, 256 / 384 /
+    // 512 / 768: 92 / 84 / 75 / 83; 192 rows of them 64 / 63 / 65 / 67; 200 behind 8000 own, 384 / 512 / 1024, 67 / 54 / 65.)
+    const auto tile_chunk = [&]() {
+        const int64_t quantum = att_tile_keys(C.dim), heads = C.kv_heads, own = pl.tile_own ? tiles : 0;
+        int64_t lo = 1, hi = (std::max((int64_t)B.n_prefix, own > 0 ? (int64_t)B.max_len : 0) + quantum - 1) / quantum;
+        while (lo < hi) {
+            const int64_t mid = (lo + hi) / 2, keys = mid * quantum;
+            if (heads * (pl.tiles_prefix * ((B.n_prefix + keys - 1) / keys) + own * ((B.max_len + keys - 1) / keys)) <= 512) hi = mid;
+            else lo = mid + 1;
+        }
+        return (int32_t)(lo * quantum);
+    };
     // The prefix: a workgroup a CU, two steps each at least of heads wider than 128.  (128 / 256 / 512 workgroups: 32 rows of 16384 keys 21 / 17 / 22, of 32768 31 / 22 / 25, 64 rows of 32768
-    // 48 / 32 / 31, 16 rows of 4096 11.8 / 13.3 / 13.0, 64 rows of 4096 16.0 / 15.5 / 19.8.  Through LDS, 256 / 512: 320 rows of 32768 84 / 96.  16 heads of 256, 5 rows of 1999: 15.9 /
+    // 48 / 32 / 31, 16 rows of 4096 11.8 / 13.3 / 13.0, 64 rows of 4096 16.0 / 15.5 / 19.8.  16 heads of 256, 5 rows of 1999: 15.9 /
     // 22.0 / 21.7, which is two steps, one and one.)
-    pl.chunk_prefix = pl.tile_prefix ? chunk(att_tile_keys(C.dim), work_prefix + (pl.tile_own ? work_own : 0), B.n_prefix)
+    pl.chunk_prefix = pl.tile_prefix ? tile_chunk()
                                      : chunk(C.dim > 128 ? 2 * step : step, work_prefix, B.n_prefix);
-    // Own items of many rows take the prefix ahead of their own keys where they fill the chip and it is not read much oftener for it, as there.
+    // Own tiles of many rows are one chunk where that is quicker than to share the chip evenly and join: they take some 1.7 us for 64 keys of 128 features, and cut into 512 parts 2.4 items / 512 and
+    // some 20 us for sums that go through memory.  (Whole / cut: prompts of 300, 400 and 512 tokens 16.9 / 23.6, 18.9 / 26.9, 21.9 / 28.9, 512 behind 1000 and 8000 own 46 / 39,
+    // 213 / 100, 1000 alone and behind 8000 35 / 49, 226 / 189, 200 behind 8000 205 / 54, four times 60 behind 2048 shared 59 / 31.)  Whole ones take the prefix, too, ahead of their own keys,
+    // unless it is read much oftener for it: the rule of the 16-bit cache.
     const int64_t beyond = tiles - (rows + pl.rows_own - 1) / pl.rows_own;   // tiles more than all rows in a row would take
-    pl.ahead = B.n_prefix > 0 && (pl.few || (pl.tile_own && items > 128 && (4 * beyond <= tiles || beyond * B.n_prefix <= 16384)));
+    const bool whole = pl.tile_own && (double)all * C.dim * (363.0 - items) <= 3.5e7;
+    pl.ahead = B.n_prefix > 0 && (pl.few || (whole && (4 * beyond <= tiles || beyond * B.n_prefix <= 16384)));
     if (pl.ahead || pl.few)
         pl.chunk_own = (int32_t)((all + 15 + step - 1) / step * step);
-    else if (pl.tile_own && items <= 128)
-        pl.chunk_own = chunk(att_tile_keys(C.dim), work_prefix + work_own, B.max_len);
+    else if (pl.tile_own && !(whole && B.n_prefix == 0))
+        pl.chunk_own = tile_chunk();
     else
         pl.chunk_own = (int32_t)((B.max_len + step - 1) / step * step);
     if (pl.ahead)

@@ -1,7 +1,11 @@
-// Attention of many rows over a cache in 4 bits: attend_tile.h with codes that become fp16 on their way into LDS, once for all 256 rows of a workgroup (128 of heads wider
-// than 128).  Four wavefronts bring in a step's keys, four its values, 16 tokens each: a lane loads 32 features of a token, which is one group or half of one.  Keys: what
-// a lane has unpacked are its own 16 bytes of as many A operands as it loaded words, queries being laid out alike.  Values go into LDS in the order in which pairs come out of a word,
-// features 0, 4, 1, 5, 2, 6, 3, 7 of every eight; that order is undone once, where the output leaves.
+// Attention of many rows over a cache in 4 bits: attend_tile.h with codes that become fp16 on their way into LDS, once for all 128 rows of a workgroup (64 of heads wider than 128).
+// Each of its four wavefronts brings in 16 tokens of a step's keys and values: a lane loads 32 features of a token, which is one group or half of one.  Keys: what a lane has
+// unpacked are its own 16 bytes of as many A operands as it loaded words, queries being laid out alike.  Values go into LDS in the order in which pairs come out of a word, features 0, 4,
+// 1, 5, 2, 6, 3, 7 of every eight; that order is undone once, where the output leaves.
+//
+// Bound by the matrix cores, reads from LDS and what stands between the two products, some 1.1, 0.9 and 1.0 us for 64 keys of 256 rows, of which two workgroups a CU, each at a place of its own,
+// overlap a part: 1.9 us.  (One workgroup of eight wavefronts a CU, whose barriers keep them in step: a prompt of 1000 tokens of 32 heads on 8 48 instead of 35 us, of 2048 72 instead of 65,
+// packed prompts of 2048, 1117, 604 and 381 tokens 77.6 instead of 75.0, 2800 tokens of 16 heads 93 instead of 82; 4 x 300 behind 2048 shared 79 instead of 85.)
 #include "attend_q4.h"
 #include "attend_tile.h"
 
@@ -12,76 +16,68 @@ struct Q4TileStage {
     using S = TileShape<DB>;
     static constexpr int W = S::NQ < 4 ? S::NQ : 4;           // words that a lane brings in
     static constexpr int PARTS = S::NQ / W;                   // ... of a token's, by as many wavefronts
-    static_assert(S::KT * PARTS * 2 == ATT_TILE_WAVES, "a tile of 16 tokens a wavefront, of keys and of values");
-    const char *pool;                        // of the kv head: keys, or values
-    uint32_t at, at_pair, to;                // the lane's place in a tile, and in a step's room
-    int32_t page;
-    uint64_t codes, pairs;
-    uint32_t w[W], pair;
+    static_assert(S::KT * PARTS == Q4_TILE_WAVES, "a wavefront brings in a tile of 16 tokens, or half of it, of keys and of values");
+    uint32_t at[2], at_pair[2], to[2];       // of keys, of values: the lane's place in a tile, and in a step's room
+    Q4Tile tile;
+    uint32_t w[2][W], pair[2];
 
-    static __device__ __forceinline__ bool is_key(int wave) { return wave < ATT_TILE_WAVES / 2; }
-    static __device__ __forceinline__ int tile_of(int wave) { return wave % (ATT_TILE_WAVES / 2) / PARTS; }
+    static __device__ __forceinline__ int tile_of(int wave) { return wave / PARTS; }
 
-    __device__ __forceinline__ Q4TileStage(const AttendQ4Params &p, const AttendItem &it, int wave, int lane)
+    __device__ __forceinline__ Q4TileStage(const AttendQ4Params &p, const AttendItem &, int wave, int lane)
     {
-        const int part = wave % PARTS, tile = tile_of(wave);
-        pool = (const char *)(is_key(wave) ? p.K : p.V) + (uint64_t)it.hk * p.s.head_bytes;
-        const int token = is_key(wave) ? lane & 15 : lane >> 2, row = tile * 16 + token;
-        const int word = is_key(wave) ? (lane >> 4) * S::NQ + part * W : (part * 4 + (lane & 3)) * W;
-        // features from dim on meet queries that are zero, or end in outputs that are not stored: some of the row's own will do
-        const int f = word * 8 < p.dim ? word * 8 : 0;
-        at = token * p.s.row_bytes + f / 2;
-        at_pair = (token * p.s.groups + (f >> p.s.group_shift)) * 4;
-        to = is_key(wave) ? (tile * S::NQ + part * W) * 1024 + lane * 16 : row * S::ROW + (word ^ tile_turn<DB>(row) << 1) * 16;
+        const int part = wave % PARTS;
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+            const int token = v ? lane >> 2 : lane & 15, row = tile_of(wave) * 16 + token;
+            const int word = v ? (part * 4 + (lane & 3)) * W : (lane >> 4) * S::NQ + part * W;
+            // features from dim on meet queries that are zero, or end in outputs that are not stored: some of the row's own will do
+            const int f = word * 8 < p.dim ? word * 8 : 0;
+            at[v] = token * p.s.row_bytes + f / 2;
+            at_pair[v] = (token * p.s.groups + (f >> p.s.group_shift)) * 4;
+            to[v] = v ? row * S::ROW + (word ^ tile_turn<DB>(row) << 1) * 16 : (tile_of(wave) * S::NQ + part * W) * 1024 + lane * 16;
+        }
     }
 
-    __device__ __forceinline__ void look_up(const AttendQ4Params &p, const AttendItem &it, int32_t key0, int wave)
-    {
-        page = att_look_up(p, it, key0 + 16 * tile_of(wave));
-    }
+    __device__ __forceinline__ void look_up(const AttendQ4Params &p, const AttendItem &it, int32_t key0, int wave) { tile.look_up(p, it, key0 + 16 * tile_of(wave)); }
 
-    __device__ __forceinline__ void place(const AttendQ4Params &p, const AttendItem &it, int32_t key0, int wave)
-    {
-        int32_t key = key0 + 16 * tile_of(wave);
-        key -= key < it.hole_end ? 0 : it.hole_end;
-        const uint32_t in = key & ((1 << p.page_shift) - 1);
-        const uint64_t block = (uint64_t)att_page(__builtin_amdgcn_readfirstlane(page), p.last_page) * (uint32_t)p.kv_heads * p.s.head_bytes;
-        codes = block + in * p.s.row_bytes;
-        pairs = block + p.s.pairs_at + in * p.s.groups * 4;
-    }
+    __device__ __forceinline__ void place(const AttendQ4Params &p, const AttendItem &it, int32_t key0, int wave) { tile.set(p, it, key0 + 16 * tile_of(wave)); }
 
     __device__ __forceinline__ void load(const AttendQ4Params &, int, int)
     {
-        if constexpr (W == 2)
-            *(uint2 *)w = *(const uint2 *)(pool + codes + at);
-        else
-            *(att_u32x4 *)w = *(const att_u32x4 *)(pool + codes + at);
-        pair = *(const uint32_t *)(pool + pairs + at_pair);
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+            const __amdgpu_buffer_rsrc_t pool = v ? tile.V : tile.K;
+            if constexpr (W == 2)
+                *(q4_u32x2 *)w[v] = __builtin_amdgcn_raw_buffer_load_b64(pool, at[v], tile.codes, 0);
+            else
+                *(att_u32x4 *)w[v] = __builtin_amdgcn_raw_buffer_load_b128(pool, at[v], tile.codes, 0);
+            pair[v] = __builtin_amdgcn_raw_buffer_load_b32(pool, at_pair[v], tile.pairs, 0);
+        }
     }
 
     // values behind the last key or in the hole, and groups of NaN, as zeros; true if there were any of these
     __device__ __forceinline__ bool clear(const AttendItem &it, int32_t key0, int wave, int lane)
     {
-        if (is_key(wave))
-            return false;
         const int32_t key = key0 + 16 * tile_of(wave) + (lane >> 2);
-        const bool in = key < it.end && !it.missing(key), odd = q4_odd(pair);
-        pair = in && !odd ? pair : 0;
+        const bool in = key < it.end && !it.missing(key), odd = q4_odd(pair[1]);
+        pair[1] = in && !odd ? pair[1] : 0;
         return in && odd;
     }
 
-    __device__ __forceinline__ void store(uint32_t keys, uint32_t vals, int wave, int) const
+    __device__ __forceinline__ void store(uint32_t keys, uint32_t vals, int, int) const
     {
-        const q4_pair scale = q4_scales(pair), middle = q4_middles(pair);
-        const uint32_t room = is_key(wave) ? keys : vals;
 #pragma unroll
-        for (int i = 0; i < W; ++i) {
-            att_u32x4 x;
+        for (int v = 0; v < 2; ++v) {
+            const q4_pair scale = q4_scales(pair[v]), middle = q4_middles(pair[v]);
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                x[j] = q4_word(q4_value_pair(w[i] >> 4 * j, scale, middle));
-            // keys: another operand, 1 KB on.  Values: the next 16 bytes, whose number's bits below the turn's or among them change
-            *(lds_u32x4 *)(uintptr_t)(room + (is_key(wave) ? to + i * 1024 : to ^ i * 16)) = x;
+            for (int i = 0; i < W; ++i) {
+                att_u32x4 x;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    x[j] = q4_word(q4_value_pair(w[v][i] >> 4 * j, scale, middle));
+                // keys: another operand, 1 KB on.  Values: the next 16 bytes, whose number's bits are below the turn's or among them
+                *(lds_u32x4 *)(uintptr_t)(v ? vals + (to[v] ^ i * 16) : keys + to[v] + i * 1024) = x;
+            }
         }
     }
 };
@@ -97,6 +93,7 @@ struct TileQ4 {
     using Params = AttendQ4Params;
     using Rows = Q4TileRows<DB>;
     using Stage = Q4TileStage<DB>;
+    static constexpr int WAVES = Q4_TILE_WAVES;
     static constexpr float LIFT = 7;                          // as in attend_q4.h
 
     static __device__ __forceinline__ att_f32x4 product(att_u32x4 a, att_u32x4 b, att_f32x4 c) { return q4_mfma(a, b, c); }

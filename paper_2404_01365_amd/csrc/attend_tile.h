@@ -1,4 +1,5 @@
 // Attention of many rows: what the kernels over caches of bf16 (attend_tile.hip) and in 4 bits (attend_q4_tile.hip) share.  F, the format, says
+//   WAVES                    of a workgroup
 //   Params, Rows, Stage      a launch's arguments, a wavefront's rows (TileRows), and a step's keys and values on their way (attend_tile.hip describes one)
 //   LIFT                     weights are 2^LIFT times what they stand for, numerator and denominator alike
 //   product, add_weights     a product of the matrix cores, and one with ones
@@ -27,7 +28,6 @@ struct TileShape {
     static constexpr int NT = DB > 128 ? 1 : 2;               // tiles of 16 rows of a wavefront
     static constexpr int ROW = DB * 2;                        // bytes of a value's row
     static constexpr int BYTES = KEYS * ROW;            // of a step's keys, and of its values
-    static constexpr int PIECES = BYTES / (16 * 64 * ATT_TILE_WAVES);      // 16-byte pieces of either that a thread brings in
 };
 
 template <int DB>
@@ -198,7 +198,7 @@ __device__ __forceinline__ void tile_softmax(bool masked, TileScores<DB> &s, att
 enum TileOwn { OWN_TILES, OWN_ROWS, OWN_EACH };
 
 template <class F, int DB, bool FULL, TileOwn OWN>
-__global__ __launch_bounds__(64 * ATT_TILE_WAVES) void attend_tile_kernel(typename F::Params p)
+__global__ __launch_bounds__(64 * F::WAVES, 2) void attend_tile_kernel(typename F::Params p)
 {
     using S = TileShape<DB>;
     using Stage = typename F::Stage;
@@ -206,16 +206,16 @@ __global__ __launch_bounds__(64 * ATT_TILE_WAVES) void attend_tile_kernel(typena
     const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)tile_lds;
     AttendItem it;
     if ((int32_t)blockIdx.x < p.wgs_prefix)
-        att_prefix_item<att_tile_rows(DB)>(p, blockIdx.x, it);
+        att_prefix_item<16 * S::NT * F::WAVES>(p, blockIdx.x, it);
     else if constexpr (OWN == OWN_TILES) {
-        if (!att_own_item<att_tile_rows(DB), true>(p, blockIdx.x - p.wgs_prefix, it))
+        if (!att_own_item<16 * S::NT * F::WAVES, true>(p, blockIdx.x - p.wgs_prefix, it))
             return;
     } else {
         int32_t id = blockIdx.x - p.wgs_prefix;
         if (OWN == OWN_EACH)
-            id = id * ATT_TILE_WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+            id = id * F::WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         if (id < p.items_own && F::own_item(p, id, it))
-            F::template own_rows<OWN == OWN_EACH ? 1 : ATT_TILE_WAVES>(p, (float *)tile_lds, it);
+            F::template own_rows<OWN == OWN_EACH ? 1 : F::WAVES>(p, (float *)tile_lds, it);
         return;
     }
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -330,9 +330,9 @@ __global__ __launch_bounds__(64 * ATT_TILE_WAVES) void attend_tile_kernel(typena
 template <class F, int DB, bool FULL, TileOwn OWN>
 static int go_tiles(const typename F::Params &p, int32_t wgs, hipStream_t st)
 {
-    constexpr int rooms = 4 * TileShape<DB>::BYTES, sums = OWN == OWN_ROWS ? att_lds_floats<DB, ATT_TILE_WAVES>() * 4 : 0, bytes = rooms > sums ? rooms : sums;
+    constexpr int rooms = 4 * TileShape<DB>::BYTES, sums = OWN == OWN_ROWS ? att_lds_floats<DB, F::WAVES>() * 4 : 0, bytes = rooms > sums ? rooms : sums;
     RAISE_LDS_LIMIT((attend_tile_kernel<F, DB, FULL, OWN>), bytes);
-    hipLaunchKernelGGL((attend_tile_kernel<F, DB, FULL, OWN>), dim3(wgs), dim3(64 * ATT_TILE_WAVES), bytes, st, p);
+    hipLaunchKernelGGL((attend_tile_kernel<F, DB, FULL, OWN>), dim3(wgs), dim3(64 * F::WAVES), bytes, st, p);
     return check_launch("attend_tile_kernel");
 }
 
@@ -341,7 +341,7 @@ static int go_tiles_and_rows(const typename F::Params &p, int32_t wgs, bool each
 {
     if constexpr (DB <= 128) {
         if (each)
-            return go_tiles<F, DB, FULL, OWN_EACH>(p, wgs + (p.items_own + ATT_TILE_WAVES - 1) / ATT_TILE_WAVES, st);
+            return go_tiles<F, DB, FULL, OWN_EACH>(p, wgs + (p.items_own + F::WAVES - 1) / F::WAVES, st);
         if (p.items_own > 0)
             return go_tiles<F, DB, FULL, OWN_ROWS>(p, wgs + p.items_own, st);
     }

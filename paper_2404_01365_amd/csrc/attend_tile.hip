@@ -24,11 +24,12 @@ namespace griffin {
 template <int DB, bool FULL>
 struct TileStage {
     using S = TileShape<DB>;
+    static constexpr int PIECES = S::BYTES / (16 * 64 * ATT_TILE_WAVES);       // 16-byte pieces of either that a thread brings in
     const char *K, *V;                       // of the kv head
     uint32_t stride, at_k, at_v;             // bytes from key to key; the lane's place in a tile
-    int32_t page[S::PIECES];
-    uint64_t base[S::PIECES];
-    att_u32x4 k[S::PIECES], v[S::PIECES];
+    int32_t page[PIECES];
+    uint64_t base[PIECES];
+    att_u32x4 k[PIECES], v[PIECES];
 
     static __device__ __forceinline__ int tile_of(int wave, int i) { return (wave + ATT_TILE_WAVES * i) / S::NQ; }
     static __device__ __forceinline__ int row_of(int wave, int lane) { return (wave * 64 / (DB / 8) + lane / (DB / 8)) & 15; }
@@ -46,21 +47,21 @@ struct TileStage {
     __device__ __forceinline__ void look_up(const AttendParams &p, const AttendItem &it, int32_t key0, int wave)
     {
 #pragma unroll
-        for (int i = 0; i < S::PIECES; ++i)
+        for (int i = 0; i < PIECES; ++i)
             page[i] = att_look_up(p, it, key0 + 16 * tile_of(wave, i));
     }
 
     __device__ __forceinline__ void place(const AttendParams &p, const AttendItem &it, int32_t key0, int wave)
     {
 #pragma unroll
-        for (int i = 0; i < S::PIECES; ++i)
+        for (int i = 0; i < PIECES; ++i)
             base[i] = att_place<2>(p, it, page[i], key0 + 16 * tile_of(wave, i));
     }
 
     __device__ __forceinline__ void load(const AttendParams &p, int wave, int lane)
     {
 #pragma unroll
-        for (int i = 0; i < S::PIECES; ++i) {
+        for (int i = 0; i < PIECES; ++i) {
             // the piece's features are the same in every round of ATT_TILE_WAVES pieces.  Keys' features from dim on are zero, as the queries' are;
             // values' end in outputs that are not stored
             if (FULL || wave % S::NQ * 32 + (lane >> 4) * 8 < p.dim)
@@ -80,7 +81,7 @@ struct TileStage {
     {
         uint32_t kept = ~0u;
 #pragma unroll
-        for (int i = 0; i < S::PIECES; ++i) {
+        for (int i = 0; i < PIECES; ++i) {
             const int32_t key = key0 + 16 * tile_of(wave, i) + row_of(wave, lane);
             const bool in = key < it.end && !it.missing(key);
 #pragma unroll
@@ -96,7 +97,7 @@ struct TileStage {
     __device__ __forceinline__ void store(uint32_t keys, uint32_t vals, int wave, int lane) const
     {
 #pragma unroll
-        for (int i = 0; i < S::PIECES; ++i) {
+        for (int i = 0; i < PIECES; ++i) {
             const int row = tile_of(wave, i) * 16 + row_of(wave, lane);
             *(lds_u32x4 *)(uintptr_t)(keys + (wave + ATT_TILE_WAVES * i) * 1024 + lane * 16) = k[i];
             *(lds_u32x4 *)(uintptr_t)(vals + row * S::ROW + (lane % (DB / 8) ^ tile_turn<DB>(row) << 1) * 16) = v[i];
@@ -134,6 +135,7 @@ struct TileBf16 {
     using Params = AttendParams;
     using Rows = TileRows<DB>;
     using Stage = TileStage<DB, FULL>;
+    static constexpr int WAVES = ATT_TILE_WAVES;
     static constexpr float LIFT = 0;
 
     static __device__ __forceinline__ att_f32x4 product(att_u32x4 a, att_u32x4 b, att_f32x4 c) { return att_mfma(a, b, c); }

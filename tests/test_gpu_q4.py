@@ -284,10 +284,11 @@ def test_attention_of_prompts_that_fill_the_chip_behind_a_prefix(dim, prefix):
 
 
 @pytest.mark.parametrize("heads,kv_heads,dim,prefix,held,new", [
-    (16, 2, 128, 9000, [0, 300, 31, 5, 64, 200, 7, 90, 3], [1, 1, 1, 2, 1, 1, 1, 1, 2]),          # 88 rows a kv head, own parts a workgroup each
+    (64, 2, 128, 25000, [0, 300, 31, 700, 64, 200, 7, 90, 3], [1, 1, 1, 2, 1, 1, 1, 1, 2]),      # 352 rows a kv head, own parts a workgroup each, cut by the device
+    (64, 2, 128, 25000, [0, 30, 31, 70, 64, 20, 7, 90, 3], [1, 1, 1, 2, 1, 1, 1, 1, 2]),         # ... too short to be cut
     (16, 8, 64, 20000, [int(x) for x in np.random.default_rng(3).integers(0, 200, 130)], [1] * 130),     # ... a wavefront each
-    (40, 1, 96, 70000, [0, 9], [1, 1]),
-    (20, 1, 256, 40000, [30, 1], [3, 1])])
+    (80, 1, 96, 71000, [0, 9, 600], [1, 1, 2]),
+    (48, 1, 256, 45000, [30, 1], [3, 1])])                                                         # own parts in a launch of their own
 def test_attention_of_own_parts_beside_tiles_of_the_prefix(heads, kv_heads, dim, prefix, held, new):
     check_attention(17, heads=heads, kv_heads=kv_heads, dim=dim, page=64, prefix=prefix, held=held, new=new, dtype=BF16)
 
@@ -390,6 +391,25 @@ def test_attention_of_places_that_hold_anything(dtype, fill):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("heads,kv_heads,dim,prefix,held,new,max_len", [
+    (4, 2, 64, 0, [5, 700, 0, 33], [1, 1, 1, 1], 4096),                  # far more room than is used
+    (8, 1, 128, 0, [900, 0, 130, 129, 127], [3, 0, 5, 1, 4], 1000),      # several tiles of rows, a sequence without new tokens
+    (8, 1, 128, 40, [900, 0, 130], [3, 2, 5], 2000),
+    (4, 4, 64, 0, [3000], [1], 3001),
+    (2, 2, 256, 10, [700, 3, 260], [1, 9, 20], 900),
+    (20, 1, 64, 0, [300, 2, 513], [2, 3, 1], 600)])                      # tiles of 32 rows
+def test_attention_of_parts_that_the_device_cuts(dtype, heads, kv_heads, dim, prefix, held, new, max_len):
+    check_attention(19, heads=heads, kv_heads=kv_heads, dim=dim, page=16, prefix=prefix, held=held, new=new, dtype=dtype, max_len=max_len)
+
+
+@pytest.mark.parametrize("n", [63, 64, 65, 200, 256])
+def test_attention_of_many_sequences_that_the_device_cuts(n):
+    rng = np.random.default_rng(n)
+    check_attention(20, heads=2, kv_heads=1, dim=64, page=16, prefix=0, held=rng.integers(0, 400, n).tolist(), new=rng.integers(0, 3, n).tolist(), dtype=BF16, max_len=450)
+    check_attention(20, heads=2, kv_heads=1, dim=64, page=16, prefix=30, held=rng.integers(0, 400, n).tolist(), new=[1] * n, dtype=BF16, max_len=450)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 def test_attention_beyond_max_len(dtype):
     check_attention(51, heads=4, kv_heads=2, dim=64, page=16, prefix=20, held=[60, 64, 100, 5], new=[8, 3, 1, 2], dtype=dtype, max_len=64)
 
@@ -488,3 +508,34 @@ def test_step_on_another_stream_and_in_a_graph():
         torch.cuda.synchronize()
         for name in ("K", "V", "q_out", "out", "k2", "v2"):
             assert torch.equal(a[name], b[name]), (i, name)
+
+
+def test_graphs_that_share_a_workspace():
+    """Two batches' calls captured into graphs with one workspace, replayed in turn on one stream"""
+    cases, graphs = [], []
+    ws = None
+    for seed, held, new, prefix in ((91, [5, 700, 33], [1, 1, 1], 0), (92, [3, 90], [4, 70], 300)):
+        c = plain.Case(seed, heads=8, kv_heads=2, dim=128, page=16, prefix=prefix, held=held, new=new, dtype=BF16)
+        K, V = q4_plain.pool_of(c.K, 32), q4_plain.pool_of(c.V, 32)
+        cases.append((cache(c, put(K), put(V), 32), batch(c), dev(c.q, BF16), torch.zeros(c.q.shape, dtype=torch.bfloat16, device="cuda"), *reference(c, K, V, 32, None)))
+    ws = workspace(max(G.griffin_attention_q4_workspace_bytes(C, B, 8) for C, B, *_ in cases))
+    stream = torch.cuda.Stream()
+    for C, B, q, out, *_ in cases:
+        torch.cuda.synchronize()
+        with torch.cuda.stream(stream):
+            G.griffin_attention_q4(C, B, q, out, workspace=ws)
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            G.griffin_attention_q4(C, B, q, out, workspace=ws)
+        graphs.append(graph)
+    for _ in range(3):
+        for _, _, _, out, *_ in cases:
+            out.zero_()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(stream):
+            for graph in graphs:
+                graph.replay()
+        stream.synchronize()
+        for _, _, _, out, ref, size in cases:
+            attention_close(to_host(out), ref, size, BF16)
