@@ -388,9 +388,15 @@ class _Types(dict):
 _TYPE = _Types()
 
 
+_i32_type = None
+
+
 def _int32():
-    import torch
-    return torch.int32
+    global _i32_type
+    if _i32_type is None:
+        import torch
+        _i32_type = torch.int32
+    return _i32_type
 
 
 def _refuse(what: str, t, shape, dtype, device=None) -> None:
@@ -414,7 +420,7 @@ def _row(what: str, t, width: int, dtype, device: int):
     """Address of a vector, or None."""
     if t is None:
         return None
-    if t.shape != (width,) or t.dtype is not dtype or t.get_device() != device or (t.stride(0) != 1 and width > 1):
+    if t.shape != (width,) or t.dtype is not dtype or t.get_device() != device or not t.is_contiguous():
         _refuse(what, t, (width,), dtype, device)
     return t.data_ptr()
 
@@ -529,60 +535,70 @@ def _check_room(where: str, C: griffin_kv_cache, B: griffin_kv_batch, device: in
         raise ValueError("%s: cache and tensors lie on %s, lens and pages on %s" % (where, _place(device), _place(device if table is None else table)))
 
 
-def _append(where: str, call, C, B: griffin_kv_batch, k, v, q, q_out, cos, sin, style: int, stream) -> None:
+# what the arguments of an append, and of an attention, are called in refusals
+def _names(where: str, *arguments):
+    return (where,) + tuple("%s: %s" % (where, a) for a in arguments)
+
+
+_APPEND, _APPEND_Q4 = (_names(w, "k", "v", "q", "q_out", "cos", "sin") for w in ("griffin_kv_append", "griffin_kv_append_q4"))
+_ATTENTION, _ATTENTION_Q4 = (_names(w, "q", "out", "workspace") for w in ("griffin_attention", "griffin_attention_q4"))
+_VERIFY = _names("griffin_verify_drafts", "p", "draft_p", "drafted", "accept_u", "draw_u", "tokens_out", "accepted", "lens", "lens_out", "workspace")
+
+
+def _append(names, call, C, B: griffin_kv_batch, k, v, q, q_out, cos, sin, style: int, stream) -> None:
     dtype, tokens, dim, device = _TYPE[C.dtype], B._total, C.dim, C._device
     if tokens is None:
         tokens = B.cu_seqlens[B.n_seqs]
     if device is None:
         device = k.get_device()
     kv, heads = (tokens, C.kv_heads, dim), 0 if q is None else q.shape[1]
-    at_k, ldk, hsk = _heads(where + ": k", k, kv, dtype, device)
-    at_v, ldv, hsv = _heads(where + ": v", v, kv, dtype, device)
-    at_q, ldq, hsq = _heads(where + ": q", q, (tokens, heads, dim), dtype, device)
-    at_o, ldo, hso = _heads(where + ": q_out", q_out, (tokens, heads, dim), dtype, device)
+    at_k, ldk, hsk = _heads(names[1], k, kv, dtype, device)
+    at_v, ldv, hsv = _heads(names[2], v, kv, dtype, device)
+    at_q, ldq, hsq = _heads(names[3], q, (tokens, heads, dim), dtype, device)
+    at_o, ldo, hso = _heads(names[4], q_out, (tokens, heads, dim), dtype, device)
     n_pos = half = 0
     at_c = at_s = None
     if cos is not None:
         n_pos, half = shape = cos.shape
         f32 = _TYPE[F32]
-        at_c, ldc = _mat(where + ": cos", cos, shape, f32, device)
-        at_s, lds = _mat(where + ": sin", sin, shape, f32, device)
+        at_c, ldc = _mat(names[5], cos, shape, f32, device)
+        at_s, lds = _mat(names[6], sin, shape, f32, device)
         if n_pos > 1 and (ldc != half or lds != half):
-            raise ValueError("%s: rows of cos and sin are not dense" % where)
-    _check_room(where, C, B, device)
-    _check(call(C, B, at_k, ldk, hsk, at_v, ldv, hsv, at_q, ldq, hsq, at_o, ldo, hso, heads, at_c, at_s, n_pos, 2 * half, style, _stream(stream)), where)
+            raise ValueError("%s: rows of cos and sin are not dense" % names[0])
+    _check_room(names[0], C, B, device)
+    _check(call(C, B, at_k, ldk, hsk, at_v, ldv, hsv, at_q, ldq, hsq, at_o, ldo, hso, heads, at_c, at_s, n_pos, 2 * half, style, _stream(stream)), names[0])
 
 
 def griffin_kv_append(C: griffin_kv_cache, B: griffin_kv_batch, k, v, *, q=None, q_out=None, cos=None, sin=None,
                       style: int = ROT_HALF, stream=None) -> None:
     """New keys (rotated) and values [tokens][kv_heads][dim] into their pages; queries [tokens][n_heads][dim] rotated into q_out.
     cos, sin: fp32 [positions][rot / 2], None: nothing is rotated."""
-    _append("griffin_kv_append", lib.griffin_kv_append, C, B, k, v, q, q_out, cos, sin, style, stream)
+    _append(_APPEND, lib.griffin_kv_append, C, B, k, v, q, q_out, cos, sin, style, stream)
 
 
 def griffin_attention_workspace_bytes(C: griffin_kv_cache, B: griffin_kv_batch, n_heads: int) -> int:
     return int(lib.griffin_attention_workspace_bytes(ctypes.byref(C), ctypes.byref(B), n_heads))
 
 
-def _attention(where: str, call, C, B: griffin_kv_batch, q, out, scale, workspace, stream) -> None:
+def _attention(names, call, C, B: griffin_kv_batch, q, out, scale, workspace, stream) -> None:
     tokens, dtype, device = B._total, _TYPE[C.dtype], C._device
     if tokens is None:
         tokens = B.cu_seqlens[B.n_seqs]
     if device is None:
         device = q.get_device()
     shape = (tokens, q.shape[1], C.dim)
-    at_q, ldq, hsq = _heads(where + ": q", q, shape, dtype, device)
-    at_o, ldo, hso = _heads(where + ": out", out, shape, dtype, device)
+    at_q, ldq, hsq = _heads(names[1], q, shape, dtype, device)
+    at_o, ldo, hso = _heads(names[2], out, shape, dtype, device)
     if workspace is not None and (workspace.get_device() != device or not workspace.is_contiguous()):
-        _refuse(where + ": workspace", workspace, workspace.shape, None, device)
-    _check_room(where, C, B, device)
+        _refuse(names[3], workspace, workspace.shape, None, device)
+    _check_room(names[0], C, B, device)
     _check(call(C, B, at_q, ldq, hsq, at_o, ldo, hso, shape[1], shape[2] ** -0.5 if scale is None else scale, _ptr(workspace), _nbytes(workspace),
-                _stream(stream)), where)
+                _stream(stream)), names[0])
 
 
 def griffin_attention(C: griffin_kv_cache, B: griffin_kv_batch, q, out, *, scale: Optional[float] = None, workspace=None, stream=None) -> None:
     """out = softmax(scale q K^T) V over the shared prefix and the sequences' own tokens; q, out [tokens][n_heads][dim]."""
-    _attention("griffin_attention", lib.griffin_attention, C, B, q, out, scale, workspace, stream)
+    _attention(_ATTENTION, lib.griffin_attention, C, B, q, out, scale, workspace, stream)
 
 
 # ------------------------------------------------------------------ a cache in 4 bits
@@ -611,7 +627,7 @@ def kv_cache_q4(K, V, *, kv_heads: int, dim: int, page_size: int, group: int = 3
 def griffin_kv_append_q4(C: griffin_kv_cache_q4, B: griffin_kv_batch, k, v, *, q=None, q_out=None, cos=None, sin=None,
                          style: int = ROT_HALF, stream=None) -> None:
     """griffin_kv_append into a cache in 4 bits."""
-    _append("griffin_kv_append_q4", lib.griffin_kv_append_q4, C, B, k, v, q, q_out, cos, sin, style, stream)
+    _append(_APPEND_Q4, lib.griffin_kv_append_q4, C, B, k, v, q, q_out, cos, sin, style, stream)
 
 
 def griffin_kv_read_q4(C: griffin_kv_cache_q4, B: griffin_kv_batch, k=None, v=None, *, stream=None) -> None:
@@ -634,7 +650,7 @@ def griffin_attention_q4_workspace_bytes(C: griffin_kv_cache_q4, B: griffin_kv_b
 
 def griffin_attention_q4(C: griffin_kv_cache_q4, B: griffin_kv_batch, q, out, *, scale: Optional[float] = None, workspace=None, stream=None) -> None:
     """griffin_attention over a cache in 4 bits."""
-    _attention("griffin_attention_q4", lib.griffin_attention_q4, C, B, q, out, scale, workspace, stream)
+    _attention(_ATTENTION_Q4, lib.griffin_attention_q4, C, B, q, out, scale, workspace, stream)
 
 
 # ------------------------------------------------------------------ drafted tokens
@@ -652,25 +668,21 @@ def griffin_verify_drafts(cu_seqlens, p, drafted, accept_u, draw_u, tokens_out, 
     """Keeps the drafted tokens that the target's probabilities p [rows][vocab] allow and draws the one behind them.  cu_seqlens: a sequence of ints or
     what cu_seqlens() made of one; drafted, accept_u, tokens_out [rows]; draw_u, accepted, lens, lens_out [sequences]."""
     cu = cu_seqlens if isinstance(cu_seqlens, ctypes.Array) else _cu_array(cu_seqlens)
-    n, device, f32, i32 = len(cu) - 1, p.get_device(), _TYPE[F32], _int32()
+    n, device, f32, i32, names = len(cu) - 1, p.get_device(), _TYPE[F32], _int32(), _VERIFY
     if n < 1:
         raise ValueError("griffin_verify_drafts: no sequences")
     rows = cu[n]
     shape = (rows, p.shape[-1])
-    at_p, ldp = _mat("griffin_verify_drafts: p", p, shape, f32, device)
-    at_q, ldq = _mat("griffin_verify_drafts: draft_p", draft_p, shape, f32, device)
+    at_p, ldp = _mat(names[1], p, shape, f32, device)
+    at_q, ldq = _mat(names[2], draft_p, shape, f32, device)
     if rows == 1:
         ldp = ldq = shape[1]
-    at_d = _row("griffin_verify_drafts: drafted", drafted, rows, i32, device)
-    at_u = _row("griffin_verify_drafts: accept_u", accept_u, rows, f32, device)
-    at_r = _row("griffin_verify_drafts: draw_u", draw_u, n, f32, device)
-    at_t = _row("griffin_verify_drafts: tokens_out", tokens_out, rows, i32, device)
-    at_a = _row("griffin_verify_drafts: accepted", accepted, n, i32, device)
-    at_l = _row("griffin_verify_drafts: lens", lens, n, i32, device)
-    at_o = _row("griffin_verify_drafts: lens_out", lens_out, n, i32, device)
+    at_d, at_u = _row(names[3], drafted, rows, i32, device), _row(names[4], accept_u, rows, f32, device)
+    at_r, at_t = _row(names[5], draw_u, n, f32, device), _row(names[6], tokens_out, rows, i32, device)
+    at_a, at_l, at_o = _row(names[7], accepted, n, i32, device), _row(names[8], lens, n, i32, device), _row(names[9], lens_out, n, i32, device)
     if workspace is not None and (workspace.get_device() != device or not workspace.is_contiguous()):
-        _refuse("griffin_verify_drafts: workspace", workspace, workspace.shape, None, device)
+        _refuse(names[10], workspace, workspace.shape, None, device)
     if device < 0:
         raise ValueError("griffin_verify_drafts: the tensors lie on the host")
     _check(lib.griffin_verify_drafts(at_p, ldp, at_q, ldq, at_d, cu, n, shape[1], at_u, at_r, at_t, at_a, at_l, at_o, _ptr(workspace), _nbytes(workspace),
-                                     _stream(stream)), "griffin_verify_drafts")
+                                     _stream(stream)), names[0])

@@ -517,15 +517,18 @@ __device__ __forceinline__ void attend_q4(const AttendQ4Params &p, float *lds, c
     }
     bool odd = false;
     if (key0 < end) {
-        // Two steps are on their way while one is computed: step i's registers take step i + 2 as soon as they have been read, and i + 4's pages are looked up
+        // Two steps are on their way while one is computed: step i's registers take step i + 2 as soon as they have been read, and i + 4's pages are looked up.  Of heads wider than
+        // 128 values are one step ahead: with two there would be registers for one wavefront a SIMD.
+        constexpr int VALS = DB > 128 ? 1 : 2;
         Q4Keys<F32, DB> fk[2];
-        Q4Vals<F32, DB> fv[2];
+        Q4Vals<F32, DB> fv[VALS];
 #pragma unroll
         for (int i = 0; i < 2; ++i)
             if (key0 + i * STRIDE < end) {
                 set(at[i], key0 + i * STRIDE);
                 in.load_keys(fk[i], at[i]);
-                in.load_vals(fv[i], at[i]);
+                if (i < VALS)
+                    in.load_vals(fv[i], at[i]);
                 look_up(at[i], key0 + (i + 2) * STRIDE);
             }
         while (true) {
@@ -544,13 +547,13 @@ __device__ __forceinline__ void attend_q4(const AttendQ4Params &p, float *lds, c
                 __builtin_amdgcn_sched_barrier(0);
                 if (key0 + S::KS > least || it.touches_hole(key0, S::KS)) {
                     q4_mask<F32, DB, NT>(s, r, it, key0, lane);
-                    odd |= q4_clear<F32, DB>(fv[i], it, key0, lane);
+                    odd |= q4_clear<F32, DB>(fv[i % VALS], it, key0, lane);
                 }
                 q4_softmax<F32, DB, NT>(s, w, r);
-                q4_weigh<F32, DB, NT>(w, fv[i], r);
+                q4_weigh<F32, DB, NT>(w, fv[i % VALS], r);
                 __builtin_amdgcn_sched_barrier(0);
-                if (more)
-                    in.load_vals(fv[i], at[i]);
+                if (VALS == 2 ? more : key0 + STRIDE < end)
+                    in.load_vals(fv[i % VALS], at[VALS == 2 ? i : i ^ 1]);
                 key0 += STRIDE;
                 if (key0 >= end)
                     goto done;

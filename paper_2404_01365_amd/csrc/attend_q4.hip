@@ -8,7 +8,7 @@ namespace griffin {
 
 // LONE: own items go a wavefront each
 template <bool F32, int DB, int NTP, int NTO, bool LONE>
-__global__ __launch_bounds__(ATT_WAVES * 64, DB > 128 || F32 ? 1 : 2) void attend_q4_kernel(AttendQ4Params p)
+__global__ __launch_bounds__(ATT_WAVES * 64, DB > 128 && F32 ? 1 : 2) void attend_q4_kernel(AttendQ4Params p)
 {
     __shared__ __align__(16) float lds[att_lds_floats<DB, ATT_WAVES>()];
     AttendItem it;

@@ -3,15 +3,18 @@
 // A sequence keeps its drafted tokens while u q(d) < p(d); where that ends a token is drawn from w = max(p - q, 0), or from p, by the inverse of the running
 // sum: the first j with w_0 + .. + w_j > r W.  Sums are in 64 bits, so that their order does not decide which token that is.
 //
-// Only the row where the kept tokens end is read whole.  A wavefront adds up a piece of 1024 tokens of it, and finds that row for itself (a few numbers a drafted token); a
-// second launch adds the pieces in order, finds the one that the sum falls into and goes through it again.
+// Only the row where the kept tokens end is read whole.  A wavefront adds up a piece of 1024 tokens of it, and finds that row for itself (a few numbers a drafted token); then
+// a workgroup a sequence adds the pieces in order, finds the one that the sum falls into and goes through it again: in a launch of its own, or, of small vocabularies, in the same.
 //
-// Bound by the two launches while there are few tokens (one sequence of 32000: 4.6 + 3.8 us), else by bytes: 64 sequences of 128001, p and q, 66 MB, 11.8 + 5.4 us.
+// Bound by latencies while there are few tokens (one sequence of 32000: 9.8 us, a launch, two steps of dependent loads to find the row, two of its pieces, one again), else by bytes: 64
+// sequences of 128001, p and q, 66 MB, 12.1 + 5.0 us, from cold caches 24.4 + 5.8.
 #include "layer.h"
 
 namespace griffin {
 
 constexpr int VERIFY_THREADS = 256;
+constexpr int VERIFY_ALONE = 1024;           // ... of a workgroup that does all of a sequence
+constexpr int VERIFY_ALONE_PIECES = 32;      // ... which has no more than so many pieces
 constexpr int VERIFY_PIECE = 1024;           // tokens of the vocabulary a wavefront adds up
 
 // Where a sequence's kept tokens end: its row, and what w is there
@@ -92,17 +95,12 @@ __device__ __forceinline__ void verify_weights(const VerifyParams &p, const Veri
     }
 }
 
-__global__ __launch_bounds__(VERIFY_THREADS) void verify_sums_kernel(VerifyParams p)
+// a piece's sum of w, by a wavefront; every lane ends with it
+__device__ __forceinline__ double verify_piece(const VerifyParams &p, const VerifyEnd &e, int32_t piece)
 {
-    const int b = blockIdx.x / p.blocks, lane = threadIdx.x & 63;
-    const int32_t piece = (blockIdx.x - b * p.blocks) * (VERIFY_THREADS / 64) + (threadIdx.x >> 6);
-    if (p.seqs.cu[b] == p.seqs.cu[b + 1] || piece >= p.pieces)
-        return;
-    const VerifyEnd e = verify_end(p, b);
-    if (piece == 0 && lane == 0)
-        p.ends[b] = e;
-    double sum = 0;
+    const int lane = threadIdx.x & 63;
     const int32_t begin = piece * VERIFY_PIECE;
+    double sum = 0;
     const auto add = [&](auto &w) {
 #pragma unroll
         for (auto &v : w)
@@ -126,14 +124,28 @@ __global__ __launch_bounds__(VERIFY_THREADS) void verify_sums_kernel(VerifyParam
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1)
         sum += __shfl_xor(sum, off);
+    return sum;
+}
+
+__global__ __launch_bounds__(VERIFY_THREADS) void verify_sums_kernel(VerifyParams p)
+{
+    const int b = blockIdx.x / p.blocks, lane = threadIdx.x & 63;
+    const int32_t piece = (blockIdx.x - b * p.blocks) * (VERIFY_THREADS / 64) + (threadIdx.x >> 6);
+    if (p.seqs.cu[b] == p.seqs.cu[b + 1] || piece >= p.pieces)
+        return;
+    const VerifyEnd e = verify_end(p, b);
+    if (piece == 0 && lane == 0)
+        p.ends[b] = e;
+    const double sum = verify_piece(p, e, piece);
     if (lane == 0)
         p.sums[(int64_t)b * p.pieces + piece] = sum;
 }
 
 // The sum of what the threads before have, and of all; called by all threads of a workgroup
+template <int THREADS>
 __device__ __forceinline__ double verify_before(double v, double &all)
 {
-    __shared__ double totals[VERIFY_THREADS / 64];
+    __shared__ double totals[THREADS / 64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     double run = v;
 #pragma unroll
@@ -148,7 +160,7 @@ __device__ __forceinline__ double verify_before(double v, double &all)
     double before = 0;
     all = 0;
 #pragma unroll
-    for (int w = 0; w < VERIFY_THREADS / 64; ++w) {
+    for (int w = 0; w < THREADS / 64; ++w) {
         before += w < wave ? totals[w] : 0.0;
         all += totals[w];
     }
@@ -157,9 +169,10 @@ __device__ __forceinline__ double verify_before(double v, double &all)
 }
 
 // the least of the threads' numbers
+template <int THREADS>
 __device__ __forceinline__ int32_t verify_least(int32_t v)
 {
-    __shared__ int32_t least[VERIFY_THREADS / 64];
+    __shared__ int32_t least[THREADS / 64];
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) {
         const int32_t other = __shfl_xor(v, off);
@@ -170,52 +183,48 @@ __device__ __forceinline__ int32_t verify_least(int32_t v)
         least[threadIdx.x >> 6] = v;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < VERIFY_THREADS / 64; ++w)
+    for (int w = 0; w < THREADS / 64; ++w)
         v = least[w] < v ? least[w] : v;
     return v;
 }
 
-// The first token of [begin, begin + 4 VERIFY_THREADS) whose running sum, with what comes before, passes the goal; INT32_MAX: none.  `before` is carried on.
+// The first token of a piece whose running sum, with what comes before, passes the goal; INT32_MAX: none.  `before` is carried on.
+template <int THREADS>
 __device__ __forceinline__ int32_t verify_find(const VerifyParams &p, const VerifyEnd &e, int32_t begin, double goal, double &before)
 {
-    const int32_t j = begin + threadIdx.x * 4;
-    float w[4];
+    constexpr int N = VERIFY_PIECE / THREADS;
+    const int32_t j = begin + threadIdx.x * N;
+    float w[N];
     verify_weights(p, e, j, w);
-    double all, run = verify_before((double)w[0] + (double)w[1] + (double)w[2] + (double)w[3], all) + before;
+    double all, mine = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        mine += w[i];
+    double run = verify_before<THREADS>(mine, all) + before;
     int32_t found = INT32_MAX;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < N; ++i) {
         run += w[i];
         if (found == INT32_MAX && j + i < p.vocab && run > goal)
             found = j + i;
     }
     before += all;
-    return verify_least(found);
+    return verify_least<THREADS>(found);
 }
 
-__global__ __launch_bounds__(VERIFY_THREADS) void verify_draw_kernel(VerifyParams p)
+// Sequence b's outcome, from where its kept tokens end and the pieces' sums there; called by all threads of a workgroup
+template <int THREADS>
+__device__ __forceinline__ void verify_draw(const VerifyParams &p, int b, VerifyEnd e, const double *sums)
 {
-    static_assert(VERIFY_PIECE == 4 * VERIFY_THREADS, "verify_find goes through a piece");
-    const int b = blockIdx.x;
     const int32_t first = p.seqs.cu[b], rows = p.seqs.cu[b + 1] - first;
-    if (rows == 0) {
-        if (threadIdx.x == 0) {
-            p.accepted[b] = 0;
-            if (p.lens_out)
-                p.lens_out[b] = p.lens[b];
-        }
-        return;
-    }
-    VerifyEnd e = p.ends[b];
     const double u = p.draw_u[b];
     // a thread takes as many pieces as its share is, one behind the other
-    const double *sums = p.sums + (int64_t)b * p.pieces;
-    const int32_t share = (p.pieces + VERIFY_THREADS - 1) / VERIFY_THREADS, from = threadIdx.x * share;
+    const int32_t share = (p.pieces + THREADS - 1) / THREADS, from = threadIdx.x * share;
     const int32_t to = from + share < p.pieces ? from + share : p.pieces;
     double mine = 0, total;
     for (int32_t i = from; i < to; ++i)
         mine += sums[i];
-    double before = verify_before(mine, total);
+    double before = verify_before<THREADS>(mine, total);
     int32_t drawn = INT32_MAX;
     if (total > 0) {
         const double goal = u * total;
@@ -229,13 +238,13 @@ __global__ __launch_bounds__(VERIFY_THREADS) void verify_draw_kernel(VerifyParam
             run += sums[i];
         }
         __shared__ double start;
-        const int32_t least = verify_least(piece);
+        const int32_t least = verify_least<THREADS>(piece);
         if (piece == least && piece != INT32_MAX)        // one thread's
             start = run;
         __syncthreads();
         if (least != INT32_MAX) {
             before = start;
-            drawn = verify_find(p, e, least * VERIFY_PIECE, goal, before);
+            drawn = verify_find<THREADS>(p, e, least * VERIFY_PIECE, goal, before);
             // where the piece's sum passes the goal and the running one, rounded otherwise, does not: its last token
             const int32_t last = (least + 1) * VERIFY_PIECE - 1;
             drawn = drawn != INT32_MAX ? drawn : last < p.vocab ? last : p.vocab - 1;
@@ -246,14 +255,14 @@ __global__ __launch_bounds__(VERIFY_THREADS) void verify_draw_kernel(VerifyParam
         e.without = -1;
         before = 0;
         for (int32_t at = 0; at < p.vocab; at += VERIFY_PIECE)
-            verify_find(p, e, at, INFINITY, before);
+            verify_find<THREADS>(p, e, at, INFINITY, before);
         const double goal = u * before;
         before = 0;
         for (int32_t at = 0; at < p.vocab && drawn == INT32_MAX; at += VERIFY_PIECE)
-            drawn = verify_find(p, e, at, goal, before);
+            drawn = verify_find<THREADS>(p, e, at, goal, before);
     }
     drawn = drawn != INT32_MAX ? drawn : p.vocab - 1;
-    for (int32_t i = threadIdx.x; i < rows; i += VERIFY_THREADS)
+    for (int32_t i = threadIdx.x; i < rows; i += THREADS)
         p.tokens_out[first + i] = i < e.kept ? p.drafted[first + i] : i == e.kept ? drawn : -1;
     if (threadIdx.x == 0) {
         p.accepted[b] = e.kept;
@@ -262,11 +271,54 @@ __global__ __launch_bounds__(VERIFY_THREADS) void verify_draw_kernel(VerifyParam
     }
 }
 
+// true, and done: a sequence without rows
+__device__ __forceinline__ bool verify_nothing(const VerifyParams &p, int b)
+{
+    if (p.seqs.cu[b] != p.seqs.cu[b + 1])
+        return false;
+    if (threadIdx.x == 0) {
+        p.accepted[b] = 0;
+        if (p.lens_out)
+            p.lens_out[b] = p.lens[b];
+    }
+    return true;
+}
+
+__global__ __launch_bounds__(VERIFY_THREADS) void verify_draw_kernel(VerifyParams p)
+{
+    const int b = blockIdx.x;
+    if (!verify_nothing(p, b))
+        verify_draw<VERIFY_THREADS>(p, b, p.ends[b], p.sums + (int64_t)b * p.pieces);
+}
+
+// All of a sequence whose vocabulary is no more than VERIFY_ALONE_PIECES pieces: sixteen wavefronts take them in turn
+__global__ __launch_bounds__(VERIFY_ALONE) void verify_alone_kernel(VerifyParams p)
+{
+    __shared__ double sums[VERIFY_ALONE_PIECES];
+    const int b = blockIdx.x;
+    if (verify_nothing(p, b))
+        return;
+    const VerifyEnd e = verify_end(p, b);
+    for (int32_t piece = threadIdx.x >> 6; piece < p.pieces; piece += VERIFY_ALONE / 64) {
+        const double sum = verify_piece(p, e, piece);
+        if ((threadIdx.x & 63) == 0)
+            sums[piece] = sum;
+    }
+    __syncthreads();
+    verify_draw<VERIFY_ALONE>(p, b, e, sums);
+}
+
 static int32_t verify_pieces(int32_t vocab) { return (vocab + VERIFY_PIECE - 1) / VERIFY_PIECE; }
+
+// Vocabularies of up to 32768 tokens go in one launch, a workgroup a sequence.  (One launch / two, us a call: one sequence of 4000 9.0 / 11.9, of 32000 10.4 / 13.2, of 65536 12.6 / 11.8, 16 of 50257
+// 12.5 / 11.5, 64 of 32000 12.1 / 12.0, of 65536 16.6 / 12.8, 256 of 32000 14.7 / 15.7.)
+static bool verify_alone(int32_t vocab) { return verify_pieces(vocab) <= VERIFY_ALONE_PIECES; }
 
 size_t verify_bytes(int32_t n_seqs, int32_t vocab)
 {
     static_assert(sizeof(VerifyEnd) == 2 * sizeof(double), "the sums behind the ends are aligned");
+    if (verify_alone(vocab))
+        return 0;
     return (size_t)n_seqs * (verify_pieces(vocab) * sizeof(double) + sizeof(VerifyEnd));
 }
 
@@ -276,14 +328,21 @@ int launch_verify(const VerifyJob &job, const SeqTable &seqs, hipStream_t st)
     p.p = job.p; p.q = job.q; p.ldp = job.ldp; p.ldq = job.ldq; p.drafted = job.drafted;
     p.accept_u = job.accept_u; p.draw_u = job.draw_u; p.tokens_out = job.tokens_out; p.accepted = job.accepted;
     p.lens = job.lens; p.lens_out = job.lens_out;
-    p.ends = (VerifyEnd *)job.ws;
-    p.sums = job.ws + 2 * seqs.n;
+    const bool alone = verify_alone(job.vocab);
+    if (!alone) {
+        p.ends = (VerifyEnd *)job.ws;
+        p.sums = job.ws + 2 * seqs.n;
+    }
     p.vocab = job.vocab;
     p.pieces = verify_pieces(job.vocab);
     p.blocks = (p.pieces + VERIFY_THREADS / 64 - 1) / (VERIFY_THREADS / 64);
     const auto wide = [](const float *at, int64_t ld) { return !at || (((uintptr_t)at & 15) == 0 && ld % 4 == 0); };
     p.wide = wide(job.p, job.ldp) && wide(job.q, job.ldq);
     p.seqs = seqs;
+    if (alone) {
+        hipLaunchKernelGGL(verify_alone_kernel, dim3(seqs.n), dim3(VERIFY_ALONE), 0, st, p);
+        return check_launch("verify_alone_kernel");
+    }
     hipLaunchKernelGGL(verify_sums_kernel, dim3((uint32_t)seqs.n * p.blocks), dim3(VERIFY_THREADS), 0, st, p);
     const int rc = check_launch("verify_sums_kernel");
     if (rc != GRIFFIN_OK)
