@@ -76,7 +76,8 @@ __device__ __forceinline__ bool q4_deal(const AttendQ4Params &p, int32_t j, bool
         all += tiles[i] * quanta[i];
     }
     const uint64_t whole = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(q4_wave_scan(all), 63) * (uint32_t)p.kv_heads;
-    const uint32_t most = (uint32_t)((whole + ((uint64_t)1 << p.deal) - 1) >> p.deal);        // below 2^31, as the sum is
+    const uint64_t share = (whole + ((uint64_t)1 << p.deal) - 1) >> p.deal;
+    const uint32_t most = share < INT32_MAX ? (uint32_t)share : INT32_MAX;
     uint32_t first = 0;                                    // parts of the sequences before these 64
     bool found = false;
 #pragma unroll

@@ -172,7 +172,8 @@ __device__ __forceinline__ bool q4_quantise_fast(const float (&x)[8], float off,
     const _Float16 middle = (_Float16)(m - me), beyond = (_Float16)(m + me);
     const float inv = __builtin_amdgcn_rcpf(step), shift = 8.0f - (float)middle * inv;
     const float near = 0.5f - (1.01f * off * inv + 0x1p-21f * size * inv + 4e-6f);
-    bool sure = scale == above && middle == beyond && size + off <= 32768.0f && step > 0;      // infinities: not sure
+    const bool same = __builtin_bit_cast(uint16_t, middle) == __builtin_bit_cast(uint16_t, beyond);        // zeros of both signs are not
+    bool sure = scale == above && same && size + off <= 32768.0f && step > 0;      // infinities: not sure
     // codes of even and of odd features in bytes, by a conversion that takes a number into a byte of a word
     uint32_t even = 0, odd = 0;
 #pragma unroll

@@ -111,6 +111,17 @@ def test_append_of_values_that_stand_out(dtype, group):
     run_append(c, group, "half", 0)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("group", [32, 64])
+def test_append_of_middles_at_zero(dtype, group):
+    """groups whose middle is zero, or next to it, and nothing else: zero's sign is the definition's, too"""
+    c = plain.Case(8, heads=2, kv_heads=2, dim=128, page=16, prefix=0, held=[0], new=[40], dtype=dtype)
+    steps = (np.arange(128) % 16 - 8.0)[None, None, :] * 2.0 ** (np.arange(40) % 12 - 6)[:, None, None]
+    c.k = plain.stored(np.broadcast_to(steps, c.k.shape), dtype)
+    c.v = np.array(-c.k)
+    run_append(c, group, "half", 0)
+
+
 def test_append_stops_at_max_len_and_clamps_pages():
     c = plain.Case(5, heads=4, kv_heads=2, dim=64, page=16, prefix=0, held=[30, 60, 64, -7], new=[5, 8, 3, 2], dtype=BF16, max_len=64)
     run_append(c, 32, "half", 64)
@@ -539,3 +550,23 @@ def test_graphs_that_share_a_workspace():
         stream.synchronize()
         for _, _, _, out, ref, size in cases:
             attention_close(to_host(out), ref, size, BF16)
+
+
+def test_append_of_more_workgroups_than_one_launch_takes():
+    """2^20 tokens of 17 workgroups each: the step goes out in parts, and its first and last tokens are what a small step makes of them"""
+    heads, dim, n, page = 544, 8, 1 << 20, 65536
+    size = G.griffin_kv_q4_page_bytes(heads, dim, page)
+    K, V = (torch.zeros(n // page, size, dtype=torch.uint8, device="cuda") for _ in range(2))
+    C = G.kv_cache_q4(K, V, kv_heads=heads, dim=dim, page_size=page, dtype=torch.bfloat16)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(4)
+    k, v = (torch.empty(n, heads, dim, dtype=torch.bfloat16, device="cuda").normal_(generator=g) for _ in range(2))
+    pages = ints([list(range(n // page))])
+    G.griffin_kv_append_q4(C, G.kv_batch([0, n], ints([0]), pages, n), k, v)
+    most = ((1 << 24) - 1) // 17                 # tokens of the first part
+    for at in (0, most - 8, n - 16):
+        back = [torch.zeros(16, heads, dim, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+        G.griffin_kv_read_q4(C, G.kv_batch([0, 16], ints([at]), pages, n), *back)
+        for x, y in zip((k, v), back):
+            codes, pairs = q4_plain.pack(to_host(x[at:at + 16]), 32)
+            assert torch.equal(y, dev(q4_plain.values(codes, pairs, dim, 32), BF16))
