@@ -7,6 +7,9 @@
 // operand is that in which they come out, and queries are laid out alike.  Values (A operand of O^T = V^T P^T): the lane holds the codes of eight keys for VD
 // neighbouring features; a byte permute puts two keys' codes of two features side by side, so the turn from rows of features to pairs of keys costs nothing beside
 // the unpacking.
+//
+// Bound by bytes where there are many, and close behind by the unpacking, some 300 instructions for 32 keys of 128 features: 32 sequences of 500 to 8000 keys, 8 heads of 128, four query heads
+// each, 175 MB, 43.6 us, 4.0 TB/s, from cold caches 78.  One sequence of 2049 keys, 32 heads, is a launch and a chain of loads, 9.4 us.
 #pragma once
 
 #include "attend_rows.h"

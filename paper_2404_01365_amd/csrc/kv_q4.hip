@@ -4,6 +4,10 @@
 // codes; a group's threads are neighbouring lanes, which exchange lo and hi.  By its definition all of it is computed in 64 bits: a value next to the border of two codes falls to
 // the side that the definition says, not to one that the order of fp32 operations chooses.  Few are that near, so everything is computed in fp32 with a bound on how far off it
 // is, and in 64 bits only by wavefronts where a rounding lies within that bound.
+//
+// Bound by its instructions, some 250 a wavefront of eight features a lane: 4150 tokens of 32 heads of 128 on as many, halves of them rotated in pairs, 155 MB, 49.6 us, from cold caches 59.5 (all
+// of it in 64 bits: 54.7); 16 tokens of 32 heads on 8 are a launch and a chain of loads, 5.1.  Reading back is bound by bytes: 32768 tokens of 8 heads of 128, 172 MB, 37.5 us, 4.6 TB/s,
+// from cold caches 59.
 #include "q4.h"
 
 namespace griffin {
