@@ -103,17 +103,31 @@ static Q4Plan attend_q4_plan(const griffin_kv_cache_q4 &C, const griffin_kv_batc
         const int64_t even = std::min((work + 255) / 256, (int64_t)keys);
         return (int32_t)((std::max(even, (int64_t)1) + quantum - 1) / quantum * quantum);
     };
-    // Tiles' chunks, the least for which no more than 512 workgroups share the prefix and, of tiles, own parts: two a CU, and none in a second round.  (320 rows of 32768 keys, 256 / 384 /
-    // 512 / 768: 92 / 84 / 75 / 83; 192 rows of them 64 / 63 / 65 / 67; 200 behind 8000 own, 384 / 512 / 1024, 67 / 54 / 65.)
+    // Tiles' chunks, the least for which no more than 512 workgroups a round share the prefix and, of tiles, own parts: two a CU.  (One round, 320 rows of 32768 keys, 256 / 384 /
+    // 512 / 768 workgroups: 92 / 84 / 75 / 83; 192 rows of them 64 / 63 / 65 / 67; 200 behind 8000 own, 384 / 512 / 1024, 67 / 54 / 65.)  Several rounds of shorter chunks where one would be far
+    // from full: a round takes some 1.9 us for 64 keys of 128 features, a chunk's sums go out and in again at some 4 TB/s.
+    // (One round / several: 800 tokens on 30000 own keys 539 / 440, 1100 on them 1018 / 705, 700 and 1100 behind 30000 shared 749 / 397, 1027 / 607, 16 heads of 256 on 8, 700 on 16000, 414 / 344.)
+    constexpr double STEP = 1.9 / (64 * 128);
+    double least = 0;                                      // us, of the chunks that were chosen
     const auto tile_chunk = [&]() {
         const int64_t quantum = att_tile_keys(C.dim), heads = C.kv_heads, own = pl.tile_own ? tiles : 0;
-        int64_t lo = 1, hi = (std::max((int64_t)B.n_prefix, own > 0 ? (int64_t)B.max_len : 0) + quantum - 1) / quantum;
-        while (lo < hi) {
-            const int64_t mid = (lo + hi) / 2, keys = mid * quantum;
-            if (heads * (pl.tiles_prefix * ((B.n_prefix + keys - 1) / keys) + own * ((B.max_len + keys - 1) / keys)) <= 512) hi = mid;
-            else lo = mid + 1;
+        const int64_t most = (std::max((int64_t)B.n_prefix, own > 0 ? (int64_t)B.max_len : 0) + quantum - 1) / quantum;
+        int64_t best = most;
+        least = 0;
+        for (int rounds = 1; rounds <= 8; ++rounds) {
+            int64_t lo = 1, hi = most;
+            while (lo < hi) {
+                const int64_t mid = (lo + hi) / 2, keys = mid * quantum;
+                if (heads * (pl.tiles_prefix * ((B.n_prefix + keys - 1) / keys) + own * ((B.max_len + keys - 1) / keys)) <= 512 * rounds) hi = mid;
+                else lo = mid + 1;
+            }
+            const double cost = rounds * (double)(lo * quantum) * C.dim * STEP + (double)rows * heads * ((most + lo - 1) / lo) * (C.dim + 2) * 2e-6;
+            if (rounds == 1 || cost < 0.9 * least) {
+                best = lo;
+                least = cost;
+            }
         }
-        return (int32_t)(lo * quantum);
+        return (int32_t)(best * quantum);
     };
     // The prefix: a workgroup a CU, two steps each at least of heads wider than 128.  (128 / 256 / 512 workgroups: 32 rows of 16384 keys 21 / 17 / 22, of 32768 31 / 22 / 25, 64 rows of 32768
     // 48 / 32 / 31, 16 rows of 4096 11.8 / 13.3 / 13.0, 64 rows of 4096 16.0 / 15.5 / 19.8.  16 heads of 256, 5 rows of 1999: 15.9 /
@@ -125,7 +139,11 @@ static Q4Plan attend_q4_plan(const griffin_kv_cache_q4 &C, const griffin_kv_batc
     // 213 / 100, 1000 alone and behind 8000 35 / 49, 226 / 189, 200 behind 8000 205 / 54, four times 60 behind 2048 shared 59 / 31.)  Whole ones take the prefix, too, ahead of their own keys,
     // unless it is read much oftener for it: the rule of the 16-bit cache.
     const int64_t beyond = tiles - (rows + pl.rows_own - 1) / pl.rows_own;   // tiles more than all rows in a row would take
-    const bool whole = pl.tile_own && (double)all * C.dim * (363.0 - items) <= 3.5e7;
+    bool whole = pl.tile_own && (double)all * C.dim * (363.0 - items) <= 3.5e7;
+    if (whole && items > 363 && B.n_prefix == 0) {         // rounds that are far from full.  (Whole / cut: 1500 tokens on 30000 own keys 1030 / 816, of 64 features 722 / 498.)
+        tile_chunk();
+        whole = 0.9 * ((items + 511) / 512 * STEP * (double)all * C.dim) <= least;
+    }
     pl.ahead = B.n_prefix > 0 && (pl.few || (whole && (4 * beyond <= tiles || beyond * B.n_prefix <= 16384)));
     if (pl.ahead || pl.few)
         pl.chunk_own = (int32_t)((all + 15 + step - 1) / step * step);

@@ -288,6 +288,43 @@ def test_attention_of_a_prompt_alone_and_row_by_row():
         assert np.all(np.abs(alone - together[i]) <= 2.0 ** -7 * np.abs(alone) + 2.0 ** -10 * 2 * 5)
 
 
+@pytest.mark.parametrize("heads,kv_heads,dim,prefix,held,new", [
+    (32, 8, 128, 0, 30000, 1100),           # 35 tiles of a kv head, parts in three rounds
+    (16, 4, 64, 0, 20000, 3000),            # more tiles than a round takes, cut
+    (32, 8, 128, 30000, 0, 700),            # a prefix in several rounds, own parts of one
+    (16, 8, 256, 9000, 7000, 700)])
+def test_attention_of_prompts_in_several_rounds_and_row_by_row(heads, kv_heads, dim, prefix, held, new):
+    """a long prompt on a long cache (through LDS, in more parts than workgroups fit the chip) and one token a call (straight from memory)"""
+    page, g = 128, torch.Generator(device="cuda")
+    g.manual_seed(dim + new)
+    keys = -(-prefix // page) * page + held + new
+    n = -(-keys // page)
+    size = G.griffin_kv_q4_page_bytes(kv_heads, dim, page)
+    K, V = (torch.zeros(n, size, dtype=torch.uint8, device="cuda") for _ in range(2))
+    C = G.kv_cache_q4(K, V, kv_heads=kv_heads, dim=dim, page_size=page, dtype=torch.bfloat16)
+    k, v = (torch.empty(keys, kv_heads, dim, dtype=torch.bfloat16, device="cuda").normal_(generator=g) for _ in range(2))
+    q = torch.empty(new, heads, dim, dtype=torch.bfloat16, device="cuda").normal_(generator=g) * 2
+    numbers = torch.randperm(n, generator=g, device="cuda").to(torch.int32)[None]
+    G.griffin_kv_append_q4(C, G.kv_batch([0, keys], ints([0]), numbers, n * page), k, v)       # the prefix's pages, then the sequence's
+    first = -(-prefix // page)
+    pages, shared = numbers[:, first:].contiguous(), numbers[0, :first].contiguous()
+
+    def run(rows, at, max_len):
+        B = G.kv_batch([0, rows.shape[0]], ints([at]), pages, max_len, prefix_pages=shared, n_prefix=prefix)
+        out = torch.full_like(rows, float("nan"))
+        ws = workspace(G.griffin_attention_q4_workspace_bytes(C, B, heads))
+        ws.fill_(0xFF)
+        G.griffin_attention_q4(C, B, rows, out, workspace=ws)
+        return to_host(out)
+
+    together = run(q, held, held + new)
+    most = float(v.abs().max())
+    for i in (0, 1, 31, 32, 63, 64, 500, new - 1):
+        alone = run(q[i:i + 1], held + i, held + new)[0]
+        # the output's rounding to bf16 twice, and weights that are cut apart from each other, 2^-10 of the values
+        assert np.all(np.abs(alone - together[i]) <= 2.0 ** -7 * np.abs(alone) + 2.0 ** -10 * 2 * most)
+
+
 @pytest.mark.parametrize("dim", [64, 128, 256])
 @pytest.mark.parametrize("prefix", [1, 64, 70])
 def test_attention_of_prompts_that_fill_the_chip_behind_a_prefix(dim, prefix):
