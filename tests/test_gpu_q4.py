@@ -387,6 +387,17 @@ def test_attention_of_small_and_large_numbers(dtype, q_scale, size):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("new", [[1, 3], [70, 40]])
+def test_attention_of_queries_that_are_zero_or_next_to_it(dtype, new):
+    """rows without a largest feature, or with one below the normal numbers of fp32, weigh all their keys alike; their neighbours do not"""
+    c = plain.Case(31, heads=8, kv_heads=4, dim=64, page=16, prefix=20, held=[300, 5], new=new, dtype=dtype)
+    c.q[0], c.q[-1, 1], c.q[1, 2] = 0.0, -0.0, plain.stored(c.q[1, 2] * 2.0 ** -135, dtype)
+    K, V = q4_plain.pool_of(c.K, 32), q4_plain.pool_of(c.V, 32)
+    ref, most = reference(c, K, V, 32, None)
+    attention_close(run_attention(c, K, V, 32), ref, most, dtype)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 def test_attention_of_queries_with_one_large_feature(dtype):
     c = plain.Case(23, heads=4, kv_heads=2, dim=128, page=16, prefix=0, held=[60], new=[2], dtype=dtype)
     c.K[..., 7] *= 2.0 ** -12
