@@ -434,7 +434,8 @@ __device__ __forceinline__ void q4_add_odd(const AttendQ4Params &p, const Attend
     }
 }
 
-// A row's queries in the order of the codes' pairs, scaled so that the largest lies in [128, 256); returns what its scores are to be multiplied by
+// A row's queries in the order of the codes' pairs, scaled so that the largest lies in [128, 256); returns what its scores are to be multiplied by: a normal number, as
+// scores that are masked are -Inf, and -Inf x 0 would be NaN.  Scores are below 2^31 before that, so a factor of 2^-126 or less leaves nothing that fp32 weights could tell from zero.
 template <bool F32, int NW>
 __device__ __forceinline__ float q4_load_row(const AttendQ4Params &p, att_u32x4 (&q)[F32 ? 2 : 1][NW], int64_t at, int lane)
 {
@@ -472,7 +473,7 @@ __device__ __forceinline__ float q4_load_row(const AttendQ4Params &p, att_u32x4 
                 q[1][w][j] = q4_word(rest);
             }
         }
-    return ldexpf(p.scale2, -up);
+    return fmaxf(ldexpf(p.scale2, -up), 0x1p-126f);
 }
 
 // The item's rows first .. first + 16 NT - 1, by the WAVES wavefronts of a workgroup (in turn, a step each) or by one alone
