@@ -472,6 +472,7 @@ int griffin_attention_q4(const griffin_kv_cache_q4 *C, const griffin_kv_batch *B
  * accept_u[r] * q_r(d_r) < p_r(d_r), product and comparison in fp32.  At the first row that is not kept a token is drawn with weights max(p_r - q_r, 0) (fp32),
  * at the last row, if all were kept, with weights p_r: the first token j with w_0 + .. + w_j > draw_u[b] * (w_0 + .. + w_(V-1)), sums in 64 bits.  Weights
  * that are all zero are replaced by p_r, and where those are, too, or the product is no less than the sum, the last token of the vocabulary comes out.
+ * (Where a running sum lies within a rounding of the product, the one or the other token beside it comes out, but none without weight.)
  *   p               [cu[n_seqs]][vocab] fp32, row stride ldp; >= 0 and finite
  *   draft_p         [cu[n_seqs]][vocab] fp32, row stride ldq, a sequence's last row is not read; NULL: every draft had all its probability on d_r
  *   drafted         [cu[n_seqs]] int32; one outside 0 .. vocab-1 is no draft: its sequence ends there, with weights p_r

@@ -188,7 +188,10 @@ __device__ __forceinline__ int32_t verify_least(int32_t v)
     return v;
 }
 
-// The first token of a piece whose running sum, with what comes before, passes the goal; INT32_MAX: none.  `before` is carried on.
+// The first token of a piece that has weight and whose running sum, with what comes before, passes the goal.  None does: VERIFY_LAST - j, more than any token, with j the piece's last token that
+// has weight; INT32_MAX: none has.  (Weight is asked for, as the sum ahead of a thread's first token is added in another order than the one behind the thread before, and may pass the goal by a
+// rounding where that did not.)  `before` is carried on.
+constexpr int32_t VERIFY_LAST = INT32_MAX - 1;
 template <int THREADS>
 __device__ __forceinline__ int32_t verify_find(const VerifyParams &p, const VerifyEnd &e, int32_t begin, double goal, double &before)
 {
@@ -205,8 +208,8 @@ __device__ __forceinline__ int32_t verify_find(const VerifyParams &p, const Veri
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         run += w[i];
-        if (found == INT32_MAX && j + i < p.vocab && run > goal)
-            found = j + i;
+        if (found >= p.vocab && w[i] > 0)
+            found = run > goal ? j + i : VERIFY_LAST - (j + i);
     }
     before += all;
     return verify_least<THREADS>(found);
@@ -231,7 +234,7 @@ __device__ __forceinline__ void verify_draw(const VerifyParams &p, int b, Verify
         int32_t piece = INT32_MAX;
         double run = before;
         for (int32_t i = from; i < to; ++i) {
-            if (run + sums[i] > goal) {
+            if (sums[i] > 0 && run + sums[i] > goal) {
                 piece = i;
                 break;
             }
@@ -245,9 +248,8 @@ __device__ __forceinline__ void verify_draw(const VerifyParams &p, int b, Verify
         if (least != INT32_MAX) {
             before = start;
             drawn = verify_find<THREADS>(p, e, least * VERIFY_PIECE, goal, before);
-            // where the piece's sum passes the goal and the running one, rounded otherwise, does not: its last token
-            const int32_t last = (least + 1) * VERIFY_PIECE - 1;
-            drawn = drawn != INT32_MAX ? drawn : last < p.vocab ? last : p.vocab - 1;
+            // where the piece's sum passes the goal and the running one, rounded otherwise, does not: its last token with weight
+            drawn = drawn < p.vocab ? drawn : VERIFY_LAST - drawn;
         }
     } else {
         // nothing left over: the target's own probabilities, by this workgroup alone
@@ -258,10 +260,10 @@ __device__ __forceinline__ void verify_draw(const VerifyParams &p, int b, Verify
             verify_find<THREADS>(p, e, at, INFINITY, before);
         const double goal = u * before;
         before = 0;
-        for (int32_t at = 0; at < p.vocab && drawn == INT32_MAX; at += VERIFY_PIECE)
+        for (int32_t at = 0; at < p.vocab && drawn >= p.vocab; at += VERIFY_PIECE)
             drawn = verify_find<THREADS>(p, e, at, goal, before);
     }
-    drawn = drawn != INT32_MAX ? drawn : p.vocab - 1;
+    drawn = drawn < p.vocab ? drawn : p.vocab - 1;
     for (int32_t i = threadIdx.x; i < rows; i += THREADS)
         p.tokens_out[first + i] = i < e.kept ? p.drafted[first + i] : i == e.kept ? drawn : -1;
     if (threadIdx.x == 0) {
