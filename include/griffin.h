@@ -478,12 +478,13 @@ int griffin_attention_q4(const griffin_kv_cache_q4 *C, const griffin_kv_batch *B
  *   drafted         [cu[n_seqs]] int32; one outside 0 .. vocab-1 is no draft: its sequence ends there, with weights p_r
  *   cu_seqlens_host HOST int32 [n_seqs+1] as in griffin_prefill_select; n_seqs <= GRIFFIN_MAX_SEQS.  Read before the call returns.
  *   accept_u        [cu[n_seqs]] fp32, draw_u [n_seqs] fp32: random numbers, uniform in [0, 1) (the library draws none)
- *   tokens_out      [cu[n_seqs]] int32: row by row the kept tokens of a sequence, the drawn one, then -1.  Not `drafted` itself.
+ *   tokens_out      [cu[n_seqs]] int32: row by row the kept tokens of a sequence, the drawn one, then -1.  Shares none with `drafted`
+ *                   (GRIFFIN_EINVAL): a sequence's are written while another's are read.
  *   accepted        [n_seqs] int32: tokens kept
  *   lens, lens_out  [n_seqs] int32 or both NULL: lens_out[b] = lens[b] + accepted[b] + 1, the tokens in the cache that count (rows of the step that are dropped
  *                   are overwritten by the next one).  lens_out may be lens itself.
  *   workspace       griffin_verify_workspace_bytes(n_seqs, vocab) bytes, 256-byte aligned (may be 0)
- * A sequence without rows keeps 0 and its length.  vocab <= 2^24; rows of any alignment.
+ * A sequence without rows keeps 0 and its length.  vocab <= 2^24; rows of any alignment.  No output shares an element with another argument, but lens_out with lens.
  */
 size_t griffin_verify_workspace_bytes(int32_t n_seqs, int32_t vocab);
 int griffin_verify_drafts(const float *p, int64_t ldp, const float *draft_p, int64_t ldq, const int32_t *drafted, const int32_t *cu_seqlens_host,

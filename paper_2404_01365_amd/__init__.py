@@ -666,7 +666,8 @@ def griffin_verify_workspace_bytes(n_seqs: int, vocab: int) -> int:
 def griffin_verify_drafts(cu_seqlens, p, drafted, accept_u, draw_u, tokens_out, accepted, *, draft_p=None, lens=None, lens_out=None, workspace=None,
                           stream=None) -> None:
     """Keeps the drafted tokens that the target's probabilities p [rows][vocab] allow and draws the one behind them.  cu_seqlens: a sequence of ints or
-    what cu_seqlens() made of one; drafted, accept_u, tokens_out [rows]; draw_u, accepted, lens, lens_out [sequences]."""
+    what cu_seqlens() made of one; drafted, accept_u, tokens_out [rows]; draw_u, accepted, lens, lens_out [sequences].  tokens_out shares no element with
+    drafted."""
     cu = cu_seqlens if isinstance(cu_seqlens, ctypes.Array) else _cu_array(cu_seqlens)
     n, device, f32, i32, names = len(cu) - 1, p.get_device(), _TYPE[F32], _int32(), _VERIFY
     if n < 1:

@@ -271,7 +271,10 @@ int griffin_verify_drafts(const float *p, int64_t ldp, const float *draft_p, int
     if (!take_seqs(cu_seqlens_host, n_seqs, seqs))
         return GRIFFIN_ESHAPE;
     const int32_t rows = seqs.cu[n_seqs];
-    if (rows > 0 && (!p || !drafted || !accept_u || !tokens_out || tokens_out == drafted))
+    if (rows > 0 && (!p || !drafted || !accept_u || !tokens_out))
+        return GRIFFIN_EINVAL;
+    // a sequence's tokens are written while another's are read
+    if ((uintptr_t)tokens_out < (uintptr_t)drafted + (uintptr_t)rows * 4 && (uintptr_t)drafted < (uintptr_t)tokens_out + (uintptr_t)rows * 4)
         return GRIFFIN_EINVAL;
     if (rows > 1 && (ldp < vocab || (draft_p && ldq < vocab)))
         return GRIFFIN_ESHAPE;
