@@ -455,9 +455,9 @@ int griffin_kv_read_q4(const griffin_kv_cache_q4 *C, const griffin_kv_batch *B, 
 /*
  * griffin_attention over such a cache: out[t][h] = sum_k softmax_k(scale * q[t][h] . K_k) V_k with the values that the cache stands for.  Products are of
  * fp16 on the matrix cores, exact for keys and values; a row of queries is scaled by a power of two and rounded to fp16 (bf16 caches: features down to 2^-24 of
- * the largest keep all their bits, below that 2^-32 of it is lost at most; fp32: to a pair of fp16, 2^-23), weights are cut to fp16 (2^-10; fp32: to a pair, 2^-20) for product
- * and sum alike.  Scores, maximum, sum and weighted sum are fp32.  Tokens that a row does not see do not reach its output, whatever their places hold; those that
- * it sees hold what griffin_kv_append_q4 has written.
+ * the largest keep all their bits, below that 2^-32 of it is lost at most; fp32: to a pair of fp16, 2^-23 of each feature and 2^-32 of the largest), weights are cut to fp16 (2^-10 of
+ * each and 2^-31 of the row's largest; fp32: rounded to a pair, 2^-22 of each and 2^-32 of the largest) for product and sum alike.  Scores, maximum, sum and weighted
+ * sum are fp32.  Tokens that a row does not see do not reach its output, whatever their places hold; those that it sees hold what griffin_kv_append_q4 has written.
  * Arguments, limits and workspace as in griffin_attention.
  */
 size_t griffin_attention_q4_workspace_bytes(const griffin_kv_cache_q4 *C, const griffin_kv_batch *B, int32_t n_heads);
@@ -478,8 +478,8 @@ int griffin_attention_q4(const griffin_kv_cache_q4 *C, const griffin_kv_batch *B
  *   drafted         [cu[n_seqs]] int32; one outside 0 .. vocab-1 is no draft: its sequence ends there, with weights p_r
  *   cu_seqlens_host HOST int32 [n_seqs+1] as in griffin_prefill_select; n_seqs <= GRIFFIN_MAX_SEQS.  Read before the call returns.
  *   accept_u        [cu[n_seqs]] fp32, draw_u [n_seqs] fp32: random numbers, uniform in [0, 1) (the library draws none)
- *   tokens_out      [cu[n_seqs]] int32: row by row the kept tokens of a sequence, the drawn one, then -1.  Shares none with `drafted`
- *                   (GRIFFIN_EINVAL): a sequence's are written while another's are read.
+ *   tokens_out      [cu[n_seqs]] int32: row by row the kept tokens of a sequence, the drawn one, then -1.  Shares no element with
+ *                   `drafted` (GRIFFIN_EINVAL): a sequence's are written while another's are read.
  *   accepted        [n_seqs] int32: tokens kept
  *   lens, lens_out  [n_seqs] int32 or both NULL: lens_out[b] = lens[b] + accepted[b] + 1, the tokens in the cache that count (rows of the step that are dropped
  *                   are overwritten by the next one).  lens_out may be lens itself.

@@ -292,8 +292,9 @@ __device__ __forceinline__ void q4_mask(Q4Scores<F32, DB, NT> &s, const Q4Rows<F
             }
 }
 
-// Scores to weights, cut to fp16 (fp32: and what that leaves, once more): the rows' reference carried on, moved only when scores outgrow it by more than 8 (base 2), so
-// that weights are up to 2^8 times its.  Sums are of the weights as they are multiplied, by a product with ones: what cutting takes off all of them cancels.
+// Scores to weights, cut to fp16 (fp32: and what that leaves rounded to fp16 in turn): the rows' reference carried on, moved only when scores outgrow it by more than 8 (base 2), so
+// that weights are up to 2^8 times its.  Sums are of the weights as they are multiplied, by a product with ones: what cutting takes off all of them cancels.  What it takes off fp16 below its normal
+// numbers is another share of each, up to all: of many keys of little weight a pair that was cut twice would lose up to twice the rounding's bound, and all of them the same way.
 template <bool F32, int DB, int NT>
 __device__ __forceinline__ void q4_softmax(Q4Scores<F32, DB, NT> &s, att_u32x4 (&w)[NT][Q4Att<F32, DB>::NF], Q4Rows<F32, DB, NT> &r)
 {
@@ -324,7 +325,7 @@ __device__ __forceinline__ void q4_softmax(Q4Scores<F32, DB, NT> &s, att_u32x4 (
         }
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        // 2^7 times the weights, up to 2^15: fp16 keeps their bits down to 2^-21 of the reference's, and 2^-31 of it below.  The quotient does not see it.
+        // 2^7 times the weights, up to 2^15: fp16 keeps their bits down to 2^-21 of the reference's, and 2^-31 of it below (of a pair, 2^-11, and 2^-32 below).  The quotient does not see it.
         const float base = r.m[n] == -INFINITY ? -7.0f : r.m[n] - 7.0f;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -336,8 +337,10 @@ __device__ __forceinline__ void q4_softmax(Q4Scores<F32, DB, NT> &s, att_u32x4 (
             for (int e = 0; e < 4; e += 2) {
                 const q4_pair v = __builtin_bit_cast(q4_pair, __builtin_amdgcn_cvt_pkrtz(x[e], x[e + 1]));
                 w[n][0][2 * i + e / 2] = q4_word(v);
-                if constexpr (F32)
-                    w[n][1][2 * i + e / 2] = q4_word(__builtin_bit_cast(q4_pair, __builtin_amdgcn_cvt_pkrtz(x[e] - (float)v[0], x[e + 1] - (float)v[1])));
+                if constexpr (F32) {
+                    const q4_pair rest = {(_Float16)(x[e] - (float)v[0]), (_Float16)(x[e + 1] - (float)v[1])};
+                    w[n][1][2 * i + e / 2] = q4_word(rest);
+                }
             }
         }
 #pragma unroll
