@@ -220,7 +220,7 @@ template <int THREADS>
 __device__ __forceinline__ void verify_draw(const VerifyParams &p, int b, VerifyEnd e, const double *sums)
 {
     const int32_t first = p.seqs.cu[b], rows = p.seqs.cu[b + 1] - first;
-    const double u = p.draw_u[b];
+    const float u = p.draw_u[b];              // widened where it is used: a register less in between
     // a thread takes as many pieces as its share is, one behind the other
     const int32_t share = (p.pieces + THREADS - 1) / THREADS, from = threadIdx.x * share;
     const int32_t to = from + share < p.pieces ? from + share : p.pieces;
@@ -230,7 +230,7 @@ __device__ __forceinline__ void verify_draw(const VerifyParams &p, int b, Verify
     double before = verify_before<THREADS>(mine, total);
     int32_t drawn = INT32_MAX;
     if (total > 0) {
-        const double goal = u * total;
+        const double goal = (double)u * total;
         int32_t piece = INT32_MAX;
         double run = before;
         for (int32_t i = from; i < to; ++i) {
@@ -258,7 +258,7 @@ __device__ __forceinline__ void verify_draw(const VerifyParams &p, int b, Verify
         before = 0;
         for (int32_t at = 0; at < p.vocab; at += VERIFY_PIECE)
             verify_find<THREADS>(p, e, at, INFINITY, before);
-        const double goal = u * before;
+        const double goal = (double)u * before;
         before = 0;
         for (int32_t at = 0; at < p.vocab && drawn >= p.vocab; at += VERIFY_PIECE)
             drawn = verify_find<THREADS>(p, e, at, goal, before);
