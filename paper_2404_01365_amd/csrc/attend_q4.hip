@@ -107,22 +107,31 @@ static Q4Plan attend_q4_plan(const griffin_kv_cache_q4 &C, const griffin_kv_batc
     // 512 / 768 workgroups: 92 / 84 / 75 / 83; 192 rows of them 64 / 63 / 65 / 67; 200 behind 8000 own, 384 / 512 / 1024, 67 / 54 / 65.)  Several rounds of shorter chunks where one would be far
     // from full: a round takes some 1.9 us for 64 keys of 128 features, a chunk's sums go out and in again at some 4 TB/s.
     // (One round / several: 800 tokens on 30000 own keys 539 / 440, 1100 on them 1018 / 705, 700 and 1100 behind 30000 shared 749 / 397, 1027 / 607, 16 heads of 256 on 8, 700 on 16000, 414 / 344.)
+    // A round that is begun for no more than one workgroup a CU takes 0.65 of a full one's time, and fewer rounds than a chunk a tile takes there cannot be.  (Beyond 512 tiles, whole / in more rounds:
+    // 2100, 2500 and 3000 tokens on 30000 own keys, 528 to 752 tiles, 1714 / 1283, 1725 / 1435, 1759 / 1763, on 16000 926 / 742, 945 / 844, 985 / 1033, on 4000 268 / 314, 291 / 336, 352 / 416, 880 tiles on
+    // 120000 9078 / 7854; 4100 and 5000 tokens on 30000, 1032 and 1256 tiles, 3004 / 2704, 2913 / 3102.)  More than 512 tiles of a prefix and of own parts together stay whole: the model, which takes all
+    // for as long as the longest, does not tell them apart.  (Whole / cut: 64 of 40 tokens behind 2000 and 32768 shared 171 / 165, 1857 / 1527, 200 of 17 behind 8000 623 / 677, 256 of 20 behind 3000 390 / 444.)
     constexpr double STEP = 1.9 / (64 * 128);
+    const auto rounds_of = [](int64_t wgs) { return wgs <= 512 ? 1.0 : (double)(wgs / 512) + (wgs % 512 > 256 ? 1.0 : wgs % 512 > 0 ? 0.65 : 0.0); };
     double least = 0;                                      // us, of the chunks that were chosen
     const auto tile_chunk = [&]() {
         const int64_t quantum = att_tile_keys(C.dim), heads = C.kv_heads, own = pl.tile_own ? tiles : 0;
         const int64_t most = (std::max((int64_t)B.n_prefix, own > 0 ? (int64_t)B.max_len : 0) + quantum - 1) / quantum;
+        const int64_t all_tiles = heads * (pl.tiles_prefix + own), first = std::max((all_tiles + 511) / 512, (int64_t)1);
         int64_t best = most;
         least = 0;
-        for (int rounds = 1; rounds <= 8; ++rounds) {
+        if (all_tiles > 512 && pl.tiles_prefix > 0 && own > 0)
+            return (int32_t)(most * quantum);
+        for (int64_t rounds = first; rounds < first + 8; ++rounds) {
             int64_t lo = 1, hi = most;
             while (lo < hi) {
                 const int64_t mid = (lo + hi) / 2, keys = mid * quantum;
                 if (heads * (pl.tiles_prefix * ((B.n_prefix + keys - 1) / keys) + own * ((B.max_len + keys - 1) / keys)) <= 512 * rounds) hi = mid;
                 else lo = mid + 1;
             }
-            const double cost = rounds * (double)(lo * quantum) * C.dim * STEP + (double)rows * heads * ((most + lo - 1) / lo) * (C.dim + 2) * 2e-6;
-            if (rounds == 1 || cost < 0.9 * least) {
+            const double taken = lo == most ? rounds_of(all_tiles) : (double)rounds;
+            const double cost = taken * (lo * quantum) * C.dim * STEP + (double)rows * heads * ((most + lo - 1) / lo) * (C.dim + 2) * 2e-6;
+            if (rounds == first || cost < 0.9 * least) {
                 best = lo;
                 least = cost;
             }
@@ -142,7 +151,7 @@ static Q4Plan attend_q4_plan(const griffin_kv_cache_q4 &C, const griffin_kv_batc
     bool whole = pl.tile_own && (double)all * C.dim * (363.0 - items) <= 3.5e7;
     if (whole && items > 363 && B.n_prefix == 0) {         // rounds that are far from full.  (Whole / cut: 1500 tokens on 30000 own keys 1030 / 816, of 64 features 722 / 498.)
         tile_chunk();
-        whole = 0.9 * ((items + 511) / 512 * STEP * (double)all * C.dim) <= least;
+        whole = 0.9 * rounds_of(items) * STEP * (double)all * C.dim <= least;
     }
     pl.ahead = B.n_prefix > 0 && (pl.few || (whole && (4 * beyond <= tiles || beyond * B.n_prefix <= 16384)));
     if (pl.ahead || pl.few)
