@@ -25,8 +25,8 @@ __device__ __forceinline__ void att_add_weights(att_f32x4 &l, att_u32x4 w)
     l = att_mfma(att_u32x4{ONES, ONES, ONES, ONES}, w, l);
 }
 
-constexpr int ATT_WAVES = 4;            // of a workgroup of attend_rows_kernel
-constexpr int ATT_FEW_WAVES = 8;        // ... of attend_few_kernel, and of own parts beside tiles
+constexpr int ATT_WAVES = 4;            // of a workgroup of attend_rows_kernel and attend_q4_kernel
+constexpr int ATT_FEW_WAVES = 8;        // ... of attend_few_kernel and attend_q4_few_kernel, and of own parts beside tiles over the 16-bit cache
 constexpr int ATT_TILE_WAVES = 8;       // ... of attend_tile.hip
 constexpr int att_tile_keys(int32_t dim) { return dim > 128 ? 32 : 64; }      // its step
 

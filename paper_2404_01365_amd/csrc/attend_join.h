@@ -125,7 +125,7 @@ static int go_join(const P &p, int32_t most, hipStream_t st)
     return check_launch("attend_join_kernel");
 }
 
-// most: chunks of a row
+// most: chunks of a row; where the device cuts own parts, what they are on average, as no more is known here
 template <class P>
 static int launch_attend_join(const P &p, bool bf16, int32_t most, hipStream_t st)
 {

@@ -167,6 +167,8 @@ static Q4Plan attend_q4_plan(const griffin_kv_cache_q4 &C, const griffin_kv_batc
     // Other own parts of a few rows, longer than a step, are cut by the device, which counts quanta in 32 bits: into 512 parts and more, behind tiles of the prefix 256.  (256 / 512 / 1024: 32
     // sequences of 500 to 8000 keys 63 / 52 / 53, 64 of 100 to 4000 60 / 51 / 55, four of 500 to 30000 33 / 25 / 27, 16 of 20 rows and 500 to 4000 31 / 26 / 33, 8 of 100 to 4000 of 16 heads of 256 43 / 40 / 45;
     // 48 of 5 to 700 behind 32768 66 / 66 / 69, 16 of five tokens there 79 / 81 / 82.  Cut by max_len instead, the best number of workgroups for each: 57, 58, 27, 33.)
+    // Parts are whole steps of a workgroup, beside tiles two: those of up to 256 keys, often all that a sequence has, stay in one piece.  (Two steps / one: 48 of 5 to 700 behind 32768 62.4 / 60.6, of
+    // 100 to 250 57.4 / 58.1, 16 of five tokens and 5 to 700 74.0 / 73.9, 17 of 130 to 255 behind 65536 51.0 / 51.4, 40 of two and 5 to 2000 behind 16384 63.0 / 59.3, 100 of 5 to 1000 there 73.7 / 73.9.)
     pl.quantum = (int32_t)(pl.beside ? ATT_FEW_WAVES / ATT_WAVES * step : step);
     pl.deal = -1;
     if (!pl.tile_own && !pl.few && !pl.lone && B.max_len > pl.quantum && tiles * ((B.max_len + (int64_t)pl.quantum - 1) / pl.quantum) < (int64_t)1 << 31) {
