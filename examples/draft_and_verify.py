@@ -35,7 +35,8 @@ class Speculation:
         self.compact = []
         up = lambda n: -(-n // PAGE)  # noqa: E731
         # a round may go past the last step that is asked for
-        self.steps, room = steps, steps + drafts + 1
+        self.steps = steps
+        self.room = room = steps + drafts + 1
         shared, own = up(prompt_len), up(room)
         self.prefix_pages = torch.arange(shared, dtype=torch.int32, device=dev)
         self.pages = shared + torch.arange(rows * own, dtype=torch.int32, device=dev).view(rows, own)
@@ -122,6 +123,8 @@ class Speculation:
     def round(self, last):
         """From every row's last token: its new tokens [rows][drafts + 1] (-1 behind them), how many drafted ones were kept, and the last again"""
         R, K = self.rows, self.drafts
+        if int(self.lens.max()) + K + 1 > self.room:
+            raise ValueError("round: the cache holds %d tokens a row" % self.room)
         tokens = torch.zeros(R, K + 1, dtype=torch.int32, device="cuda")
         tokens[:, 0] = last
         draft_p = torch.empty(R, K + 1, self.vocab, device="cuda")          # a row's last probabilities are never read
