@@ -9,7 +9,7 @@
 // the unpacking.
 //
 // Bound by bytes where there are many, and close behind by the unpacking, some 300 instructions for 32 keys of 128 features: 32 sequences of 500 to 8000 keys, 8 heads of 128, four query heads
-// each, 175 MB, 43.6 us, 4.0 TB/s, from cold caches 78.  One sequence of 2049 keys, 32 heads, is a launch and a chain of loads, 9.4 us.
+// each, 175 MB, 45 us, 3.9 TB/s, and 50 where 1.6 GB of caches take turns.  One sequence of 2049 keys, 32 heads, is a launch and a chain of loads, 9.7 us.
 #pragma once
 
 #include "attend_rows.h"

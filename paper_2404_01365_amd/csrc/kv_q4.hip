@@ -5,9 +5,9 @@
 // the side that the definition says, not to one that the order of fp32 operations chooses.  Few are that near, so everything is computed in fp32 with a bound on how far off it
 // is, and in 64 bits only by wavefronts where a rounding lies within that bound.
 //
-// Bound by its instructions, some 250 a wavefront of eight features a lane: 4150 tokens of 32 heads of 128 on as many, halves of them rotated in pairs, 155 MB, 49.6 us, from cold caches 59.5 (all
-// of it in 64 bits: 54.7); 16 tokens of 32 heads on 8 are a launch and a chain of loads, 5.1.  Reading back is bound by bytes: 32768 tokens of 8 heads of 128, 172 MB, 37.5 us, 4.6 TB/s,
-// from cold caches 59.
+// Bound by its instructions, some 250 a wavefront of eight features a lane: 4150 tokens of 32 heads of 128 on as many, halves of them rotated in pairs, 155 MB, 50 us (all
+// of it in 64 bits: 54.7), 57 where 1.3 GB of states take turns; 16 tokens of 32 heads on 8 are a launch and a chain of loads, 5.0.  Reading back: 32768 tokens of 8 heads of 128, 172 MB, 37.6 us, 4.6 TB/s,
+// again and again, part of it cached; where states take turns 54.4, 3.2 TB/s, two thirds of a copy's rate: a thread's 16 or 32 bytes wait for a length, a page and a code one after the other.
 #include "q4.h"
 
 namespace griffin {

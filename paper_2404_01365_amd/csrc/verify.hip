@@ -7,7 +7,7 @@
 // a workgroup a sequence adds the pieces in order, finds the one that the sum falls into and goes through it again: in a launch of its own, or, of small vocabularies, in the same.
 //
 // Bound by latencies while there are few tokens (one sequence of 32000: 9.8 us, a launch, two steps of dependent loads to find the row, two of its pieces, one again), else by bytes: 64
-// sequences of 128001, p and q, 66 MB, 12.1 + 5.0 us, from cold caches 24.4 + 5.8.
+// sequences of 128001, p and q, 66 MB, 11.4 + 5.3 us, and 13.1 + 5.0 where 1.3 GB of states take turns.
 #include "layer.h"
 
 namespace griffin {
