@@ -95,7 +95,10 @@ static Q4Plan attend_q4_plan(const griffin_kv_cache_q4 &C, const griffin_kv_batc
     pl.tiles_prefix = B.n_prefix > 0 ? (int32_t)((rows + pl.rows_prefix - 1) / pl.rows_prefix) : 0;
     const int64_t step = ATT_WAVES * 32, all = (int64_t)B.n_prefix + B.max_len, items = C.kv_heads * tiles;
     // Own parts that fill the chip as they are go a wavefront each, and parts so few and short that a step of twice as many wavefronts is cheaper than a second launch take the
-    // prefix, too, all in one launch: rules of the 16-bit cache (attend.hip), whose parts are as many steps long.
+    // prefix, too, all in one launch: rules of the 16-bit cache (attend.hip), whose parts are as many steps long.  (A wavefront each / cut by the device, 32 kv heads of 128: 100 of 5 to 120 keys 17 / 25,
+    // 40 of 5 to 250 16.6 / 19.2, 128 of 100 to 255 36 / 49, 200 of 5 to 60 behind 1000 42 / 77; 200 of 5 to 250, 8 heads of 64, 13.5 / 19.5.  One launch / not: one of 250 keys 8.0 / 11.8, 16 of three tokens
+    // behind 200 8.5 / 12.6, 64 of 10 to 250 12.3 / 12.2, 16 of them of 32 kv heads 12.1 / 11.6.  Both end earlier than they could: 100 of 200 to 500 a wavefront each 45 / 54, one of 500 in one launch 9.5 / 11.9, but 64
+    // of 260 to 500 16.2 / 15.0.)
     pl.lone = !pl.tile_own && items >= 1024 && B.max_len <= 256;
     pl.few = longest <= 16 && !pl.tile_prefix && items <= 512 && all <= ATT_FEW_WAVES / ATT_WAVES * step && C.dim <= 128;
     const int64_t work_prefix = C.kv_heads * (int64_t)pl.tiles_prefix * B.n_prefix;
